@@ -73,7 +73,8 @@ typedef enum s2a_status {
                                  rows in a backward, device is not sm_100 */
     S2A_ERR_CUDA = -3,        /* a CUDA call failed while enqueuing; see s2a_last_cuda_error() */
     S2A_ERR_TIMEOUT = -4,     /* reported by s2a_device_status(): a bounded device-side wait expired */
-    S2A_ERR_TOO_LARGE = -5    /* s2a_bwd_noalloc only: B*H*N is more than its built-in scratch holds */
+    S2A_ERR_TOO_LARGE = -5,   /* s2a_bwd_noalloc only: B*H*N is more than its built-in scratch holds */
+    S2A_ERR_BAD_INDEX = -6    /* reported by s2a_device_status(): a table, starts or lengths of the paged cache held a value out of range */
 } s2a_status;
 
 /*
@@ -239,6 +240,73 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
                      void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Serving from a paged cache of keys and values.  (The paper fine-tunes with S2-Attn and leaves the model "original, standard
+ * self-attention" at inference; these entry points are that attention where the keys and values of earlier tokens are
+ * kept, as a program that serves the model needs it.)
+ *
+ * The cache is a pool of pages for k and one for v, owned by the caller like every tensor: [pages, Hkv, page_size, d], page_size
+ * a power of two from 16 to 256, d in {64, 128}.
+ *   S2A_CACHE_BF16  values in bf16
+ *   S2A_CACHE_E4M3  8-bit floats (e4m3) with a power of two for every row (token and head): value = code * 2^exp, exp in
+ *                   k_exp and v_exp [pages, Hkv, page_size].  Every value that s2a_cache_write leaves is a bf16 number.
+ *                   exp = -128 marks a row that reads back as NaN throughout.
+ * pages * Hkv * page_size must not exceed 2^31 - 1.
+ *
+ * A batch holds new tokens of B sequences.  Row starts[b] + i of its tensors is new token i of sequence b, which has
+ * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows, and rows that belong to no sequence are neither read
+ * nor written.  lengths[b] counts the tokens that sequence b has in the cache INCLUDING its new ones, so new token i is at
+ * position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
+ * (j + 1) * page_size - 1; entries past a sequence's last page are not used.  Sequences may share pages, but not those that one call
+ * writes to.
+ * table, starts and lengths are DEVICE pointers and read on the device when the kernels run: a captured graph follows what they
+ * hold when it is replayed.  Their contents are checked there.  What is out of range (starts that fall or leave [0, T], a length
+ * below the number of new tokens or above width * page_size, a page outside the pool, more new tokens than max_new) is skipped
+ * and reported like an expired wait: it is STICKY, kernels behind it return at once, entry points return S2A_ERR_BAD_INDEX until
+ * s2a_device_status() has read it, and the outputs of that call are undefined.
+ */
+enum { S2A_CACHE_BF16 = 0, S2A_CACHE_E4M3 = 1 };
+typedef struct s2a_cache {
+    void* k;            /* 16-byte aligned, like v, k_exp and v_exp */
+    void* v;
+    signed char* k_exp; /* S2A_CACHE_E4M3 only */
+    signed char* v_exp;
+    int type;           /* S2A_CACHE_... */
+    int pages, Hkv, page_size, d;
+} s2a_cache;
+typedef struct s2a_batch {
+    const int* table;   /* [B, width] */
+    const int* starts;  /* [B + 1] */
+    const int* lengths; /* [B] */
+    int width, B, T;
+} s2a_batch;
+
+/*
+ * The new tokens' k and v [T, Hkv, d] (bf16) into their places in the cache.  Into an S2A_CACHE_E4M3 cache each row goes with the
+ * least exponent e >= -126 for which max |x| <= 448 * 2^e, every value rounded once to the nearest code (ties to even).  (Where
+ * e = 120 the largest code is 240, so that the value stays a bf16 number.)  A row with an infinity or a NaN is marked (exp = -128).
+ */
+int s2a_cache_write(const void* k, const void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream);
+
+/*
+ * What the cache holds for the rows of the batch, as bf16 k and v [T, Hkv, d]: the last starts[b+1] - starts[b] tokens of every sequence.
+ */
+int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void* v, void* stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds them already (s2a_cache_write).  A token at position p attends the
+ * cached tokens j <= p of its sequence, all of them (window = 0) or those with j > p - window or j < sinks.  Query head h reads KV head
+ * floor(h / (H / Hkv)); H a multiple of Hkv.
+ *   in : q [T, H, d] bf16        out: o [T, H, d] bf16, rounded once from fp32; lse [H, T] fp32, natural-log sum-exp of the scaled scores
+ * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels, so a tight value is
+ * fastest (1 where every sequence has one new token).
+ * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product.  Cached values at positions that
+ * a token does not see are not assumed finite if they lie past the end of the sequence; a NaN or infinity at a position of the
+ * sequence itself can reach the outputs of the other new tokens of the same call and sequence.  Deterministic: no atomics.
+ */
+int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch, void* o, float* lse, int H, int max_new, float scale,
+                  int window, int sinks, void* stream);
+
+/*
  * Diagnostic (the paper has no counterpart): enqueues one tiny kernel on `stream` in which a single
  * warp waits, with the library's own bounded wait and a limit of `limit_cycles` SM clock cycles
  * (1 .. 2,000,000,000; a million is well under a millisecond), on a barrier that nothing ever arrives
@@ -251,7 +319,8 @@ int s2a_selftest_wait_expiry(long long limit_cycles, void* stream);
 /*
  * Reads (and clears) the device-side status word of the current device.  Synchronises the device.
  * Returns S2A_OK, S2A_ERR_TIMEOUT (a bounded wait expired in some kernel since the last call; if
- * `where` is non-NULL it receives a code naming the kernel and the wait), or S2A_ERR_CUDA.
+ * `where` is non-NULL it receives a code naming the kernel and the wait), S2A_ERR_BAD_INDEX (a batch of the paged cache
+ * held a value out of range; `where`: 1001 starts, 1002 lengths, 1003 table, 1004 more new tokens than max_new), or S2A_ERR_CUDA.
  */
 int s2a_device_status(int* where);
 

@@ -23,10 +23,11 @@ S2A_ERR_UNSUPPORTED = -2
 S2A_ERR_CUDA = -3
 S2A_ERR_TIMEOUT = -4
 S2A_ERR_TOO_LARGE = -5
+S2A_ERR_BAD_INDEX = -6
 
 EXPORTS = [
     "s2a_fwd", "s2a_bwd", "s2a_bwd_workspace_bytes", "s2a_bwd_workspace_bytes_fast", "s2a_fwd_ex", "s2a_bwd_ex", "s2a_bwd_stage", "s2a_fwd_bwd_host",
-    "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed",
+    "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed", "s2a_cache_write", "s2a_cache_read", "s2a_paged_fwd",
     "s2a_selftest_wait_expiry", "s2a_device_status", "s2a_status_string", "s2a_last_cuda_error", "s2a_version",
 ]
 
@@ -75,6 +76,13 @@ def load() -> ctypes.CDLL:
     lib.s2a_bwd_workspace_bytes_fast.restype = Z
     lib.s2a_fwd_bwd_host.argtypes = [P] * 18 + [I] * 6 + [P, Z, P]
     lib.s2a_fwd_bwd_host.restype = I
+    # (ctypes callers of the paged cache's entry points pass its two structs by reference)
+    lib.s2a_cache_write.argtypes = [P, P, P, P, P]
+    lib.s2a_cache_write.restype = I
+    lib.s2a_cache_read.argtypes = [P, P, P, P, P]
+    lib.s2a_cache_read.restype = I
+    lib.s2a_paged_fwd.argtypes = [P, P, P, P, P, I, I, F, I, I, P]
+    lib.s2a_paged_fwd.restype = I
     lib.s2a_selftest_wait_expiry.argtypes = [ctypes.c_longlong, P]
     lib.s2a_selftest_wait_expiry.restype = I
     lib.s2a_device_status.argtypes = [ctypes.POINTER(I)]
@@ -371,13 +379,132 @@ def s2a_fwd_bwd_host(host_in, host_out, dev, G, workspace, stream=None):
     _check(rc, "s2a_fwd_bwd_host")
 
 
+class PagedCache:
+    """A paged cache of keys and values: pools k, v [pages, Hkv, page_size, d] in bf16, or in float8_e4m3fn with the exponents
+    k_exp, v_exp [pages, Hkv, page_size] (int8) of their rows.  It only holds the tensors; the calls check them."""
+
+    __slots__ = ("k", "v", "k_exp", "v_exp")
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+
+    @classmethod
+    def empty(cls, pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
+        """Pools of `pages` pages whose contents are undefined; dtype torch.bfloat16 or torch.float8_e4m3fn."""
+        if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError(f"a cache has dtype torch.bfloat16 or torch.float8_e4m3fn, not {dtype}")
+        shape = (pages, Hkv, page_size, d)
+        pools = [torch.empty(shape, dtype=dtype, device=device) for _ in range(2)]
+        if dtype == torch.float8_e4m3fn:
+            pools += [torch.empty(shape[:3], dtype=torch.int8, device=device) for _ in range(2)]
+        return cls(*pools)
+
+
+def _check_cache(cache, table, starts, lengths):
+    if not isinstance(cache, PagedCache):
+        raise ValueError("cache must be a PagedCache")
+    codes = isinstance(cache.k, torch.Tensor) and cache.k.dtype == torch.float8_e4m3fn
+    dtype = torch.float8_e4m3fn if codes else torch.bfloat16
+    _require(cache.k, dtype, "cache.k")
+    if cache.k.dim() != 4:
+        raise ValueError(f"cache.k must be [pages, Hkv, page_size, d], not {tuple(cache.k.shape)}")
+    device = cache.k.device
+    _require(cache.v, dtype, "cache.v", shape=cache.k.shape, device=device)
+    for t, name in ((cache.k_exp, "cache.k_exp"), (cache.v_exp, "cache.v_exp")):
+        if codes:
+            _require(t, torch.int8, name, shape=cache.k.shape[:3], device=device)
+        elif t is not None:
+            raise ValueError(f"{name} belongs to a cache in float8_e4m3fn")
+    _require(table, torch.int32, "table", device=device)
+    if table.dim() != 2:
+        raise ValueError(f"table must be [B, pages of a sequence], not {tuple(table.shape)}")
+    _require(starts, torch.int32, "starts", shape=(table.shape[0] + 1,), device=device)
+    _require(lengths, torch.int32, "lengths", shape=(table.shape[0],), device=device)
+    return device
+
+
+def _check_rows(x, name, cache, device, heads=None):
+    """x [T, heads, d] beside the cache."""
+    _require(x, torch.bfloat16, name, device=device)
+    d = cache.k.shape[3]
+    if x.dim() != 3 or x.shape[2] != d or (heads is not None and x.shape[1] != heads):
+        raise ValueError(f"{name} must be [T, {'H' if heads is None else heads}, {d}], not {tuple(x.shape)}")
+
+
+def _check_cache_write(cache, k, v, table, starts, lengths):
+    device = _check_cache(cache, table, starts, lengths)
+    _check_rows(k, "k", cache, device, cache.k.shape[1])
+    _require(v, torch.bfloat16, "v", shape=k.shape, device=device)
+
+
+def _check_cache_read(cache, table, starts, lengths, tokens, k, v):
+    device = _check_cache(cache, table, starts, lengths)
+    if tokens < 0 or tokens > 0x7FFFFFFF:
+        raise ValueError(f"tokens must be in [0, 2^31), not {tokens}")
+    for t, name in ((k, "k"), (v, "v")):
+        if t is not None:
+            _require(t, torch.bfloat16, name, shape=(tokens, cache.k.shape[1], cache.k.shape[3]), device=device)
+
+
+def _check_paged_fwd(q, cache, table, starts, lengths, o, lse):
+    device = _check_cache(cache, table, starts, lengths)
+    _check_rows(q, "q", cache, device)
+    if o is not None:
+        _require(o, torch.bfloat16, "o", shape=q.shape, device=device)
+    if lse is not None:
+        _require(lse, torch.float32, "lse", shape=(q.shape[1], q.shape[0]), device=device)
+
+
+def _pools(cache):
+    return (cache.k, cache.v, cache.k_exp, cache.v_exp) if cache.__class__ is PagedCache else (None,) * 4
+
+
+def s2a_cache_write(cache, k, v, table, starts, lengths, stream=None) -> None:
+    """The new tokens' k, v [T, Hkv, d] into the pages of `cache`: sequence b has the rows starts[b] to starts[b+1] - 1, which
+    are the last ones of its lengths[b] cached tokens, and table[b, i] is the page of its positions i * page_size on (int32 CUDA tensors;
+    see include/s2a.h).  Into a cache in float8_e4m3fn every row goes with a power of two of its own."""
+    pools = _pools(cache)
+    hot = _hot or _hot_for(_check_cache_write, cache, k, v, table, starts, lengths)
+    rc = hot.cache_write(*pools, k, v, table, starts, lengths, _given_stream(stream))
+    if rc != S2A_OK:
+        _result(rc, "s2a_cache_write", _check_cache_write, cache, k, v, table, starts, lengths)
+
+
+def s2a_cache_read(cache, table, starts, lengths, tokens=None, k=None, v=None, stream=None):
+    """k, v [tokens, Hkv, d] in bf16: what the cache holds for the last starts[b+1] - starts[b] tokens of every sequence.  `tokens`
+    (the rows of the results, at least starts[B]) is taken from a given k or v."""
+    if tokens is None:
+        given = k if k is not None else v
+        if not isinstance(given, torch.Tensor) or given.dim() != 3:
+            raise ValueError("tokens is needed where neither k nor v is given as [tokens, Hkv, d]")
+        tokens = given.shape[0]
+    pools = _pools(cache)
+    hot = _hot or _hot_for(_check_cache_read, cache, table, starts, lengths, tokens, k, v)
+    return _result(hot.cache_read(*pools, table, starts, lengths, tokens, k, v, _given_stream(stream)), "s2a_cache_read", _check_cache_read, cache,
+                   table, starts, lengths, tokens, k, v)
+
+
+def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, window=0, sinks=0, o=None, lse=None, stream=None):
+    """o [T, H, d] bf16 and lse [H, T] fp32: every new token attends the cached tokens of its sequence up to itself, with `window` > 0
+    the last `window` of them and the sequence's first `sinks`.  `cache` holds the new tokens already (s2a_cache_write); `max_new` is
+    the largest number of new tokens a sequence has (default T; a tight value is fastest, 1 for single tokens).  Rows that belong
+    to no sequence are left as they were."""
+    pools = _pools(cache)
+    hot = _hot or _hot_for(_check_paged_fwd, q, cache, table, starts, lengths, o, lse)
+    r = hot.paged_fwd(q, *pools, table, starts, lengths, max_new, scale, window, sinks, o, lse, _given_stream(stream))
+    if r.__class__ is not tuple:
+        _result(r, "s2a_paged_fwd", _check_paged_fwd, q, cache, table, starts, lengths, o, lse)
+    return r if q.__class__ in _PLAIN else _typed(r, (None if o is not None else q, None))
+
+
 def selftest_wait_expiry(limit_cycles: int = 1_000_000, stream=None) -> None:
     """Enqueue the diagnostic kernel whose bounded wait runs out after `limit_cycles` SM cycles."""
     _check(load().s2a_selftest_wait_expiry(int(limit_cycles), _stream_ptr(stream)), "s2a_selftest_wait_expiry")
 
 
 def device_status():
-    """(status, where): S2A_OK, or S2A_ERR_TIMEOUT with the code of the wait that expired."""
+    """(status, where): S2A_OK, S2A_ERR_TIMEOUT with the code of the wait that expired, or S2A_ERR_BAD_INDEX with that of the value
+    that was out of range."""
     where = ctypes.c_int(0)
     rc = load().s2a_device_status(ctypes.byref(where))
     return int(rc), int(where.value)

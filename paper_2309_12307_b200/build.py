@@ -10,8 +10,8 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libs2a.so")
-SOURCES = ["api.cu", "fwd_kernel.cu", "bwd_kernels.cu"]
-HEADERS = ["host_plan.h", "s2a_params.h", "sm100_ptx.cuh", os.path.join("..", "..", "include", "s2a.h")]
+SOURCES = ["api.cu", "api_paged.cu", "fwd_kernel.cu", "bwd_kernels.cu", "cache_kernels.cu", "paged_fwd.cu"]
+HEADERS = ["host_plan.h", "host_state.h", "paged.h", "paged_device.cuh", "s2a_params.h", "sm100_ptx.cuh", os.path.join("..", "..", "include", "s2a.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -30,7 +30,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, *NVCC_FLAGS, "-shared", "-o", LIB, *srcs]
+    cmd = [nvcc, *NVCC_FLAGS, "--threads", "8", "-shared", "-o", LIB, *srcs]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

@@ -6,10 +6,10 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <mutex>
-
 #include "../../include/s2a.h"
 #include "host_plan.h"
+#include "host_state.h"
+#include "paged.h"
 #include "s2a_params.h"
 #include "sm100_ptx.cuh"
 
@@ -32,19 +32,6 @@ bool g_host_status_registered = false;
 thread_local int tl_last_cuda_error = 0;
 
 constexpr int kMaxDevices = 64;
-struct DeviceState {
-    bool ready = false;
-    int* status_ptr = nullptr;        // device address of g_status_word
-    volatile int* host_word = nullptr;  // this device's mirror, host address
-    int* host_word_dev = nullptr;     // the same word as the device sees it
-    int n_sm = 0;                     // multiprocessors
-    // s2a_fwd_bwd_host only: copy streams and the events that order them against the caller's stream
-    bool host_path_ready = false;
-    cudaStream_t copy_in = nullptr, copy_out = nullptr;
-    cudaEvent_t ev_start = nullptr, ev_done = nullptr, ev_in_done = nullptr;
-    cudaEvent_t ev_qkv = nullptr, ev_do = nullptr, ev_fwd = nullptr, ev_bwd = nullptr;  // recorded again for every chunk
-    std::mutex host_path;  // held by the call that enqueues: its events must not be recorded by another one in between
-};
 DeviceState g_dev[kMaxDevices];
 static_assert(kMaxDevices == kMaxDevicesMirror, "one mirror word per device");
 std::mutex g_dev_mutex;  // guards the one-time set-up of a DeviceState (calls may come from several host threads)
@@ -54,12 +41,13 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn g_encode = nullptr;
 
+}  // namespace
+
 int cuda_fail(cudaError_t e) {
     tl_last_cuda_error = static_cast<int>(e);
     return S2A_ERR_CUDA;
 }
 
-// Per-device set-up: architecture check, shared-memory attributes, address of the status word.
 int prepare_device(DeviceState** out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -86,6 +74,8 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_bwd();
         if (e != cudaSuccess) return cuda_fail(e);
+        e = configure_paged();
+        if (e != cudaSuccess) return cuda_fail(e);
         e = cudaGetSymbolAddress(reinterpret_cast<void**>(&ds.status_ptr), g_status_word);
         if (e != cudaSuccess) return cuda_fail(e);
         if (!g_host_status_registered) {
@@ -102,16 +92,27 @@ int prepare_device(DeviceState** out) {
     return S2A_OK;
 }
 
-int encode_tmap(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+int standing_status(const DeviceState* ds) {
+    const int word = *ds->host_word;
+    return word == 0 ? S2A_OK : word >= kBadIndexCode ? S2A_ERR_BAD_INDEX : S2A_ERR_TIMEOUT;
+}
+
+int encode_tmap(CUtensorMap* tm, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* base, int rank, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box) {
     const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    const CUresult r = g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr,
-                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUresult r = g_encode(tm, type, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         tl_last_cuda_error = static_cast<int>(cudaErrorInvalidValue);
         return S2A_ERR_CUDA;
     }
     return S2A_OK;
+}
+
+namespace {
+
+int encode_bf16(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    return encode_tmap(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, base, rank, dims, strides, box);
 }
 
 // bf16 tensor [B, N, heads, d] viewed as (d, heads, N, B); box = 64 columns x `box_rows` tokens of
@@ -123,7 +124,7 @@ int make_tmap(CUtensorMap* tm, const void* base, int d, int heads, int N, int B,
     const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)N, (cuuint64_t)B};
     const cuuint64_t strides[3] = {(cuuint64_t)d * 2, (cuuint64_t)tok_stride * 2, (cuuint64_t)N * tok_stride * 2};
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)box_rows, 1};
-    return encode_tmap(tm, base, 4, dims, strides, box);
+    return encode_bf16(tm, base, 4, dims, strides, box);
 }
 
 // The same tensor and swizzle with boxes of 64 columns x 128 tokens in the order 0 2 1 3, 4 6 5 7, ... (N % 4 = 0): a
@@ -134,7 +135,7 @@ int make_tmap_exchanged(CUtensorMap* tm, const void* base, int d, int heads, int
     const cuuint64_t dims[5] = {(cuuint64_t)heads * d, 2, 2, (cuuint64_t)N / 4, (cuuint64_t)B};
     const cuuint64_t strides[4] = {2 * tok, tok, 4 * tok, N * tok};
     const cuuint32_t box[5] = {64, 2, 2, kTile / 4, 1};
-    return encode_tmap(tm, base, 5, dims, strides, box);
+    return encode_bf16(tm, base, 5, dims, strides, box);
 }
 
 // variants 2 and 3 of Appendix B exclude each other; no other bits are defined
@@ -142,8 +143,6 @@ bool flags_ok(unsigned flags) {
     return (flags & ~static_cast<unsigned>(S2A_FLAG_LEAK_FREE | S2A_FLAG_SWAP_WRAPPED)) == 0 &&
            flags != (S2A_FLAG_LEAK_FREE | S2A_FLAG_SWAP_WRAPPED);
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int check_shape(int B, int N, int H, int Hkv, int d, int G, float scale, int n_unshifted, int shift) {
     if (B <= 0 || N <= 0 || H <= 0 || Hkv <= 0 || d <= 0 || G <= 0) return S2A_ERR_INVALID_ARG;
@@ -249,7 +248,7 @@ using namespace s2a;
 #pragma GCC visibility push(default)
 extern "C" {
 
-int s2a_version(void) { return 200; }
+int s2a_version(void) { return 300; }
 
 int s2a_last_cuda_error(void) { return tl_last_cuda_error; }
 
@@ -260,6 +259,7 @@ const char* s2a_status_string(int status) {
         case S2A_ERR_UNSUPPORTED: return "unsupported shape or device (need d in {64,128}, G and shift multiples of 4 tokens, N >= 128, sm_100)";
         case S2A_ERR_CUDA: return "a CUDA call failed; see s2a_last_cuda_error()";
         case S2A_ERR_TIMEOUT: return "a bounded device-side wait expired";
+        case S2A_ERR_BAD_INDEX: return "a block table, starts or lengths of an earlier paged call held a value out of range";
         case S2A_ERR_TOO_LARGE: return "B*H*N exceeds the built-in scratch of s2a_bwd_noalloc (see s2a_bwd_noalloc_max_rows)";
         default: return "unknown status";
     }
@@ -281,7 +281,7 @@ int fwd_impl(const void* q, const void* k, const void* v, void* o, float* lse, i
     DeviceState* ds = nullptr;
     rc = prepare_device(&ds);
     if (rc != S2A_OK) return rc;
-    if (*ds->host_word != 0) return S2A_ERR_TIMEOUT;  // an earlier launch gave up: see s2a_device_status()
+    if ((rc = standing_status(ds)) != S2A_OK) return rc;  // an earlier launch gave up: see s2a_device_status()
 
     FwdParams p;
     memset(&p, 0, sizeof p);
@@ -381,7 +381,7 @@ int bwd_impl(const void* q, const void* k, const void* v, const void* o, const f
     DeviceState* ds = nullptr;
     rc = prepare_device(&ds);
     if (rc != S2A_OK) return rc;
-    if (*ds->host_word != 0) return S2A_ERR_TIMEOUT;  // an earlier launch gave up: see s2a_device_status()
+    if ((rc = standing_status(ds)) != S2A_OK) return rc;  // an earlier launch gave up: see s2a_device_status()
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!flags_ok(flags)) return S2A_ERR_INVALID_ARG;
     const Geometry geo = make_geometry(B, N, H, Hkv, G, n_unshifted, shift, flags);
@@ -534,7 +534,7 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
     if (workspace_bytes < s2a_bwd_workspace_bytes(B, N, H, Hkv, d, G)) return S2A_ERR_INVALID_ARG;
     DeviceState* ds = nullptr;
     if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
-    if (*ds->host_word != 0) return S2A_ERR_TIMEOUT;  // an earlier launch gave up: see s2a_device_status()
+    if ((rc = standing_status(ds)) != S2A_OK) return rc;  // an earlier launch gave up: see s2a_device_status()
     cudaError_t e;
     std::lock_guard<std::mutex> lock(ds->host_path);
     if (!ds->host_path_ready) {
@@ -715,7 +715,7 @@ int s2a_device_status(int* where) {
         if (e != cudaSuccess) return cuda_fail(e);
         *ds->host_word = 0;
         if (where) *where = word;
-        return S2A_ERR_TIMEOUT;
+        return word >= kBadIndexCode ? S2A_ERR_BAD_INDEX : S2A_ERR_TIMEOUT;
     }
     if (where) *where = 0;
     return S2A_OK;

@@ -1,0 +1,104 @@
+// Host side of the paged cache's part of include/s2a.h: argument validation and kernel launches.
+#include <math.h>
+#include <string.h>
+
+#include "../../include/s2a.h"
+#include "host_state.h"
+#include "paged.h"
+
+namespace s2a {
+namespace {
+
+constexpr long long kIntMax = 0x7fffffffLL;
+
+int check_cache(const s2a_cache* c) {
+    if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return S2A_ERR_INVALID_ARG;
+    if (c->type != S2A_CACHE_BF16 && c->type != S2A_CACHE_E4M3) return S2A_ERR_INVALID_ARG;
+    if (c->type == S2A_CACHE_E4M3 && (!c->k_exp || !c->v_exp || !aligned16(c->k_exp) || !aligned16(c->v_exp))) return S2A_ERR_INVALID_ARG;
+    if (c->pages <= 0 || c->Hkv <= 0 || c->page_size <= 0 || c->d <= 0) return S2A_ERR_INVALID_ARG;
+    if (c->d != 64 && c->d != 128) return S2A_ERR_UNSUPPORTED;
+    if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) != 0) return S2A_ERR_UNSUPPORTED;
+    if (static_cast<long long>(c->pages) * c->Hkv > kIntMax / c->page_size) return S2A_ERR_UNSUPPORTED;
+    return S2A_OK;
+}
+
+int check_batch(const s2a_batch* b, const s2a_cache* c) {
+    if (!b || !b->table || !b->starts || !b->lengths) return S2A_ERR_INVALID_ARG;
+    if (b->B <= 0 || b->T <= 0 || b->width <= 0) return S2A_ERR_INVALID_ARG;
+    if (static_cast<long long>(b->T) * 2 * c->Hkv > kIntMax || static_cast<long long>(b->width) * c->page_size > kIntMax / 2) return S2A_ERR_UNSUPPORTED;
+    return S2A_OK;
+}
+
+PagedBatch batch_of(const s2a_batch* b) {
+    PagedBatch r;
+    r.table = b->table, r.starts = b->starts, r.lengths = b->lengths, r.width = b->width, r.B = b->B, r.T = b->T;
+    return r;
+}
+
+PagedPool pool_of(const s2a_cache* c) {
+    PagedPool r;
+    r.k = c->k, r.v = c->v, r.k_exp = reinterpret_cast<int8_t*>(c->k_exp), r.v_exp = reinterpret_cast<int8_t*>(c->v_exp);
+    r.pages = c->pages, r.Hkv = c->Hkv, r.page_log2 = 0;
+    while ((1 << r.page_log2) < c->page_size) ++r.page_log2;
+    return r;
+}
+
+int copy_impl(void* k, void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream, bool write) {
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return S2A_ERR_INVALID_ARG;
+    int rc = check_cache(cache);
+    if (rc != S2A_OK) return rc;
+    if ((rc = check_batch(batch, cache)) != S2A_OK) return rc;
+    DeviceState* ds = nullptr;
+    if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
+    if ((rc = standing_status(ds)) != S2A_OK) return rc;
+    CacheCopyParams p;
+    memset(&p, 0, sizeof p);
+    p.batch = batch_of(batch), p.pool = pool_of(cache);
+    p.k = static_cast<__nv_bfloat16*>(k), p.v = static_cast<__nv_bfloat16*>(v);
+    p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
+    const auto launch = write ? launch_cache_write : launch_cache_read;
+    const cudaError_t e = launch(p, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? S2A_OK : cuda_fail(e);
+}
+
+}  // namespace
+}  // namespace s2a
+
+using namespace s2a;
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+int s2a_cache_write(const void* k, const void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream) {
+    return copy_impl(const_cast<void*>(k), const_cast<void*>(v), cache, batch, stream, true);
+}
+
+int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void* v, void* stream) {
+    return copy_impl(k, v, cache, batch, stream, false);
+}
+
+int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch, void* o, float* lse, int H, int max_new, float scale,
+                  int window, int sinks, void* stream) {
+    if (!q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned16(lse)) return S2A_ERR_INVALID_ARG;
+    int rc = check_cache(cache);
+    if (rc != S2A_OK) return rc;
+    if ((rc = check_batch(batch, cache)) != S2A_OK) return rc;
+    if (H <= 0 || H % cache->Hkv != 0 || max_new <= 0 || max_new > batch->T || window < 0 || sinks < 0) return S2A_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !isfinite(scale)) return S2A_ERR_INVALID_ARG;
+    if (static_cast<long long>(batch->T) * H > kIntMax) return S2A_ERR_UNSUPPORTED;
+    DeviceState* ds = nullptr;
+    if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
+    if ((rc = standing_status(ds)) != S2A_OK) return rc;
+    PagedFwdParams p;
+    memset(&p, 0, sizeof p);
+    p.batch = batch_of(batch), p.pool = pool_of(cache);
+    p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
+    p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
+    p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new, p.window = window, p.sinks = sinks;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    const cudaError_t e = launch_paged_fwd(p, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? S2A_OK : cuda_fail(e);
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

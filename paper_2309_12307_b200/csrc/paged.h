@@ -1,0 +1,133 @@
+// The paged cache of keys and values: its layout, where the tokens of a batch lie in it, and the parameter blocks of
+// the kernels that write, read and attend it.
+//
+// A pool holds pages of 2^page_log2 tokens: row (page * Hkv + hk) * page_size + slot is one token of one KV head, d
+// values.  So the tokens of a head lie together within a page, and a run of them is one box of a two-dimensional tensor
+// map over (d, rows) or one piece of memory.
+//
+// The new tokens of B sequences are rows starts[b] .. starts[b+1]-1 of one tensor; sequence b has lengths[b] tokens
+// in the cache, of which they are the last ones.  table[b * width + i] is the page of its tokens i * page_size on.
+// All three arrays are read on the device, so a captured graph follows what they hold when it is replayed, and what
+// they hold is checked there: a kernel skips what is out of range and reports it (kBadIndexCode), it never follows it.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "s2a_params.h"
+
+namespace s2a {
+
+// Codes in the device status word for values out of range, beside those of waits that ran out (WaitCode).
+constexpr int kBadIndexCode = 1000;
+enum BadIndex : int {
+    kBadStarts = kBadIndexCode + 1,  // starts out of [0, T] or falling
+    kBadLength = kBadIndexCode + 2,  // a length below the sequence's new tokens or above what its row of the table holds
+    kBadPage = kBadIndexCode + 3,    // a page that is not in the pool
+    kBadNew = kBadIndexCode + 4,     // more new tokens than the caller said a sequence has at most
+};
+
+struct PagedBatch {
+    const int* table;    // [B, width]
+    const int* starts;   // [B + 1]
+    const int* lengths;  // [B]
+    int width, B, T;
+};
+
+struct PagedPool {
+    void* k;
+    void* v;
+    int8_t* k_exp;  // [pages, Hkv, page_size]: value = code * 2^exp, kExpNotFinite = a row that is NaN throughout
+    int8_t* v_exp;
+    int pages, Hkv, page_log2;
+};
+constexpr int kExpLeast = -126, kExpNotFinite = -128;
+
+struct Sequence {
+    int row0, n, length;  // first row, new tokens, tokens in the cache
+};
+
+#if defined(__CUDA_ARCH__)
+#define S2A_LOAD(p) __ldg(p)
+#else
+#define S2A_LOAD(p) (*(p))
+#endif
+
+// Sequence b of the batch; 0, or the code of what is wrong with it (then n = 0).  most_new: new tokens a sequence has at most.
+__host__ __device__ inline int sequence_of(const PagedBatch& batch, int page_log2, int most_new, int b, Sequence* s) {
+    const int row0 = S2A_LOAD(batch.starts + b), end = S2A_LOAD(batch.starts + b + 1), length = S2A_LOAD(batch.lengths + b);
+    s->row0 = row0, s->n = 0, s->length = length;
+    if (row0 < 0 || end < row0 || end > batch.T) return kBadStarts;
+    if (length < end - row0 || length > static_cast<long long>(batch.width) << page_log2) return kBadLength;
+    if (end - row0 > most_new) return kBadNew;
+    s->n = end - row0;
+    return 0;
+}
+
+// The last sequence that starts at or before `row`, which need not reach it.
+__host__ __device__ inline int find_sequence(const int* starts, int B, int row) {
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (S2A_LOAD(starts + mid) <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Page of the tokens i * page_size on of sequence b, or -1 where the table holds none of the pool's.
+__host__ __device__ inline int page_of(const PagedBatch& batch, int pages, int b, int i) {
+    const int page = S2A_LOAD(batch.table + static_cast<long long>(b) * batch.width + i);
+    return static_cast<unsigned>(page) < static_cast<unsigned>(pages) ? page : -1;
+}
+
+// Row of the pools of position `pos` of sequence b in KV head 0 (head hk: + hk << page_log2), or -1.
+__host__ __device__ inline long long pool_row(const PagedBatch& batch, const PagedPool& pool, int b, int pos) {
+    const int page = page_of(batch, pool.pages, b, pos >> pool.page_log2);
+    if (page < 0) return -1;
+    return ((static_cast<long long>(page) * pool.Hkv) << pool.page_log2) + (pos & ((1 << pool.page_log2) - 1));
+}
+
+// The power of two of a row whose largest magnitude has these bf16 bits: the least e >= kExpLeast with
+// max |x| <= 448 * 2^e, 448 = 1.75 * 2^8 being the largest 8-bit float.  A power of two costs nothing (the 8-bit values
+// have an exponent of their own, so none of their three bits of fraction is lost) and makes the product with 2^-e, and
+// the value that a code stands for, exact: a bf16 value.
+__host__ __device__ inline int row_exponent(uint32_t most_bits) {
+    if (most_bits >= 0x7f80u) return kExpNotFinite;  // an infinity or a NaN
+    const int e = static_cast<int>(most_bits >> 7) - 127 - 8 + ((most_bits & 0x7fu) > 0x60u ? 1 : 0);
+    return e < kExpLeast ? kExpLeast : e;
+}
+
+struct CacheCopyParams {
+    PagedBatch batch;
+    PagedPool pool;
+    __nv_bfloat16* k;  // [T, Hkv, d]: read by the writing kernel, written by the reading one
+    __nv_bfloat16* v;
+    int* status;
+    int* host_status;
+    int tokens_per_block;
+};
+
+struct alignas(64) PagedFwdParams {
+    PagedBatch batch;
+    PagedPool pool;
+    const __nv_bfloat16* q;  // [T, H, d]
+    __nv_bfloat16* o;        // [T, H, d]
+    float* lse;              // [H, T]
+    int* status;
+    int* host_status;
+    int H, rep, most_new;
+    int window, sinks;       // window 0: none
+    float scale_log2;
+    FastDiv by_rep;
+};
+
+// Enqueue on `stream`; return the launch error, if any.
+cudaError_t launch_cache_write(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t configure_paged();
+
+}  // namespace s2a

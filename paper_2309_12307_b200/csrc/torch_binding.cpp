@@ -317,6 +317,112 @@ py::object bwd_packed(py::handle qkv_, py::handle o_, py::handle lse_, py::handl
 }
 
 // ---------------------------------------------------------------------------------------------
+// the paged cache
+// ---------------------------------------------------------------------------------------------
+// Pools [pages, Hkv, page_size, d] of bf16 or 8-bit floats, for the latter exponents [pages, Hkv, page_size]; `device`: where the
+// first pool is, current while the object lives.
+struct PagedArgs {
+    Arg k, v, k_exp, v_exp, table, starts, lengths;
+    s2a_cache cache = {};
+    s2a_batch batch = {};
+    c10::cuda::OptionalCUDAGuard device;
+    PagedArgs(py::handle k_, py::handle v_, py::handle k_exp_, py::handle v_exp_, py::handle table_, py::handle starts_, py::handle lengths_)
+        : k(k_), v(v_), k_exp(k_exp_), v_exp(v_exp_), table(table_), starts(starts_), lengths(lengths_) {}
+    bool dense(const Tensor& t, int64_t dim, at::ScalarType type) const { return is_dense(t, type) && t.dim() == dim && t.device() == k.t.device(); }
+    // false: binding.py names what is wrong
+    bool check() {
+        for (const Arg* a : {&k, &v, &k_exp, &v_exp, &table, &starts, &lengths})
+            if (a->bad) return false;
+        if (!k.t.defined()) return false;
+        const bool codes = k.t.scalar_type() == at::kFloat8_e4m3fn;
+        const auto type = codes ? at::kFloat8_e4m3fn : at::kBFloat16;
+        if (!dense(k.t, 4, type) || !dense(v.t, 4, type) || v.t.sizes() != k.t.sizes() || k_exp.given != codes || v_exp.given != codes) return false;
+        if (codes && !(dense(k_exp.t, 3, at::kChar) && dense(v_exp.t, 3, at::kChar) && k_exp.t.sizes() == k.t.sizes().slice(0, 3) && v_exp.t.sizes() == k_exp.t.sizes()))
+            return false;
+        if (!dense(table.t, 2, at::kInt) || !dense(starts.t, 1, at::kInt) || !dense(lengths.t, 1, at::kInt)) return false;
+        if (starts.t.size(0) != table.t.size(0) + 1 || lengths.t.size(0) != table.t.size(0)) return false;
+        for (int64_t x : {k.t.size(0), k.t.size(1), k.t.size(2), k.t.size(3), table.t.size(0), table.t.size(1)})
+            if (!fits_int(x)) return false;
+        cache.k = k.t.data_ptr(), cache.v = v.t.data_ptr();
+        cache.k_exp = codes ? static_cast<signed char*>(k_exp.t.data_ptr()) : nullptr;
+        cache.v_exp = codes ? static_cast<signed char*>(v_exp.t.data_ptr()) : nullptr;
+        cache.type = codes ? S2A_CACHE_E4M3 : S2A_CACHE_BF16;
+        cache.pages = k.t.size(0), cache.Hkv = k.t.size(1), cache.page_size = k.t.size(2), cache.d = k.t.size(3);
+        batch.table = static_cast<const int*>(table.t.data_ptr()), batch.starts = static_cast<const int*>(starts.t.data_ptr());
+        batch.lengths = static_cast<const int*>(lengths.t.data_ptr());
+        batch.B = table.t.size(0), batch.width = table.t.size(1);
+        device.reset_device(k.t.device());
+        return true;
+    }
+    // x [T, heads, d] of bf16 beside the cache
+    bool rows(const Tensor& x) const { return dense(x, 3, at::kBFloat16) && x.size(2) == cache.d && fits_int(x.size(0)) && fits_int(x.size(1)); }
+};
+
+py::object cache_write(py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle k_, py::handle v_, py::handle table, py::handle starts,
+                       py::handle lengths, std::optional<int64_t> stream) {
+    PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
+    Arg k(k_), v(v_);
+    if (k.bad || v.bad || !a.check() || !a.rows(k.t) || k.t.size(1) != a.cache.Hkv || !a.rows(v.t) || v.t.sizes() != k.t.sizes()) return py::none();
+    a.batch.T = k.t.size(0);
+    CallStream on(stream, k.t);
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_cache_write(k.t.data_ptr(), v.t.data_ptr(), &a.cache, &a.batch, st);
+    }
+    return py::int_(rc);
+}
+
+py::object cache_read(py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle table, py::handle starts, py::handle lengths, int64_t tokens,
+                      py::handle k_, py::handle v_, std::optional<int64_t> stream) {
+    PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
+    Arg k(k_), v(v_);
+    if (k.bad || v.bad || !a.check() || !fits_int(tokens)) return py::none();
+    a.batch.T = static_cast<int>(tokens);
+    CallStream on(stream, a.k.t);
+    const at::DimVector shape{tokens, a.cache.Hkv, a.cache.d};
+    for (Arg* x : {&k, &v}) {
+        if (!x->given) x->t = on.output(at::empty(shape, a.k.t.options().dtype(at::kBFloat16)));
+        else if (!same_shape(x->t, shape, a.k.t, at::kBFloat16)) return py::none();
+    }
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_cache_read(&a.cache, &a.batch, k.t.data_ptr(), v.t.data_ptr(), st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    return py::make_tuple(k.t, v.t);
+}
+
+py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle table, py::handle starts, py::handle lengths,
+                     std::optional<int64_t> max_new, std::optional<double> scale, int64_t window, int64_t sinks, py::handle o_, py::handle lse_,
+                     std::optional<int64_t> stream) {
+    PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
+    Arg q(q_), o(o_), lse(lse_);
+    if (q.bad || o.bad || lse.bad || !a.check() || !a.rows(q.t)) return py::none();
+    const int64_t T = q.t.size(0), H = q.t.size(1), most = max_new ? *max_new : T;
+    // what does not fit an int is refused by the library as any negative size is
+    auto as_int = [](int64_t x) { return fits_int(x) ? static_cast<int>(x) : -1; };
+    a.batch.T = static_cast<int>(T);
+    CallStream on(stream, q.t);
+    if (!o.given) o.t = on.output(new_like(q.t));
+    else if (!same_shape(o.t, q.t.sizes(), q.t, at::kBFloat16)) return py::none();
+    if (!lse.given) lse.t = on.output(at::empty({H, T}, q.t.options().dtype(at::kFloat)));
+    else if (!same_shape(lse.t, {H, T}, q.t, at::kFloat)) return py::none();
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_paged_fwd(q.t.data_ptr(), &a.cache, &a.batch, o.t.data_ptr(), static_cast<float*>(lse.t.data_ptr()), static_cast<int>(H), as_int(most),
+                           static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(a.cache.d))), as_int(window), as_int(sinks), st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    return py::make_tuple(o.t, lse.t);
+}
+
+// ---------------------------------------------------------------------------------------------
 // differentiable front end
 // ---------------------------------------------------------------------------------------------
 // Raises binding.S2AError; callable from the threads of the autograd engine.
@@ -395,5 +501,8 @@ PYBIND11_MODULE(_s2a_torch, m) {
     m.def("bwd_ex", &bwd_ex);
     m.def("bwd_packed", &bwd_packed);
     m.def("bwd_noalloc", &bwd_noalloc);
+    m.def("cache_write", &cache_write);
+    m.def("cache_read", &cache_read);
+    m.def("paged_fwd", &paged_fwd);
     m.def("s2_attn", torch::wrap_pybind_function(&s2_attn));
 }

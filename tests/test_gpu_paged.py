@@ -1,0 +1,379 @@
+"""The paged cache on the GPU against its definition in 64 bits (oracle/paged_torch.py)."""
+import math
+
+import pytest
+import torch
+
+from oracle import paged_torch as ref
+from paper_2309_12307_b200 import binding as s2a
+
+pytestmark = pytest.mark.gpu
+BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
+
+
+class Job:
+    """A batch with its cache.  `sizes`: (new tokens, length) of every sequence; `before`, `after`: rows of no sequence.  What the
+    sequences do not hold is NaN (in 8 bits: rows marked as NaN), and so are the rows of no sequence."""
+
+    def __init__(self, sizes, H=4, Hkv=2, d=64, page=16, dtype=BF16, before=0, after=0, seed=0, wider=0, normal=1.0):
+        g = torch.Generator().manual_seed(seed)
+        self.sizes, self.H, self.Hkv, self.d, self.page, self.dtype = sizes, H, Hkv, d, page, dtype
+        B = len(sizes)
+        starts = [before]
+        for n, _ in sizes:
+            starts.append(starts[-1] + n)
+        self.T = starts[-1] + after
+        need = [-(-length // page) for _, length in sizes]
+        pages = sum(need) + 2
+        order = torch.randperm(pages, generator=g).tolist()
+        table = torch.full((B, max(1, max(need)) + wider), -1, dtype=torch.int32)
+        for b, n in enumerate(need):
+            table[b, :n] = torch.tensor([order.pop() for _ in range(n)], dtype=torch.int32)
+        self.table, self.starts, self.lengths = (x.cuda() for x in (table, torch.tensor(starts, dtype=torch.int32),
+                                                                     torch.tensor([length for _, length in sizes], dtype=torch.int32)))
+        self.cache = s2a.PagedCache.empty(pages, Hkv, page, d, dtype)
+        for pool in (self.cache.k, self.cache.v):
+            pool.view(torch.uint8).fill_(255)  # NaN in either type
+        if dtype == E4M3:
+            self.cache.k_exp.fill_(ref.NOT_FINITE), self.cache.v_exp.fill_(ref.NOT_FINITE)
+        # every token of the sequences, written as one batch of new tokens
+        all_starts = [0]
+        for _, length in sizes:
+            all_starts.append(all_starts[-1] + length)
+        self.all_starts = torch.tensor(all_starts, dtype=torch.int32).cuda()
+        self.all_k, self.all_v = ((torch.randn(max(1, all_starts[-1]), Hkv, d, generator=g) * normal).to(BF16).cuda() for _ in range(2))
+        s2a.s2a_cache_write(self.cache, self.all_k, self.all_v, self.table, self.all_starts, self.lengths)
+        self.q = torch.randn(self.T, H, d, generator=g).to(BF16)
+        self.q[:before] = math.nan
+        self.q[starts[-1]:] = math.nan
+        self.q = self.q.cuda()
+
+    @property
+    def where(self):
+        return self.table, self.starts, self.lengths
+
+    def host_cache(self):
+        out = {}
+        for x in ("k", "v"):
+            pool = getattr(self.cache, x)
+            out[x] = pool.view(torch.uint8).cpu() if self.dtype == E4M3 else pool.cpu()
+            if self.dtype == E4M3:
+                out[x + "_exp"] = getattr(self.cache, x + "_exp").cpu()
+        return out
+
+    def rows(self):
+        """Rows that belong to a sequence."""
+        inside = torch.zeros(self.T, dtype=torch.bool)
+        inside[int(self.starts[0]):int(self.starts[-1])] = True
+        return inside
+
+    def attend(self, **kw):
+        kw.setdefault("max_new", max(1, max(n for n, _ in self.sizes)))
+        return s2a.s2a_paged_fwd(self.q, self.cache, *self.where, **kw)
+
+    def check(self, scale=None, window=0, sinks=0, **kw):
+        scale = 1 / math.sqrt(self.d) if scale is None else scale
+        mark = torch.full((self.T, self.H, self.d), 7.0, dtype=BF16, device="cuda")
+        o, lse = self.attend(scale=scale, window=window, sinks=sinks, o=mark, lse=torch.full((self.H, self.T), 7.0, device="cuda"), **kw)
+        torch.cuda.synchronize()
+        assert s2a.device_status() == (0, 0)
+        want, want_lse, size = ref.paged_fwd(self.q.cpu(), self.host_cache(), self.table.cpu(), self.starts.cpu(), self.lengths.cpu(), scale, window, sinks)
+        compare(o.cpu(), lse.cpu(), want, want_lse, size, self.rows(), max(length for _, length in self.sizes), self.d, scale,
+                float(self.q.cpu()[self.rows()].double().norm(dim=-1).max()) if self.rows().any() else 0.0, self.all_k)
+
+
+def compare(o, lse, want, want_lse, size, inside, longest, d, scale, q_norm, k):
+    """Rows of no sequence untouched; the others as near as the roundings allow: weights and results to bf16 (half a step, 2^-8, each),
+    scores as sums of d products in 32 bits (each addition 2^-24 of a partial sum, that at most |q| |k|), sums over the keys likewise."""
+    assert (o[~inside] == 7).all() and (lse[:, ~inside] == 7).all()
+    o, want, size = o[inside].double(), want[inside], size[inside]
+    score = d * 2.0**-24 * scale * q_norm * float(k.double().norm(dim=-1).max()) + 2.0**-20
+    slack = longest * 2.0**-24
+    off = (o - want).abs()
+    allowed = (2.0**-8 + 2 * score + slack) * size + 2.0**-8 * (want.abs() + 2.0**-8 * size) + 1e-30
+    assert (off <= allowed).all(), float((off / allowed).max())
+    off = (lse[:, inside].double() - want_lse[:, inside]).abs()
+    assert (off <= score + slack + want_lse[:, inside].abs() * 2.0**-22).all(), float(off.max())
+
+
+# ---------------------------------------------------------------------------------------------- writing and reading
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("Hkv,d,page", [(1, 64, 16), (2, 128, 16), (5, 64, 64), (8, 128, 128), (40, 128, 32), (3, 128, 256)])
+def test_written_tokens_come_back_and_nothing_else_changes(dtype, Hkv, d, page):
+    job = Job([(3, 50), (0, 0), (1, 1), (0, 17), (33, 33), (page, 3 * page), (1, page + 1)], Hkv=Hkv, H=Hkv, d=d, page=page, dtype=dtype, before=2, after=3)
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(job.T, Hkv, d, generator=g).to(BF16) for _ in range(2))
+    k[4] *= 2.0**-128  # subnormal numbers
+    v[5] *= 2.0**119
+    v[6] = 0
+    k[7] = 3.5  # 448 * 2^-7
+    before = job.host_cache()
+    s2a.s2a_cache_write(job.cache, k.cuda(), v.cuda(), *job.where)
+    out = [torch.full((job.T, Hkv, d), 7.0, dtype=BF16, device="cuda") for _ in range(2)]
+    back = s2a.s2a_cache_read(job.cache, *job.where, k=out[0], v=out[1])
+    assert back[0] is out[0] and back[1] is out[1]
+    after = job.host_cache()
+    assert s2a.device_status() == (0, 0)
+    starts, table = job.starts.tolist(), job.table.cpu()
+    new = torch.zeros(after["k"].shape[:3], dtype=torch.bool)
+    inside = job.rows()
+    for x, rows, got in (("k", k, back[0].cpu()), ("v", v, back[1].cpu())):
+        assert (got[~inside] == 7).all()
+        for b, (n, length) in enumerate(job.sizes):
+            for i in range(n):
+                pos = length - n + i
+                at = int(table[b, pos // page]), slice(None), pos % page
+                new[at] = True
+                for hk in range(Hkv):
+                    row = rows[starts[b] + i, hk]
+                    cell = after[x][at[0], hk, at[2]]
+                    if dtype == BF16:
+                        assert torch.equal(cell, row) and torch.equal(got[starts[b] + i, hk], row)
+                    else:
+                        codes, e = ref.quantised_row(row)
+                        assert torch.equal(cell, codes) and int(after[x + "_exp"][at[0], hk, at[2]]) == e
+                        assert torch.equal(got[starts[b] + i, hk].double(), ref.code_values()[codes.long()] * math.ldexp(1.0, e))
+    for x in after:
+        changed = (after[x].view(torch.uint8) != before[x].view(torch.uint8)) if after[x].dim() == 3 else (after[x].view(torch.uint8) != before[x].view(torch.uint8)).any(-1)
+        assert not (changed & ~new).any(), x
+
+
+def test_every_finite_bf16_number_is_rounded_to_the_nearest_code():
+    every = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(BF16)
+    every = every[torch.isfinite(every.float())]
+    size = every.float().abs()
+    # rows of one magnitude keep all their bits in reach, rows of random ones have values far below the largest
+    order = torch.argsort(size)
+    rows = torch.cat((every[order], every[torch.randperm(len(every), generator=torch.Generator().manual_seed(0))]))
+    rows = rows[:len(rows) // 64 * 64].view(-1, 1, 64)
+    T = len(rows)
+    cache = s2a.PagedCache.empty(-(-T // 16), 1, 16, 64, E4M3)
+    table = torch.arange(cache.k.shape[0], dtype=torch.int32, device="cuda")[None]
+    starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, T], [T]))
+    s2a.s2a_cache_write(cache, rows.cuda(), rows.cuda(), table, starts, lengths)
+    k, v = s2a.s2a_cache_read(cache, table, starts, lengths, tokens=T)
+    codes, e = cache.k.view(torch.uint8).cpu().view(-1, 64), cache.k_exp.cpu().view(-1)
+    assert torch.equal(k, v) and torch.isfinite(k.float()).all()
+    for t in range(T):
+        want, want_e = ref.quantised_row(rows[t, 0])
+        assert int(e[t]) == want_e and torch.equal(codes[t], want), t
+    # what these codes stand for are bf16 numbers
+    values = ref.code_values()[codes[:T].long()] * torch.exp2(e[:T].double())[:, None]
+    assert torch.equal(k.cpu()[:, 0].double(), values)
+
+
+def test_a_row_that_is_not_finite_reads_back_as_nan():
+    job = Job([(6, 20)], Hkv=2, H=2, d=64, dtype=E4M3)
+    k = torch.randn(6, 2, 64).to(BF16)
+    k[1, 0, 5], k[2, 1, 0], k[3, 0, 63] = math.inf, math.nan, -math.inf
+    s2a.s2a_cache_write(job.cache, k.cuda(), k.cuda(), *job.where)
+    got, _ = s2a.s2a_cache_read(job.cache, *job.where, tokens=6)
+    bad = torch.zeros(6, 2, dtype=torch.bool)
+    bad[1, 0] = bad[2, 1] = bad[3, 0] = True
+    nan = torch.isnan(got.cpu().float())
+    assert nan[bad].all() and not nan[~bad].any() and s2a.device_status() == (0, 0)
+
+
+# ---------------------------------------------------------------------------------------------- attention
+FORMS = [  # (H, Hkv, d, page)
+    (4, 4, 64, 16), (4, 2, 128, 16), (8, 1, 64, 64), (6, 2, 128, 128), (5, 5, 64, 32), (14, 2, 128, 256), (16, 1, 128, 16), (20, 1, 64, 16), (40, 1, 128, 64),
+]
+SINGLE = [(1, 1), (1, 2), (1, 15), (1, 16), (1, 17), (1, 31), (0, 40), (1, 64), (1, 127), (1, 128), (1, 129), (1, 300), (0, 0)]
+DRAFTS = [(2, 2), (4, 100), (3, 129), (1, 260), (0, 9), (4, 17), (2, 128)]
+PIECES = [(1, 5), (130, 130), (17, 300), (128, 256), (129, 140), (0, 70), (257, 400), (64, 64), (1, 333)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("sizes", [SINGLE, DRAFTS, PIECES], ids=["single", "drafts", "pieces"])
+def test_attention(sizes, form, dtype):
+    H, Hkv, d, page = form
+    if sizes is PIECES and H > 8:
+        sizes = [(1, 5), (131, 150), (40, 300), (0, 70)]
+    Job(sizes, H=H, Hkv=Hkv, d=d, page=page, dtype=dtype, before=1, after=3, wider=2).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (17, 0), (100, 16), (128, 128), (129, 1), (200, 130), (1000, 4), (64, 1000)])
+@pytest.mark.parametrize("sizes", [SINGLE, DRAFTS, PIECES], ids=["single", "drafts", "pieces"])
+def test_attention_with_a_window_and_the_first_tokens(sizes, window, sinks, dtype):
+    Job(sizes, H=4, Hkv=2, d=64, page=16, dtype=dtype, after=1).check(window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("sizes", [SINGLE, PIECES], ids=["single", "pieces"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 3)])
+def test_large_scores(sizes, window, sinks, dtype):
+    """Scores of hundreds: rows whose weights all lie on one key, and a running maximum that grows along the way."""
+    Job(sizes, H=2, Hkv=1, d=128, page=32, dtype=dtype, normal=30.0).check(window=window, sinks=sinks, scale=0.2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("new", [1, 70])
+def test_a_long_sequence(new, dtype):
+    """Many keys for few rows: the work on one sequence is split over the keys."""
+    Job([(new, 5000)], H=2, Hkv=1, d=64, page=64, dtype=dtype).check()
+    Job([(new, 5000)], H=2, Hkv=1, d=64, page=64, dtype=dtype).check(window=3001, sinks=5)
+
+
+def test_a_loose_bound_on_the_new_tokens_changes_no_more_than_roundings():
+    for sizes in (SINGLE, DRAFTS):
+        job = Job(sizes, H=4, Hkv=2, d=128)
+        job.check(max_new=job.T)
+        job.check(max_new=min(20, job.T))
+
+
+def test_the_same_call_gives_the_same_bits():
+    for sizes, dtype in ((SINGLE, BF16), (DRAFTS, E4M3), (PIECES, BF16), (PIECES, E4M3)):
+        job = Job(sizes, H=8, Hkv=2, d=128, dtype=dtype)
+        first = [t.clone() for t in job.attend()]
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(first, job.attend()))
+
+
+def test_sequences_may_share_pages():
+    job = Job([(1, 200), (1, 200), (1, 130)], H=4, Hkv=4, d=64, page=64)
+    job.table[1] = job.table[0]
+    job.table[2, :2] = job.table[0, :2]
+    job.check()
+
+
+# ---------------------------------------------------------------------------------------------- as they are used
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_a_prompt_in_pieces_and_then_single_tokens(dtype):
+    """Two prompts go into the cache in pieces and are continued token by token; the result is that of the causal attention of the whole
+    sequences (s2a_fwd_ex with one group), on the values that the cache stands for."""
+    H, Hkv, d, page, N = 8, 2, 64, 16, 384
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(2, N, h, d, generator=g).to(BF16).cuda() for h in (H, Hkv, Hkv))
+    cache = s2a.PagedCache.empty(2 * N // page, Hkv, page, d, dtype)
+    table = torch.randperm(2 * N // page, generator=g).to(torch.int32).view(2, -1).cuda()
+    o = torch.empty_like(q)
+    lse = torch.empty((2, H, N), device="cuda")
+    done = [0, 0]
+    for step in [(200, 1), (129, 255), (0, 100)] + [(1, 1)] * 28 + [(27, 0)]:
+        rows = [slice(done[b], done[b] + step[b]) for b in range(2)]
+        starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, step[0], sum(step)], [done[b] + step[b] for b in range(2)]))
+        new = [torch.cat([x[b, rows[b]] for b in range(2)]) for x in (q, k, v)]
+        s2a.s2a_cache_write(cache, new[1], new[2], table, starts, lengths)
+        got, got_lse = s2a.s2a_paged_fwd(new[0], cache, table, starts, lengths, max_new=max(step))
+        for b, at in enumerate((slice(0, step[0]), slice(step[0], sum(step)))):
+            o[b, rows[b]], lse[b, :, rows[b]] = got[at], got_lse[:, at]
+            done[b] += step[b]
+    assert done == [N, N]
+    all_starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, N, 2 * N], [N, N]))
+    held = [x.view(2, N, Hkv, d) for x in s2a.s2a_cache_read(cache, table, all_starts, lengths, tokens=2 * N)]
+    if dtype == BF16:
+        assert torch.equal(held[0], k) and torch.equal(held[1], v)
+    want, want_lse = s2a.s2a_fwd_ex(q, *held, N, n_unshifted=H, shift=0)
+    assert s2a.device_status() == (0, 0)
+    # two results that each have rounded weights and themselves to bf16: 4 * 2^-8 of sum w |v|, which is at most max |v|
+    assert float((o.float() - want.float()).abs().max()) <= 4 * 2.0**-8 * float(held[1].float().abs().max())
+    assert float((lse - want_lse).abs().max()) <= 2e-4
+
+
+def test_a_captured_step_follows_the_lengths():
+    """A decoding loop as one captured step: starts, lengths and the table are read when the graph runs."""
+    job = Job([(1, 100), (1, 30), (1, 1)], H=4, Hkv=2, d=128, wider=2)
+    most = job.table.shape[1] * job.page
+    for b in range(3):  # pages for every position of the table
+        job.table[b] = torch.arange(job.table.shape[1], dtype=torch.int32) + b * job.table.shape[1]
+    job.cache = s2a.PagedCache.empty(3 * job.table.shape[1], 2, 16, 128)
+    job.cache.k.normal_(), job.cache.v.normal_()
+    new_k, new_v = (torch.randn(3, 2, 128, device="cuda").to(BF16) for _ in range(2))
+
+    def step():
+        s2a.s2a_cache_write(job.cache, new_k, new_v, *job.where)
+        return s2a.s2a_paged_fwd(job.q, job.cache, *job.where, max_new=1)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for lengths in ([100, 30, 1], [101, 31, 2], [most, 1, 57]):
+        job.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+        job.q.normal_(), new_k.normal_(), new_v.normal_()
+        graph.replay()
+        replayed = [t.clone() for t in got]
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, want))
+    assert s2a.device_status() == (0, 0)
+
+
+def test_another_stream():
+    for sizes in (SINGLE, PIECES):
+        job = Job(sizes, H=4, Hkv=2, d=64)
+        want = [t.clone() for t in job.attend()]
+        rows = job.rows().cuda()
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(50_000_000)
+        got = job.attend(stream=side)
+        side.synchronize()
+        assert torch.equal(got[0][rows], want[0][rows]) and torch.equal(got[1][:, rows], want[1][:, rows])
+
+
+def test_results_have_the_class_of_q():
+    class Marked(torch.Tensor):
+        pass
+
+    job = Job([(1, 20)])
+    o, lse = s2a.s2a_paged_fwd(job.q.as_subclass(Marked), job.cache, *job.where)
+    assert type(o) is Marked and type(lse) is torch.Tensor
+    assert type(s2a.s2a_cache_read(job.cache, *job.where, tokens=1)[0]) is torch.Tensor
+
+
+def test_refusals_reach_the_caller():
+    job = Job([(2, 20)], H=4, Hkv=2)
+    for kw in (dict(max_new=3), dict(max_new=0), dict(scale=-1.0), dict(window=-1), dict(sinks=1 << 40)):
+        with pytest.raises(s2a.S2AError) as e:
+            job.attend(**kw)
+        assert e.value.status == s2a.S2A_ERR_INVALID_ARG
+    with pytest.raises(s2a.S2AError) as e:
+        s2a.s2a_paged_fwd(job.q[:, :3].contiguous(), job.cache, *job.where)  # 3 heads on 2
+    assert e.value.status == s2a.S2A_ERR_INVALID_ARG
+    with pytest.raises(ValueError, match="q must be a CUDA tensor"):
+        s2a.s2a_paged_fwd(job.q.cpu(), job.cache, *job.where)
+    with pytest.raises(ValueError, match="lse must have dtype"):
+        job.attend(lse=torch.empty((4, 2), dtype=torch.float64, device="cuda"))
+    with pytest.raises(ValueError, match="tokens must be"):
+        s2a.s2a_cache_read(job.cache, *job.where, tokens=-1)
+    cache = s2a.PagedCache.empty(2, 2, 24, 64)
+    with pytest.raises(s2a.S2AError) as e:
+        s2a.s2a_paged_fwd(job.q, cache, *job.where)
+    assert e.value.status == s2a.S2A_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("sizes", [[(1, 40), (1, 100)], [(1, 40), (150, 190)]], ids=["single", "pieces"])
+@pytest.mark.parametrize("what", ["page", "negative page", "length", "short length", "starts", "new"])
+def test_values_out_of_range_are_reported_and_not_followed(what, sizes, dtype):
+    job = Job(sizes, H=4, Hkv=2, d=64, dtype=dtype)
+    kw, code = {}, {"page": 1003, "negative page": 1003, "length": 1002, "short length": 1002, "starts": 1001, "new": 1004}[what]
+    n = sizes[1][0]
+    if what == "page":
+        job.table[1, 1] = job.cache.k.shape[0]
+    elif what == "negative page":
+        job.table[1, 1] = -1
+    elif what == "length":
+        job.lengths[1] = job.table.shape[1] * job.page + 1
+    elif what == "short length":
+        job.lengths[1] = n - 1
+    elif what == "starts":
+        job.starts[1] = job.T + 1
+    else:
+        job.starts.copy_(torch.tensor([0, 0, n + 1], dtype=torch.int32))
+        kw = dict(max_new=n)
+    job.attend(**kw)
+    torch.cuda.synchronize()
+    with pytest.raises(s2a.S2AError) as e:  # nothing more until it has been read
+        job.attend()
+    assert e.value.status == s2a.S2A_ERR_BAD_INDEX
+    assert s2a.device_status() == (s2a.S2A_ERR_BAD_INDEX, code) and s2a.device_status() == (0, 0)
+    if what != "new":
+        bad_read = dict(k=torch.zeros(job.T, 2, 64, dtype=BF16, device="cuda"), v=torch.zeros(job.T, 2, 64, dtype=BF16, device="cuda"))
+        s2a.s2a_cache_read(job.cache, *job.where, **bad_read)
+        # the bad page holds none of the new tokens
+        assert s2a.device_status() == ((0, 0) if "page" in what else (s2a.S2A_ERR_BAD_INDEX, code))
