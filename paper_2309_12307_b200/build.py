@@ -10,7 +10,7 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libs2a.so")
-SOURCES = ["api.cu", "api_paged.cu", "fwd_kernel.cu", "bwd_kernels.cu", "cache_kernels.cu", "paged_fwd.cu"]
+SOURCES = ["api.cu", "api_paged.cu", "fwd_kernel.cu", "bwd_kernels.cu", "cache_kernels.cu", "paged_fwd.cu", "paged_split.cu"]
 HEADERS = ["host_plan.h", "host_state.h", "paged.h", "paged_device.cuh", "s2a_params.h", "sm100_ptx.cuh", os.path.join("..", "..", "include", "s2a.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -5,6 +5,7 @@
 #include "../../include/s2a.h"
 #include "host_state.h"
 #include "paged.h"
+#include "s2a_params.h"
 
 namespace s2a {
 namespace {
@@ -41,6 +42,25 @@ PagedPool pool_of(const s2a_cache* c) {
     r.pages = c->pages, r.Hkv = c->Hkv, r.page_log2 = 0;
     while ((1 << r.page_log2) < c->page_size) ++r.page_log2;
     return r;
+}
+
+// The rows of a pool, a box of `keys` of them (or a page, where that is less) by 128 bytes (or a row); see swizzled() for how a box lies
+// in shared memory.
+int cache_tmap(CUtensorMap* tm, const s2a_cache* c, const void* pool, int keys) {
+    const bool codes = c->type == S2A_CACHE_E4M3;
+    const cuuint64_t row_bytes = static_cast<cuuint64_t>(c->d) * (codes ? 1 : 2);
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(row_bytes < 128 ? c->d : codes ? 128 : 64), static_cast<cuuint32_t>(c->page_size < keys ? c->page_size : keys)};
+    return encode_tmap(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, row_bytes < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                       pool, 2, dims, &row_bytes, box);
+}
+
+// Blocks that share a unit's keys: enough to fill the GPU a few times over, unless a block would be left without a whole turn of
+// its warps (`turn` keys).
+int choose_split(long long units, long long reach, int turn, int n_sm) {
+    int split = 1;
+    while (split < 16 && units * split < 4LL * n_sm && reach > static_cast<long long>(split) * turn) split *= 2;
+    return split;
 }
 
 int copy_impl(void* k, void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream, bool write) {
@@ -89,15 +109,40 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     DeviceState* ds = nullptr;
     if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
     if ((rc = standing_status(ds)) != S2A_OK) return rc;
+    const bool e4m3 = cache->type == S2A_CACHE_E4M3;
+    const long long most_rows = static_cast<long long>(max_new) * (H / cache->Hkv);
     PagedFwdParams p;
     memset(&p, 0, sizeof p);
     p.batch = batch_of(batch), p.pool = pool_of(cache);
+    // Sequences with few rows are the splitting kernel's, the others the other one's.  A batch of one sequence that may have many is
+    // the latter's without a second launch, however many it turns out to have.
+    p.few_rows = most_rows > kFewRows && batch->B == 1 ? 0 : kFewRows;
     p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new, p.window = window, p.sinks = sinks;
     p.scale_log2 = scale * 1.4426950408889634f;
-    const cudaError_t e = launch_paged_fwd(p, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
-    return e == cudaSuccess ? S2A_OK : cuda_fail(e);
+    cudaError_t e;
+    if (p.few_rows > 0) {
+        PagedSplitParams ps;
+        memset(&ps, 0, sizeof ps);
+        ps.a = p;
+        if ((rc = cache_tmap(&ps.tm_k, cache, cache->k, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
+        if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
+        ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + 15) / 16;
+        const long long units = static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks;
+        long long reach = static_cast<long long>(batch->width) * cache->page_size;
+        if (window > 0 && reach > static_cast<long long>(window) + sinks + max_new) reach = static_cast<long long>(window) + sinks + max_new;
+        ps.split = choose_split(units, reach, 4 * split_keys(e4m3, cache->d), ds->n_sm);
+        if (units * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
+        ps.by_split = FastDiv(ps.split), ps.by_row_blocks = FastDiv(ps.row_blocks), ps.by_heads = FastDiv(cache->Hkv), ps.by_rep = FastDiv(p.rep);
+        e = launch_paged_split(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    if (most_rows > kFewRows) {
+        e = launch_paged_fwd(p, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    return S2A_OK;
 }
 
 }  // extern "C"

@@ -110,7 +110,38 @@ struct CacheCopyParams {
     int tokens_per_block;
 };
 
-struct alignas(64) PagedFwdParams {
+// The keys that the new tokens at positions first .. last attend, in blocks of `block` keys: with a window the blocks that hold the
+// first `sinks` tokens, then those of the window, else all up to the last token.  Numbered from 0: block at(i) for i < count.
+struct KeyBlocks {
+    int sink_blocks, low_block, count;
+    __host__ __device__ int at(int i) const { return i < sink_blocks ? i : low_block + i - sink_blocks; }
+};
+__host__ __device__ inline KeyBlocks key_blocks(int first, int last, int window, int sinks, int block) {
+    KeyBlocks k;
+    const int low = window > 0 && first - window + 1 > 0 ? first - window + 1 : 0;
+    k.low_block = low / block;
+    const int reach = (sinks < low ? sinks : low);
+    k.sink_blocks = (reach + block - 1) / block;
+    if (k.sink_blocks > k.low_block) k.sink_blocks = k.low_block;
+    k.count = k.sink_blocks + last / block + 1 - k.low_block;
+    return k;
+}
+// Whether a token at position `p` attends key j.
+__host__ __device__ inline bool attends(int p, int j, int window, int sinks) { return j <= p && (window == 0 || j > p - window || j < sinks); }
+// Whether any of the tokens at positions first .. last does.
+__host__ __device__ inline bool any_attends(int first, int last, int j, int window, int sinks) {
+    return j <= last && (window == 0 || j > first - window || j < sinks);
+}
+// Whether the tokens at positions first .. last attend every key from j to j + n - 1.
+__host__ __device__ inline bool all_attend(int first, int last, int j, int n, int window, int sinks) {
+    return j + n - 1 <= first && (window == 0 || j > last - window || j + n <= sinks);
+}
+
+// Rows (new tokens times query heads of a KV head) up to which a sequence is worked on by the kernel that splits its keys.
+constexpr int kFewRows = 64;
+
+// What both attention kernels take.
+struct PagedFwdParams {
     PagedBatch batch;
     PagedPool pool;
     const __nv_bfloat16* q;  // [T, H, d]
@@ -120,14 +151,24 @@ struct alignas(64) PagedFwdParams {
     int* host_status;
     int H, rep, most_new;
     int window, sinks;       // window 0: none
+    int few_rows;            // sequences with at most so many rows are the splitting kernel's, the others the other one's
     float scale_log2;
-    FastDiv by_rep;
+};
+
+struct alignas(64) PagedSplitParams {
+    CUtensorMap tm_k, tm_v;  // bytes or bf16 (d, rows of the pool), box (128 bytes or a row, min(page_size, keys of a block))
+    PagedFwdParams a;
+    int split;               // blocks of a cluster, which share the keys of a unit
+    int row_blocks;          // of 16 rows
+    FastDiv by_split, by_row_blocks, by_heads, by_rep;
 };
 
 // Enqueue on `stream`; return the launch error, if any.
 cudaError_t launch_cache_write(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream);
-cudaError_t configure_paged();
+cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream);
+int split_keys(bool e4m3, int d);  // keys of a block of the splitting kernel
+cudaError_t configure_paged_split();
 
 }  // namespace s2a

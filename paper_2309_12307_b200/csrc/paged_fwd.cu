@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(128) s2a_paged_fwd_kernel(const __grid_constan
     const int b = find_sequence(p.batch.starts, p.batch.B, t);
     Sequence s;
     if (sequence_of(p.batch, p.pool.page_log2, p.most_new, b, &s) != 0 || t < s.row0 || t >= s.row0 + s.n) return;
+    if (s.n * p.rep <= p.few_rows) return;
     const int pos = s.length - s.n + t - s.row0;
     const int low = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;  // first key of the window
     const int sinks = p.sinks < low ? p.sinks : low;
@@ -84,8 +85,6 @@ __global__ void __launch_bounds__(128) s2a_paged_fwd_kernel(const __grid_constan
 }
 
 }  // namespace
-
-cudaError_t configure_paged() { return cudaSuccess; }
 
 cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.batch.T) * p.H + 3) / 4);

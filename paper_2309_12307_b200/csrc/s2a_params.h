@@ -17,6 +17,8 @@ enum WaitCode : int {
     kWaitBwdDq = 200,
     kWaitBwdDkDv = 300,
     kWaitBwdDqSpill = 400,
+    kWaitPagedSplit = 500,
+    kWaitPagedFwd = 600,
 };
 
 // Block order shared by the tensor-core kernels.  A "unit" is one (batch, head, group); it has

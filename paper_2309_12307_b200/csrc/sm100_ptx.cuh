@@ -150,6 +150,11 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* t
         ::"r"(smem_u32(smem_dst)), "l"(tmap), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap* tmap, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_dst),
+                 "l"(tmap), "r"(bar), "r"(c0), "r"(c1)
+                 : "memory");
+}
 // 1-D bulk copy global -> shared (addresses 16-byte aligned, size a multiple of 16 bytes).
 __device__ __forceinline__ void bulk_load_1d(void* smem_dst, const void* gmem_src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -200,6 +205,32 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) 
         : "r"(id), "r"(threads), "r"(ok ? 1u : 0u)
         : "memory");
     return all != 0;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Thread-block clusters
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a float of another block of the cluster, at this block's address `saddr`
+__device__ __forceinline__ float load_remote(uint32_t saddr, uint32_t rank) {
+    float x;
+    asm volatile(
+        "{\n"
+        ".reg .u32 a;\n"
+        "mapa.shared::cluster.u32 a, %1, %2;\n"
+        "ld.shared::cluster.f32 %0, [a];\n"
+        "}\n"
+        : "=f"(x)
+        : "r"(saddr), "r"(rank)
+        : "memory");
+    return x;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -447,6 +478,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                  : "memory");
+}
+
+// C += A B of one warp: A 16 x 16, B 16 x 8 bf16, C 16 x 8 fp32.  With g = lane / 4, t = lane % 4 a thread holds A(g, 2t..), A(g + 8, 2t..),
+// A(g, 2t + 8..), A(g + 8, 2t + 8..) as pairs, B(2t.., g), B(2t + 8.., g) as pairs, and C(g, 2t), C(g, 2t + 1), C(g + 8, 2t), C(g + 8, 2t + 1).
+// For kernels that are bound by their loads: where matrix products count, tcgen05 is several times faster.
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 // ---------------------------------------------------------------------------------------------
