@@ -59,7 +59,7 @@ int cache_tmap(CUtensorMap* tm, const s2a_cache* c, const void* pool, int keys) 
 // its warps (`turn` keys).
 int choose_split(long long units, long long reach, int turn, int n_sm) {
     int split = 1;
-    while (split < 16 && units * split < 4LL * n_sm && reach > static_cast<long long>(split) * turn) split *= 2;
+    while (split < kMostSplit && units * split < 4LL * n_sm && reach > static_cast<long long>(split) * turn) split *= 2;
     return split;
 }
 
@@ -128,7 +128,8 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         ps.a = p;
         if ((rc = cache_tmap(&ps.tm_k, cache, cache->k, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
-        ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + 15) / 16;
+        ps.unit_rows = most_rows <= 8 ? 8 : 16;
+        ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + ps.unit_rows - 1) / ps.unit_rows;
         const long long units = static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks;
         long long reach = static_cast<long long>(batch->width) * cache->page_size;
         if (window > 0 && reach > static_cast<long long>(window) + sinks + max_new) reach = static_cast<long long>(window) + sinks + max_new;

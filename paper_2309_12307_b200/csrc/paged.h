@@ -155,11 +155,13 @@ struct PagedFwdParams {
     float scale_log2;
 };
 
+constexpr int kMostSplit = 16;
 struct alignas(64) PagedSplitParams {
     CUtensorMap tm_k, tm_v;  // bytes or bf16 (d, rows of the pool), box (128 bytes or a row, min(page_size, keys of a block))
     PagedFwdParams a;
-    int split;               // blocks of a cluster, which share the keys of a unit
-    int row_blocks;          // of 16 rows
+    int split;               // blocks of a cluster, which share the keys of a unit: 1 .. kMostSplit
+    int unit_rows;           // 8 or 16
+    int row_blocks;          // of unit_rows rows, that a sequence and KV head has at most
     FastDiv by_split, by_row_blocks, by_heads, by_rep;
 };
 

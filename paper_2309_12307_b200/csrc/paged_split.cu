@@ -7,12 +7,14 @@
 // running maximum and sum for its rows and the weighted sum of v in registers.  What the warps and then the blocks have is
 // joined through shared memory and the cluster's: no second launch, no workspace, no atomics.
 //
-// Products of a warp: S = Q K^T and O += P V, 16 rows at a time (mma.sync: the tensor work is a tenth of the time).  Which columns
-// of a head go into which product does not matter as long as Q and K agree, so a thread takes what lies together in
-// shared memory; the two keys of a pair of P are next to each other in the accumulator of S, as P's operand needs them.
+// Products of a warp, with the keys and the columns of V as the 16 rows of an mma.sync product and the rows of the unit as its 8 columns
+// (twice where there are more than 8): S^T = K Q^T, O^T += V^T P^T.  Which columns of a head go into which product does not matter as
+// long as K and Q agree, so a thread takes what lies together in shared memory.
 //
-// Cached 8-bit floats become bf16 in registers by moving bits (e4m3_spread).  K's power of two multiplies the scores, V's the
-// weights before they are rounded: both exactly.
+// Cached 8-bit floats become fp16, which has them all (one conversion for two values; as bf16 they take five instructions).  Q, in bf16, goes
+// to fp16 with a power of two for each row that brings its largest value near fp16's: nothing is lost of values within 2^-29 of it.  K's
+// power of two multiplies the scores.  V's multiplies the weights, relative to the largest V's of the warp so far, so that they stay in
+// fp16's range: with weights up to 2^15 for the largest, those down to 2^-29 of it have all 11 bits (bf16 has 8).
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -31,7 +33,7 @@ struct SplitCfg {
     static constexpr int kStages = 24576 / kStageBytes;           // 24 KB in flight for each warp, two blocks on an SM
     static constexpr int kExpBytes = kE4M3 ? 2 * kKeys : 0;       // exponents of K and V
     static constexpr int kSmemBytes = kWarps * kStages * (kStageBytes + kExpBytes) + kWarps * kStages * 8 + 16;  // and the abort flag
-    static constexpr int kPartFloats = 16 * HD + 32;              // a warp's result: O, m, l
+    static constexpr int kPartFloats = 16 * HD + 4 * 16;          // a warp's result: O, m, l, and the joined m, l
     static_assert(kPartFloats * 4 <= kStages * kStageBytes, "the ring holds a result");
     static_assert(kTile % 1024 == 0, "swizzle atoms");
 };
@@ -61,11 +63,16 @@ __device__ __forceinline__ float exponent_factor(int e) {
     return e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
-constexpr float kLeast = -3.0e38f;  // stands for "no key yet": finite, so that differences are numbers
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }  // -127 <= e <= 127, -127: zero
 
-template <int HD, bool kE4M3>
+constexpr float kLeast = -3.0e38f;   // stands for "no key yet": finite, so that differences are numbers
+constexpr float kLazy = 8.0f;        // a running maximum (of log2) that is exceeded by less stays
+
+template <int HD, bool kE4M3, int kRowTiles>
 __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_split_kernel(const __grid_constant__ PagedSplitParams p) {
     using C = SplitCfg<HD, kE4M3>;
+    constexpr int kRows = 8 * kRowTiles;     // of a unit
+    constexpr float kUp = kE4M3 ? 7.f : 0.f;  // weights are 2^kUp as large, see above
     extern __shared__ __align__(1024) uint8_t smem[];
     const PagedFwdParams& a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -93,9 +100,9 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     const int b = p.by_heads(p.by_row_blocks(unit, &row_block), &hk);
     Sequence s;
     if (sequence_of(a.batch, a.pool.page_log2, a.most_new, b, &s) != 0) return;  // (the same for all blocks of the cluster)
-    const int all_rows = s.n * a.rep, r0 = row_block * 16;
+    const int all_rows = s.n * a.rep, r0 = row_block * kRows;
     if (r0 >= all_rows || all_rows > a.few_rows) return;
-    const int rows = all_rows - r0 < 16 ? all_rows - r0 : 16;
+    const int rows = all_rows - r0 < kRows ? all_rows - r0 : kRows;
     const int first_pos = s.length - s.n + p.by_rep(r0), last_pos = s.length - s.n + p.by_rep(r0 + rows - 1);
     const KeyBlocks blocks = key_blocks(first_pos, last_pos, a.window, a.sinks, C::kKeys);
     const int share = (blocks.count + p.split - 1) / p.split;
@@ -104,7 +111,8 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     if (__any_sync(0xffffffffu, *ctx.abort_flag != 0)) steps = 0;
 
     // ---- loads of this warp: pages of its next 32 steps are in its lanes; lane 0 (and 1, where a step spans two pages) requests
-    const int piece_log2 = a.pool.page_log2 < (C::kKeys == 16 ? 4 : 5) ? a.pool.page_log2 : (C::kKeys == 16 ? 4 : 5);
+    constexpr int kKeysLog2 = C::kKeys == 16 ? 4 : 5;
+    const int piece_log2 = a.pool.page_log2 < kKeysLog2 ? a.pool.page_log2 : kKeysLog2;
     const int pieces = C::kKeys >> piece_log2;
     int page[2] = {-1, -1};
     auto look_up = [&](int from) {
@@ -150,42 +158,49 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     };
     for (int c = 0; c < C::kStages && c < steps; ++c) request(c);
 
-    // ---- the rows of Q that this thread's products take: rows g and g + 8; of every line of a key's row the 32 bytes from 32 t on
-    // (16 from 16 t on where a line has 64), as pairs in the order in which K's come out of their words
-    constexpr int kSteps = HD / 16;          // products of a score tile
-    uint32_t q[2][2 * kSteps];
-    int pos[2];
+    // ---- Q: row g of every eight, of every 64 columns (of all, in 8 bits) the quarter t, as pairs in the order of K's words
+    constexpr int kPer = kE4M3 ? HD / 4 : 16;  // columns that lie together
+    uint32_t q[kRowTiles][HD / 8];
+    float score_scale[kRowTiles][2];  // of the rows 2 t and 2 t + 1 of every eight
+    int pos[kRowTiles][2];            // their positions
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = r0 + (g + 8 * half < rows ? g + 8 * half : rows - 1);  // rows past the end follow the last one
+    for (int r = 0; r < kRowTiles; ++r) {
+        auto row_of = [&](int x, int* hh) {  // rows past the end follow the last one
+            const int row = 8 * r + x < rows ? 8 * r + x : rows - 1;
+            return p.by_rep(r0 + row, hh);
+        };
         int hh;
-        const int i = p.by_rep(r, &hh);
-        pos[half] = s.length - s.n + i;
-        const __nv_bfloat16* src = a.q + (static_cast<long long>(s.row0 + i) * a.H + hk * a.rep + hh) * HD;
+        pos[r][0] = s.length - s.n + row_of(2 * t, &hh), pos[r][1] = s.length - s.n + row_of(2 * t + 1, &hh);
+        const int i = row_of(g, &hh);
+        const __nv_bfloat16* src = a.q + (static_cast<long long>(s.row0 + i) * a.H + hk * a.rep + hh) * HD + kPer * t;
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * c + (c * 8 / kPer) * (64 - kPer) * (kE4M3 ? 0 : 1));
+            q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
+        }
+        score_scale[r][0] = score_scale[r][1] = a.scale_log2;
         if constexpr (kE4M3) {
-            constexpr int kPer = HD / 4;  // values of a thread
+            uint32_t most = 0;
 #pragma unroll
-            for (int c = 0; c < kPer / 8; ++c) {
-                const uint4 x = *reinterpret_cast<const uint4*>(src + kPer * t + 8 * c);
-                q[half][4 * c] = __byte_perm(x.x, x.y, 0x5410), q[half][4 * c + 1] = __byte_perm(x.x, x.y, 0x7632);
-                q[half][4 * c + 2] = __byte_perm(x.z, x.w, 0x5410), q[half][4 * c + 3] = __byte_perm(x.z, x.w, 0x7632);
-            }
-        } else {
+            for (int c = 0; c < HD / 8; ++c) most = max(most, max(q[r][c] & 0x7fffu, q[r][c] >> 16 & 0x7fffu));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            // the largest goes to [2^14, 2^15); a row that is not finite stays so
+            int up = most >= 0x7f80u || most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);
+            up = up > 126 ? 126 : up;
+            const float f = power_of_two(up);
 #pragma unroll
-            for (int x = 0; x < C::kBoxes; ++x)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(src + 64 * x + 16 * t + 8 * c);
-                    uint32_t* to = &q[half][8 * x + 4 * c];
-                    to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
-                }
+            for (int c = 0; c < HD / 8; ++c) q[r][c] = pack_f16(bf16_low(q[r][c]) * f, bf16_high(q[r][c]) * f);
+            score_scale[r][0] *= power_of_two(-__shfl_sync(0xffffffffu, up, 8 * t));
+            score_scale[r][1] *= power_of_two(-__shfl_sync(0xffffffffu, up, 8 * t + 4));
         }
     }
 
-    float o[HD / 8][4];
+    float o[kRowTiles][HD / 16][4] = {};
+    float m[kRowTiles][2], l[kRowTiles][2];  // running maximum in use and this thread's part of the sum, rows 2 t and 2 t + 1
 #pragma unroll
-    for (int x = 0; x < HD / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-    float m[2] = {kLeast, kLeast}, l[2] = {0.f, 0.f};
+    for (int r = 0; r < kRowTiles; ++r) m[r][0] = m[r][1] = kLeast, l[r][0] = l[r][1] = 0.f;
+    int v_most = kExpLeast;  // the largest exponent of V so far (8 bits): O is in units of 2^v_most
     bool ok = true;
     int c = 0;
     for (; c < steps; ++c) {
@@ -194,129 +209,154 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         const uint32_t sK = smem_u32(ring + st * C::kStageBytes), sV = sK + C::kTile, sE = smem_u32(exps + st * C::kExpBytes);
         const int key0 = blocks.at(i0 + c * C::kWarps) * C::kKeys;
         const bool masked = !all_attend(first_pos, last_pos, key0, C::kKeys, a.window, a.sinks);
-        constexpr int kTiles = C::kKeys / 8;
-        float sc[kTiles][4];
+        constexpr int kTiles = C::kKeys / 16;
+        float sc[kTiles][kRowTiles][4];
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
-            sc[u][0] = sc[u][1] = sc[u][2] = sc[u][3] = 0.f;
-            const int key = 8 * u + g;
+#pragma unroll
+            for (int r = 0; r < kRowTiles; ++r) sc[u][r][0] = sc[u][r][1] = sc[u][r][2] = sc[u][r][3] = 0.f;
+            const int key = 16 * u + g;
+            auto product = [&](int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+                for (int r = 0; r < kRowTiles; ++r) mma_16x8x16<kE4M3>(sc[u][r], a0, a1, a2, a3, q[r][2 * k], q[r][2 * k + 1]);
+            };
             if constexpr (kE4M3) {
 #pragma unroll
                 for (int x = 0; x < HD / 64; ++x) {
-                    const uint4 w4 = lds128(swizzled<C::kLine>(sK, key, HD / 4 * t + 16 * x));
-                    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                    const uint4 w = lds128(swizzled<C::kLine>(sK, key, HD / 4 * t + 16 * x)), z = lds128(swizzled<C::kLine>(sK, key + 8, HD / 4 * t + 16 * x));
+                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w}, zz[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
-                        uint32_t lo, hi;
-                        e4m3_spread(w[y], lo, hi);
-                        const int k = 4 * x + y;
-                        mma_16x8x16(sc[u], q[0][2 * k], q[1][2 * k], q[0][2 * k + 1], q[1][2 * k + 1], bf16x2_mul(lo, kTwoTo120), bf16x2_mul(hi, kTwoTo120));
+                        uint32_t w0, w1, z0, z1;
+                        e4m3_to_f16(ww[y], w0, w1);
+                        e4m3_to_f16(zz[y], z0, z1);
+                        product(4 * x + y, w0, z0, w1, z1);
                     }
                 }
             } else {
 #pragma unroll
                 for (int x = 0; x < 2 * C::kBoxes; ++x) {
-                    const uint4 w = lds128(swizzled<C::kLine>(sK + (x >> 1) * C::kKeys * C::kLine, key, 32 * t + 16 * (x & 1)));
-                    mma_16x8x16(sc[u], q[0][4 * x], q[1][4 * x], q[0][4 * x + 1], q[1][4 * x + 1], w.x, w.y);
-                    mma_16x8x16(sc[u], q[0][4 * x + 2], q[1][4 * x + 2], q[0][4 * x + 3], q[1][4 * x + 3], w.z, w.w);
+                    const uint32_t box = sK + (x >> 1) * C::kKeys * C::kLine;
+                    const uint4 w = lds128(swizzled<C::kLine>(box, key, 32 * t + 16 * (x & 1))), z = lds128(swizzled<C::kLine>(box, key + 8, 32 * t + 16 * (x & 1)));
+                    product(2 * x, w.x, z.x, w.y, z.y);
+                    product(2 * x + 1, w.z, z.z, w.w, z.w);
                 }
             }
         }
-        // scores in units of log2, keys 8 u + 2 t + (x & 1), rows g + 8 (x >> 1)
+        // scores in units of log2: keys 16 u + g + 8 (x >> 1), rows 8 r + 2 t + (x & 1)
         float v_factor[kTiles][2];
-        float top[2] = {m[0], m[1]};
+        int v_exp[kTiles][2];
+        bool grows = false;
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
-            float factor[2] = {a.scale_log2, a.scale_log2};
+            float k_factor[2] = {1.f, 1.f};
             if constexpr (kE4M3) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    factor[x] *= exponent_factor(lds_s8(sE + 8 * u + 2 * t + x));
-                    v_factor[u][x] = exponent_factor(lds_s8(sE + C::kKeys + 8 * u + 2 * t + x));
+                    k_factor[x] = exponent_factor(lds_s8(sE + 16 * u + 8 * x + g));
+                    v_exp[u][x] = lds_s8(sE + C::kKeys + 16 * u + 8 * x + g);
+                    // (what lies there for keys past the end of the sequence can be anything: it must not set the scale)
+                    if (masked && !any_attends(first_pos, last_pos, key0 + 16 * u + 8 * x + g, a.window, a.sinks)) v_exp[u][x] = kExpLeast;
+                    grows |= v_exp[u][x] > v_most;
                 }
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                sc[u][x] *= factor[x & 1];
-                if (masked && !attends(pos[x >> 1], key0 + 8 * u + 2 * t + (x & 1), a.window, a.sinks)) sc[u][x] = -INFINITY;
-                top[x >> 1] = fmaxf(top[x >> 1], sc[u][x]);
-            }
-        }
-        uint32_t changed = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-            changed |= top[h] != m[h];
-        }
-        if (__any_sync(0xffffffffu, changed)) {
-            const float down[2] = {fast_exp2(m[0] - top[0]), fast_exp2(m[1] - top[1])};
-            l[0] *= down[0], l[1] *= down[1];
-#pragma unroll
-            for (int x = 0; x < HD / 8; ++x) o[x][0] *= down[0], o[x][1] *= down[0], o[x][2] *= down[1], o[x][3] *= down[1];
-            m[0] = top[0], m[1] = top[1];
-        }
-        uint32_t w[kTiles][2];  // weights of rows g and g + 8 as pairs of keys
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            float e[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                e[x] = fast_exp2(sc[u][x] - m[x >> 1]);
-                l[x >> 1] += e[x];
-                if constexpr (kE4M3) e[x] = masked && sc[u][x] == -INFINITY ? 0.f : e[x] * v_factor[u][x & 1];
-            }
-            w[u][0] = pack_bf16(e[0], e[1]), w[u][1] = pack_bf16(e[2], e[3]);
-        }
-        // O += P V, 16 keys at a time: a thread loads 8 (or 16) columns from column 8 g (16 g) on of the keys 2 t, 2 t + 1 of either tile
-#pragma unroll
-        for (int u = 0; u < kTiles; u += 2) {
-            const int keys[4] = {8 * u + 2 * t, 8 * u + 2 * t + 1, 8 * u + 8 + 2 * t, 8 * u + 9 + 2 * t};
-            if constexpr (kE4M3) {
-                constexpr int kWords = HD / 32;
-                uint32_t v[4][kWords];
+            for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    if constexpr (HD == 128) {
-                        const uint4 r = lds128(swizzled<C::kLine>(sV, keys[x], 16 * g));
-                        v[x][0] = r.x, v[x][1] = r.y, v[x][2] = r.z, v[x][3] = r.w;
+                    sc[u][r][x] *= score_scale[r][x & 1];
+                    if constexpr (kE4M3) sc[u][r][x] *= k_factor[x >> 1];
+                    if (masked && !attends(pos[r][x & 1], key0 + 16 * u + 8 * (x >> 1) + g, a.window, a.sinks)) sc[u][r][x] = -INFINITY;
+                    grows |= sc[u][r][x] > m[r][x & 1] + kLazy;
+                }
+        }
+        if (__any_sync(0xffffffffu, grows)) {
+            float v_down = 1.f;
+            if constexpr (kE4M3) {
+                int most = v_most;
+#pragma unroll
+                for (int u = 0; u < kTiles; ++u) most = max(most, max(v_exp[u][0], v_exp[u][1]));
+                most = __reduce_max_sync(0xffffffffu, most);
+                v_down = power_of_two(max(v_most - most, -127));
+                v_most = most;
+            }
+#pragma unroll
+            for (int r = 0; r < kRowTiles; ++r) {
+                float down[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float top = m[r][h];
+#pragma unroll
+                    for (int u = 0; u < kTiles; ++u) top = fmax3(top, sc[u][r][h], sc[u][r][h + 2]);
+#pragma unroll
+                    for (int off = 4; off < 32; off *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                    down[h] = fast_exp2(m[r][h] - top);
+                    m[r][h] = top;
+                    l[r][h] *= down[h];
+                    down[h] *= v_down;
+                }
+#pragma unroll
+                for (int x = 0; x < HD / 16; ++x) o[r][x][0] *= down[0], o[r][x][1] *= down[1], o[r][x][2] *= down[0], o[r][x][3] *= down[1];
+            }
+        }
+        uint32_t w[kTiles][kRowTiles][2];  // weights of rows 8 r + g, keys 16 u + 2 t.. and 16 u + 8 + 2 t.. as pairs
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            if constexpr (kE4M3) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) v_factor[u][x] = v_exp[u][x] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(v_exp[u][x] - v_most, -127));
+            }
+#pragma unroll
+            for (int r = 0; r < kRowTiles; ++r) {
+                float e[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    e[x] = fast_exp2(sc[u][r][x] - (m[r][x & 1] - kUp));
+                    l[r][x & 1] += e[x];
+                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : e[x] * v_factor[u][x >> 1];
+                }
+                w[u][r][0] = transpose_8x8(kE4M3 ? pack_f16(e[0], e[1]) : pack_bf16(e[0], e[1]));
+                w[u][r][1] = transpose_8x8(kE4M3 ? pack_f16(e[2], e[3]) : pack_bf16(e[2], e[3]));
+            }
+        }
+        // O^T += V^T P^T, 16 keys at a time.  A thread loads 8 (or 16) columns from column 8 g (16 g) on of the keys 2 t, 2 t + 1, 2 t + 8 and
+        // 2 t + 9; two neighbouring columns are rows g and g + 8 of a product.
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            constexpr int kLoad = kE4M3 && HD == 64 ? 8 : 16;  // bytes
+#pragma unroll
+            for (int bx = 0; bx < C::kBoxes; ++bx) {
+                uint32_t v[4][4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int key = 16 * u + 2 * t + (x & 1) + 8 * (x >> 1);
+                    const uint32_t from = swizzled<C::kLine>(sV + bx * C::kKeys * C::kLine, key, kLoad * g);
+                    if constexpr (kLoad == 16) {
+                        const uint4 y = lds128(from);
+                        v[x][0] = y.x, v[x][1] = y.y, v[x][2] = y.z, v[x][3] = y.w;
                     } else {
-                        const uint2 r = lds64(swizzled<C::kLine>(sV, keys[x], 8 * g));
-                        v[x][0] = r.x, v[x][1] = r.y;
+                        const uint2 y = lds64(from);
+                        v[x][0] = y.x, v[x][1] = y.y, v[x][2] = v[x][3] = 0u;
                     }
+                    // what no row attends may be anything (positions past the end of the sequence hold whatever the page held
+                    // before), and a weight of zero does not make a NaN go away
+                    if (masked && !any_attends(first_pos, last_pos, key0 + key, a.window, a.sinks)) v[x][0] = v[x][1] = v[x][2] = v[x][3] = 0u;
                 }
+                auto product = [&](int x, uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3) {  // a pair of columns of the four keys
+                    const uint32_t a0 = __byte_perm(p0, p1, 0x5410), a1 = __byte_perm(p0, p1, 0x7632), a2 = __byte_perm(p2, p3, 0x5410), a3 = __byte_perm(p2, p3, 0x7632);
 #pragma unroll
-                for (int y = 0; y < kWords; ++y) {
-                    uint32_t lo[4], hi[4];
+                    for (int r = 0; r < kRowTiles; ++r) mma_16x8x16<kE4M3>(o[r][x], a0, a1, a2, a3, w[u][r][0], w[u][r][1]);
+                };
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        e4m3_spread(v[x][y], lo[x], hi[x]);
-                        lo[x] = bf16x2_mul(lo[x], kTwoTo120), hi[x] = bf16x2_mul(hi[x], kTwoTo120);
-                    }
-                    mma_16x8x16(o[4 * y], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(lo[0], lo[1], 0x5410), __byte_perm(lo[2], lo[3], 0x5410));
-                    mma_16x8x16(o[4 * y + 1], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(hi[0], hi[1], 0x5410), __byte_perm(hi[2], hi[3], 0x5410));
-                    mma_16x8x16(o[4 * y + 2], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(lo[0], lo[1], 0x7632), __byte_perm(lo[2], lo[3], 0x7632));
-                    mma_16x8x16(o[4 * y + 3], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(hi[0], hi[1], 0x7632), __byte_perm(hi[2], hi[3], 0x7632));
-                }
-            } else {
+                for (int y = 0; y < kLoad / 4; ++y) {
+                    if constexpr (kE4M3) {
+                        uint32_t lo[4], hi[4];
 #pragma unroll
-                for (int bx = 0; bx < C::kBoxes; ++bx) {
-                    uint32_t v[4][4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const uint4 r = lds128(swizzled<C::kLine>(sV + bx * C::kKeys * C::kLine, keys[x], 16 * g));
-                        v[x][0] = r.x, v[x][1] = r.y, v[x][2] = r.z, v[x][3] = r.w;
-                        // what no row attends may be anything (positions past the end of the sequence hold whatever the page held
-                        // before), and a weight of zero does not make a NaN go away
-                        if (masked && !any_attends(first_pos, last_pos, key0 + keys[x], a.window, a.sinks))
-                            v[x][0] = v[x][1] = v[x][2] = v[x][3] = 0u;
-                    }
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        mma_16x8x16(o[8 * bx + 2 * y], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(v[0][y], v[1][y], 0x5410),
-                                    __byte_perm(v[2][y], v[3][y], 0x5410));
-                        mma_16x8x16(o[8 * bx + 2 * y + 1], w[u][0], w[u][1], w[u + 1][0], w[u + 1][1], __byte_perm(v[0][y], v[1][y], 0x7632),
-                                    __byte_perm(v[2][y], v[3][y], 0x7632));
+                        for (int x = 0; x < 4; ++x) e4m3_to_f16(v[x][y], lo[x], hi[x]);
+                        product(2 * y, lo[0], lo[1], lo[2], lo[3]);
+                        product(2 * y + 1, hi[0], hi[1], hi[2], hi[3]);
+                    } else {
+                        product(4 * bx + y, v[0][y], v[1][y], v[2][y], v[3][y]);
                     }
                 }
             }
@@ -328,22 +368,25 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         for (int x = c; x < steps && x < c + C::kStages; ++x) mbar_wait_drain(&full[x % C::kStages], (x / C::kStages) & 1);
     __syncwarp();
 
-    // ---- this warp's result into its ring: [16][HD] of O, then m and l of the 16 rows
+    // ---- this warp's result into its ring: O of the rows, then m and l
     float* mine = reinterpret_cast<float*>(ring);
+    constexpr int kM = kRows * HD, kL = kM + kRows, kJoined = kL + kRows;
+    constexpr int kCols = kE4M3 ? HD / 8 : 8;  // columns of a thread that lie together
+    const float v_up = kE4M3 ? power_of_two(v_most) : 1.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        if (t == 0) mine[16 * HD + g + 8 * h] = m[h], mine[16 * HD + 16 + g + 8 * h] = l[h];
-    }
-    // product x of a group of kCols has the columns kCols * (2 t) + x and kCols * (2 t + 1) + x of the group's 8 * kCols
-    constexpr int kCols = kE4M3 ? HD / 8 : 8;
+    for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-    for (int x = 0; x < HD / 8; ++x) {
-        const int col = x / kCols * (8 * kCols) + kCols * 2 * t + x % kCols;
-        mine[g * HD + col] = o[x][0], mine[g * HD + col + kCols] = o[x][1];
-        mine[(g + 8) * HD + col] = o[x][2], mine[(g + 8) * HD + col + kCols] = o[x][3];
-    }
+        for (int h = 0; h < 2; ++h) {
+            const int row = 8 * r + 2 * t + h;
+#pragma unroll
+            for (int off = 4; off < 32; off *= 2) l[r][h] += __shfl_xor_sync(0xffffffffu, l[r][h], off);
+            if (g == 0) mine[kM + row] = m[r][h], mine[kL + row] = l[r][h];
+#pragma unroll
+            for (int x = 0; x < HD / 16; ++x) {
+                float2* to = reinterpret_cast<float2*>(mine + row * HD + 2 * x / kCols * (8 * kCols) + kCols * g + 2 * x % kCols);
+                *to = make_float2(o[r][x][h] * v_up, o[r][x][h + 2] * v_up);
+            }
+        }
     __syncthreads();
 
     auto finish = [&](int e, float value, float top, float sum) {
@@ -353,7 +396,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         const long long to = static_cast<long long>(s.row0 + i);
         if (abort_flag != 0) return;
         a.o[(to * a.H + h) * HD + col] = __float2bfloat16(value / sum);
-        if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top + log2f(sum)) * 0.6931471805599453f;
+        if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top - kUp + log2f(sum)) * 0.6931471805599453f;
     };
     // ---- the four warps' results joined, into the first ring
     constexpr int kRing = C::kStages * C::kStageBytes / 4;  // floats of a ring
@@ -362,11 +405,11 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         const int row = e / HD;
         float top = kLeast, sum = 0.f, value = 0.f;
 #pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) top = fmaxf(top, first[w * kRing + 16 * HD + row]);
+        for (int w = 0; w < C::kWarps; ++w) top = fmaxf(top, first[w * kRing + kM + row]);
 #pragma unroll
         for (int w = 0; w < C::kWarps; ++w) {
-            const float f = fast_exp2(first[w * kRing + 16 * HD + row] - top);
-            sum += f * first[w * kRing + 16 * HD + 16 + row];
+            const float f = fast_exp2(first[w * kRing + kM + row] - top);
+            sum += f * first[w * kRing + kL + row];
             value += f * first[w * kRing + e];
         }
         if (p.split == 1) {
@@ -374,7 +417,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         } else {
             first[e] = value;  // only this thread reads and writes this place
             // (m and l of the first warp are still read for other columns: the joined ones go behind them)
-            if (e % HD == 0) first[16 * HD + 32 + row] = top, first[16 * HD + 48 + row] = sum;
+            if (e % HD == 0) first[kJoined + row] = top, first[kJoined + kRows + row] = sum;
         }
     }
     if (p.split == 1) return;
@@ -383,17 +426,17 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     const uint32_t at = smem_u32(first);
     for (int e = part * C::kThreads + static_cast<int>(threadIdx.x); e < rows * HD; e += p.split * C::kThreads) {
         const int row = e / HD;
-        float tops[16], top = kLeast, sum = 0.f, value = 0.f;
+        float tops[kMostSplit], top = kLeast, sum = 0.f, value = 0.f;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            tops[x] = x < p.split ? load_remote(at + (16 * HD + 32 + row) * 4, x) : kLeast;
+        for (int x = 0; x < kMostSplit; ++x) {
+            tops[x] = x < p.split ? load_remote(at + (kJoined + row) * 4, x) : kLeast;
             top = fmaxf(top, tops[x]);
         }
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
+        for (int x = 0; x < kMostSplit; ++x)
             if (x < p.split) {
                 const float f = fast_exp2(tops[x] - top);
-                sum += f * load_remote(at + (16 * HD + 48 + row) * 4, x);
+                sum += f * load_remote(at + (kJoined + kRows + row) * 4, x);
                 value += f * load_remote(at + e * 4, x);
             }
         finish(e, value, top, sum);
@@ -401,14 +444,14 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     cluster_sync();  // nobody leaves while its results are read
 }
 
-template <int HD, bool kE4M3>
+template <int HD, bool kE4M3, int kRowTiles>
 cudaError_t configure_one() {
-    auto kernel = s2a_paged_split_kernel<HD, kE4M3>;
+    auto kernel = s2a_paged_split_kernel<HD, kE4M3, kRowTiles>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitCfg<HD, kE4M3>::kSmemBytes);
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
-template <int HD, bool kE4M3>
+template <int HD, bool kE4M3, int kRowTiles>
 cudaError_t launch_one(const PagedSplitParams& p, cudaStream_t stream) {
     using C = SplitCfg<HD, kE4M3>;
     cudaLaunchConfig_t config = {};
@@ -423,7 +466,7 @@ cudaError_t launch_one(const PagedSplitParams& p, cudaStream_t stream) {
     attribute[1].val.clusterDim.x = static_cast<unsigned>(p.split), attribute[1].val.clusterDim.y = attribute[1].val.clusterDim.z = 1;
     config.attrs = attribute;
     config.numAttrs = 2;
-    return cudaLaunchKernelEx(&config, s2a_paged_split_kernel<HD, kE4M3>, p);
+    return cudaLaunchKernelEx(&config, s2a_paged_split_kernel<HD, kE4M3, kRowTiles>, p);
 }
 
 }  // namespace
@@ -433,16 +476,16 @@ int split_keys(bool e4m3, int d) {
 }
 
 cudaError_t configure_paged_split() {
-    cudaError_t e = configure_one<64, false>();
-    if (e == cudaSuccess) e = configure_one<64, true>();
-    if (e == cudaSuccess) e = configure_one<128, false>();
-    if (e == cudaSuccess) e = configure_one<128, true>();
-    return e;
+    for (const cudaError_t e : {configure_one<64, false, 1>(), configure_one<64, false, 2>(), configure_one<64, true, 1>(), configure_one<64, true, 2>(),
+                                configure_one<128, false, 1>(), configure_one<128, false, 2>(), configure_one<128, true, 1>(), configure_one<128, true, 2>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
 }
 
 cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream) {
-    if (d == 64) return e4m3 ? launch_one<64, true>(p, stream) : launch_one<64, false>(p, stream);
-    return e4m3 ? launch_one<128, true>(p, stream) : launch_one<128, false>(p, stream);
+    auto launch = p.unit_rows == 8 ? (d == 64 ? (e4m3 ? launch_one<64, true, 1> : launch_one<64, false, 1>) : (e4m3 ? launch_one<128, true, 1> : launch_one<128, false, 1>))
+                                   : (d == 64 ? (e4m3 ? launch_one<64, true, 2> : launch_one<64, false, 2>) : (e4m3 ? launch_one<128, true, 2> : launch_one<128, false, 2>));
+    return launch(p, stream);
 }
 
 }  // namespace s2a

@@ -480,13 +480,25 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
                  : "memory");
 }
 
-// C += A B of one warp: A 16 x 16, B 16 x 8 bf16, C 16 x 8 fp32.  With g = lane / 4, t = lane % 4 a thread holds A(g, 2t..), A(g + 8, 2t..),
-// A(g, 2t + 8..), A(g + 8, 2t + 8..) as pairs, B(2t.., g), B(2t + 8.., g) as pairs, and C(g, 2t), C(g, 2t + 1), C(g + 8, 2t), C(g + 8, 2t + 1).
-// For kernels that are bound by their loads: where matrix products count, tcgen05 is several times faster.
+// C += A B of one warp: A 16 x 16, B 16 x 8 of bf16 or fp16, C 16 x 8 fp32.  With g = lane / 4, t = lane % 4 a thread holds A(g, 2t..),
+// A(g + 8, 2t..), A(g, 2t + 8..), A(g + 8, 2t + 8..) as pairs, B(2t.., g), B(2t + 8.., g) as pairs, and C(g, 2t), C(g, 2t + 1),
+// C(g + 8, 2t), C(g + 8, 2t + 1).  For kernels that are bound by their loads: where matrix products count, tcgen05 is several times faster.
+template <bool kHalf>
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if constexpr (kHalf)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transpose of an 8 x 8 matrix of 16-bit values: row g's values 2t, 2t + 1 in, column g's values 2t, 2t + 1 out.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -568,6 +580,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// two fp32 -> packed fp16x2 (lo in the low half)
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// four 8-bit floats (e4m3) -> fp16, exactly: values 0 and 1 in the first word, 2 and 3 in the second
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n"
+        ".reg .b16 a, b;\n"
+        "mov.b32 {a, b}, %2;\n"
+        "cvt.rn.f16x2.e4m3x2 %0, a;\n"
+        "cvt.rn.f16x2.e4m3x2 %1, b;\n"
+        "}\n"
+        : "=r"(lo), "=r"(hi)
+        : "r"(w));
 }
 
 }  // namespace s2a
