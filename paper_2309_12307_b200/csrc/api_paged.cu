@@ -44,23 +44,52 @@ PagedPool pool_of(const s2a_cache* c) {
     return r;
 }
 
-// The rows of a pool, a box of `keys` of them (or a page, where that is less) by 128 bytes (or a row); see swizzled() for how a box lies
-// in shared memory.
+// The rows of a pool, as lines of 128 bytes (or of a row, where that is less); a box is `keys` rows, or a page where that is less, one line after
+// the other.  See swizzled() for how a line's box lies in shared memory.
 int cache_tmap(CUtensorMap* tm, const s2a_cache* c, const void* pool, int keys) {
     const bool codes = c->type == S2A_CACHE_E4M3;
-    const cuuint64_t row_bytes = static_cast<cuuint64_t>(c->d) * (codes ? 1 : 2);
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(row_bytes < 128 ? c->d : codes ? 128 : 64), static_cast<cuuint32_t>(c->page_size < keys ? c->page_size : keys)};
-    return encode_tmap(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, row_bytes < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-                       pool, 2, dims, &row_bytes, box);
+    const cuuint32_t size = codes ? 1 : 2, row_bytes = static_cast<cuuint32_t>(c->d) * size, line = row_bytes < 128 ? row_bytes : 128;
+    const cuuint64_t dims[3] = {line / size, static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size, row_bytes / line};
+    const cuuint64_t strides[2] = {row_bytes, line};
+    const cuuint32_t box[3] = {line / size, static_cast<cuuint32_t>(c->page_size < keys ? c->page_size : keys), row_bytes / line};
+    return encode_tmap(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, line < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                       pool, 3, dims, strides, box);
 }
 
-// Blocks that share a unit's keys: enough to fill the GPU a few times over, unless a block would be left without a whole turn of
-// its warps (`turn` keys).
-int choose_split(long long units, long long reach, int turn, int n_sm) {
-    int split = 1;
-    while (split < kMostSplit && units * split < 4LL * n_sm && reach > static_cast<long long>(split) * turn) split *= 2;
-    return split;
+// How the keys of the units (8 or 16 rows of a sequence and KV head) are dealt out: blocks of `warps` warps, `split` of them in a cluster
+// for each unit, whatever should be done first by this estimate, in microseconds:
+//   - the bytes of all units at the memory's rate.  A batch's sequences differ in length: the average is taken as 0.7 of the longest.
+//   - half of what the longest piece takes by itself (a block of four warps needs 11 to 13 ns for a key of 128 columns): the blocks end that much
+//     apart.  Of a single sequence all pieces are alike: its blocks run in whole waves instead.
+//   - 8 us for every block that a place on the GPU sees: the launch, the addresses, the first loads' latency, joining the results.
+// Measured (us, by blocks in a cluster, of four warps): 16 x up to 8192 tokens of 32 heads of 128 1 190, 2 170, 3 171, 4 181; 8 x up to 32k of 8 heads
+// in 8 bits 4 117, 6 94, 8 96, 10 88, 12 99; 16 x up to 32k of 8 heads in 8 bits 4 136, 6 114, 8 126; 4 x 8192 of 40 heads 2 112, 3 126, 4 104, 6 115;
+// one of 100,000 of 32 heads in 8 bits 6 229, 8 193, 10 159, 12 203; 64 x up to 1024 of 32 heads, one block of two warps 89, of four 92.
+void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, int key_bytes, bool e4m3, int d) {
+    const long long units = static_cast<long long>(p->a.batch.B) * p->a.pool.Hkv * p->row_blocks;
+    const double rate = 6.5e6, block_start = 8.0;  // bytes and key times in microseconds
+    const double key_time = (e4m3 ? 0.0105 : 0.0128) * d / 128;
+    double best = 0;
+    p->warps = 4, p->split = 1;
+    for (int warps = 4; warps >= 1; warps /= 2)
+        for (int split = 1; split <= kMostSplit; ++split) {
+            const int slots = ds->cluster_slots[split] * (4 / warps);
+            const long long blocks = units * split;
+            if (slots <= 0 || (split > 1 && reach <= static_cast<long long>(split - 1) * warps * split_keys(e4m3, d))) continue;
+            const double piece = static_cast<double>((reach + split - 1) / split), alone = piece * key_time * 4 / warps, waves = static_cast<double>(blocks) / slots;
+            double t;
+            if (p->a.batch.B > 1) {
+                t = 0.7 * units * reach * key_bytes / rate + 0.5 * alone + block_start * (waves < 1 ? 1 : waves);
+            } else {
+                t = 0;
+                for (double left = waves; left > 0; left -= 1) {
+                    if (left > 64) t += left, left = 1;  // (never met: one sequence has few units)
+                    const double bytes = (left < 1 ? left : 1) * slots * piece * key_bytes / rate;
+                    t += (bytes > alone ? bytes : alone) + block_start;
+                }
+            }
+            if (best == 0 || t < best) best = t, p->warps = warps, p->split = split;
+        }
 }
 
 int copy_impl(void* k, void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream, bool write) {
@@ -130,11 +159,10 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         ps.unit_rows = most_rows <= 8 ? 8 : 16;
         ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + ps.unit_rows - 1) / ps.unit_rows;
-        const long long units = static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks;
         long long reach = static_cast<long long>(batch->width) * cache->page_size;
         if (window > 0 && reach > static_cast<long long>(window) + sinks + max_new) reach = static_cast<long long>(window) + sinks + max_new;
-        ps.split = choose_split(units, reach, 4 * split_keys(e4m3, cache->d), ds->n_sm);
-        if (units * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
+        choose_pieces(&ps, ds, reach, 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
+        if (static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
         ps.by_split = FastDiv(ps.split), ps.by_row_blocks = FastDiv(ps.row_blocks), ps.by_heads = FastDiv(cache->Hkv), ps.by_rep = FastDiv(p.rep);
         e = launch_paged_split(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) return cuda_fail(e);

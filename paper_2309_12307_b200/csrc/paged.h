@@ -157,8 +157,9 @@ struct PagedFwdParams {
 
 constexpr int kMostSplit = 16;
 struct alignas(64) PagedSplitParams {
-    CUtensorMap tm_k, tm_v;  // bytes or bf16 (d, rows of the pool), box (128 bytes or a row, min(page_size, keys of a block))
+    CUtensorMap tm_k, tm_v;  // (columns of a line of at most 128 bytes, rows of the pool, lines of a row), box (all, min(page_size, keys of a step), all)
     PagedFwdParams a;
+    int warps;               // of a block: 1, 2 or 4
     int split;               // blocks of a cluster, which share the keys of a unit: 1 .. kMostSplit
     int unit_rows;           // 8 or 16
     int row_blocks;          // of unit_rows rows, that a sequence and KV head has at most
@@ -171,6 +172,7 @@ cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaSt
 cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream);
 int split_keys(bool e4m3, int d);  // keys of a block of the splitting kernel
-cudaError_t configure_paged_split();
+// slots[n]: blocks of four warps that the GPU runs at a time in clusters of n, 1 .. kMostSplit (0: none)
+cudaError_t configure_paged_split(int* slots);
 
 }  // namespace s2a

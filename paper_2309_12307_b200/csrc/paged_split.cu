@@ -3,7 +3,7 @@
 // A row is a new token and a query head; the rows of a sequence and KV head (new tokens times query heads of a KV head) read the
 // same keys.  With at most 64 of them the work is reading the cache: 4 d multiply-adds for each row and key against 4 d
 // bytes of bf16.  So the keys are split: a unit, 16 rows of one sequence and KV head, is worked on by a cluster of blocks, each
-// with a share of the keys, its four warps taking 16 or 32 keys in turn.  A warp has a ring of its own that TMA fills, a
+// with a share of the keys, its warps taking 16 or 32 keys in turn.  A warp has a ring of its own that TMA fills, a
 // running maximum and sum for its rows and the weighted sum of v in registers.  What the warps and then the blocks have is
 // joined through shared memory and the cluster's: no second launch, no workspace, no atomics.
 //
@@ -23,16 +23,17 @@ namespace {
 
 template <int HD, bool kE4M3>
 struct SplitCfg {
-    static constexpr int kWarps = 4, kThreads = 32 * kWarps;
+    static constexpr int kMostWarps = 4;
     static constexpr int kRowBytes = HD * (kE4M3 ? 1 : 2);        // a key's row
     static constexpr int kKeys = kRowBytes == 256 ? 16 : 32;      // keys of a warp's step
     static constexpr int kLine = kRowBytes < 128 ? kRowBytes : 128;  // bytes of a row in one box
     static constexpr int kBoxes = kRowBytes / kLine;
     static constexpr int kTile = kKeys * kRowBytes;               // K or V of a step
     static constexpr int kStageBytes = 2 * kTile;
-    static constexpr int kStages = 24576 / kStageBytes;           // 24 KB in flight for each warp, two blocks on an SM
+    static constexpr int kStages = 16384 / kStageBytes;           // 16 KB in flight for each warp, twelve warps on an SM
     static constexpr int kExpBytes = kE4M3 ? 2 * kKeys : 0;       // exponents of K and V
-    static constexpr int kSmemBytes = kWarps * kStages * (kStageBytes + kExpBytes) + kWarps * kStages * 8 + 16;  // and the abort flag
+    static constexpr int kWarpBytes = kStages * (kStageBytes + kExpBytes + 8);  // ring, exponents, barriers
+    static constexpr int smem_bytes(int warps) { return warps * kWarpBytes + 16; }  // and the abort flag
     static constexpr int kPartFloats = 16 * HD + 4 * 16;          // a warp's result: O, m, l, and the joined m, l
     static_assert(kPartFloats * 4 <= kStages * kStageBytes, "the ring holds a result");
     static_assert(kTile % 1024 == 0, "swizzle atoms");
@@ -69,17 +70,18 @@ constexpr float kLeast = -3.0e38f;   // stands for "no key yet": finite, so that
 constexpr float kLazy = 8.0f;        // a running maximum (of log2) that is exceeded by less stays
 
 template <int HD, bool kE4M3, int kRowTiles>
-__global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_split_kernel(const __grid_constant__ PagedSplitParams p) {
+__global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_paged_split_kernel(const __grid_constant__ PagedSplitParams p) {
     using C = SplitCfg<HD, kE4M3>;
     constexpr int kRows = 8 * kRowTiles;     // of a unit
     constexpr float kUp = kE4M3 ? 7.f : 0.f;  // weights are 2^kUp as large, see above
     extern __shared__ __align__(1024) uint8_t smem[];
     const PagedFwdParams& a = p.a;
+    const int warps = p.warps, threads = 32 * warps;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     uint8_t* ring = smem + warp * (C::kStages * C::kStageBytes);
-    uint8_t* exps = smem + C::kWarps * C::kStages * C::kStageBytes + warp * (C::kStages * C::kExpBytes);
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kWarps * C::kStages * (C::kStageBytes + C::kExpBytes)) + warp * C::kStages;
-    volatile int& abort_flag = *reinterpret_cast<volatile int*>(smem + C::kSmemBytes - 16);
+    uint8_t* exps = smem + warps * C::kStages * C::kStageBytes + warp * (C::kStages * C::kExpBytes);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + warps * C::kStages * (C::kStageBytes + C::kExpBytes)) + warp * C::kStages;
+    volatile int& abort_flag = *reinterpret_cast<volatile int*>(smem + warps * C::kWarpBytes);
 
     if (lane == 0) {
         for (int s = 0; s < C::kStages; ++s) mbar_init(&full[s], 1);
@@ -87,11 +89,11 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         tma_prefetch_desc(&p.tm_k);
         tma_prefetch_desc(&p.tm_v);
     }
+    if (threadIdx.x == 0) abort_flag = 0;
+    __syncthreads();
     release_successor();
     wait_for_predecessor();
-    // an earlier report: nothing is read or written, but every block of a cluster goes on to the end with the others
-    if (threadIdx.x == 0) abort_flag = *reinterpret_cast<volatile int*>(a.status);
-    __syncthreads();
+    const int standing = *reinterpret_cast<volatile int*>(a.status);
     if (blockIdx.x == 0) check_batch(a.batch, a.pool.page_log2, a.most_new, a.status, a.host_status);
     const WaitCtx ctx{&abort_flag, a.status, a.host_status};
 
@@ -107,8 +109,12 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     const KeyBlocks blocks = key_blocks(first_pos, last_pos, a.window, a.sinks, C::kKeys);
     const int share = (blocks.count + p.split - 1) / p.split;
     const int i0 = part * share + warp, i1 = (part + 1) * share < blocks.count ? (part + 1) * share : blocks.count;
-    int steps = i0 < i1 ? (i1 - i0 + C::kWarps - 1) / C::kWarps : 0;
-    if (__any_sync(0xffffffffu, *ctx.abort_flag != 0)) steps = 0;
+    int steps = i0 < i1 ? (i1 - i0 + warps - 1) / warps : 0;
+    // an earlier report: nothing is read or written, but every block of a cluster goes on to the end with the others
+    if (__any_sync(0xffffffffu, standing != 0)) {
+        steps = 0;
+        if (lane == 0) abort_flag = standing;
+    }
 
     // ---- loads of this warp: pages of its next 32 steps are in its lanes; lane 0 (and 1, where a step spans two pages) requests
     constexpr int kKeysLog2 = C::kKeys == 16 ? 4 : 5;
@@ -119,7 +125,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         const int x = from + lane;
         page[0] = page[1] = -1;
         if (x < steps) {
-            const int key = blocks.at(i0 + x * C::kWarps) * C::kKeys;
+            const int key = blocks.at(i0 + x * warps) * C::kKeys;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int k = key + (i << piece_log2);
@@ -133,7 +139,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     auto request = [&](int c) {
         if ((c & 31) == 0) look_up(c);
         const int st = c % C::kStages;
-        const int key = blocks.at(i0 + c * C::kWarps) * C::kKeys;
+        const int key = blocks.at(i0 + c * warps) * C::kKeys;
         const int p0 = __shfl_sync(0xffffffffu, page[0], c & 31), p1 = __shfl_sync(0xffffffffu, page[1], c & 31);
         const int mine = lane == 0 ? p0 : lane == 1 ? p1 : -1;
         const uint32_t bytes = static_cast<uint32_t>((2 * C::kRowBytes + (kE4M3 ? 2 : 0)) << piece_log2);
@@ -143,11 +149,8 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
             const int slot = (key + (lane << piece_log2)) & ((1 << a.pool.page_log2) - 1);
             const int row = ((mine * a.pool.Hkv + hk) << a.pool.page_log2) + slot;
             const uint32_t bar = smem_u32(&full[st]), dst = smem_u32(ring + st * C::kStageBytes) + ((lane << piece_log2) * C::kLine);
-#pragma unroll
-            for (int x = 0; x < C::kBoxes; ++x) {
-                tma_load_2d(dst + x * C::kKeys * C::kLine, &p.tm_k, bar, x * (C::kLine / (kE4M3 ? 1 : 2)), row);
-                tma_load_2d(dst + C::kTile + x * C::kKeys * C::kLine, &p.tm_v, bar, x * (C::kLine / (kE4M3 ? 1 : 2)), row);
-            }
+            tma_load_3d(dst, &p.tm_k, bar, 0, row, 0);
+            tma_load_3d(dst + C::kTile, &p.tm_v, bar, 0, row, 0);
             if constexpr (kE4M3) {
                 uint8_t* e = exps + st * C::kExpBytes + (lane << piece_log2);
                 bulk_load_1d(e, a.pool.k_exp + row, 1u << piece_log2, &full[st]);
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         const int st = c % C::kStages;
         if (!mbar_wait_uniform(&full[st], (c / C::kStages) & 1, ctx, kWaitPagedSplit + 1)) { ok = false; break; }
         const uint32_t sK = smem_u32(ring + st * C::kStageBytes), sV = sK + C::kTile, sE = smem_u32(exps + st * C::kExpBytes);
-        const int key0 = blocks.at(i0 + c * C::kWarps) * C::kKeys;
+        const int key0 = blocks.at(i0 + c * warps) * C::kKeys;
         const bool masked = !all_attend(first_pos, last_pos, key0, C::kKeys, a.window, a.sinks);
         constexpr int kTiles = C::kKeys / 16;
         float sc[kTiles][kRowTiles][4];
@@ -398,16 +401,18 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
         a.o[(to * a.H + h) * HD + col] = __float2bfloat16(value / sum);
         if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top - kUp + log2f(sum)) * 0.6931471805599453f;
     };
-    // ---- the four warps' results joined, into the first ring
+    // ---- the warps' results joined, into the first ring
     constexpr int kRing = C::kStages * C::kStageBytes / 4;  // floats of a ring
     float* first = reinterpret_cast<float*>(smem);
-    for (int e = threadIdx.x; e < rows * HD; e += C::kThreads) {
+    for (int e = threadIdx.x; e < rows * HD; e += threads) {
         const int row = e / HD;
         float top = kLeast, sum = 0.f, value = 0.f;
 #pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) top = fmaxf(top, first[w * kRing + kM + row]);
+        for (int w = 0; w < C::kMostWarps; ++w)
+            if (w < warps) top = fmaxf(top, first[w * kRing + kM + row]);
 #pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) {
+        for (int w = 0; w < C::kMostWarps; ++w) {
+            if (w >= warps) break;
             const float f = fast_exp2(first[w * kRing + kM + row] - top);
             sum += f * first[w * kRing + kL + row];
             value += f * first[w * kRing + e];
@@ -424,7 +429,7 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
     cluster_sync();
     // ---- the blocks' results joined, a share of the elements in each block
     const uint32_t at = smem_u32(first);
-    for (int e = part * C::kThreads + static_cast<int>(threadIdx.x); e < rows * HD; e += p.split * C::kThreads) {
+    for (int e = part * threads + static_cast<int>(threadIdx.x); e < rows * HD; e += p.split * threads) {
         const int row = e / HD;
         float tops[kMostSplit], top = kLeast, sum = 0.f, value = 0.f;
 #pragma unroll
@@ -447,26 +452,34 @@ __global__ void __launch_bounds__(SplitCfg<HD, kE4M3>::kThreads, 2) s2a_paged_sp
 template <int HD, bool kE4M3, int kRowTiles>
 cudaError_t configure_one() {
     auto kernel = s2a_paged_split_kernel<HD, kE4M3, kRowTiles>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitCfg<HD, kE4M3>::kSmemBytes);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               SplitCfg<HD, kE4M3>::smem_bytes(SplitCfg<HD, kE4M3>::kMostWarps));
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
+template <int HD, bool kE4M3>
+struct SplitLaunch {
+    cudaLaunchConfig_t config = {};
+    cudaLaunchAttribute attribute[2] = {};
+    SplitLaunch(const PagedSplitParams& p, unsigned grid, cudaStream_t stream) {
+        config.gridDim = dim3(grid);
+        config.blockDim = dim3(32u * static_cast<unsigned>(p.warps));
+        config.dynamicSmemBytes = SplitCfg<HD, kE4M3>::smem_bytes(p.warps);
+        config.stream = stream;
+        attribute[0].id = cudaLaunchAttributeClusterDimension;
+        attribute[0].val.clusterDim.x = static_cast<unsigned>(p.split), attribute[0].val.clusterDim.y = attribute[0].val.clusterDim.z = 1;
+        attribute[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attribute[1].val.programmaticStreamSerializationAllowed = 1;
+        config.attrs = attribute;
+        config.numAttrs = 2;
+    }
+};
+
 template <int HD, bool kE4M3, int kRowTiles>
 cudaError_t launch_one(const PagedSplitParams& p, cudaStream_t stream) {
-    using C = SplitCfg<HD, kE4M3>;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(p.split) * static_cast<unsigned>(p.row_blocks) * static_cast<unsigned>(p.a.batch.B) * static_cast<unsigned>(p.a.pool.Hkv));
-    config.blockDim = dim3(C::kThreads);
-    config.dynamicSmemBytes = C::kSmemBytes;
-    config.stream = stream;
-    cudaLaunchAttribute attribute[2] = {};
-    attribute[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attribute[0].val.programmaticStreamSerializationAllowed = 1;
-    attribute[1].id = cudaLaunchAttributeClusterDimension;
-    attribute[1].val.clusterDim.x = static_cast<unsigned>(p.split), attribute[1].val.clusterDim.y = attribute[1].val.clusterDim.z = 1;
-    config.attrs = attribute;
-    config.numAttrs = 2;
-    return cudaLaunchKernelEx(&config, s2a_paged_split_kernel<HD, kE4M3, kRowTiles>, p);
+    const unsigned units = static_cast<unsigned>(p.row_blocks) * static_cast<unsigned>(p.a.batch.B) * static_cast<unsigned>(p.a.pool.Hkv);
+    const SplitLaunch<HD, kE4M3> launch(p, units * static_cast<unsigned>(p.split), stream);
+    return cudaLaunchKernelEx(&launch.config, s2a_paged_split_kernel<HD, kE4M3, kRowTiles>, p);
 }
 
 }  // namespace
@@ -475,10 +488,22 @@ int split_keys(bool e4m3, int d) {
     return d == 64 ? (e4m3 ? SplitCfg<64, true>::kKeys : SplitCfg<64, false>::kKeys) : (e4m3 ? SplitCfg<128, true>::kKeys : SplitCfg<128, false>::kKeys);
 }
 
-cudaError_t configure_paged_split() {
+cudaError_t configure_paged_split(int* slots) {
     for (const cudaError_t e : {configure_one<64, false, 1>(), configure_one<64, false, 2>(), configure_one<64, true, 1>(), configure_one<64, true, 2>(),
                                 configure_one<128, false, 1>(), configure_one<128, false, 2>(), configure_one<128, true, 1>(), configure_one<128, true, 2>()})
         if (e != cudaSuccess) return e;
+    // (what limits the blocks on an SM is shared memory, of which all forms take the same)
+    for (int split = 1; split <= kMostSplit; ++split) {
+        PagedSplitParams p = {};
+        p.warps = 4, p.split = split;
+        SplitLaunch<128, true> launch(p, static_cast<unsigned>(split), nullptr);
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, s2a_paged_split_kernel<128, true, 1>, &launch.config) != cudaSuccess) {
+            cudaGetLastError();  // clusters of this size are not to be had
+            clusters = 0;
+        }
+        slots[split] = clusters * split;
+    }
     return cudaSuccess;
 }
 
