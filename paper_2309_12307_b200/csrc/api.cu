@@ -76,6 +76,8 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_paged_split(ds.cluster_slots);
         if (e != cudaSuccess) return cuda_fail(e);
+        e = configure_paged_fwd();
+        if (e != cudaSuccess) return cuda_fail(e);
         e = cudaGetSymbolAddress(reinterpret_cast<void**>(&ds.status_ptr), g_status_word);
         if (e != cudaSuccess) return cuda_fail(e);
         if (!g_host_status_registered) {

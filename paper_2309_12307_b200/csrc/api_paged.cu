@@ -56,6 +56,28 @@ int cache_tmap(CUtensorMap* tm, const s2a_cache* c, const void* pool, int keys) 
                        pool, 3, dims, strides, box);
 }
 
+// The tensor maps of the tiling kernel, see PagedTileParams.
+int tile_tmaps(PagedTileParams* p, const s2a_cache* c, const void* q, int H, int T) {
+    const cuuint64_t d = static_cast<cuuint64_t>(c->d), rows = static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size;
+    const cuuint32_t keys = static_cast<cuuint32_t>(c->page_size < kTile ? c->page_size : kTile);
+    const cuuint64_t q_dims[3] = {d, static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(T)}, q_strides[2] = {2 * d, 2 * d * H};
+    const cuuint32_t q_box[3] = {64, 1u << p->pack_log2, static_cast<cuuint32_t>(kTile) >> p->pack_log2};
+    int rc = encode_tmap(&p->tm_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, q, 3, q_dims, q_strides, q_box);
+    if (rc != S2A_OK) return rc;
+    const cuuint64_t dims[2] = {d, rows};
+    if (c->type == S2A_CACHE_E4M3) {
+        const cuuint32_t box[2] = {static_cast<cuuint32_t>(d), keys};
+        rc = encode_tmap(&p->tm_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_NONE, c->k, 2, dims, &d, box);
+        return rc != S2A_OK ? rc : encode_tmap(&p->tm_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_NONE, c->v, 2, dims, &d, box);
+    }
+    const cuuint64_t row_bytes = 2 * d;
+    const cuuint32_t box[2] = {64, keys};
+    const cuuint64_t k_dims[4] = {d, 2, 2, rows / 4}, k_strides[3] = {2 * row_bytes, row_bytes, 4 * row_bytes};
+    const cuuint32_t k_box[4] = {64, 2, 2, keys / 4};
+    rc = encode_tmap(&p->tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->k, 4, k_dims, k_strides, k_box);
+    return rc != S2A_OK ? rc : encode_tmap(&p->tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->v, 2, dims, &row_bytes, box);
+}
+
 // How the keys of the units (8 or 16 rows of a sequence and KV head) are dealt out: blocks of `warps` warps, `split` of them in a cluster
 // for each unit, whatever should be done first by this estimate, in microseconds:
 //   - the bytes of all units at the memory's rate.  A batch's sequences differ in length: the average is taken as 0.7 of the longest.
@@ -139,6 +161,9 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
     if ((rc = standing_status(ds)) != S2A_OK) return rc;
     const bool e4m3 = cache->type == S2A_CACHE_E4M3;
+    const int longest = batch->width * cache->page_size;  // no sequence has more tokens
+    if (window >= longest) window = 0;
+    if (sinks > longest) sinks = longest;
     const long long most_rows = static_cast<long long>(max_new) * (H / cache->Hkv);
     PagedFwdParams p;
     memset(&p, 0, sizeof p);
@@ -159,7 +184,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         ps.unit_rows = most_rows <= 8 ? 8 : 16;
         ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + ps.unit_rows - 1) / ps.unit_rows;
-        long long reach = static_cast<long long>(batch->width) * cache->page_size;
+        long long reach = longest;
         if (window > 0 && reach > static_cast<long long>(window) + sinks + max_new) reach = static_cast<long long>(window) + sinks + max_new;
         choose_pieces(&ps, ds, reach, 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
         if (static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
@@ -168,7 +193,20 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         if (e != cudaSuccess) return cuda_fail(e);
     }
     if (most_rows > kFewRows) {
-        e = launch_paged_fwd(p, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+        PagedTileParams pt;
+        memset(&pt, 0, sizeof pt);
+        pt.a = p;
+        while (pt.pack_log2 < 6 && p.rep % (2 << pt.pack_log2) == 0) ++pt.pack_log2;
+        if ((rc = tile_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
+        const int groups = H >> pt.pack_log2;
+        // single tiles where pairs would leave multiprocessors without work
+        pt.span_log2 = 8 - pt.pack_log2;
+        pt.single = static_cast<long long>(first_slot(batch->T, batch->B, pt.span_log2)) * groups <= ds->n_sm;
+        if (pt.single) --pt.span_log2;
+        pt.slots = first_slot(batch->T, batch->B, pt.span_log2);
+        if (static_cast<long long>(pt.slots) * groups > kIntMax) return S2A_ERR_UNSUPPORTED;
+        pt.by_slots = FastDiv(pt.slots), pt.by_groups_of_kv = FastDiv(p.rep >> pt.pack_log2);
+        e = launch_paged_fwd(pt, e4m3, cache->d, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return S2A_OK;

@@ -166,13 +166,39 @@ struct alignas(64) PagedSplitParams {
     FastDiv by_split, by_row_blocks, by_heads, by_rep;
 };
 
+// Places of the tiling kernel's work items.  Sequence b has the places from first_slot() on, one for each 2^span_log2 of its tokens;
+// first_slot(starts[b + 1], b + 1) leaves it enough of them whatever `starts` are, so the places are known without adding up.
+__host__ __device__ inline int first_slot(int row0, int b, int span_log2) { return (row0 >> span_log2) + b; }
+__host__ __device__ inline int find_slot(const int* starts, int B, int span_log2, int slot) {
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (first_slot(S2A_LOAD(starts + mid), mid, span_log2) <= slot) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+struct alignas(64) PagedTileParams {
+    CUtensorMap tm_q;        // bf16 (d, H, T), box (64, pack, 128 / pack), 128-byte swizzle
+    CUtensorMap tm_k, tm_v;  // V in bf16 (d, rows of the pool), box (64, min(page_size, 128)), swizzled; K the same with the two middle ones of every
+                             // four rows exchanged; in 8 bits both (d, rows of the pool), box (d, min(page_size, 128)), not swizzled
+    PagedFwdParams a;
+    int pack_log2;           // query heads of a KV head that are rows of one tile
+    int span_log2;           // tokens of a work item: two tiles, or one (`single`)
+    bool single;
+    int slots;               // of a head group: first_slot(T, B)
+    FastDiv by_slots, by_groups_of_kv;  // head groups of a KV head: rep / pack
+};
+
 // Enqueue on `stream`; return the launch error, if any.
 cudaError_t launch_cache_write(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
-cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream);
 int split_keys(bool e4m3, int d);  // keys of a block of the splitting kernel
 // slots[n]: blocks of four warps that the GPU runs at a time in clusters of n, 1 .. kMostSplit (0: none)
 cudaError_t configure_paged_split(int* slots);
+cudaError_t configure_paged_fwd();
 
 }  // namespace s2a

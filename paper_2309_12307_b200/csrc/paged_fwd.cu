@@ -1,11 +1,25 @@
-// Attention of new tokens over the paged cache.
+// Attention of many rows over the paged cache, for sm_100a: pieces of prompts.
 //
-// With p the position of a new token, s_j = scale * q . k_j over the visible keys j <= p (with a window also j > p - window or
-// j < sinks): o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), lse = m + log of that sum, in one pass with a running
-// maximum m.
+// With p the position of a new token, s_j = scale * q . k_j over the keys j it attends (j <= p, with a window also j > p - window or
+// j < sinks): o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), lse = m + log of that sum, in one pass with a running maximum m.
 //
-// One warp for each new token and query head.  32 keys at a time: every lane has one key and its whole score, then every lane
-// has d / 32 columns of o and adds the 32 weighted rows of v.
+// A tile is 128 rows that read the same KV head: `pack` query heads (the largest power of two that divides the query heads of a KV head) of
+// 128 / pack neighbouring tokens, token by token, which is one TMA box of q.  A work item is a pair of neighbouring tiles of a sequence
+// and head group, against which the cache is streamed in tiles of 128 keys: the blocks of key_blocks(), which are the first
+// tokens' and the window's where there is a window.  A key tile is one TMA box for each page (or 128 keys of one).
+//
+// One persistent block per SM, 512 threads, with the roles and the tensor-memory layout of s2a_fwd_kernel (fwd_kernel.cu), whose
+// comments say what they are for:
+//   warps 0-3, 4-7   softmax, two groups that take the tiles of an item in turn: one thread per score row
+//   warps 8-11       O / l -> bf16 -> global memory; with a cache in 8 bits also K and V to bf16
+//   warp 12          work items (cluster launch control), pages and TMA loads, running ahead across items
+//   warps 13, 14     tcgen05 MMAs: S = Q K_j^T of both tiles in turn / O += P V_j
+// Tensor memory: O of either tile, P of either tile, then one score buffer (HD = 128) or two.
+//
+// 8-bit caches: TMA brings the codes to a ring of two raw tiles, warps 8-11 write them as bf16, times their row's power of two,
+// where the products read them.  Both steps are exact (paged.h).  These warps have one instruction stream on each scheduler beside the
+// softmax's two; multiplying the scores and the weights by the powers instead would be about as many instructions, in the
+// warps that everything waits for.
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -13,84 +27,667 @@ namespace s2a {
 namespace {
 
 template <int HD, bool kE4M3>
-__device__ __forceinline__ float cached_value(const void* pool, long long row, int c, float factor) {
-    if constexpr (kE4M3) {
-        uint32_t lo, hi;
-        e4m3_spread(static_cast<const uint8_t*>(pool)[row * HD + c], lo, hi);
-        return bf16_low(bf16x2_mul(lo, kTwoTo120)) * factor;
-    } else {
-        return __bfloat162float(static_cast<const __nv_bfloat16*>(pool)[row * HD + c]);
-    }
-}
-__device__ __forceinline__ float exponent_factor(int e) {
-    return e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+struct PagedCfg {
+    static constexpr int kThreads = 512;
+    static constexpr int kBoxes = HD / 64;                  // 64-column boxes per tile
+    static constexpr int kBoxBytes = kTile * 128;           // 128 rows x 128 bytes
+    static constexpr int kTileBytes = kBoxes * kBoxBytes;   // one Q, K or V tile in bf16
+    static constexpr int kRing = (HD == 128) ? 4 : 8;       // K and V tiles in flight: K_0 V_0 K_1 V_1 ...
+    static constexpr int kRawRing = kE4M3 ? 2 : 0;          // the same as codes
+    static constexpr int kRawBytes = kTile * HD;
+    static constexpr int kStatBytes = 2 * 2 * kTile * 4;    // row statistics handed to the read-out
+    // Items in flight: as many as s2a_fwd_kernel's for its ring, see there.
+    static constexpr int kSched = (HD == 128) ? 6 : 8;
+    static_assert(kSched % 2 == 0 && kSched >= kRing / 2 + 3, "an item's slot is free when it is written again");
+    static constexpr int kBarBytes = (HD == 128) ? 1024 : 2048;
+    static constexpr int kSmemBytes = (2 + kRing) * kTileBytes + kRawRing * kRawBytes + kBarBytes + kStatBytes;
+    static_assert(kSmemBytes <= 232448, "shared memory");
+    static constexpr int kTmemCols = 512;
+    static constexpr int kColO = 0, kColP = 2 * HD, kColS = 2 * HD + 2 * 64;
+    static constexpr int kScoreBufs = (HD == 128) ? 1 : 2;
+    static_assert(kColS + kScoreBufs * kTile <= kTmemCols, "tensor memory");
+    // registers per thread after the split; the launch gives kRegsLaunch to each of the 512
+    static constexpr int kRegsLaunch = 128, kRegsSoftmax = 192, kRegsReadOut = 80, kRegsIssue = 48;
+    static_assert(2 * kRegsSoftmax + kRegsReadOut + kRegsIssue <= 4 * kRegsLaunch, "register split");
+};
+
+struct PagedItem {
+    int b, group;          // sequence (-1: no more items), head group
+    int row[2], tokens[2];  // of either tile: first row of q and o, tokens (0: no such tile)
+    int pos;               // position of the token at row[1]
+    int n[2];              // key tiles that either tile's products take: the first n of the item's
+    int sink_blocks, low_block;
+    __device__ __forceinline__ int key_tile(int j) const { return j < sink_blocks ? j : low_block + j - sink_blocks; }
+    // (indexed by a variable, a copy in registers would have to go through local memory)
+    __device__ __forceinline__ int row_of(int t) const { return t ? row[1] : row[0]; }
+    __device__ __forceinline__ int tokens_of(int t) const { return t ? tokens[1] : tokens[0]; }
+    __device__ __forceinline__ int first_pos(int t) const { return t ? pos : pos - (row[1] - row[0]); }
+};
+
+template <int HD, bool kE4M3>
+struct PagedBars {
+    using C = PagedCfg<HD, kE4M3>;
+    // by group of softmax warps
+    uint64_t q_full[2], q_empty[2];
+    uint64_t s_full[2], s_empty[2];
+    uint64_t p_full[2], p_rest[2], p_empty[2];
+    uint64_t o_full[2], o_empty[2];
+    uint64_t stat_full[2], stat_empty[2];
+    uint64_t kv_full[C::kRing], kv_empty[C::kRing];
+    uint64_t raw_full[2], raw_empty[2];
+    uint64_t sched_full[C::kSched];
+    uint64_t list_full[2][C::kSched];
+    uint64_t clc, drain[2];
+    alignas(16) uint8_t clc_resp[16];
+    alignas(16) int8_t exps[2][kE4M3 ? kTile : 16];  // of the raw tiles
+    PagedItem item[C::kSched];
+    uint8_t list_slot[2][C::kSched];
+    uint32_t tmem_slot;
+    int abort_flag;
+};
+
+// The later tile of a pair is the only one where an item has one; the groups of softmax warps take it in turn (see s2a_fwd_kernel).
+__device__ __forceinline__ int group_of_tile(int item, int t) { return (item & 1) ^ t ^ 1; }
+__device__ __forceinline__ int tile_of_group(int item, int group) { return (item & 1) ^ group ^ 1; }
+
+constexpr float kLazyRescale = 8.0f;
+constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
+__device__ __forceinline__ constexpr int key_of_column(int x) { return (x & ~3) | ((x & 1) << 1) | ((x >> 1) & 1); }
+
+// Work item `id`; false: there is none (the places of a sequence are counted generously, see PagedTileParams::slots).
+__device__ __forceinline__ bool paged_item(const PagedTileParams& p, int id, PagedItem* w) {
+    const PagedFwdParams& a = p.a;
+    int slot;
+    w->group = p.by_slots(id, &slot);
+    slot = p.slots - 1 - slot;  // the last tiles first: they have most keys
+    const int b = find_slot(a.batch.starts, a.batch.B, p.span_log2, slot);
+    Sequence s;
+    if (sequence_of(a.batch, a.pool.page_log2, a.most_new, b, &s) != 0 || s.n * a.rep <= a.few_rows) return false;
+    const long long at = static_cast<long long>(slot - first_slot(s.row0, b, p.span_log2)) << p.span_log2;
+    if (at < 0 || at >= s.n) return false;
+    const int first = static_cast<int>(at), left = s.n - first, tile = kTile >> p.pack_log2;
+    w->b = b;
+    const bool two = !p.single && left > tile;
+    w->tokens[0] = two ? tile : 0;
+    w->tokens[1] = two ? (left - tile < tile ? left - tile : tile) : (left < tile ? left : tile);
+    w->row[0] = s.row0 + first;
+    w->row[1] = w->row[0] + w->tokens[0];
+    w->pos = s.length - s.n + first + w->tokens[0];
+    const KeyBlocks k = key_blocks(w->pos - w->tokens[0], w->pos + w->tokens[1] - 1, a.window, a.sinks, kTile);
+    w->sink_blocks = k.sink_blocks, w->low_block = k.low_block;
+    w->n[1] = k.count;
+    w->n[0] = two ? k.sink_blocks + (w->pos - 1) / kTile + 1 - k.low_block : 0;
+    return true;
 }
 
 template <int HD, bool kE4M3>
-__global__ void __launch_bounds__(128) s2a_paged_fwd_kernel(const __grid_constant__ PagedFwdParams p) {
-    constexpr int kCols = HD / 32;
-    __shared__ float s_q[4][HD];
-    release_successor();
+__global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fwd_kernel(const __grid_constant__ PagedTileParams p) {
+    using C = PagedCfg<HD, kE4M3>;
+    using Bars = PagedBars<HD, kE4M3>;
+    static_assert(sizeof(Bars) <= C::kBarBytes, "barrier block");
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* sQ = smem;                                // two query tiles
+    uint8_t* sKV = sQ + 2 * C::kTileBytes;             // ring of K and V tiles
+    uint8_t* sRaw = sKV + C::kRing * C::kTileBytes;    // ring of their codes
+    Bars* bars = reinterpret_cast<Bars*>(sRaw + C::kRawRing * C::kRawBytes);
+    float* sStat = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + C::kBarBytes);  // [group][m, l][128 rows]
+    const PagedFwdParams& a = p.a;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&bars->q_full[t], 1);
+            mbar_init(&bars->q_empty[t], 1);
+            mbar_init(&bars->s_full[t], 1);
+            mbar_init(&bars->s_empty[t], 4);
+            mbar_init(&bars->p_empty[t], 1);
+            mbar_init(&bars->p_full[t], 4);
+            mbar_init(&bars->p_rest[t], 4);
+            mbar_init(&bars->o_full[t], 1);
+            mbar_init(&bars->o_empty[t], 4);
+            mbar_init(&bars->stat_full[t], 4);
+            mbar_init(&bars->stat_empty[t], 4);
+            mbar_init(&bars->drain[t], 1);
+            mbar_init(&bars->raw_full[t], 1);
+            mbar_init(&bars->raw_empty[t], 4);
+        }
+        for (int x = 0; x < C::kRing; ++x) {
+            mbar_init(&bars->kv_full[x], kE4M3 ? 4 : 1);
+            mbar_init(&bars->kv_empty[x], 1);
+        }
+        for (int x = 0; x < C::kSched; ++x) {
+            mbar_init(&bars->sched_full[x], 1);
+            mbar_init(&bars->list_full[0][x], 1);
+            mbar_init(&bars->list_full[1][x], 1);
+        }
+        mbar_init(&bars->clc, 1);
+        fence_barrier_init();
+        tma_prefetch_desc(&p.tm_q);
+        tma_prefetch_desc(&p.tm_k);
+        tma_prefetch_desc(&p.tm_v);
+    }
+    if (warp == 13) {
+        tmem_alloc(&bars->tmem_slot, C::kTmemCols);
+        tmem_relinquish();
+    }
     wait_for_predecessor();
-    if (*reinterpret_cast<volatile int*>(p.status) != 0) return;
-    if (blockIdx.x == 0) check_batch(p.batch, p.pool.page_log2, p.most_new, p.status, p.host_status);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long id = static_cast<long long>(blockIdx.x) * 4 + warp;
-    if (id >= static_cast<long long>(p.batch.T) * p.H) return;
-    const int t = static_cast<int>(id / p.H), h = static_cast<int>(id % p.H), hk = h / p.rep;
-    const int b = find_sequence(p.batch.starts, p.batch.B, t);
-    Sequence s;
-    if (sequence_of(p.batch, p.pool.page_log2, p.most_new, b, &s) != 0 || t < s.row0 || t >= s.row0 + s.n) return;
-    if (s.n * p.rep <= p.few_rows) return;
-    const int pos = s.length - s.n + t - s.row0;
-    const int low = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;  // first key of the window
-    const int sinks = p.sinks < low ? p.sinks : low;
-    for (int c = lane; c < HD; c += 32) s_q[warp][c] = __bfloat162float(p.q[(static_cast<long long>(t) * p.H + h) * HD + c]);
-    __syncwarp();
-    float m = -INFINITY, l = 0.f, acc[kCols] = {};
-    const int visible = sinks + pos + 1 - low;
-    for (int first = 0; first < visible; first += 32) {
-        const int x = first + lane, j = x < sinks ? x : low + x - sinks;
-        long long row = -1;
-        float score = -INFINITY, v_factor = 1.f;
-        if (x < visible) {
-            row = pool_row(p.batch, p.pool, b, j);
-            if (row < 0) report_bad_index(p.status, p.host_status, kBadPage);
+    // An earlier report (a wait that expired, a value out of range) leaves the status word set: nothing is done then.
+    if (threadIdx.x == 0) bars->abort_flag = *reinterpret_cast<volatile int*>(a.status);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    release_successor();
+    const uint32_t tmem_base = bars->tmem_slot;
+    if (bars->abort_flag != 0) {
+        if (warp == 13) tmem_dealloc(tmem_base, C::kTmemCols);
+        return;
+    }
+    if (blockIdx.x == 0) check_batch(a.batch, a.pool.page_log2, a.most_new, a.status, a.host_status);
+    const WaitCtx ctx{&bars->abort_flag, a.status, a.host_status};
+
+    auto next_item = [&](int k, int where, PagedItem* w) -> bool {
+        if (!mbar_wait_uniform(&bars->sched_full[k % C::kSched], (k / C::kSched) & 1, ctx, where)) return false;
+        *w = bars->item[k % C::kSched];
+        return w->b >= 0;
+    };
+
+    if (warp >= 12) {
+        setmaxnreg_dec<C::kRegsIssue>();
+        if (warp == 12) {
+            // ======================= work items, TMA loads ===========================================
+            // The whole warp walks the loop: lane i requests the i-th page of a tile, and has looked up that of the next
+            // tile before it waits for room.
+            uint32_t kv = 0;              // K and V tiles requested so far
+            uint32_t n_q[2] = {0, 0};     // query tiles requested so far for either group
+            uint32_t n_list[2] = {0, 0};  // items in the list of either group
+            uint32_t n_clc = 0;
+            bool ok = true;
+            int id = static_cast<int>(blockIdx.x);
+            const int piece_log2 = a.pool.page_log2 < 7 ? a.pool.page_log2 : 7;  // keys of a box
+            auto next_id = [&]() {
+                if (lane == 0) {
+                    mbar_expect_tx(&bars->clc, 16);
+                    clc_try_cancel(bars->clc_resp, &bars->clc);
+                }
+                __syncwarp();
+                if (!mbar_wait_uniform(&bars->clc, n_clc & 1, ctx, kWaitPagedFwd + 1)) {
+                    if (lane == 0) mbar_wait_drain(&bars->clc, n_clc & 1);  // the answer must not land after the block has gone
+                    ok = false;
+                    return -1;
+                }
+                ++n_clc;
+                const int x = clc_granted_block(bars->clc_resp);
+                fence_proxy_async();  // the answer has been read before the next one is written
+                __syncwarp();
+                return x;
+            };
+            auto load_q = [&](const PagedItem& w, int t, int g) {
+                const uint32_t n = g ? n_q[1]++ : n_q[0]++;
+                if (!mbar_wait_uniform(&bars->q_empty[g], (n & 1) ^ 1, ctx, kWaitPagedFwd + 2)) {
+                    --(g ? n_q[1] : n_q[0]);
+                    ok = false;
+                    return;
+                }
+                if (lane == 0) {
+                    mbar_expect_tx(&bars->q_full[g], C::kTileBytes);
+                    for (int bx = 0; bx < C::kBoxes; ++bx)
+                        tma_load_3d(smem_u32(sQ + g * C::kTileBytes + bx * C::kBoxBytes), &p.tm_q, smem_u32(&bars->q_full[g]), bx * 64,
+                                    w.group << p.pack_log2, w.row_of(t));
+                }
+                __syncwarp();
+            };
+            // pool row (in head hk) of the piece of key tile `tile` that is this lane's, -1: none
+            auto look_up = [&](const PagedItem& w, int hk, int length, int tile) {
+                const int key = tile * kTile + (lane << piece_log2);
+                if (lane >= kTile >> piece_log2 || key >= length) return -1;
+                const int page = page_of(a.batch, a.pool.pages, w.b, key >> a.pool.page_log2);
+                if (page < 0) {
+                    report_bad_index(a.status, a.host_status, kBadPage);
+                    return -1;
+                }
+                return ((page * a.pool.Hkv + hk) << a.pool.page_log2) + (key & ((1 << a.pool.page_log2) - 1));
+            };
+            auto load_kv = [&](int row, bool k_tile) {
+                const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
+                if constexpr (kE4M3) {
+                    const int st = kv % 2;
+                    if (!mbar_wait_uniform(&bars->raw_empty[st], ((kv / 2) & 1) ^ 1, ctx, kWaitPagedFwd + 3)) { ok = false; return; }
+                    if (lane == 0) mbar_expect_tx(&bars->raw_full[st], static_cast<uint32_t>((boxes * (HD + 1)) << piece_log2));
+                    __syncwarp();
+                    if (row >= 0) {
+                        const int at = lane << piece_log2;
+                        tma_load_2d(smem_u32(sRaw + st * C::kRawBytes + at * HD), k_tile ? &p.tm_k : &p.tm_v, smem_u32(&bars->raw_full[st]), 0, row);
+                        bulk_load_1d(&bars->exps[st][at], (k_tile ? a.pool.k_exp : a.pool.v_exp) + row, 1u << piece_log2, &bars->raw_full[st]);
+                    }
+                } else {
+                    const int st = kv % C::kRing;
+                    if (!mbar_wait_uniform(&bars->kv_empty[st], ((kv / C::kRing) & 1) ^ 1, ctx, kWaitPagedFwd + 3)) { ok = false; return; }
+                    if (lane == 0) mbar_expect_tx(&bars->kv_full[st], static_cast<uint32_t>((boxes * HD * 2) << piece_log2));
+                    __syncwarp();
+                    if (row >= 0) {
+                        const uint32_t dst = smem_u32(sKV + st * C::kTileBytes) + (lane << piece_log2) * 128, bar = smem_u32(&bars->kv_full[st]);
+                        for (int bx = 0; bx < C::kBoxes; ++bx) {
+                            if (k_tile) tma_load_4d_at(dst + bx * C::kBoxBytes, &p.tm_k, bar, bx * 64, 0, 0, row / 4);
+                            else tma_load_2d(dst + bx * C::kBoxBytes, &p.tm_v, bar, bx * 64, row);
+                        }
+                    }
+                }
+                __syncwarp();
+                ++kv;
+            };
+            for (int k = 0; ok; ++k) {
+                PagedItem w;
+                while (id >= 0 && !paged_item(p, id, &w)) id = next_id();
+                if (id < 0) w.b = -1;
+                const int g1 = group_of_tile(k, 1), g0 = group_of_tile(k, 0);
+                if (lane == 0) {
+                    bars->item[k % C::kSched] = w;
+                    mbar_arrive(&bars->sched_full[k % C::kSched]);  // release: the item is visible to whoever sees the phase
+                }
+                auto enlist = [&](int g) {
+                    const uint32_t n = g ? n_list[1]++ : n_list[0]++;
+                    if (lane == 0) {
+                        bars->list_slot[g][n % C::kSched] = static_cast<uint8_t>(k % C::kSched);
+                        mbar_arrive(&bars->list_full[g][n % C::kSched]);
+                    }
+                };
+                enlist(g1);
+                if (id < 0 || w.n[0] > 0) enlist(g0);
+                __syncwarp();
+                if (id < 0) break;
+                const int hk = p.by_groups_of_kv(w.group), length = w.pos + w.tokens[1];  // (keys behind the last token are nobody's)
+                int row = look_up(w, hk, length, w.key_tile(0));
+                for (int j = 0; ok && j < w.n[1]; ++j) {
+                    const int next = j + 1 < w.n[1] ? look_up(w, hk, length, w.key_tile(j + 1)) : -1;
+                    load_kv(row, true);
+                    if (j == 0 && ok) load_q(w, 1, g1);
+                    if (j == 0 && ok && w.n[0] > 0) load_q(w, 0, g0);
+                    if (ok) load_kv(row, false);
+                    row = next;
+                }
+                if (ok) id = next_id();
+            }
+            // nothing may land after the block has gone
+            if (__any_sync(0xffffffffu, bars->abort_flag != 0) && lane == 0) {
+                for (int t = 0; t < 2; ++t)
+                    if (n_q[t] > 0) mbar_wait_drain(&bars->q_full[t], (n_q[t] - 1) & 1);
+                constexpr uint32_t kIn = kE4M3 ? 2 : C::kRing;
+                for (uint32_t x = (kv > kIn ? kv - kIn : 0); x < kv; ++x)
+                    mbar_wait_drain(kE4M3 ? &bars->raw_full[x % 2] : &bars->kv_full[x % C::kRing], (x / kIn) & 1);
+            }
+            __syncwarp();
+        } else if (warp <= 14) {
+            // ======================= MMA issuers: warp 13 for S = Q K^T, warp 14 for O += P V ============
+            constexpr uint32_t idesc_s = idesc_bf16(128, kTile, 0, 0);  // S = Q K^T   (both K-major)
+            constexpr uint32_t idesc_o = idesc_bf16(128, HD, 0, 1);     // O += P V    (V is MN-major)
+            const bool is_s = warp == 13;
+            const uint32_t aKV = smem_u32(sKV), dQ0 = desc_lo_k_major(smem_u32(sQ));
+            uint32_t kv = 0;                    // ring position of the item's K_0
+            uint32_t n_it[2] = {0, 0};          // items of either group so far
+            uint32_t n_st[2] = {0, 0}, n_s = 0; // steps of either group, score products
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                PagedItem w;
+                if (!next_item(k, kWaitPagedFwd + 10, &w)) break;
+                const int n1 = w.n[1], n0 = w.n[0];
+                const int end = w.pos + w.tokens[1];  // keys from here on are no key of the item
+#pragma unroll 1
+                for (int h = 0; ok && h < 2 * n1; ++h) {
+                    const int t = (h & 1) ^ 1, j = h >> 1, n = t ? n1 : n0, g = group_of_tile(k, t);
+                    if (j >= n) continue;
+                    const uint32_t x = kv + 2 * j + (is_s ? 0 : 1);
+                    const bool last_use = t == 0 || j >= n0;  // of this K or V tile
+                    const uint32_t st = (g ? n_st[1] : n_st[0]) & 1, it = (g ? n_it[1] : n_it[0]) & 1;
+                    // what tile 1 has used, tile 0 need not wait for again
+                    if (t == 1 && !mbar_wait_uniform(&bars->kv_full[x % C::kRing], (x / C::kRing) & 1, ctx, kWaitPagedFwd + 5)) { ok = false; break; }
+                    if (is_s) {
+                        if (j == 0 && !mbar_wait_uniform(&bars->q_full[g], it, ctx, kWaitPagedFwd + 4)) { ok = false; break; }
+                        const int buf = C::kScoreBufs == 1 ? 0 : g;
+                        const uint32_t use = C::kScoreBufs == 1 ? n_s & 1 : st;
+                        if (!mbar_wait_uniform(&bars->s_empty[buf], use ^ 1, ctx, kWaitPagedFwd + 6)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t at_g = dQ0 + g * (C::kTileBytes >> 4);
+                        const uint32_t at_x = desc_lo_k_major(aKV + (x % C::kRing) * C::kTileBytes);
+                        const uint32_t acc = tmem_base + C::kColS + buf * kTile;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < HD / 16; ++kk)
+                                mma_ss(acc, at_g + desc_step_k_major(kk, C::kBoxBytes), at_x + desc_step_k_major(kk, C::kBoxBytes), idesc_s, kk > 0);
+                            mma_commit(&bars->s_full[g]);
+                            if (last_use) mma_commit(&bars->kv_empty[x % C::kRing]);
+                            if (j == n - 1) mma_commit(&bars->q_empty[g]);
+                        }
+                        __syncwarp();
+                        ++n_s;
+                    } else {
+                        if (!kE4M3 && t == 1) {
+                            // The rows of V past the last key hold whatever the page held before, or what the ring did: a weight of
+                            // zero does not make a NaN go away.  (8-bit tiles are written without them.)
+                            const int valid = end - w.key_tile(j) * kTile;
+                            if (valid < kTile) {
+                                for (int c = valid * 8 + lane; c < kTile * 8; c += 32)
+                                    for (int bx = 0; bx < C::kBoxes; ++bx)
+                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(aKV + (x % C::kRing) * C::kTileBytes + bx * C::kBoxBytes + c * 16),
+                                                     "r"(0)
+                                                     : "memory");
+                                fence_proxy_async();
+                                __syncwarp();
+                            }
+                        }
+                        if (j == 0 && !mbar_wait_uniform(&bars->o_empty[g], it ^ 1, ctx, kWaitPagedFwd + 7)) { ok = false; break; }
+                        const uint32_t at_x = desc_lo_mn_major(aKV + (x % C::kRing) * C::kTileBytes, C::kBoxBytes);
+                        const uint32_t at_g = tmem_base + C::kColP + g * 64, acc = tmem_base + C::kColO + g * HD;
+                        if (!mbar_wait_uniform(&bars->p_full[g], st, ctx, kWaitPagedFwd + 8)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < 6; ++kk) mma_ts(acc, at_g + kk * 8, at_x + kk * kDescStepMn, idesc_o, (j > 0) || (kk > 0));
+                        }
+                        __syncwarp();
+                        if (!mbar_wait_uniform(&bars->p_rest[g], st, ctx, kWaitPagedFwd + 9)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 6; kk < 8; ++kk) mma_ts(acc, at_g + kk * 8, at_x + kk * kDescStepMn, idesc_o, 1);
+                            mma_commit(&bars->p_empty[g]);
+                            if (last_use) mma_commit(&bars->kv_empty[x % C::kRing]);
+                            if (j == n - 1) mma_commit(&bars->o_full[g]);
+                        }
+                        __syncwarp();
+                    }
+                    if (g) ++n_st[1], n_it[1] += j == n - 1;
+                    else ++n_st[0], n_it[0] += j == n - 1;
+                }
+                kv += 2 * n1;
+            }
+            // MMAs already issued must finish before tensor memory is released
+            if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&bars->abort_flag) != 0)) {
+                if (elect_one()) {
+                    mma_commit(&bars->drain[is_s]);
+                    mbar_wait_drain(&bars->drain[is_s], 0);
+                }
+            }
+            __syncwarp();
         }
-        if (row >= 0) {
-            row += static_cast<long long>(hk) << p.pool.page_log2;
-            float k_factor = 1.f;
-            if (kE4M3) k_factor = exponent_factor(p.pool.k_exp[row]), v_factor = exponent_factor(p.pool.v_exp[row]);
-            score = 0.f;
-            for (int c = 0; c < HD; ++c) score = fmaf(s_q[warp][c], cached_value<HD, kE4M3>(p.pool.k, row, c, k_factor), score);
-            score *= p.scale_log2;
+    } else if (warp >= 8) {
+        // =========================== read-out, codes to bf16 ==========================================
+        setmaxnreg_dec<C::kRegsReadOut>();
+        const int quad = warp & 3;
+        const int row = quad * 32 + lane;
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
+        uint32_t n_o[2] = {0, 0};
+        auto read_out = [&](int k, const PagedItem& w) -> bool {
+#pragma unroll 1
+            for (int t = 0; t < 2; ++t) {
+                if (w.tokens_of(t) == 0) continue;
+                const int g = group_of_tile(k, t);
+                const uint32_t n_done = g ? n_o[1]++ : n_o[0]++;
+                if (!mbar_wait_uniform(&bars->stat_full[g], n_done & 1, ctx, kWaitPagedFwd + 12) ||
+                    !mbar_wait_uniform(&bars->o_full[g], n_done & 1, ctx, kWaitPagedFwd + 13))
+                    return false;
+                tc_fence_after();
+                const float m = sStat[g * 256 + row], l = sStat[g * 256 + 128 + row];
+                mbar_arrive_warp(&bars->stat_empty[g]);
+                const float inv_l = 1.0f / l;
+                const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
+                const bool valid = token < w.tokens_of(t);  // the others are rows of another sequence, or of none
+                const long long at = w.row_of(t) + token;
+                uint4* dst = reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD);
+#pragma unroll 1
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t r[32];
+                    tmem_ld_32x32(t_row + C::kColO + g * HD + c * 32, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint4 pk;
+                        pk.x = pack_bf16(__uint_as_float(r[8 * e + 0]) * inv_l, __uint_as_float(r[8 * e + 1]) * inv_l);
+                        pk.y = pack_bf16(__uint_as_float(r[8 * e + 2]) * inv_l, __uint_as_float(r[8 * e + 3]) * inv_l);
+                        pk.z = pack_bf16(__uint_as_float(r[8 * e + 4]) * inv_l, __uint_as_float(r[8 * e + 5]) * inv_l);
+                        pk.w = pack_bf16(__uint_as_float(r[8 * e + 6]) * inv_l, __uint_as_float(r[8 * e + 7]) * inv_l);
+                        if (valid) dst[4 * c + e] = pk;
+                    }
+                }
+                tc_fence_before();
+                mbar_arrive_warp(&bars->o_empty[g]);
+                if (valid) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
+            }
+            return true;
+        };
+        if constexpr (!kE4M3) {
+            for (int k = 0;; ++k) {
+                PagedItem w;
+                if (!next_item(k, kWaitPagedFwd + 11, &w)) break;
+                if (!read_out(k, w)) break;
+            }
+        } else {
+            // The tiles of an item, and between its first ones the read-out of the item before: those tiles need no room that
+            // the read-out has to make first (the ring's), and what comes behind them would have to wait for the item's products anyway.
+            uint32_t kv = 0;
+            bool ok = true;
+            PagedItem before;
+            before.b = -1;
+            for (int k = 0; ok; ++k) {
+                PagedItem w;
+                const bool more = next_item(k, kWaitPagedFwd + 11, &w);
+                const int tiles = more ? 2 * w.n[1] : 0, pause = tiles < C::kRing - 1 ? tiles : C::kRing - 1;
+                const int end = more ? w.pos + w.tokens[1] : 0;
+                for (int x = 0; ok && x <= tiles; ++x) {
+                    if (x == pause && before.b >= 0) ok = read_out(k - 1, before);
+                    if (!ok || x == tiles) break;
+                    const int raw = kv % 2, st = kv % C::kRing;
+                    if (!mbar_wait_uniform(&bars->raw_full[raw], (kv / 2) & 1, ctx, kWaitPagedFwd + 18) ||
+                        !mbar_wait_uniform(&bars->kv_empty[st], ((kv / C::kRing) & 1) ^ 1, ctx, kWaitPagedFwd + 19)) {
+                        ok = false;
+                        break;
+                    }
+                    const bool is_v = (x & 1) != 0;
+                    const int valid = end - w.key_tile(x >> 1) * kTile;  // rows of the tile that hold keys
+                    const uint32_t src = smem_u32(sRaw + raw * C::kRawBytes), dst = smem_u32(sKV + st * C::kTileBytes), es = smem_u32(bars->exps[raw]);
+                    constexpr int kLanes = HD / 16, kRowsAtOnce = 128 / kLanes;  // 16 codes a thread
+                    const int part = (threadIdx.x & 127) % kLanes, r0 = (threadIdx.x & 127) / kLanes;
+#pragma unroll 4
+                    for (int i = 0; i < kTile / kRowsAtOnce; ++i) {
+                        const int r = r0 + i * kRowsAtOnce;
+                        uint32_t w4[4];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w4[0]), "=r"(w4[1]), "=r"(w4[2]), "=r"(w4[3]) : "r"(src + r * HD + part * 16));
+                        int e;
+                        asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e) : "r"(es + r));
+                        const RowFactor f = row_factor(e);
+                        uint32_t out[8];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            uint32_t even, odd;
+                            e4m3_spread(w4[y], even, odd);
+                            even = bf16x2_mul(bf16x2_mul(even, f.first), f.second), odd = bf16x2_mul(bf16x2_mul(odd, f.first), f.second);
+                            out[2 * y] = __byte_perm(even, odd, 0x5410), out[2 * y + 1] = __byte_perm(even, odd, 0x7632);
+                        }
+                        // rows past the last key: whatever lies there (a weight of zero does not make a NaN go away)
+                        if (is_v && r >= valid)
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) out[y] = 0u;
+                        const int to_row = is_v ? r : key_of_column(r);
+                        // 16-byte chunks 2 part and 2 part + 1 of the row, swizzled as a TMA box would be; half of the lanes begin with the
+                        // second one, so that eight lanes fill all banks
+                        const uint32_t to = dst + (part >> 2) * C::kBoxBytes + to_row * 128;
+                        const int first = HD == 128 ? part >> 2 : r0 & 1;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int c = y ^ first;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * (part & 3) + c) ^ (to_row & 7)) << 4)),
+                                         "r"(c ? out[4] : out[0]), "r"(c ? out[5] : out[1]), "r"(c ? out[6] : out[2]), "r"(c ? out[7] : out[3])
+                                         : "memory");
+                        }
+                    }
+                    fence_proxy_async();
+                    mbar_arrive_warp(&bars->kv_full[st]);
+                    mbar_arrive_warp(&bars->raw_empty[raw]);
+                    ++kv;
+                }
+                if (!more) break;
+                before = w;
+            }
         }
-        float top = score;
-        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-        top = fmaxf(fmaxf(top, m), -3.0e38f);
-        const float w = exp2f(score - top), alpha = exp2f(m - top);
-        m = top;
-        l = l * alpha + w;
-        for (int c = 0; c < kCols; ++c) acc[c] *= alpha;
-        for (int i = 0; i < 32; ++i) {
-            const float wi = __shfl_sync(0xffffffffu, w, i), fi = __shfl_sync(0xffffffffu, v_factor, i);
-            const long long ri = __shfl_sync(0xffffffffu, row, i);
-            if (ri < 0) continue;
-            for (int c = 0; c < kCols; ++c) acc[c] = fmaf(wi, cached_value<HD, kE4M3>(p.pool.v, ri, c * 32 + lane, fi), acc[c]);
+    } else {
+        // =========================== softmax =========================================================
+        setmaxnreg_inc<C::kRegsSoftmax>();
+        const int group = HD == 128 ? __shfl_sync(0xffffffffu, warp >> 2, 0) : warp >> 2;
+        const int quad = warp & 3;             // tensor-memory lane quadrant this warp may access
+        const int row = quad * 32 + lane;
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t tS = t_row + C::kColS + (C::kScoreBufs == 1 ? 0 : group * kTile), tP = t_row + C::kColP + group * 64;
+        const float c2 = a.scale_log2;
+        const uint64_t c2x2 = f2_pack(c2, c2);
+        uint32_t n_s = 0, n_it = 0;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            if (!mbar_wait_uniform(&bars->list_full[group][k % C::kSched], (k / C::kSched) & 1, ctx, kWaitPagedFwd + 14)) break;
+            const int slot = bars->list_slot[group][k % C::kSched];
+            const PagedItem w = bars->item[slot];
+            if (w.b < 0) break;
+            const int tile = tile_of_group(slot, group), n = tile ? w.n[1] : w.n[0];
+            const int first_pos = w.first_pos(tile), last_pos = first_pos + w.tokens_of(tile) - 1;
+            const int pos = first_pos + (row >> p.pack_log2);
+            float m_used = 0.f;   // running maximum in use, scaled to log2 units
+            float l[2] = {0.f, 0.f};
+            for (int j = 0; j < n; ++j, ++n_s) {
+                const int key0 = w.key_tile(j) * kTile;
+                if (!mbar_wait_uniform(&bars->s_full[group], n_s & 1, ctx, kWaitPagedFwd + 15)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t s[4][32];
+                tmem_ld_32x32(tS, s[0]);
+                tmem_ld_32x32(tS + 32, s[1]);
+                tmem_ld_32x32(tS + 64, s[2]);
+                tmem_ld_32x32(tS + 96, s[3]);
+                tmem_wait_ld();
+                tc_fence_before();
+                mbar_arrive_warp(&bars->s_empty[C::kScoreBufs == 1 ? 0 : group]);
+                if (!all_attend(first_pos, last_pos, key0, kTile, a.window, a.sinks)) {
+                    const int last = pos - key0;                                // keys up to here,
+                    const int low = a.window > 0 ? last - a.window + 1 : -1;    // from here on
+                    const int sinks = a.window > 0 ? a.sinks - key0 : 0;        // or below this
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int x = c * 32 + key_of_column(e);
+                            if (x > last || (x < low && x >= sinks)) s[c][e] = 0xff800000u;  // -inf
+                        }
+                }
+                float mx4[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    mx4[c] = fmaxf(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
+#pragma unroll
+                    for (int e = 2; e < 32; e += 2) mx4[c] = fmax3(mx4[c], __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+                }
+                const float m_new = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c2;
+                // the P.V product of this tile's step before is done: P and O may be written
+                if (n_s > 0 && !mbar_wait_uniform(&bars->p_empty[group], (n_s - 1) & 1, ctx, kWaitPagedFwd + 17)) { ok = false; break; }
+                tc_fence_after();
+                if (j == 0) {
+                    m_used = fmaxf(m_new, kLeast);  // (a row can have no key in the first tile of a window)
+                } else {
+                    const bool need = (m_new - m_used) > kLazyRescale;
+                    if (__any_sync(0xffffffffu, need)) {
+                        const float alpha = need ? fast_exp2(m_used - m_new) : 1.0f;
+                        l[0] *= alpha, l[1] *= alpha;
+#pragma unroll 1
+                        for (int c = 0; c < HD / 16; ++c) {
+                            uint32_t o[16];
+                            const uint32_t t_o = t_row + C::kColO + group * HD + c * 16;
+                            tmem_ld_32x16(t_o, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                            tmem_st_32x16(t_o, o);
+                        }
+                        if (need) m_used = m_new;
+                    }
+                }
+                const uint64_t nm = f2_pack(-m_used, -m_used);
+                uint64_t sum[2];  // of a half of the tile: chains 0 and 1, chains 2 and 3 (see key_of_column in fwd_kernel.cu)
+                auto add_chunk = [&](int c) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        auto weight = [&](int x) { return __uint_as_float(s[c][4 * e + x]); };
+                        const uint64_t pairs = f2_add(f2_pack(weight(0), weight(1)), f2_pack(weight(2), weight(3)));
+                        sum[e & 1] = (c & 1) == 0 && e < 2 ? pairs : f2_add(sum[e & 1], pairs);
+                    }
+                    if (c & 1) {
+                        float a0, a1, b0, b1;
+                        f2_unpack(sum[0], a0, a1);
+                        f2_unpack(sum[1], b0, b1);
+                        l[c >> 1] += (a0 + a1) + (b0 + b1);
+                    }
+                };
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float p0, p1, p2, p3;  // weights of the keys 4 e to 4 e + 3
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[c][4 * e]), __uint_as_float(s[c][4 * e + 1])), c2x2, nm), p0, p2);
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[c][4 * e + 2]), __uint_as_float(s[c][4 * e + 3])), c2x2, nm), p1, p3);
+                        p0 = fast_exp2(p0), p1 = fast_exp2(p1), p2 = fast_exp2(p2), p3 = fast_exp2(p3);
+                        s[c][4 * e] = __float_as_uint(p0), s[c][4 * e + 1] = __float_as_uint(p2);
+                        s[c][4 * e + 2] = __float_as_uint(p1), s[c][4 * e + 3] = __float_as_uint(p3);
+                        pk[2 * e] = pack_bf16(p0, p1), pk[2 * e + 1] = pack_bf16(p2, p3);
+                    }
+                    tmem_st_32x16(tP + c * 16, pk);
+                    if (c >= 2) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive_warp(c == 2 ? &bars->p_full[group] : &bars->p_rest[group]);
+                    }
+                    if (c > 0) add_chunk(c - 1);
+                    if (c == 3) add_chunk(3);
+                }
+            }
+            if (!ok || !mbar_wait_uniform(&bars->stat_empty[group], (n_it & 1) ^ 1, ctx, kWaitPagedFwd + 16)) break;
+            ++n_it;
+            sStat[group * 256 + row] = m_used;
+            sStat[group * 256 + 128 + row] = l[0] + l[1];
+            mbar_arrive_warp(&bars->stat_full[group]);
         }
     }
-    for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-    for (int c = 0; c < kCols; ++c) p.o[(static_cast<long long>(t) * p.H + h) * HD + c * 32 + lane] = __float2bfloat16(acc[c] / l);
-    if (lane == 0) p.lse[static_cast<long long>(h) * p.batch.T + t] = (m + log2f(l)) * 0.6931471805599453f;
+
+    // ---- teardown ------------------------------------------------------------------------------
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 13) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, C::kTmemCols);
+    }
+}
+
+template <int HD, bool kE4M3>
+cudaError_t configure_one() {
+    using C = PagedCfg<HD, kE4M3>;
+    // the register split of the kernel draws on what a block is launched with
+    cudaFuncAttributes attributes;
+    cudaError_t e = cudaFuncGetAttributes(&attributes, s2a_paged_fwd_kernel<HD, kE4M3>);
+    if (e != cudaSuccess) return e;
+    if (attributes.numRegs < C::kRegsLaunch || attributes.sharedSizeBytes != 0) return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(s2a_paged_fwd_kernel<HD, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_fwd(const PagedFwdParams& p, bool e4m3, int d, cudaStream_t stream) {
-    const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.batch.T) * p.H + 3) / 4);
-    auto kernel = d == 64 ? (e4m3 ? s2a_paged_fwd_kernel<64, true> : s2a_paged_fwd_kernel<64, false>)
-                          : (e4m3 ? s2a_paged_fwd_kernel<128, true> : s2a_paged_fwd_kernel<128, false>);
-    return launch_kernel(kernel, grid, 128, 0, stream, p, true);
+cudaError_t configure_paged_fwd() {
+    for (const cudaError_t e : {configure_one<64, false>(), configure_one<64, true>(), configure_one<128, false>(), configure_one<128, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+
+cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream) {
+    const unsigned grid = static_cast<unsigned>(p.slots) * static_cast<unsigned>(p.a.H >> p.pack_log2);
+    auto launch = [&](auto kernel, int smem) { return launch_kernel(kernel, grid, 512, smem, stream, p, true); };
+    if (d == 64)
+        return e4m3 ? launch(s2a_paged_fwd_kernel<64, true>, PagedCfg<64, true>::kSmemBytes) : launch(s2a_paged_fwd_kernel<64, false>, PagedCfg<64, false>::kSmemBytes);
+    return e4m3 ? launch(s2a_paged_fwd_kernel<128, true>, PagedCfg<128, true>::kSmemBytes) : launch(s2a_paged_fwd_kernel<128, false>, PagedCfg<128, false>::kSmemBytes);
 }
 
 }  // namespace s2a

@@ -99,7 +99,68 @@ static int exponents() {
     return 0;
 }
 
+// Every token of a batch is in exactly one of the tiling kernel's places, whatever lengths the sequences have.
+static int slots() {
+    std::srand(6);
+    for (int round = 0; round < 3000; ++round) {
+        const int B = 1 + std::rand() % 9, span_log2 = 1 + std::rand() % 8;
+        std::vector<int> starts(B + 1);
+        starts[0] = std::rand() % 4 == 0 ? std::rand() % 300 : 0;
+        for (int b = 0; b < B; ++b) starts[b + 1] = starts[b] + (std::rand() % 3 == 0 ? 0 : std::rand() % 700);
+        const int T = starts[B] + std::rand() % 300 + 1, count = first_slot(T, B, span_log2);
+        std::vector<int> seen(T, 0);
+        for (int slot = 0; slot < count; ++slot) {
+            const int b = find_slot(starts.data(), B, span_log2, slot);
+            if (b < 0 || b >= B) return fail("place in no sequence", slot, b);
+            const long long at = static_cast<long long>(slot - first_slot(starts[b], b, span_log2)) << span_log2;
+            if (at < 0) continue;
+            for (long long i = at; i < at + (1 << span_log2) && i < starts[b + 1] - starts[b]; ++i) ++seen[starts[b] + i];
+        }
+        for (int t = 0; t < T; ++t)
+            if (seen[t] != (t >= starts[0] && t < starts[B])) return fail("token in another number of places than one", t, seen[t]);
+        for (int i = 0; i < 20; ++i) {
+            for (int& x : starts) x = std::rand() - RAND_MAX / 2;
+            const int got = find_slot(starts.data(), B, span_log2, std::rand() % count);
+            if (got < 0 || got >= B) return fail("wild starts", got);
+        }
+    }
+    return 0;
+}
+
+// The blocks of keys are each named once, in order, and hold every key that a token attends.
+static int blocks() {
+    std::srand(7);
+    for (int round = 0; round < 20000; ++round) {
+        const int block = round % 2 ? 16 : 128, first = std::rand() % 700, last = first + std::rand() % 260;
+        const int window = std::rand() % 3 == 0 ? 0 : 1 + std::rand() % (std::rand() % 2 ? 20 : 500), sinks = std::rand() % 3 == 0 ? 0 : std::rand() % 300;
+        const KeyBlocks k = key_blocks(first, last, window, sinks, block);
+        std::vector<int> held(last / block + 1, 0);
+        int before = -1;
+        for (int i = 0; i < k.count; ++i) {
+            const int x = k.at(i);
+            if (x <= before || x > last / block) return fail("blocks out of order", x, before);
+            before = x, held[x] = 1;
+        }
+        for (int j = 0; j <= last; ++j) {
+            bool any = false;
+            for (int p = first; p <= last; ++p) any |= attends(p, j, window, sinks);
+            if (any != any_attends(first, last, j, window, sinks)) return fail("some attend", j, any);
+            if (any && !held[j / block]) return fail("a key is left out", j);
+            if (j % block == 0) {
+                bool all = true;
+                for (int p = first; p <= last; ++p)
+                    for (int x = j; x < j + block; ++x) all &= attends(p, x, window, sinks);
+                const bool said = all_attend(first, last, j, block, window, sinks);
+                if (said && !all) return fail("not all attend", j, first);
+                if (all && !said && window == 0) return fail("all attend", j, first);
+            }
+        }
+        if (held[last / block] == 0) return fail("the last block is left out", last);
+    }
+    return 0;
+}
+
 int main() {
-    if (batches() || exponents()) return 1;
+    if (batches() || exponents() || slots() || blocks()) return 1;
     std::printf("ok\n");
 }
