@@ -16,10 +16,14 @@
 //   warps 13, 14     tcgen05 MMAs: S = Q K_j^T of both tiles in turn / O += P V_j
 // Tensor memory: O of either tile, P of either tile, then one score buffer (HD = 128) or two.
 //
-// 8-bit caches: TMA brings the codes to a ring of two raw tiles, warps 8-11 write them as bf16, times their row's power of two,
-// where the products read them.  Both steps are exact (paged.h).  These warps have one instruction stream on each scheduler beside the
-// softmax's two; multiplying the scores and the weights by the powers instead would be about as many instructions, in the
-// warps that everything waits for.
+// 8-bit caches are multiplied in fp16, which has their values with room for a power of two.  TMA brings the codes to a ring of two raw tiles;
+// warps 8-11 write them where the products read them, each row times its power of two relative to the tile's largest (6 binary
+// places up: the tile's largest value is below 2^15 and values down to 2^-29 of it keep all their bits).  Q they turn from bf16 to fp16, each row times
+// a power of two that brings its largest value to [2^14, 2^15).  What is the tile's, or the row's, then multiplies scores and weights for
+// nothing: it goes into the constants of exp2(score * c - m).  Weights are 2^7 as large as with bf16, so that those down to 2^-21 of the
+// largest have all of fp16's 11 bits (bf16 has 8) and those below 2^-32 of it vanish; O is in units of the largest tile exponent of V so far,
+// rescaled like a running maximum.  As bf16, values take five instructions instead of one and a half and the four warps cannot
+// keep up: 32k tokens, 2048 new ones, 64 heads over 8 3.03 ms.
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -33,13 +37,14 @@ struct PagedCfg {
     static constexpr int kBoxBytes = kTile * 128;           // 128 rows x 128 bytes
     static constexpr int kTileBytes = kBoxes * kBoxBytes;   // one Q, K or V tile in bf16
     static constexpr int kRing = (HD == 128) ? 4 : 8;       // K and V tiles in flight: K_0 V_0 K_1 V_1 ...
-    static constexpr int kRawRing = kE4M3 ? 2 : 0;          // the same as codes
+    static constexpr int kRawRing = kE4M3 ? (HD == 128 ? 2 : 6) : 0;  // the same as codes
     static constexpr int kRawBytes = kTile * HD;
-    static constexpr int kStatBytes = 2 * 2 * kTile * 4;    // row statistics handed to the read-out
-    // Items in flight: as many as s2a_fwd_kernel's for its ring, see there.
-    static constexpr int kSched = (HD == 128) ? 6 : 8;
-    static_assert(kSched % 2 == 0 && kSched >= kRing / 2 + 3, "an item's slot is free when it is written again");
-    static constexpr int kBarBytes = (HD == 128) ? 1024 : 2048;
+    static constexpr int kStatBytes = 2 * kTile * 4 + (kE4M3 ? 2 * 2 * kTile : 0);  // factors for the read-out, exponents of Q's rows
+    // Items in flight: as many as s2a_fwd_kernel's for its ring, see there; with raw tiles those that the warps which turn them
+    // into operands are behind with come on top.
+    static constexpr int kSched = (HD == 128) ? 6 : kE4M3 ? 12 : 8;
+    static_assert(kSched % 2 == 0 && kSched >= (kRing + kRawRing) / 2 + 3, "an item's slot is free when it is written again");
+    static constexpr int kBarBytes = (HD == 128) ? 1536 : 4096;
     static constexpr int kSmemBytes = (2 + kRing) * kTileBytes + kRawRing * kRawBytes + kBarBytes + kStatBytes;
     static_assert(kSmemBytes <= 232448, "shared memory");
     static constexpr int kTmemCols = 512;
@@ -57,6 +62,7 @@ struct PagedItem {
     int pos;               // position of the token at row[1]
     int n[2];              // key tiles that either tile's products take: the first n of the item's
     int sink_blocks, low_block;
+    uint32_t kv0;          // ring position of its first K tile
     __device__ __forceinline__ int key_tile(int j) const { return j < sink_blocks ? j : low_block + j - sink_blocks; }
     // (indexed by a variable, a copy in registers would have to go through local memory)
     __device__ __forceinline__ int row_of(int t) const { return t ? row[1] : row[0]; }
@@ -74,21 +80,33 @@ struct PagedBars {
     uint64_t o_full[2], o_empty[2];
     uint64_t stat_full[2], stat_empty[2];
     uint64_t kv_full[C::kRing], kv_empty[C::kRing];
-    uint64_t raw_full[2], raw_empty[2];
+    uint64_t raw_full[kE4M3 ? C::kRawRing : 1], raw_empty[kE4M3 ? C::kRawRing : 1], q_ready[2];
     uint64_t sched_full[C::kSched];
     uint64_t list_full[2][C::kSched];
     uint64_t clc, drain[2];
     alignas(16) uint8_t clc_resp[16];
-    alignas(16) int8_t exps[2][kE4M3 ? kTile : 16];  // of the raw tiles
+    alignas(16) int8_t exps[kE4M3 ? C::kRawRing : 1][kTile];  // of the raw tiles
+    int8_t tile_exp[16];  // of the K and V tiles by ring position: one is written again when its step is long over
     PagedItem item[C::kSched];
     uint8_t list_slot[2][C::kSched];
     uint32_t tmem_slot;
     int abort_flag;
 };
 
+// With 8-bit caches the tiles of an item's keys are requested and written in the order K_0 K_1 V_0 K_2 V_1 .. K_n-1 V_n-2 V_n-1: K's room is free a
+// step earlier than V's, and in the order of the ring (K_0 V_0 K_1 V_1) it would be written behind V.  Tile x of 2 n: of K or V, and which.
+struct TileOfItem {
+    bool is_v;
+    int j;
+    __device__ __forceinline__ TileOfItem(int x, int n) : is_v(x > 0 && ((x & 1) == 0 || x == 2 * n - 1)), j(x == 2 * n - 1 ? n - 1 : is_v ? x / 2 - 1 : (x + 1) / 2) {}
+};
+
 // The later tile of a pair is the only one where an item has one; the groups of softmax warps take it in turn (see s2a_fwd_kernel).
 __device__ __forceinline__ int group_of_tile(int item, int t) { return (item & 1) ^ t ^ 1; }
 __device__ __forceinline__ int tile_of_group(int item, int group) { return (item & 1) ^ group ^ 1; }
+
+// times 2^e, -127 (which stands for less than that) <= e <= 127
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
 
 constexpr float kLazyRescale = 8.0f;
 constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
@@ -130,7 +148,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
     uint8_t* sKV = sQ + 2 * C::kTileBytes;             // ring of K and V tiles
     uint8_t* sRaw = sKV + C::kRing * C::kTileBytes;    // ring of their codes
     Bars* bars = reinterpret_cast<Bars*>(sRaw + C::kRawRing * C::kRawBytes);
-    float* sStat = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + C::kBarBytes);  // [group][m, l][128 rows]
+    float* sStat = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + C::kBarBytes);  // [group][128 rows]
+    int8_t* sQExp = reinterpret_cast<int8_t*>(sStat + 2 * kTile);  // [group][item of the group, odd or even][128 rows]
     const PagedFwdParams& a = p.a;
 
     const int warp = threadIdx.x >> 5;
@@ -150,8 +169,11 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             mbar_init(&bars->stat_full[t], 4);
             mbar_init(&bars->stat_empty[t], 4);
             mbar_init(&bars->drain[t], 1);
-            mbar_init(&bars->raw_full[t], 1);
-            mbar_init(&bars->raw_empty[t], 4);
+            mbar_init(&bars->q_ready[t], 4);
+        }
+        for (int x = 0; x < C::kRawRing; ++x) {
+            mbar_init(&bars->raw_full[x], 1);
+            mbar_init(&bars->raw_empty[x], 4);
         }
         for (int x = 0; x < C::kRing; ++x) {
             mbar_init(&bars->kv_full[x], kE4M3 ? 4 : 1);
@@ -252,8 +274,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             auto load_kv = [&](int row, bool k_tile) {
                 const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
                 if constexpr (kE4M3) {
-                    const int st = kv % 2;
-                    if (!mbar_wait_uniform(&bars->raw_empty[st], ((kv / 2) & 1) ^ 1, ctx, kWaitPagedFwd + 3)) { ok = false; return; }
+                    const int st = kv % C::kRawRing;
+                    if (!mbar_wait_uniform(&bars->raw_empty[st], ((kv / C::kRawRing) & 1) ^ 1, ctx, kWaitPagedFwd + 3)) { ok = false; return; }
                     if (lane == 0) mbar_expect_tx(&bars->raw_full[st], static_cast<uint32_t>((boxes * (HD + 1)) << piece_log2));
                     __syncwarp();
                     if (row >= 0) {
@@ -282,6 +304,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 while (id >= 0 && !paged_item(p, id, &w)) id = next_id();
                 if (id < 0) w.b = -1;
                 const int g1 = group_of_tile(k, 1), g0 = group_of_tile(k, 0);
+                w.kv0 = kv;
                 if (lane == 0) {
                     bars->item[k % C::kSched] = w;
                     mbar_arrive(&bars->sched_full[k % C::kSched]);  // release: the item is visible to whoever sees the phase
@@ -299,7 +322,21 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 if (id < 0) break;
                 const int hk = p.by_groups_of_kv(w.group), length = w.pos + w.tokens[1];  // (keys behind the last token are nobody's)
                 int row = look_up(w, hk, length, w.key_tile(0));
-                for (int j = 0; ok && j < w.n[1]; ++j) {
+                if constexpr (kE4M3) {  // in the order of TileOfItem
+                    int next = w.n[1] > 1 ? look_up(w, hk, length, w.key_tile(1)) : -1;
+                    load_kv(row, true);
+                    if (ok) load_q(w, 1, g1);
+                    if (ok && w.n[0] > 0) load_q(w, 0, g0);
+                    for (int j = 1; ok && j < w.n[1]; ++j) {
+                        const int before = row;
+                        row = next;
+                        next = j + 1 < w.n[1] ? look_up(w, hk, length, w.key_tile(j + 1)) : -1;
+                        load_kv(row, true);
+                        if (ok) load_kv(before, false);
+                    }
+                    if (ok) load_kv(row, false);
+                }
+                for (int j = 0; !kE4M3 && ok && j < w.n[1]; ++j) {
                     const int next = j + 1 < w.n[1] ? look_up(w, hk, length, w.key_tile(j + 1)) : -1;
                     load_kv(row, true);
                     if (j == 0 && ok) load_q(w, 1, g1);
@@ -313,15 +350,15 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             if (__any_sync(0xffffffffu, bars->abort_flag != 0) && lane == 0) {
                 for (int t = 0; t < 2; ++t)
                     if (n_q[t] > 0) mbar_wait_drain(&bars->q_full[t], (n_q[t] - 1) & 1);
-                constexpr uint32_t kIn = kE4M3 ? 2 : C::kRing;
+                constexpr uint32_t kIn = kE4M3 ? C::kRawRing : C::kRing;
                 for (uint32_t x = (kv > kIn ? kv - kIn : 0); x < kv; ++x)
-                    mbar_wait_drain(kE4M3 ? &bars->raw_full[x % 2] : &bars->kv_full[x % C::kRing], (x / kIn) & 1);
+                    mbar_wait_drain(kE4M3 ? &bars->raw_full[x % kIn] : &bars->kv_full[x % kIn], (x / kIn) & 1);
             }
             __syncwarp();
         } else if (warp <= 14) {
             // ======================= MMA issuers: warp 13 for S = Q K^T, warp 14 for O += P V ============
-            constexpr uint32_t idesc_s = idesc_bf16(128, kTile, 0, 0);  // S = Q K^T   (both K-major)
-            constexpr uint32_t idesc_o = idesc_bf16(128, HD, 0, 1);     // O += P V    (V is MN-major)
+            constexpr uint32_t idesc_s = kE4M3 ? idesc_f16(128, kTile, 0, 0) : idesc_bf16(128, kTile, 0, 0);  // S = Q K^T   (both K-major)
+            constexpr uint32_t idesc_o = kE4M3 ? idesc_f16(128, HD, 0, 1) : idesc_bf16(128, HD, 0, 1);        // O += P V    (V is MN-major)
             const bool is_s = warp == 13;
             const uint32_t aKV = smem_u32(sKV), dQ0 = desc_lo_k_major(smem_u32(sQ));
             uint32_t kv = 0;                    // ring position of the item's K_0
@@ -343,7 +380,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                     // what tile 1 has used, tile 0 need not wait for again
                     if (t == 1 && !mbar_wait_uniform(&bars->kv_full[x % C::kRing], (x / C::kRing) & 1, ctx, kWaitPagedFwd + 5)) { ok = false; break; }
                     if (is_s) {
-                        if (j == 0 && !mbar_wait_uniform(&bars->q_full[g], it, ctx, kWaitPagedFwd + 4)) { ok = false; break; }
+                        if (j == 0 && !mbar_wait_uniform(kE4M3 ? &bars->q_ready[g] : &bars->q_full[g], it, ctx, kWaitPagedFwd + 4)) { ok = false; break; }
                         const int buf = C::kScoreBufs == 1 ? 0 : g;
                         const uint32_t use = C::kScoreBufs == 1 ? n_s & 1 : st;
                         if (!mbar_wait_uniform(&bars->s_empty[buf], use ^ 1, ctx, kWaitPagedFwd + 6)) { ok = false; break; }
@@ -418,6 +455,12 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
         const int row = quad * 32 + lane;
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
         uint32_t n_o[2] = {0, 0};
+        auto lds = [](uint32_t at, uint32_t (&x)[4]) {
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+        };
+        auto sts = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t u) {
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(u) : "memory");
+        };
         auto read_out = [&](int k, const PagedItem& w) -> bool {
 #pragma unroll 1
             for (int t = 0; t < 2; ++t) {
@@ -428,9 +471,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                     !mbar_wait_uniform(&bars->o_full[g], n_done & 1, ctx, kWaitPagedFwd + 13))
                     return false;
                 tc_fence_after();
-                const float m = sStat[g * 256 + row], l = sStat[g * 256 + 128 + row];
+                const float inv_l = sStat[g * kTile + row];
                 mbar_arrive_warp(&bars->stat_empty[g]);
-                const float inv_l = 1.0f / l;
                 const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
                 const bool valid = token < w.tokens_of(t);  // the others are rows of another sequence, or of none
                 const long long at = w.row_of(t) + token;
@@ -452,7 +494,6 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 }
                 tc_fence_before();
                 mbar_arrive_warp(&bars->o_empty[g]);
-                if (valid) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
             }
             return true;
         };
@@ -463,8 +504,44 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 if (!read_out(k, w)) break;
             }
         } else {
-            // The tiles of an item, and between its first ones the read-out of the item before: those tiles need no room that
-            // the read-out has to make first (the ring's), and what comes behind them would have to wait for the item's products anyway.
+            // Q of a tile, one row a thread, in place.
+            uint32_t n_q[2] = {0, 0};
+            auto convert_q = [&](int g) -> bool {
+                const uint32_t n = g ? n_q[1]++ : n_q[0]++;
+                if (!mbar_wait_uniform(&bars->q_full[g], n & 1, ctx, kWaitPagedFwd + 20)) return false;
+                const uint32_t at = smem_u32(sQ + g * C::kTileBytes) + row * 128;
+                uint32_t most = 0;
+#pragma unroll 4
+                for (int c = 0; c < HD / 8; ++c) {
+                    uint32_t x[4];
+                    lds(at + (c >> 3) * C::kBoxBytes + (((c ^ row) & 7) << 4), x);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) most = max(most, max(x[y] & 0x7fffu, x[y] >> 16 & 0x7fffu));
+                }
+                int up = most >= 0x7f80u || most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);  // (a row that is not finite stays so)
+                up = up > 126 ? 126 : up;
+                const float f = power_of_two(up);
+#pragma unroll 4
+                for (int c = 0; c < HD / 8; ++c) {
+                    uint32_t x[4];
+                    const uint32_t chunk = at + (c >> 3) * C::kBoxBytes + (((c ^ row) & 7) << 4);
+                    lds(chunk, x);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) x[y] = pack_f16(bf16_low(x[y]) * f, bf16_high(x[y]) * f);
+                    sts(chunk, x[0], x[1], x[2], x[3]);
+                }
+                sQExp[(2 * g + (n & 1)) * kTile + row] = static_cast<int8_t>(up);
+                fence_proxy_async();
+                mbar_arrive_warp(&bars->q_ready[g]);
+                return true;
+            };
+            // The tiles of an item, and between its first ones its Q and the read-out of the item before: those tiles need no room that
+            // the read-out has to make first (the ring's), and what comes behind them would have to wait for products anyway.
+            // Eight lanes at a time read 128 bytes that lie in all banks and write 16-byte chunks that do: half of a row and the other half of the
+            // next (or, of 64 columns, two rows).  In K's tile the rows are those of key_of_column().
+            const int to_row = HD == 128 ? 2 * (lane >> 4) + ((lane >> 2) & 1) : lane >> 2;  // of a warp's first turn
+            const int part = HD == 128 ? (lane & 3) | (((lane >> 2) ^ (lane >> 3)) & 1) << 2 : lane & 3;
+            const int chunk0 = (2 * (part & 3)) ^ (to_row & 7);
             uint32_t kv = 0;
             bool ok = true;
             PagedItem before;
@@ -475,52 +552,66 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 const int tiles = more ? 2 * w.n[1] : 0, pause = tiles < C::kRing - 1 ? tiles : C::kRing - 1;
                 const int end = more ? w.pos + w.tokens[1] : 0;
                 for (int x = 0; ok && x <= tiles; ++x) {
-                    if (x == pause && before.b >= 0) ok = read_out(k - 1, before);
+                    if (x == pause) {
+                        if (more) ok = convert_q(group_of_tile(k, 1)) && (w.n[0] == 0 || convert_q(group_of_tile(k, 0)));
+                        if (ok && before.b >= 0) ok = read_out(k - 1, before);
+                    }
                     if (!ok || x == tiles) break;
-                    const int raw = kv % 2, st = kv % C::kRing;
-                    if (!mbar_wait_uniform(&bars->raw_full[raw], (kv / 2) & 1, ctx, kWaitPagedFwd + 18) ||
-                        !mbar_wait_uniform(&bars->kv_empty[st], ((kv / C::kRing) & 1) ^ 1, ctx, kWaitPagedFwd + 19)) {
+                    const TileOfItem tile(x, w.n[1]);
+                    const uint32_t at = w.kv0 + 2 * tile.j + tile.is_v;  // ring position
+                    const int raw = kv % C::kRawRing, st = at % C::kRing;
+                    if (!mbar_wait_uniform(&bars->raw_full[raw], (kv / C::kRawRing) & 1, ctx, kWaitPagedFwd + 18) ||
+                        !mbar_wait_uniform(&bars->kv_empty[st], ((at / C::kRing) & 1) ^ 1, ctx, kWaitPagedFwd + 19)) {
                         ok = false;
                         break;
                     }
-                    const bool is_v = (x & 1) != 0;
-                    const int valid = end - w.key_tile(x >> 1) * kTile;  // rows of the tile that hold keys
-                    const uint32_t src = smem_u32(sRaw + raw * C::kRawBytes), dst = smem_u32(sKV + st * C::kTileBytes), es = smem_u32(bars->exps[raw]);
-                    constexpr int kLanes = HD / 16, kRowsAtOnce = 128 / kLanes;  // 16 codes a thread
-                    const int part = (threadIdx.x & 127) % kLanes, r0 = (threadIdx.x & 127) / kLanes;
-#pragma unroll 4
-                    for (int i = 0; i < kTile / kRowsAtOnce; ++i) {
-                        const int r = r0 + i * kRowsAtOnce;
-                        uint32_t w4[4];
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w4[0]), "=r"(w4[1]), "=r"(w4[2]), "=r"(w4[3]) : "r"(src + r * HD + part * 16));
-                        int e;
-                        asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e) : "r"(es + r));
-                        const RowFactor f = row_factor(e);
-                        uint32_t out[8];
+                    const bool is_v = tile.is_v;
+                    const int valid = end - w.key_tile(tile.j) * kTile;  // rows of the tile that hold keys
+                    const uint32_t src = smem_u32(sRaw + raw * C::kRawBytes), dst = smem_u32(sKV + st * C::kTileBytes);
+                    // the largest exponent of the rows that hold keys: four rows a lane
+                    const uint32_t four = *reinterpret_cast<const volatile uint32_t*>(&bars->exps[raw][4 * lane]);
+                    int most = kExpNotFinite;
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            uint32_t even, odd;
-                            e4m3_spread(w4[y], even, odd);
-                            even = bf16x2_mul(bf16x2_mul(even, f.first), f.second), odd = bf16x2_mul(bf16x2_mul(odd, f.first), f.second);
-                            out[2 * y] = __byte_perm(even, odd, 0x5410), out[2 * y + 1] = __byte_perm(even, odd, 0x7632);
+                    for (int y = 0; y < 4; ++y)
+                        if (4 * lane + y < valid) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
+                    most = max(__reduce_max_sync(0xffffffffu, most), kExpLeast);
+                    // A warp takes 32 rows, kRows at a time, 16 codes a lane.  Lane i has the factor of the warp's row i.
+                    const int e = bars->exps[raw][32 * quad + lane];
+                    const float f = e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(e - most + 6, -127));
+                    const uint32_t factors = pack_f16(f, f);
+                    constexpr int kRows = 512 / HD;
+                    const int src_row = is_v ? to_row : key_of_column(to_row);
+                    uint32_t from = src + (32 * quad + src_row) * HD + part * 16, to = dst + (part >> 2) * C::kBoxBytes + (32 * quad + to_row) * 128;
+                    // (one short loop: written out, the code that the softmax warps run beside costs more than its branches, 604 against 467 us
+                    // for 1024 new tokens of 12,000 on 64 heads over 8)
+#pragma unroll 1
+                    for (int i0 = 0; i0 < 32 / kRows; i0 += 2) {
+                        uint32_t codes[2][4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) lds(from + i * kRows * HD, codes[i]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t ff = __shfl_sync(0xffffffffu, factors, src_row + (i0 + i) * kRows);
+                            uint32_t out[8];
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                e4m3_to_f16(codes[i][y], out[2 * y], out[2 * y + 1]);
+                                out[2 * y] = f16x2_mul(out[2 * y], ff), out[2 * y + 1] = f16x2_mul(out[2 * y + 1], ff);
+                            }
+                            // chunks 2 part and 2 part + 1 of the row, swizzled as a TMA box would be
+                            const uint32_t chunk = to + i * kRows * 128 + ((HD == 128 && i == 1 ? chunk0 ^ 4 : chunk0) << 4);
+                            sts(chunk, out[0], out[1], out[2], out[3]);
+                            sts(chunk ^ 16, out[4], out[5], out[6], out[7]);
                         }
-                        // rows past the last key: whatever lies there (a weight of zero does not make a NaN go away)
-                        if (is_v && r >= valid)
-#pragma unroll
-                            for (int y = 0; y < 8; ++y) out[y] = 0u;
-                        const int to_row = is_v ? r : key_of_column(r);
-                        // 16-byte chunks 2 part and 2 part + 1 of the row, swizzled as a TMA box would be; half of the lanes begin with the
-                        // second one, so that eight lanes fill all banks
-                        const uint32_t to = dst + (part >> 2) * C::kBoxBytes + to_row * 128;
-                        const int first = HD == 128 ? part >> 2 : r0 & 1;
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int c = y ^ first;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * (part & 3) + c) ^ (to_row & 7)) << 4)),
-                                         "r"(c ? out[4] : out[0]), "r"(c ? out[5] : out[1]), "r"(c ? out[6] : out[2]), "r"(c ? out[7] : out[3])
-                                         : "memory");
-                        }
+                        from += 2 * kRows * HD, to += 2 * kRows * 128;
                     }
+                    if (is_v && valid < kTile) {
+                        // rows past the last key: whatever lies there (a weight of zero does not make a NaN go away)
+                        __syncwarp();
+                        for (int c = max(valid - 32 * quad, 0) * 8 + lane; c < 32 * 8; c += 32)
+                            for (int bx = 0; bx < C::kBoxes; ++bx) sts(dst + bx * C::kBoxBytes + quad * 32 * 128 + c * 16, 0, 0, 0, 0);
+                    }
+                    if (threadIdx.x == 256) bars->tile_exp[at % 16] = static_cast<int8_t>(most);
                     fence_proxy_async();
                     mbar_arrive_warp(&bars->kv_full[st]);
                     mbar_arrive_warp(&bars->raw_empty[raw]);
@@ -538,8 +629,6 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
         const int row = quad * 32 + lane;
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
         const uint32_t tS = t_row + C::kColS + (C::kScoreBufs == 1 ? 0 : group * kTile), tP = t_row + C::kColP + group * 64;
-        const float c2 = a.scale_log2;
-        const uint64_t c2x2 = f2_pack(c2, c2);
         uint32_t n_s = 0, n_it = 0;
         bool ok = true;
         for (int k = 0; ok; ++k) {
@@ -552,10 +641,17 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             const int pos = first_pos + (row >> p.pack_log2);
             float m_used = 0.f;   // running maximum in use, scaled to log2 units
             float l[2] = {0.f, 0.f};
+            float c2 = a.scale_log2;
+            int up = 0, v_most = 0;  // 8 bits: the exponent of the row of Q, the largest tile exponent of V so far
             for (int j = 0; j < n; ++j, ++n_s) {
                 const int key0 = w.key_tile(j) * kTile;
                 if (!mbar_wait_uniform(&bars->s_full[group], n_s & 1, ctx, kWaitPagedFwd + 15)) { ok = false; break; }
                 tc_fence_after();
+                if constexpr (kE4M3) {
+                    if (j == 0) up = sQExp[(2 * group + (n_it & 1)) * kTile + row];
+                    c2 = a.scale_log2 * 0.015625f * power_of_two(bars->tile_exp[(w.kv0 + 2 * j) % 16]) * power_of_two(-up);  // (K is 2^6 as large)
+                }
+                const uint64_t c2x2 = f2_pack(c2, c2);
                 uint32_t s[4][32];
                 tmem_ld_32x32(tS, s[0]);
                 tmem_ld_32x32(tS + 32, s[1]);
@@ -587,13 +683,29 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 // the P.V product of this tile's step before is done: P and O may be written
                 if (n_s > 0 && !mbar_wait_uniform(&bars->p_empty[group], (n_s - 1) & 1, ctx, kWaitPagedFwd + 17)) { ok = false; break; }
                 tc_fence_after();
+                float down_v = 1.f, tile_up = 1.f, shift = 0.f;  // of O; of the sums of the tile's weights; of their exponents
+                if constexpr (kE4M3) {
+                    // (V of this step has been written by now, or is about to be)
+                    const uint32_t x = w.kv0 + 2 * j + 1;
+                    if (!mbar_wait_uniform(&bars->kv_full[x % C::kRing], (x / C::kRing) & 1, ctx, kWaitPagedFwd + 21)) { ok = false; break; }
+                    const int v_exp = bars->tile_exp[x % 16];
+                    if (j == 0) {
+                        v_most = v_exp;
+                    } else if (v_exp > v_most) {
+                        down_v = power_of_two(max(v_most - v_exp, -127));
+                        v_most = v_exp;
+                    }
+                    const int below = max(v_exp - v_most, -60);  // (weights of 2^-45 are none in fp16: V that small counts for nothing beside the largest)
+                    shift = static_cast<float>(7 + below), tile_up = power_of_two(-below);
+                }
                 if (j == 0) {
                     m_used = fmaxf(m_new, kLeast);  // (a row can have no key in the first tile of a window)
                 } else {
                     const bool need = (m_new - m_used) > kLazyRescale;
-                    if (__any_sync(0xffffffffu, need)) {
-                        const float alpha = need ? fast_exp2(m_used - m_new) : 1.0f;
+                    if (__any_sync(0xffffffffu, need || (kE4M3 && down_v != 1.f))) {
+                        float alpha = need ? fast_exp2(m_used - m_new) : 1.0f;
                         l[0] *= alpha, l[1] *= alpha;
+                        if (kE4M3) alpha *= down_v;
 #pragma unroll 1
                         for (int c = 0; c < HD / 16; ++c) {
                             uint32_t o[16];
@@ -607,7 +719,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         if (need) m_used = m_new;
                     }
                 }
-                const uint64_t nm = f2_pack(-m_used, -m_used);
+                const uint64_t nm = f2_pack(shift - m_used, shift - m_used);
                 uint64_t sum[2];  // of a half of the tile: chains 0 and 1, chains 2 and 3 (see key_of_column in fwd_kernel.cu)
                 auto add_chunk = [&](int c) {
 #pragma unroll
@@ -620,7 +732,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         float a0, a1, b0, b1;
                         f2_unpack(sum[0], a0, a1);
                         f2_unpack(sum[1], b0, b1);
-                        l[c >> 1] += (a0 + a1) + (b0 + b1);
+                        if constexpr (kE4M3) l[c >> 1] = fmaf((a0 + a1) + (b0 + b1), tile_up, l[c >> 1]);
+                        else l[c >> 1] += (a0 + a1) + (b0 + b1);
                     }
                 };
 #pragma unroll
@@ -634,7 +747,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         p0 = fast_exp2(p0), p1 = fast_exp2(p1), p2 = fast_exp2(p2), p3 = fast_exp2(p3);
                         s[c][4 * e] = __float_as_uint(p0), s[c][4 * e + 1] = __float_as_uint(p2);
                         s[c][4 * e + 2] = __float_as_uint(p1), s[c][4 * e + 3] = __float_as_uint(p3);
-                        pk[2 * e] = pack_bf16(p0, p1), pk[2 * e + 1] = pack_bf16(p2, p3);
+                        pk[2 * e] = kE4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1), pk[2 * e + 1] = kE4M3 ? pack_f16(p2, p3) : pack_bf16(p2, p3);
                     }
                     tmem_st_32x16(tP + c * 16, pk);
                     if (c >= 2) {
@@ -648,9 +761,13 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             }
             if (!ok || !mbar_wait_uniform(&bars->stat_empty[group], (n_it & 1) ^ 1, ctx, kWaitPagedFwd + 16)) break;
             ++n_it;
-            sStat[group * 256 + row] = m_used;
-            sStat[group * 256 + 128 + row] = l[0] + l[1];
+            // O is in units of 2^(v_most - 6) (8 bits), weights and their sums in units of 2^-7
+            const float sum_l = l[0] + l[1];
+            sStat[group * kTile + row] = (kE4M3 ? power_of_two(v_most) * 0.015625f : 1.0f) / sum_l;
             mbar_arrive_warp(&bars->stat_full[group]);
+            const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
+            if (token < w.tokens_of(tile))  // natural-log sum-exp of the scaled scores
+                a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = (m_used - (kE4M3 ? 7.f : 0.f) + log2f(sum_l)) * 0.6931471805599453f;
         }
     }
 

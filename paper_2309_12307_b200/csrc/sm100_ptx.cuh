@@ -442,6 +442,9 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn, int b_
            | ((uint32_t)(M >> 4) << 24);  // M / 16
 }
 
+// The same for fp16 A and B.
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) { return idesc_bf16(M, N, a_mn, b_mn) & ~((1u << 7) | (1u << 10)); }
+
 // D[tmem] (+)= A[smem] * B[smem]; issued by ONE thread.  a_lo / b_lo: descriptor low words.
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
                                        uint32_t accumulate) {
@@ -598,6 +601,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2_mul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 // four 8-bit floats (e4m3) -> fp16, exactly: values 0 and 1 in the first word, 2 and 3 in the second
