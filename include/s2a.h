@@ -299,12 +299,22 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
  *   in : q [T, H, d] bf16        out: o [T, H, d] bf16, rounded once from fp32; lse [H, T] fp32, natural-log sum-exp of the scaled scores
  * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels, so a tight value is
  * fastest (1 where every sequence has one new token).
- * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product.  Cached values at positions that
- * a token does not see are not assumed finite if they lie past the end of the sequence; a NaN or infinity at a position of the
- * sequence itself can reach the outputs of the other new tokens of the same call and sequence.  Deterministic: no atomics.
+ * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 (to fp16 over an S2A_CACHE_E4M3 cache) before the second
+ * product.  Cached values at positions that a token does not see are not assumed finite if they lie past the end of the sequence; a NaN
+ * or infinity at a position of the sequence itself can reach the outputs of the other new tokens of the same call and sequence.
+ * Deterministic: no atomics.
+ *   workspace: caller-owned device scratch, 256-byte aligned, or NULL.  Pieces of a prompt that do not fill the GPU evenly are split over
+ *              their keys where it has s2a_paged_workspace_bytes(...) bytes; without it, or with less, they are not.  Its contents before
+ *              the call do not matter; calls that can overlap on the GPU need a workspace each.
  */
 int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch, void* o, float* lse, int H, int max_new, float scale,
-                  int window, int sinks, void* stream);
+                  int window, int sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Bytes of scratch with which s2a_paged_fwd is fastest for these sizes on the current device (0: it needs none, or the sizes are
+ * invalid).  Only the sizes in `cache` and `batch` are looked at and that their pointers are there.
+ */
+size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks);
 
 /*
  * Diagnostic (the paper has no counterpart): enqueues one tiny kernel on `stream` in which a single

@@ -28,6 +28,7 @@ S2A_ERR_BAD_INDEX = -6
 EXPORTS = [
     "s2a_fwd", "s2a_bwd", "s2a_bwd_workspace_bytes", "s2a_bwd_workspace_bytes_fast", "s2a_fwd_ex", "s2a_bwd_ex", "s2a_bwd_stage", "s2a_fwd_bwd_host",
     "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed", "s2a_cache_write", "s2a_cache_read", "s2a_paged_fwd",
+    "s2a_paged_workspace_bytes",
     "s2a_selftest_wait_expiry", "s2a_device_status", "s2a_status_string", "s2a_last_cuda_error", "s2a_version",
 ]
 
@@ -81,7 +82,9 @@ def load() -> ctypes.CDLL:
     lib.s2a_cache_write.restype = I
     lib.s2a_cache_read.argtypes = [P, P, P, P, P]
     lib.s2a_cache_read.restype = I
-    lib.s2a_paged_fwd.argtypes = [P, P, P, P, P, I, I, F, I, I, P]
+    lib.s2a_paged_fwd.argtypes = [P, P, P, P, P, I, I, F, I, I, P, Z, P]
+    lib.s2a_paged_workspace_bytes.argtypes = [P, P, I, I, I, I]
+    lib.s2a_paged_workspace_bytes.restype = Z
     lib.s2a_paged_fwd.restype = I
     lib.s2a_selftest_wait_expiry.argtypes = [ctypes.c_longlong, P]
     lib.s2a_selftest_wait_expiry.restype = I
@@ -446,13 +449,15 @@ def _check_cache_read(cache, table, starts, lengths, tokens, k, v):
             _require(t, torch.bfloat16, name, shape=(tokens, cache.k.shape[1], cache.k.shape[3]), device=device)
 
 
-def _check_paged_fwd(q, cache, table, starts, lengths, o, lse):
+def _check_paged_fwd(q, cache, table, starts, lengths, o, lse, workspace=None):
     device = _check_cache(cache, table, starts, lengths)
     _check_rows(q, "q", cache, device)
     if o is not None:
         _require(o, torch.bfloat16, "o", shape=q.shape, device=device)
     if lse is not None:
         _require(lse, torch.float32, "lse", shape=(q.shape[1], q.shape[0]), device=device)
+    if workspace is not None:
+        _check_workspace(workspace, device)
 
 
 def _pools(cache):
@@ -484,16 +489,16 @@ def s2a_cache_read(cache, table, starts, lengths, tokens=None, k=None, v=None, s
                    table, starts, lengths, tokens, k, v)
 
 
-def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, window=0, sinks=0, o=None, lse=None, stream=None):
+def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, window=0, sinks=0, o=None, lse=None, workspace=None, stream=None):
     """o [T, H, d] bf16 and lse [H, T] fp32: every new token attends the cached tokens of its sequence up to itself, with `window` > 0
     the last `window` of them and the sequence's first `sinks`.  `cache` holds the new tokens already (s2a_cache_write); `max_new` is
     the largest number of new tokens a sequence has (default T; a tight value is fastest, 1 for single tokens).  Rows that belong
-    to no sequence are left as they were."""
+    to no sequence are left as they were.  Scratch that the call can use is allocated unless a `workspace` (uint8, any size) is given."""
     pools = _pools(cache)
-    hot = _hot or _hot_for(_check_paged_fwd, q, cache, table, starts, lengths, o, lse)
-    r = hot.paged_fwd(q, *pools, table, starts, lengths, max_new, scale, window, sinks, o, lse, _given_stream(stream))
+    hot = _hot or _hot_for(_check_paged_fwd, q, cache, table, starts, lengths, o, lse, workspace)
+    r = hot.paged_fwd(q, *pools, table, starts, lengths, max_new, scale, window, sinks, o, lse, workspace, _given_stream(stream))
     if r.__class__ is not tuple:
-        _result(r, "s2a_paged_fwd", _check_paged_fwd, q, cache, table, starts, lengths, o, lse)
+        _result(r, "s2a_paged_fwd", _check_paged_fwd, q, cache, table, starts, lengths, o, lse, workspace)
     return r if q.__class__ in _PLAIN else _typed(r, (None if o is not None else q, None))
 
 

@@ -114,6 +114,58 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
         }
 }
 
+// The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.
+// A single tile's step of 128 keys takes as long as a pair's, so items are pairs unless the GPU can work on all single tiles at a time (1024
+// new tokens of 8192 on 32 heads, 128 pairs: 105 us, as 256 single tiles 201).  One sequence that has fewer items than the GPU works
+// on at a time is split: each item into pieces of its keys, a step of which counts as one and the start and end of a piece as two.  (With
+// more items than that, splitting those of the last, partial wave brings nothing: with fewer multiprocessors busy those
+// run at a higher clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
+bool plan_tiles(PagedTileParams* p, int n_sm, long long longest) {
+    const PagedFwdParams& a = p->a;
+    p->pack_log2 = 0;
+    while (p->pack_log2 < 6 && a.rep % (2 << p->pack_log2) == 0) ++p->pack_log2;
+    const long long groups = a.H >> p->pack_log2;
+    p->span_log2 = 7 - p->pack_log2;
+    p->single = slot_count(a.batch.T, a.batch.B, p->span_log2) * groups <= n_sm;
+    if (!p->single) ++p->span_log2;
+    p->slots = slot_count(a.batch.T, a.batch.B, p->span_log2);
+    const long long items = p->slots * groups;
+    if (items * kMostSplit > 0x7fffffffLL) return false;
+    p->ranked = a.batch.B > 1 && a.batch.B <= kMostRanked;
+    p->first_split = static_cast<int>(items), p->split = 1;
+    if (a.batch.B == 1 && items < n_sm) {
+        long long keys = longest;
+        if (a.window > 0 && keys > static_cast<long long>(a.window) + a.sinks + (1 << p->span_log2)) keys = static_cast<long long>(a.window) + a.sinks + (1 << p->span_log2);
+        const double tiles = static_cast<double>(keys + kTile - 1) / kTile;
+        double best = 0.9 * tiles - 6;  // (the second launch)
+        for (int split = 2; split <= kMostSplit && 4 * split <= tiles; ++split) {
+            const double t = static_cast<double>((items * split + n_sm - 1) / n_sm) * (tiles / split + 2);
+            if (t < best) best = t, p->split = split, p->first_split = 0;
+        }
+    }
+    p->by_slots = FastDiv(p->slots), p->by_groups = FastDiv(static_cast<int>(groups)), p->by_groups_of_kv = FastDiv(a.rep >> p->pack_log2);
+    return true;
+}
+
+int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    if (H <= 0 || H % cache->Hkv != 0 || max_new <= 0 || max_new > batch->T || window < 0 || sinks < 0) return S2A_ERR_INVALID_ARG;
+    return static_cast<long long>(batch->T) * H > kIntMax ? S2A_ERR_UNSUPPORTED : S2A_OK;
+}
+
+// What a call's sizes say; its pointers and the scale are still missing.
+PagedFwdParams fwd_params(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    PagedFwdParams p;
+    memset(&p, 0, sizeof p);
+    p.batch = batch_of(batch), p.pool = pool_of(cache);
+    const int longest = batch->width * cache->page_size;  // no sequence has more tokens
+    p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new;
+    p.window = window >= longest ? 0 : window, p.sinks = sinks > longest ? longest : sinks;
+    // Sequences with few rows are the splitting kernel's, the others the other one's.  A batch of one sequence that may have many is
+    // the latter's without a second launch, however many it turns out to have.
+    p.few_rows = static_cast<long long>(max_new) * p.rep > kFewRows && batch->B == 1 ? 0 : kFewRows;
+    return p;
+}
+
 int copy_impl(void* k, void* v, const s2a_cache* cache, const s2a_batch* batch, void* stream, bool write) {
     if (!k || !v || !aligned16(k) || !aligned16(v)) return S2A_ERR_INVALID_ARG;
     int rc = check_cache(cache);
@@ -149,31 +201,24 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
 }
 
 int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch, void* o, float* lse, int H, int max_new, float scale,
-                  int window, int sinks, void* stream) {
+                  int window, int sinks, void* workspace, size_t workspace_bytes, void* stream) {
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return S2A_ERR_INVALID_ARG;
     if (!q || !o || !lse || !aligned16(q) || !aligned16(o) || !aligned16(lse)) return S2A_ERR_INVALID_ARG;
     int rc = check_cache(cache);
     if (rc != S2A_OK) return rc;
     if ((rc = check_batch(batch, cache)) != S2A_OK) return rc;
-    if (H <= 0 || H % cache->Hkv != 0 || max_new <= 0 || max_new > batch->T || window < 0 || sinks < 0) return S2A_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !isfinite(scale)) return S2A_ERR_INVALID_ARG;
-    if (static_cast<long long>(batch->T) * H > kIntMax) return S2A_ERR_UNSUPPORTED;
+    if ((rc = check_heads(cache, batch, H, max_new, window, sinks)) != S2A_OK) return rc;
     DeviceState* ds = nullptr;
     if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
     if ((rc = standing_status(ds)) != S2A_OK) return rc;
     const bool e4m3 = cache->type == S2A_CACHE_E4M3;
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
-    if (window >= longest) window = 0;
-    if (sinks > longest) sinks = longest;
     const long long most_rows = static_cast<long long>(max_new) * (H / cache->Hkv);
-    PagedFwdParams p;
-    memset(&p, 0, sizeof p);
-    p.batch = batch_of(batch), p.pool = pool_of(cache);
-    // Sequences with few rows are the splitting kernel's, the others the other one's.  A batch of one sequence that may have many is
-    // the latter's without a second launch, however many it turns out to have.
-    p.few_rows = most_rows > kFewRows && batch->B == 1 ? 0 : kFewRows;
+    PagedFwdParams p = fwd_params(cache, batch, H, max_new, window, sinks);
+    window = p.window, sinks = p.sinks;
     p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
-    p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new, p.window = window, p.sinks = sinks;
     p.scale_log2 = scale * 1.4426950408889634f;
     cudaError_t e;
     if (p.few_rows > 0) {
@@ -196,20 +241,28 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         PagedTileParams pt;
         memset(&pt, 0, sizeof pt);
         pt.a = p;
-        while (pt.pack_log2 < 6 && p.rep % (2 << pt.pack_log2) == 0) ++pt.pack_log2;
+        if (!plan_tiles(&pt, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
+        pt.beside = p.few_rows > 0;
+        const size_t piece_bytes = paged_piece_bytes(cache->d), items = static_cast<size_t>(pt.slots) * (H >> pt.pack_log2);
+        if (!workspace || (items - pt.first_split) * pt.split * piece_bytes > workspace_bytes) pt.first_split = static_cast<int>(items), pt.split = 1;
+        pt.pieces = static_cast<float*>(workspace);
+        pt.by_split = FastDiv(pt.split);
         if ((rc = tile_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
-        const int groups = H >> pt.pack_log2;
-        // single tiles where pairs would leave multiprocessors without work
-        pt.span_log2 = 8 - pt.pack_log2;
-        pt.single = static_cast<long long>(first_slot(batch->T, batch->B, pt.span_log2)) * groups <= ds->n_sm;
-        if (pt.single) --pt.span_log2;
-        pt.slots = first_slot(batch->T, batch->B, pt.span_log2);
-        if (static_cast<long long>(pt.slots) * groups > kIntMax) return S2A_ERR_UNSUPPORTED;
-        pt.by_slots = FastDiv(pt.slots), pt.by_groups_of_kv = FastDiv(p.rep >> pt.pack_log2);
         e = launch_paged_fwd(pt, e4m3, cache->d, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return S2A_OK;
+}
+
+size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    DeviceState* ds = nullptr;
+    if (check_cache(cache) != S2A_OK || check_batch(batch, cache) != S2A_OK || check_heads(cache, batch, H, max_new, window, sinks) != S2A_OK) return 0;
+    if (static_cast<long long>(max_new) * (H / cache->Hkv) <= kFewRows || prepare_device(&ds) != S2A_OK) return 0;
+    PagedTileParams p;
+    memset(&p, 0, sizeof p);
+    p.a = fwd_params(cache, batch, H, max_new, window, sinks);
+    if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size)) return 0;
+    return (static_cast<size_t>(p.slots) * (H >> p.pack_log2) - p.first_split) * p.split * paged_piece_bytes(cache->d);
 }
 
 }  // extern "C"

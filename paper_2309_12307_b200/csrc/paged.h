@@ -167,8 +167,10 @@ struct alignas(64) PagedSplitParams {
 };
 
 // Places of the tiling kernel's work items.  Sequence b has the places from first_slot() on, one for each 2^span_log2 of its tokens;
-// first_slot(starts[b + 1], b + 1) leaves it enough of them whatever `starts` are, so the places are known without adding up.
+// first_slot(starts[b + 1], b + 1) leaves it enough of them whatever `starts` are, so the places are known without adding up; there are
+// slot_count() of them.
 __host__ __device__ inline int first_slot(int row0, int b, int span_log2) { return (row0 >> span_log2) + b; }
+__host__ __device__ inline int slot_count(int T, int B, int span_log2) { return first_slot(T - 1, B, span_log2); }
 __host__ __device__ inline int find_slot(const int* starts, int B, int span_log2, int slot) {
     int lo = 0, hi = B;
     while (hi - lo > 1) {
@@ -179,6 +181,7 @@ __host__ __device__ inline int find_slot(const int* starts, int B, int span_log2
     return lo;
 }
 
+constexpr int kMostRanked = 64;  // sequences of a batch whose items are put in order
 struct alignas(64) PagedTileParams {
     CUtensorMap tm_q;        // bf16 (d, H, T), box (64, pack, 128 / pack), 128-byte swizzle
     CUtensorMap tm_k, tm_v;  // V in bf16 (d, rows of the pool), box (64, min(page_size, 128)), swizzled; K the same with the two middle ones of every
@@ -187,14 +190,20 @@ struct alignas(64) PagedTileParams {
     int pack_log2;           // query heads of a KV head that are rows of one tile
     int span_log2;           // tokens of a work item: two tiles, or one (`single`)
     bool single;
-    int slots;               // of a head group: first_slot(T, B)
-    FastDiv by_slots, by_groups_of_kv;  // head groups of a KV head: rep / pack
+    bool ranked;             // the items' order follows the sequences' lengths, see Ranking
+    bool beside;             // launched behind the splitting kernel of the same call
+    int slots;               // of a head group: slot_count()
+    // Items from first_split on are split (batches of one sequence only): `split` pieces of their keys each, which leave their results in `pieces`.
+    int first_split, split;
+    float* pieces;
+    FastDiv by_split, by_slots, by_groups, by_groups_of_kv;  // head groups, and those of a KV head: rep / pack
 };
 
 // Enqueue on `stream`; return the launch error, if any.
 cudaError_t launch_cache_write(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream);
+size_t paged_piece_bytes(int d);  // what a piece of a split item leaves
 cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream);
 int split_keys(bool e4m3, int d);  // keys of a block of the splitting kernel
 // slots[n]: blocks of four warps that the GPU runs at a time in clusters of n, 1 .. kMostSplit (0: none)

@@ -62,8 +62,10 @@ struct PagedItem {
     int pos;               // position of the token at row[1]
     int n[2];              // key tiles that either tile's products take: the first n of the item's
     int sink_blocks, low_block;
+    int j0;                // first of its key tiles among those of key_blocks()
+    int piece;             // -1, or which piece of the split items it is
     uint32_t kv0;          // ring position of its first K tile
-    __device__ __forceinline__ int key_tile(int j) const { return j < sink_blocks ? j : low_block + j - sink_blocks; }
+    __device__ __forceinline__ int key_tile(int j) const { return j0 + j < sink_blocks ? j0 + j : low_block + j0 + j - sink_blocks; }
     // (indexed by a variable, a copy in registers would have to go through local memory)
     __device__ __forceinline__ int row_of(int t) const { return t ? row[1] : row[0]; }
     __device__ __forceinline__ int tokens_of(int t) const { return t ? tokens[1] : tokens[0]; }
@@ -112,19 +114,13 @@ constexpr float kLazyRescale = 8.0f;
 constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
 __device__ __forceinline__ constexpr int key_of_column(int x) { return (x & ~3) | ((x & 1) << 1) | ((x >> 1) & 1); }
 
-// Work item `id`; false: there is none (the places of a sequence are counted generously, see PagedTileParams::slots).
-__device__ __forceinline__ bool paged_item(const PagedTileParams& p, int id, PagedItem* w) {
+// The item of head group `group` whose tokens begin with token `first` of sequence b; false: the sequence has none.
+__device__ __forceinline__ bool item_at(const PagedTileParams& p, int group, int b, long long first_token, PagedItem* w) {
     const PagedFwdParams& a = p.a;
-    int slot;
-    w->group = p.by_slots(id, &slot);
-    slot = p.slots - 1 - slot;  // the last tiles first: they have most keys
-    const int b = find_slot(a.batch.starts, a.batch.B, p.span_log2, slot);
     Sequence s;
-    if (sequence_of(a.batch, a.pool.page_log2, a.most_new, b, &s) != 0 || s.n * a.rep <= a.few_rows) return false;
-    const long long at = static_cast<long long>(slot - first_slot(s.row0, b, p.span_log2)) << p.span_log2;
-    if (at < 0 || at >= s.n) return false;
-    const int first = static_cast<int>(at), left = s.n - first, tile = kTile >> p.pack_log2;
-    w->b = b;
+    if (sequence_of(a.batch, a.pool.page_log2, a.most_new, b, &s) != 0 || s.n * a.rep <= a.few_rows || first_token < 0 || first_token >= s.n) return false;
+    const int first = static_cast<int>(first_token), left = s.n - first, tile = kTile >> p.pack_log2;
+    w->b = b, w->group = group;
     const bool two = !p.single && left > tile;
     w->tokens[0] = two ? tile : 0;
     w->tokens[1] = two ? (left - tile < tile ? left - tile : tile) : (left < tile ? left : tile);
@@ -135,7 +131,87 @@ __device__ __forceinline__ bool paged_item(const PagedTileParams& p, int id, Pag
     w->sink_blocks = k.sink_blocks, w->low_block = k.low_block;
     w->n[1] = k.count;
     w->n[0] = two ? k.sink_blocks + (w->pos - 1) / kTile + 1 - k.low_block : 0;
+    w->j0 = 0, w->piece = -1;
     return true;
+}
+
+// Item `item` as a whole, of a batch of one sequence or of more than kRanked.  The places of one head group lie together (they read the
+// same keys), the last ones first: they have most.
+__device__ __forceinline__ bool whole_item(const PagedTileParams& p, int item, PagedItem* w) {
+    int slot;
+    const int group = p.by_slots(item, &slot);
+    slot = p.slots - 1 - slot;
+    const int b = find_slot(p.a.batch.starts, p.a.batch.B, p.span_log2, slot);
+    return item_at(p, group, b, static_cast<long long>(slot - first_slot(__ldg(p.a.batch.starts + b), b, p.span_log2)) << p.span_log2, w);
+}
+
+// Batches of 2 .. kRanked sequences: a warp knows how many items each has (of a head group) and puts them in order, those with most keys
+// first, the head groups of a place side by side.  The last items to be begun are then short ones: a launch ends about as late as
+// its last item is long.  (Sequences of 400 to 4001 tokens with 1 to 701 new ones, 32 heads over 8 of 64, in their own order 129 us.)
+constexpr int kRanked = kMostRanked;
+struct Ranking {
+    int start[kRanked / 32], count[kRanked / 32], total;  // of sequences lane and lane + 32
+    __device__ __forceinline__ void set(const PagedTileParams& p) {
+        const PagedFwdParams& a = p.a;
+        const int lane = threadIdx.x & 31;
+        int keys[kRanked / 32];
+        total = 0;
+#pragma unroll
+        for (int u = 0; u < kRanked / 32; ++u) {
+            Sequence s;
+            start[u] = count[u] = keys[u] = 0;
+            const int b = lane + 32 * u;
+            if (b < a.batch.B && sequence_of(a.batch, a.pool.page_log2, a.most_new, b, &s) == 0 && s.n > 0 && s.n * a.rep > a.few_rows) {
+                count[u] = (s.n + (1 << p.span_log2) - 1) >> p.span_log2;
+                keys[u] = key_blocks(s.length - s.n, s.length - 1, a.window, a.sinks, kTile).count;
+            }
+            total += __reduce_add_sync(0xffffffffu, count[u]);
+        }
+        for (int i = 0; i < a.batch.B; ++i) {
+            const int n = __shfl_sync(0xffffffffu, i < 32 ? count[0] : count[1], i & 31), k = __shfl_sync(0xffffffffu, i < 32 ? keys[0] : keys[1], i & 31);
+#pragma unroll
+            for (int u = 0; u < kRanked / 32; ++u)
+                if (k > keys[u] || (k == keys[u] && i < lane + 32 * u)) start[u] += n;
+        }
+    }
+    // by a whole warp
+    __device__ __forceinline__ bool item(const PagedTileParams& p, int id, PagedItem* w) const {
+        int group;
+        const int place = p.by_groups(id, &group);
+        if (place >= total) return false;
+        int b = 0, x = 0;
+#pragma unroll
+        for (int u = 0; u < kRanked / 32; ++u) {
+            const uint32_t found = __ballot_sync(0xffffffffu, place >= start[u] && place < start[u] + count[u]);
+            const int from = __ffs(found) - 1, left = __shfl_sync(0xffffffffu, start[u] + count[u] - 1 - place, from & 31);
+            if (found != 0) b = from + 32 * u, x = left;
+        }
+        return item_at(p, group, b, static_cast<long long>(x) << p.span_log2, w);
+    }
+};
+
+// Key tiles of a piece of a split item (the last piece has fewer, or there are fewer pieces).
+__device__ __forceinline__ int piece_tiles(const PagedTileParams& p, const PagedItem& whole) { return (whole.n[1] + p.split - 1) / p.split; }
+
+// Work item `id`, by a whole warp: the items before first_split, then the pieces of the others.
+__device__ __forceinline__ bool paged_item(const PagedTileParams& p, const Ranking& ranking, int id, PagedItem* w) {
+    if (p.ranked) return ranking.item(p, id, w);
+    if (id < p.first_split) return whole_item(p, id, w);
+    const int piece = id - p.first_split;
+    int part;
+    if (!whole_item(p, p.first_split + p.by_split(piece, &part), w)) return false;
+    const int tiles = piece_tiles(p, *w), j0 = part * tiles;
+    if (j0 >= w->n[1]) return false;
+    w->j0 = j0, w->piece = piece;
+    w->n[1] = w->n[1] - j0 < tiles ? w->n[1] - j0 : tiles;
+    w->n[0] = w->n[0] - j0 < tiles ? w->n[0] - j0 : tiles;
+    if (w->n[0] <= 0) w->n[0] = 0, w->tokens[0] = 0, w->row[0] = w->row[1];  // (the earlier tile attends none of the piece's keys)
+    return true;
+}
+// What pieces leave for s2a_paged_join_kernel: of piece x and tile t O [d / 4][128 rows] by fours, then the running maximum and the sum of the rows.
+template <int HD>
+__device__ __forceinline__ float* piece_result(const PagedTileParams& p, int piece, int t) {
+    return p.pieces + (2ll * piece + t) * (kTile * (HD + 2));
 }
 
 template <int HD, bool kE4M3>
@@ -194,7 +270,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
         tmem_alloc(&bars->tmem_slot, C::kTmemCols);
         tmem_relinquish();
     }
-    wait_for_predecessor();
+    // (behind the splitting kernel of the same call there is nothing to wait for but what that one has waited for; see the end)
+    if (!p.beside) wait_for_predecessor();
     // An earlier report (a wait that expired, a value out of range) leaves the status word set: nothing is done then.
     if (threadIdx.x == 0) bars->abort_flag = *reinterpret_cast<volatile int*>(a.status);
     tc_fence_before();
@@ -204,6 +281,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
     const uint32_t tmem_base = bars->tmem_slot;
     if (bars->abort_flag != 0) {
         if (warp == 13) tmem_dealloc(tmem_base, C::kTmemCols);
+        if (p.beside) wait_for_predecessor();
         return;
     }
     if (blockIdx.x == 0) check_batch(a.batch, a.pool.page_log2, a.most_new, a.status, a.host_status);
@@ -227,6 +305,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             uint32_t n_clc = 0;
             bool ok = true;
             int id = static_cast<int>(blockIdx.x);
+            Ranking ranking;
+            if (p.ranked) ranking.set(p);
             const int piece_log2 = a.pool.page_log2 < 7 ? a.pool.page_log2 : 7;  // keys of a box
             auto next_id = [&]() {
                 if (lane == 0) {
@@ -301,7 +381,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             };
             for (int k = 0; ok; ++k) {
                 PagedItem w;
-                while (id >= 0 && !paged_item(p, id, &w)) id = next_id();
+                while (id >= 0 && !paged_item(p, ranking, id, &w)) id = next_id();
                 if (id < 0) w.b = -1;
                 const int g1 = group_of_tile(k, 1), g0 = group_of_tile(k, 0);
                 w.kv0 = kv;
@@ -471,17 +551,25 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                     !mbar_wait_uniform(&bars->o_full[g], n_done & 1, ctx, kWaitPagedFwd + 13))
                     return false;
                 tc_fence_after();
-                const float inv_l = sStat[g * kTile + row];
+                const float inv_l = sStat[g * kTile + row];  // (of a piece: 1, or the unit of O)
                 mbar_arrive_warp(&bars->stat_empty[g]);
                 const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
                 const bool valid = token < w.tokens_of(t);  // the others are rows of another sequence, or of none
                 const long long at = w.row_of(t) + token;
                 uint4* dst = reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD);
+                float4* partial = reinterpret_cast<float4*>(piece_result<HD>(p, w.piece, t)) + row;
 #pragma unroll 1
                 for (int c = 0; c < HD / 32; ++c) {
                     uint32_t r[32];
                     tmem_ld_32x32(t_row + C::kColO + g * HD + c * 32, r);
                     tmem_wait_ld();
+                    if (w.piece >= 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            partial[(8 * c + e) * kTile] = make_float4(__uint_as_float(r[4 * e]) * inv_l, __uint_as_float(r[4 * e + 1]) * inv_l,
+                                                                       __uint_as_float(r[4 * e + 2]) * inv_l, __uint_as_float(r[4 * e + 3]) * inv_l);
+                        continue;
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         uint4 pk;
@@ -763,8 +851,14 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             ++n_it;
             // O is in units of 2^(v_most - 6) (8 bits), weights and their sums in units of 2^-7
             const float sum_l = l[0] + l[1];
-            sStat[group * kTile + row] = (kE4M3 ? power_of_two(v_most) * 0.015625f : 1.0f) / sum_l;
+            const float unit = kE4M3 ? power_of_two(v_most) * 0.015625f : 1.0f;
+            sStat[group * kTile + row] = w.piece >= 0 ? unit : unit / sum_l;
             mbar_arrive_warp(&bars->stat_full[group]);
+            if (w.piece >= 0) {
+                float* stats = piece_result<HD>(p, w.piece, tile) + kTile * HD;
+                stats[row] = m_used, stats[kTile + row] = sum_l;
+                continue;
+            }
             const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
             if (token < w.tokens_of(tile))  // natural-log sum-exp of the scaled scores
                 a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = (m_used - (kE4M3 ? 7.f : 0.f) + log2f(sum_l)) * 0.6931471805599453f;
@@ -772,11 +866,49 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
     }
 
     // ---- teardown ------------------------------------------------------------------------------
+    if (p.beside) wait_for_predecessor();  // whoever waits for this kernel waits for that one too
     tc_fence_before();
     __syncthreads();
     if (warp == 13) {
         tc_fence_after();
         tmem_dealloc(tmem_base, C::kTmemCols);
+    }
+}
+
+// Joins the pieces of the split items, one block for each tile.  A thread has eight columns of a row at a time.
+template <int HD, bool kE4M3>
+__global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_constant__ PagedTileParams p) {
+    const PagedFwdParams& a = p.a;
+    release_successor();
+    wait_for_predecessor();
+    if (*reinterpret_cast<volatile int*>(a.status) != 0) return;
+    PagedItem w;
+    const int x = static_cast<int>(blockIdx.x) >> 1, t = static_cast<int>(blockIdx.x) & 1;
+    if (!whole_item(p, p.first_split + x, &w)) return;
+    const int tiles = piece_tiles(p, w), n = t ? w.n[1] : w.n[0], pieces = (n + tiles - 1) / tiles;
+    if (pieces == 0) return;
+    for (int i = threadIdx.x; i < kTile * (HD / 8); i += 256) {
+        const int row = i % kTile, c = i / kTile;
+        const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
+        if (token >= w.tokens_of(t)) continue;
+        float m = kLeast;
+        for (int y = 0; y < pieces; ++y) m = fmaxf(m, piece_result<HD>(p, x * p.split + y, t)[kTile * HD + row]);
+        float l = 0.f, o[8] = {};
+        for (int y = 0; y < pieces; ++y) {
+            const float* from = piece_result<HD>(p, x * p.split + y, t);
+            const float f = fast_exp2(from[kTile * HD + row] - m);
+            l = fmaf(from[kTile * HD + kTile + row], f, l);
+            const float4 u = reinterpret_cast<const float4*>(from)[2 * c * kTile + row], v = reinterpret_cast<const float4*>(from)[(2 * c + 1) * kTile + row];
+            o[0] = fmaf(u.x, f, o[0]), o[1] = fmaf(u.y, f, o[1]), o[2] = fmaf(u.z, f, o[2]), o[3] = fmaf(u.w, f, o[3]);
+            o[4] = fmaf(v.x, f, o[4]), o[5] = fmaf(v.y, f, o[5]), o[6] = fmaf(v.z, f, o[6]), o[7] = fmaf(v.w, f, o[7]);
+        }
+        const float inv_l = 1.0f / l;
+        const long long at = w.row_of(t) + token;
+        uint4 pk;
+        pk.x = pack_bf16(o[0] * inv_l, o[1] * inv_l), pk.y = pack_bf16(o[2] * inv_l, o[3] * inv_l);
+        pk.z = pack_bf16(o[4] * inv_l, o[5] * inv_l), pk.w = pack_bf16(o[6] * inv_l, o[7] * inv_l);
+        reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD)[c] = pk;
+        if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m - (kE4M3 ? 7.f : 0.f) + log2f(l)) * 0.6931471805599453f;
     }
 }
 
@@ -799,12 +931,20 @@ cudaError_t configure_paged_fwd() {
     return cudaSuccess;
 }
 
-cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream) {
-    const unsigned grid = static_cast<unsigned>(p.slots) * static_cast<unsigned>(p.a.H >> p.pack_log2);
-    auto launch = [&](auto kernel, int smem) { return launch_kernel(kernel, grid, 512, smem, stream, p, true); };
-    if (d == 64)
-        return e4m3 ? launch(s2a_paged_fwd_kernel<64, true>, PagedCfg<64, true>::kSmemBytes) : launch(s2a_paged_fwd_kernel<64, false>, PagedCfg<64, false>::kSmemBytes);
-    return e4m3 ? launch(s2a_paged_fwd_kernel<128, true>, PagedCfg<128, true>::kSmemBytes) : launch(s2a_paged_fwd_kernel<128, false>, PagedCfg<128, false>::kSmemBytes);
+template <int HD, bool kE4M3>
+static cudaError_t launch_one(const PagedTileParams& p, cudaStream_t stream) {
+    const int items = p.slots * (p.a.H >> p.pack_log2), split_items = items - p.first_split;
+    const unsigned grid = static_cast<unsigned>(p.first_split) + static_cast<unsigned>(split_items) * static_cast<unsigned>(p.split);
+    const cudaError_t e = launch_kernel(s2a_paged_fwd_kernel<HD, kE4M3>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
+    if (e != cudaSuccess || split_items == 0) return e;
+    return launch_kernel(s2a_paged_join_kernel<HD, kE4M3>, 2u * static_cast<unsigned>(split_items), 256, 0, stream, p, true);
 }
+
+cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream) {
+    if (d == 64) return e4m3 ? launch_one<64, true>(p, stream) : launch_one<64, false>(p, stream);
+    return e4m3 ? launch_one<128, true>(p, stream) : launch_one<128, false>(p, stream);
+}
+
+size_t paged_piece_bytes(int d) { return sizeof(float) * 2 * kTile * (d + 2); }
 
 }  // namespace s2a

@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     }
     if (threadIdx.x == 0) abort_flag = 0;
     __syncthreads();
-    release_successor();
     wait_for_predecessor();
+    release_successor();  // (not before: the tiling kernel of the same call relies on what this one has waited for)
     const int standing = *reinterpret_cast<volatile int*>(a.status);
     if (blockIdx.x == 0) check_batch(a.batch, a.pool.page_log2, a.most_new, a.status, a.host_status);
     const WaitCtx ctx{&abort_flag, a.status, a.host_status};

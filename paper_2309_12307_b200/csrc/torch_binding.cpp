@@ -398,10 +398,10 @@ py::object cache_read(py::handle kp, py::handle vp, py::handle ke, py::handle ve
 
 py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle table, py::handle starts, py::handle lengths,
                      std::optional<int64_t> max_new, std::optional<double> scale, int64_t window, int64_t sinks, py::handle o_, py::handle lse_,
-                     std::optional<int64_t> stream) {
+                     py::handle ws_, std::optional<int64_t> stream) {
     PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
-    Arg q(q_), o(o_), lse(lse_);
-    if (q.bad || o.bad || lse.bad || !a.check() || !a.rows(q.t)) return py::none();
+    Arg q(q_), o(o_), lse(lse_), ws(ws_);
+    if (q.bad || o.bad || lse.bad || ws.bad || !a.check() || !a.rows(q.t)) return py::none();
     const int64_t T = q.t.size(0), H = q.t.size(1), most = max_new ? *max_new : T;
     // what does not fit an int is refused by the library as any negative size is
     auto as_int = [](int64_t x) { return fits_int(x) ? static_cast<int>(x) : -1; };
@@ -411,12 +411,18 @@ py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke,
     else if (!same_shape(o.t, q.t.sizes(), q.t, at::kBFloat16)) return py::none();
     if (!lse.given) lse.t = on.output(at::empty({H, T}, q.t.options().dtype(at::kFloat)));
     else if (!same_shape(lse.t, {H, T}, q.t, at::kFloat)) return py::none();
+    if (ws.given) {
+        if (!is_dense(ws.t, at::kByte) || ws.t.device() != q.t.device()) return py::none();
+    } else if (const size_t bytes = s2a_paged_workspace_bytes(&a.cache, &a.batch, static_cast<int>(H), as_int(most), as_int(window), as_int(sinks))) {
+        ws.t = at::empty({static_cast<int64_t>(bytes)}, q.t.options().dtype(at::kByte));
+    }
     void* st = on.begin();
     int rc;
     {
         py::gil_scoped_release nogil;
         rc = s2a_paged_fwd(q.t.data_ptr(), &a.cache, &a.batch, o.t.data_ptr(), static_cast<float*>(lse.t.data_ptr()), static_cast<int>(H), as_int(most),
-                           static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(a.cache.d))), as_int(window), as_int(sinks), st);
+                           static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(a.cache.d))), as_int(window), as_int(sinks),
+                           ws.t.defined() ? ws.t.data_ptr() : nullptr, ws.t.defined() ? static_cast<size_t>(ws.t.numel()) : 0, st);
     }
     if (rc != S2A_OK) return py::int_(rc);
     return py::make_tuple(o.t, lse.t);

@@ -107,7 +107,7 @@ static int slots() {
         std::vector<int> starts(B + 1);
         starts[0] = std::rand() % 4 == 0 ? std::rand() % 300 : 0;
         for (int b = 0; b < B; ++b) starts[b + 1] = starts[b] + (std::rand() % 3 == 0 ? 0 : std::rand() % 700);
-        const int T = starts[B] + std::rand() % 300 + 1, count = first_slot(T, B, span_log2);
+        const int T = starts[B] + (std::rand() % 2 ? std::rand() % 300 : 0) + (starts[B] == 0), count = slot_count(T, B, span_log2);
         std::vector<int> seen(T, 0);
         for (int slot = 0; slot < count; ++slot) {
             const int b = find_slot(starts.data(), B, span_log2, slot);

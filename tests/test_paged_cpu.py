@@ -150,15 +150,15 @@ def test_the_library_refuses_without_a_device():
 
     lib = ctypes.CDLL(build.build())
     P, I = ctypes.c_void_p, ctypes.c_int
-    lib.s2a_paged_fwd.argtypes = [P, P, P, P, P, I, I, ctypes.c_float, I, I, P]
+    lib.s2a_paged_fwd.argtypes = [P, P, P, P, P, I, I, ctypes.c_float, I, I, P, ctypes.c_size_t, P]
     lib.s2a_cache_write.argtypes = lib.s2a_cache_read.argtypes = [P] * 5
     buf = (ctypes.c_char * 4096)()
     a = (ctypes.addressof(buf) + 255) & ~255  # never dereferenced on these paths
 
-    def call(cache=(), batch=(), q=a, o=a, lse=a, H=4, max_new=1, scale=1.0, window=0, sinks=0):
+    def call(cache=(), batch=(), q=a, o=a, lse=a, H=4, max_new=1, scale=1.0, window=0, sinks=0, workspace=None):
         c = Cache(**{**dict(k=a, v=a, k_exp=a, v_exp=a, type=1, pages=4, Hkv=2, page_size=16, d=64), **dict(cache)})
         b = Batch(**{**dict(table=a, starts=a, lengths=a, width=2, B=3, T=5), **dict(batch)})
-        attend = lib.s2a_paged_fwd(q, ctypes.byref(c), ctypes.byref(b), o, lse, H, max_new, scale, window, sinks, None)
+        attend = lib.s2a_paged_fwd(q, ctypes.byref(c), ctypes.byref(b), o, lse, H, max_new, scale, window, sinks, workspace, 0, None)
         return attend, lib.s2a_cache_write(q, o, ctypes.byref(c), ctypes.byref(b), None), lib.s2a_cache_read(ctypes.byref(c), ctypes.byref(b), q, o, None)
 
     invalid, unsupported = s2a.S2A_ERR_INVALID_ARG, s2a.S2A_ERR_UNSUPPORTED
@@ -174,6 +174,6 @@ def test_the_library_refuses_without_a_device():
     for change in (dict(q=None), dict(o=a + 8)):
         assert call(**change) == (invalid,) * 3, change
     for change in (dict(lse=a + 4), dict(lse=None), dict(H=3), dict(H=0), dict(max_new=0), dict(max_new=6), dict(scale=0.0), dict(scale=float("nan")),
-                   dict(scale=float("inf")), dict(window=-1), dict(sinks=-1)):
+                   dict(scale=float("inf")), dict(window=-1), dict(sinks=-1), dict(workspace=a + 16)):
         assert call(**change)[0] == invalid, change
-    assert lib.s2a_cache_write(a, a, None, None, None) == invalid and lib.s2a_paged_fwd(a, None, None, a, a, 4, 1, 1.0, 0, 0, None) == invalid
+    assert lib.s2a_cache_write(a, a, None, None, None) == invalid and lib.s2a_paged_fwd(a, None, None, a, a, 4, 1, 1.0, 0, 0, None, 0, None) == invalid
