@@ -108,6 +108,7 @@ struct CacheCopyParams {
     int* status;
     int* host_status;
     int tokens_per_block;
+    FastDiv by_rows;  // rows of a token: heads of k and of v
 };
 
 // The keys that the new tokens at positions first .. last attend, in blocks of `block` keys: with a window the blocks that hold the
