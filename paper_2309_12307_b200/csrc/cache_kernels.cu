@@ -2,8 +2,9 @@
 //
 // A block takes a few tokens with all their heads, k and v: one thread for each token finds its sequence and page, then a few lanes take a row
 // of d values, 16 or 32 bytes of bf16 a lane.  Both directions move each byte once; what bounds them is HBM, and for a step of single
-// tokens the launch.  So a thread has the loads of several rows in flight (with one row at a time 8192 and 5735 tokens of 32 heads of 128 took 165 us
-// into 8 bits and back, 4.2 TB/s).
+// tokens the launch.  So a thread has the loads of four rows in flight, and when it writes those of its first rows before it is known where
+// they go.  8192 and 5735 tokens of 32 heads of 128: 64 us into 8 bits and 68 back (5.4 and 5.0 TB/s), 73 and 73 in bf16 (6.2 TB/s); with one row
+// at a time 82 and 82 in 8 bits.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -20,11 +21,11 @@ constexpr int kMostTokens = 64;  // of a block
 template <int HD, bool kE4M3, bool kWrite>
 struct CopyCfg {
     // Of a lane.  16 codes are stored at once; eight of them are loaded, so that what they stand for, 16 bytes a lane, lies together
-    // for a warp's store (with 16 a lane every store instruction fills half of its sectors, 70 against 62 us for 14,000 tokens of 32 heads of 128).
+    // for a warp's store (with 16 a lane every store instruction fills half of its sectors).
     static constexpr int kValues = kE4M3 && kWrite ? 16 : 8;
     static constexpr int kLanes = HD / kValues;  // lanes of a row
     static constexpr int kRowsAtOnce = kCopyThreads / kLanes;
-    static constexpr int kRows = kE4M3 && !kWrite ? 8 : 4;  // of a thread
+    static constexpr int kRows = 4;              // of a thread
     using Cached = typename std::conditional<kE4M3 && !kWrite, uint2, uint4>::type;
 };
 
