@@ -12,7 +12,7 @@
 // long as K and Q agree, so a thread takes what lies together in shared memory.
 //
 // Cached 8-bit floats become fp16, which has them all (one conversion for two values; as bf16 they take five instructions).  Q, in bf16, goes
-// to fp16 with a power of two for each row that brings its largest value near fp16's: nothing is lost of values within 2^-29 of it.  K's
+// to fp16 with a power of two that brings the unit's largest value near fp16's: nothing is lost of values within 2^-29 of it.  K's
 // power of two multiplies the scores.  V's multiplies the weights, relative to the largest V's of the warp so far, so that they stay in
 // fp16's range: with weights up to 2^15 for the largest, those down to 2^-29 of it have all 11 bits (bf16 has 8).
 #include "paged_device.cuh"
@@ -116,38 +116,27 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         if (lane == 0) abort_flag = standing;
     }
 
-    // ---- loads of this warp: pages of its next 32 steps are in its lanes; lane 0 (and 1, where a step spans two pages) requests
+    // ---- loads of this warp: lane 0 (and 1, where a step spans two pages) requests, and has looked up the page of the next step before
     constexpr int kKeysLog2 = C::kKeys == 16 ? 4 : 5;
     const int piece_log2 = a.pool.page_log2 < kKeysLog2 ? a.pool.page_log2 : kKeysLog2;
-    const int pieces = C::kKeys >> piece_log2;
-    int page[2] = {-1, -1};
-    auto look_up = [&](int from) {
-        const int x = from + lane;
-        page[0] = page[1] = -1;
-        if (x < steps) {
-            const int key = blocks.at(i0 + x * warps) * C::kKeys;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int k = key + (i << piece_log2);
-                if (i < pieces && k < s.length) {
-                    page[i] = page_of(a.batch, a.pool.pages, b, k >> a.pool.page_log2);
-                    if (page[i] < 0) report_bad_index(a.status, a.host_status, kBadPage);
-                }
+    int next_row = -1;  // pool row that this lane requests for the next step
+    auto look_up = [&](int c) {
+        next_row = -1;
+        if (lane < C::kKeys >> piece_log2 && c < steps) {
+            const int key = blocks.at(i0 + c * warps) * C::kKeys + (lane << piece_log2);
+            if (key < s.length) {
+                const int page = page_of(a.batch, a.pool.pages, b, key >> a.pool.page_log2);
+                if (page < 0) report_bad_index(a.status, a.host_status, kBadPage);
+                else next_row = ((page * a.pool.Hkv + hk) << a.pool.page_log2) + (key & ((1 << a.pool.page_log2) - 1));
             }
         }
     };
     auto request = [&](int c) {
-        if ((c & 31) == 0) look_up(c);
-        const int st = c % C::kStages;
-        const int key = blocks.at(i0 + c * warps) * C::kKeys;
-        const int p0 = __shfl_sync(0xffffffffu, page[0], c & 31), p1 = __shfl_sync(0xffffffffu, page[1], c & 31);
-        const int mine = lane == 0 ? p0 : lane == 1 ? p1 : -1;
-        const uint32_t bytes = static_cast<uint32_t>((2 * C::kRowBytes + (kE4M3 ? 2 : 0)) << piece_log2);
-        if (lane == 0) mbar_expect_tx(&full[st], bytes * ((p0 >= 0) + (p1 >= 0)));
+        const int st = c % C::kStages, row = next_row;
+        const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        if (lane == 0) mbar_expect_tx(&full[st], static_cast<uint32_t>(boxes * (2 * C::kRowBytes + (kE4M3 ? 2 : 0))) << piece_log2);
         __syncwarp();
-        if (mine >= 0) {
-            const int slot = (key + (lane << piece_log2)) & ((1 << a.pool.page_log2) - 1);
-            const int row = ((mine * a.pool.Hkv + hk) << a.pool.page_log2) + slot;
+        if (row >= 0) {
             const uint32_t bar = smem_u32(&full[st]), dst = smem_u32(ring + st * C::kStageBytes) + ((lane << piece_log2) * C::kLine);
             tma_load_3d(dst, &p.tm_k, bar, 0, row, 0);
             tma_load_3d(dst + C::kTile, &p.tm_v, bar, 0, row, 0);
@@ -157,15 +146,16 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                 bulk_load_1d(e + C::kKeys, a.pool.v_exp + row, 1u << piece_log2, &full[st]);
             }
         }
+        look_up(c + 1);
         __syncwarp();
     };
+    look_up(0);
     for (int c = 0; c < C::kStages && c < steps; ++c) request(c);
 
     // ---- Q: row g of every eight, of every 64 columns (of all, in 8 bits) the quarter t, as pairs in the order of K's words
     constexpr int kPer = kE4M3 ? HD / 4 : 16;  // columns that lie together
     uint32_t q[kRowTiles][HD / 8];
-    float score_scale[kRowTiles][2];  // of the rows 2 t and 2 t + 1 of every eight
-    int pos[kRowTiles][2];            // their positions
+    int pos[kRowTiles][2];  // positions of the rows 2 t and 2 t + 1 of every eight
 #pragma unroll
     for (int r = 0; r < kRowTiles; ++r) {
         auto row_of = [&](int x, int* hh) {  // rows past the end follow the last one
@@ -181,22 +171,27 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * c + (c * 8 / kPer) * (64 - kPer) * (kE4M3 ? 0 : 1));
             q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
         }
-        score_scale[r][0] = score_scale[r][1] = a.scale_log2;
-        if constexpr (kE4M3) {
-            uint32_t most = 0;
+    }
+    float score_scale = a.scale_log2;
+    if constexpr (kE4M3) {
+        uint32_t most = 0;
 #pragma unroll
-            for (int c = 0; c < HD / 8; ++c) most = max(most, max(q[r][c] & 0x7fffu, q[r][c] >> 16 & 0x7fffu));
-            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            // the largest goes to [2^14, 2^15); a row that is not finite stays so
-            int up = most >= 0x7f80u || most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);
-            up = up > 126 ? 126 : up;
-            const float f = power_of_two(up);
+        for (int r = 0; r < kRowTiles; ++r) {
+            uint32_t row_most = 0;
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) row_most = max(row_most, max(q[r][c] & 0x7fffu, q[r][c] >> 16 & 0x7fffu));
+            most = max(most, row_most < 0x7f80u ? row_most : 0u);  // (a row that is not finite stays so, and sets no scale)
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        // the largest goes to [2^14, 2^15)
+        int up = most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);
+        up = up > 126 ? 126 : up;
+        const float f = power_of_two(up);
+        score_scale *= power_of_two(-up);
+#pragma unroll
+        for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
             for (int c = 0; c < HD / 8; ++c) q[r][c] = pack_f16(bf16_low(q[r][c]) * f, bf16_high(q[r][c]) * f);
-            score_scale[r][0] *= power_of_two(-__shfl_sync(0xffffffffu, up, 8 * t));
-            score_scale[r][1] *= power_of_two(-__shfl_sync(0xffffffffu, up, 8 * t + 4));
-        }
     }
 
     float o[kRowTiles][HD / 16][4] = {};
@@ -246,29 +241,30 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                 }
             }
         }
-        // scores in units of log2: keys 16 u + g + 8 (x >> 1), rows 8 r + 2 t + (x & 1)
-        float v_factor[kTiles][2];
-        int v_exp[kTiles][2];
+        // Exponents of the step's keys (8 bits): lane i has those of key i, as what a score is multiplied with and as it is.
+        float k_scale = score_scale;
+        int v_exp = kExpLeast;
         bool grows = false;
+        if constexpr (kE4M3) {
+            k_scale *= exponent_factor(lds_s8(sE + lane));
+            v_exp = lds_s8(sE + C::kKeys + lane);
+            // (what lies there for keys past the end of the sequence can be anything: it must not set the scale)
+            if (masked && !any_attends(first_pos, last_pos, key0 + lane, a.window, a.sinks)) v_exp = kExpLeast;
+            grows = v_exp > v_most;
+        }
+        // scores in units of log2: keys 16 u + g + 8 (x >> 1), rows 8 r + 2 t + (x & 1)
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
-            float k_factor[2] = {1.f, 1.f};
+            float scale[2] = {k_scale, k_scale};
             if constexpr (kE4M3) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    k_factor[x] = exponent_factor(lds_s8(sE + 16 * u + 8 * x + g));
-                    v_exp[u][x] = lds_s8(sE + C::kKeys + 16 * u + 8 * x + g);
-                    // (what lies there for keys past the end of the sequence can be anything: it must not set the scale)
-                    if (masked && !any_attends(first_pos, last_pos, key0 + 16 * u + 8 * x + g, a.window, a.sinks)) v_exp[u][x] = kExpLeast;
-                    grows |= v_exp[u][x] > v_most;
-                }
+                for (int x = 0; x < 2; ++x) scale[x] = __shfl_sync(0xffffffffu, k_scale, 16 * u + 8 * x + g);
             }
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    sc[u][r][x] *= score_scale[r][x & 1];
-                    if constexpr (kE4M3) sc[u][r][x] *= k_factor[x >> 1];
+                    sc[u][r][x] *= scale[x >> 1];
                     if (masked && !attends(pos[r][x & 1], key0 + 16 * u + 8 * (x >> 1) + g, a.window, a.sinks)) sc[u][r][x] = -INFINITY;
                     grows |= sc[u][r][x] > m[r][x & 1] + kLazy;
                 }
@@ -276,10 +272,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         if (__any_sync(0xffffffffu, grows)) {
             float v_down = 1.f;
             if constexpr (kE4M3) {
-                int most = v_most;
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u) most = max(most, max(v_exp[u][0], v_exp[u][1]));
-                most = __reduce_max_sync(0xffffffffu, most);
+                const int most = max(v_most, __reduce_max_sync(0xffffffffu, v_exp));
                 v_down = power_of_two(max(v_most - most, -127));
                 v_most = most;
             }
@@ -302,12 +295,15 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                 for (int x = 0; x < HD / 16; ++x) o[r][x][0] *= down[0], o[r][x][1] *= down[1], o[r][x][2] *= down[0], o[r][x][3] *= down[1];
             }
         }
+        float v_scale = 1.f;  // lane i's of key i
+        if constexpr (kE4M3) v_scale = v_exp == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(v_exp - v_most, -127));
         uint32_t w[kTiles][kRowTiles][2];  // weights of rows 8 r + g, keys 16 u + 2 t.. and 16 u + 8 + 2 t.. as pairs
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
+            float v_factor[2] = {1.f, 1.f};
             if constexpr (kE4M3) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) v_factor[u][x] = v_exp[u][x] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(v_exp[u][x] - v_most, -127));
+                for (int x = 0; x < 2; ++x) v_factor[x] = __shfl_sync(0xffffffffu, v_scale, 16 * u + 8 * x + g);
             }
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r) {
@@ -316,7 +312,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                 for (int x = 0; x < 4; ++x) {
                     e[x] = fast_exp2(sc[u][r][x] - (m[r][x & 1] - kUp));
                     l[r][x & 1] += e[x];
-                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : e[x] * v_factor[u][x >> 1];
+                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : e[x] * v_factor[x >> 1];
                 }
                 w[u][r][0] = transpose_8x8(kE4M3 ? pack_f16(e[0], e[1]) : pack_bf16(e[0], e[1]));
                 w[u][r][1] = transpose_8x8(kE4M3 ? pack_f16(e[2], e[3]) : pack_bf16(e[2], e[3]));
