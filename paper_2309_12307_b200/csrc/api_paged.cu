@@ -79,39 +79,43 @@ int tile_tmaps(PagedTileParams* p, const s2a_cache* c, const void* q, int H, int
 }
 
 // How the keys of the units (8 or 16 rows of a sequence and KV head) are dealt out: blocks of `warps` warps, `split` of them in a cluster
-// for each unit, whatever should be done first by this estimate, in microseconds:
-//   - the bytes of all units at the memory's rate.  A batch's sequences differ in length: the average is taken as 0.7 of the longest.
-//   - half of what the longest piece takes by itself (a block of four warps needs 11 to 13 ns for a key of 128 columns): the blocks end that much
-//     apart.  Of a single sequence all pieces are alike: its blocks run in whole waves instead.
+// for each unit, whatever should be done first by this estimate, in microseconds.
+//   - All units' bytes at the memory's rate.  A batch's sequences differ in length: the average is taken as 0.7 of the longest.
+//   - What a piece takes: a block of four warps needs 13 ns (8 bits: 10) for a key of 128 columns when it is alone on its multiprocessor, 1.23
+//     times that beside another one and 1.6 times beside two.  Blocks of a batch end about half of the longest piece's time apart.  Of a
+//     single sequence all pieces are alike and run in waves.
 //   - 8 us for every block that a place on the GPU sees: the launch, the addresses, the first loads' latency, joining the results.
 // Measured (us, by blocks in a cluster, of four warps): 16 x up to 8192 tokens of 32 heads of 128 1 190, 2 170, 3 171, 4 181; 8 x up to 32k of 8 heads
 // in 8 bits 4 117, 6 94, 8 96, 10 88, 12 99; 16 x up to 32k of 8 heads in 8 bits 4 136, 6 114, 8 126; 4 x 8192 of 40 heads 2 112, 3 126, 4 104, 6 115;
-// one of 100,000 of 32 heads in 8 bits 6 229, 8 193, 10 159, 12 203; 64 x up to 1024 of 32 heads, one block of two warps 89, of four 92.
+// one of 100,000 of 32 heads in 8 bits 4 255, 6 198, 7 172, 8 153, 9 171, 10 155, 12 201, in bf16 4 356, 6 267, 7 243, 8 263, 10 256; 64 x up to 1024 of 32
+// heads, one block of two warps 89, of four 92.
 void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, int key_bytes, bool e4m3, int d) {
     const long long units = static_cast<long long>(p->a.batch.B) * p->a.pool.Hkv * p->row_blocks;
-    const double rate = 6.5e6, block_start = 8.0;  // bytes and key times in microseconds
-    const double key_time = (e4m3 ? 0.0105 : 0.0128) * d / 128;
+    const double rate = 6.5e6, block_start = 8.0;  // bytes in a microsecond, microseconds
+    const double key_time = (e4m3 ? 0.010 : 0.013) * d / 128, beside[4] = {0, 1.0, 1.23, 1.6};
     double best = 0;
-    p->warps = 4, p->split = 1;
+    p->warps = 4, p->split = 1, p->blocks = 3;
     for (int warps = 4; warps >= 1; warps /= 2)
         for (int split = 1; split <= kMostSplit; ++split) {
-            const int slots = ds->cluster_slots[split] * (4 / warps);
             const long long blocks = units * split;
-            if (slots <= 0 || (split > 1 && reach <= static_cast<long long>(split - 1) * warps * split_keys(e4m3, d))) continue;
-            const double piece = static_cast<double>((reach + split - 1) / split), alone = piece * key_time * 4 / warps, waves = static_cast<double>(blocks) / slots;
+            auto slots = [&](int on_sm) { return static_cast<long long>(ds->cluster_slots[on_sm][split]) * (4 / warps); };
+            if (slots(3) <= 0 || (split > 1 && reach <= static_cast<long long>(split - 1) * warps * split_keys(e4m3, d))) continue;
+            auto on_sm = [&](long long n) { return n <= slots(1) ? 1 : n <= slots(2) ? 2 : 3; };  // blocks beside one another when n run
+            const double piece = static_cast<double>((reach + split - 1) / split), alone = piece * key_time * 4 / warps;
             double t;
             if (p->a.batch.B > 1) {
+                const double waves = static_cast<double>(blocks) / slots(3);
                 t = 0.7 * units * reach * key_bytes / rate + 0.5 * alone + block_start * (waves < 1 ? 1 : waves);
             } else {
-                t = 0;
-                for (double left = waves; left > 0; left -= 1) {
-                    if (left > 64) t += left, left = 1;  // (never met: one sequence has few units)
-                    const double bytes = (left < 1 ? left : 1) * slots * piece * key_bytes / rate;
-                    t += (bytes > alone ? bytes : alone) + block_start;
-                }
+                auto wave = [&](long long n) {
+                    const double bytes = n * piece * key_bytes / rate, work = alone * beside[on_sm(n)];
+                    return n == 0 ? 0 : (bytes > work ? bytes : work) + block_start;
+                };
+                t = static_cast<double>(blocks / slots(3)) * wave(slots(3)) + wave(blocks % slots(3));
             }
-            if (best == 0 || t < best) best = t, p->warps = warps, p->split = split;
+            if (best == 0 || t < best) best = t, p->warps = warps, p->split = split, p->blocks = on_sm(blocks);
         }
+    p->stages = split_stages(e4m3, d, p->blocks);  // where fewer blocks run at a time, each has more in flight
 }
 
 // The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.

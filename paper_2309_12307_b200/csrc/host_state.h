@@ -15,7 +15,7 @@ struct DeviceState {
     volatile int* host_word = nullptr;  // this device's mirror, host address
     int* host_word_dev = nullptr;     // the same word as the device sees it
     int n_sm = 0;                     // multiprocessors
-    int cluster_slots[17] = {};       // blocks of the paged cache's splitting kernel (of four warps) that run at a time in clusters of 1 .. 16
+    int cluster_slots[4][17] = {};    // of the paged cache's splitting kernel, see configure_paged_split()
     // s2a_fwd_bwd_host only: copy streams and the events that order them against the caller's stream
     bool host_path_ready = false;
     cudaStream_t copy_in = nullptr, copy_out = nullptr;

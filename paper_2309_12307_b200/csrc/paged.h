@@ -161,6 +161,7 @@ struct alignas(64) PagedSplitParams {
     CUtensorMap tm_k, tm_v;  // (columns of a line of at most 128 bytes, rows of the pool, lines of a row), box (all, min(page_size, keys of a step), all)
     PagedFwdParams a;
     int warps;               // of a block: 1, 2 or 4
+    int blocks, stages;      // blocks of four warps on an SM that the shared memory is divided among, 1 .. 3, and the stages that leaves a warp
     int split;               // blocks of a cluster, which share the keys of a unit: 1 .. kMostSplit
     int unit_rows;           // 8 or 16
     int row_blocks;          // of unit_rows rows, that a sequence and KV head has at most
@@ -206,9 +207,10 @@ cudaError_t launch_cache_read(const CacheCopyParams& p, bool e4m3, int d, cudaSt
 cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream);
 size_t paged_piece_bytes(int d);  // what a piece of a split item leaves
 cudaError_t launch_paged_split(const PagedSplitParams& p, bool e4m3, int d, cudaStream_t stream);
-int split_keys(bool e4m3, int d);  // keys of a block of the splitting kernel
-// slots[n]: blocks of four warps that the GPU runs at a time in clusters of n, 1 .. kMostSplit (0: none)
-cudaError_t configure_paged_split(int* slots);
+int split_keys(bool e4m3, int d);  // keys of a step of a warp of the splitting kernel
+int split_stages(bool e4m3, int d, int blocks);
+// slots[b][n]: blocks of four warps, meant for b on an SM, that the GPU runs at a time in clusters of n, 1 .. kMostSplit (0: none)
+cudaError_t configure_paged_split(int (*slots)[kMostSplit + 1]);
 cudaError_t configure_paged_fwd();
 
 }  // namespace s2a

@@ -30,12 +30,17 @@ struct SplitCfg {
     static constexpr int kBoxes = kRowBytes / kLine;
     static constexpr int kTile = kKeys * kRowBytes;               // K or V of a step
     static constexpr int kStageBytes = 2 * kTile;
-    static constexpr int kStages = 16384 / kStageBytes;           // 16 KB in flight for each warp, twelve warps on an SM
     static constexpr int kExpBytes = kE4M3 ? 2 * kKeys : 0;       // exponents of K and V
-    static constexpr int kWarpBytes = kStages * (kStageBytes + kExpBytes + 8);  // ring, exponents, barriers
-    static constexpr int smem_bytes(int warps) { return warps * kWarpBytes + 16; }  // and the abort flag
+    // A warp's ring: 16 KB where three blocks of four warps are on an SM, 24 KB for two, 48 KB for one, so that what is in flight there is the
+    // same 192 KB (a token over 100,000 of 32 heads in 8 bits, 256 blocks: 16 KB 193 us, 24 KB 154).
+    static constexpr int ring_bytes(int blocks) { return blocks == 3 ? 16384 : blocks == 2 ? 24576 : 49152; }
+    static constexpr int stages(int blocks) { return ring_bytes(blocks) / kStageBytes; }
+    static constexpr int smem_bytes(int blocks, int warps) {  // rings, exponents, barriers, the abort flag
+        return warps * (ring_bytes(blocks) + stages(blocks) * (kExpBytes + 8)) + 16;
+    }
     static constexpr int kPartFloats = 16 * HD + 4 * 16;          // a warp's result: O, m, l, and the joined m, l
-    static_assert(kPartFloats * 4 <= kStages * kStageBytes, "the ring holds a result");
+    static_assert(kPartFloats * 4 <= ring_bytes(3), "the ring holds a result");
+    static_assert(ring_bytes(3) % kStageBytes == 0 && ring_bytes(2) % kStageBytes == 0, "whole stages");
     static_assert(kTile % 1024 == 0, "swizzle atoms");
 };
 
@@ -78,13 +83,14 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     const PagedFwdParams& a = p.a;
     const int warps = p.warps, threads = 32 * warps;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    uint8_t* ring = smem + warp * (C::kStages * C::kStageBytes);
-    uint8_t* exps = smem + warps * C::kStages * C::kStageBytes + warp * (C::kStages * C::kExpBytes);
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + warps * C::kStages * (C::kStageBytes + C::kExpBytes)) + warp * C::kStages;
-    volatile int& abort_flag = *reinterpret_cast<volatile int*>(smem + warps * C::kWarpBytes);
+    const int stages = p.stages, ring_bytes = stages * C::kStageBytes;
+    uint8_t* ring = smem + warp * ring_bytes;
+    uint8_t* exps = smem + warps * ring_bytes + warp * (stages * C::kExpBytes);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + warps * stages * (C::kStageBytes + C::kExpBytes)) + warp * stages;
+    volatile int& abort_flag = *reinterpret_cast<volatile int*>(smem + warps * stages * (C::kStageBytes + C::kExpBytes + 8));
 
     if (lane == 0) {
-        for (int s = 0; s < C::kStages; ++s) mbar_init(&full[s], 1);
+        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1);
         fence_barrier_init();
         tma_prefetch_desc(&p.tm_k);
         tma_prefetch_desc(&p.tm_v);
@@ -131,8 +137,8 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             }
         }
     };
-    auto request = [&](int c) {
-        const int st = c % C::kStages, row = next_row;
+    auto request = [&](int c, int st) {
+        const int row = next_row;
         const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
         if (lane == 0) mbar_expect_tx(&full[st], static_cast<uint32_t>(boxes * (2 * C::kRowBytes + (kE4M3 ? 2 : 0))) << piece_log2);
         __syncwarp();
@@ -150,7 +156,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         __syncwarp();
     };
     look_up(0);
-    for (int c = 0; c < C::kStages && c < steps; ++c) request(c);
+    for (int c = 0; c < stages && c < steps; ++c) request(c, c);
 
     // ---- Q: row g of every eight, of every 64 columns (of all, in 8 bits) the quarter t, as pairs in the order of K's words
     constexpr int kPer = kE4M3 ? HD / 4 : 16;  // columns that lie together
@@ -200,10 +206,9 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     for (int r = 0; r < kRowTiles; ++r) m[r][0] = m[r][1] = kLeast, l[r][0] = l[r][1] = 0.f;
     int v_most = kExpLeast;  // the largest exponent of V so far (8 bits): O is in units of 2^v_most
     bool ok = true;
-    int c = 0;
+    int c = 0, st = 0, phase = 0;  // step, its stage, and which use of the stage it is (odd or even)
     for (; c < steps; ++c) {
-        const int st = c % C::kStages;
-        if (!mbar_wait_uniform(&full[st], (c / C::kStages) & 1, ctx, kWaitPagedSplit + 1)) { ok = false; break; }
+        if (!mbar_wait_uniform(&full[st], phase, ctx, kWaitPagedSplit + 1)) { ok = false; break; }
         const uint32_t sK = smem_u32(ring + st * C::kStageBytes), sV = sK + C::kTile, sE = smem_u32(exps + st * C::kExpBytes);
         const int key0 = blocks.at(i0 + c * warps) * C::kKeys;
         const bool masked = !all_attend(first_pos, last_pos, key0, C::kKeys, a.window, a.sinks);
@@ -361,10 +366,14 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             }
         }
         __syncwarp();
-        if (c + C::kStages < steps) request(c + C::kStages);
+        if (c + stages < steps) request(c + stages, st);
+        if (++st == stages) st = 0, phase ^= 1;
     }
     if (!ok && lane == 0)  // loads in flight land before the memory is used for something else
-        for (int x = c; x < steps && x < c + C::kStages; ++x) mbar_wait_drain(&full[x % C::kStages], (x / C::kStages) & 1);
+        for (int x = c; x < steps && x < c + stages; ++x) {
+            mbar_wait_drain(&full[st], phase);
+            if (++st == stages) st = 0, phase ^= 1;
+        }
     __syncwarp();
 
     // ---- this warp's result into its ring: O of the rows, then m and l
@@ -398,20 +407,20 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top - kUp + log2f(sum)) * 0.6931471805599453f;
     };
     // ---- the warps' results joined, into the first ring
-    constexpr int kRing = C::kStages * C::kStageBytes / 4;  // floats of a ring
+    const int ring_floats = ring_bytes / 4;
     float* first = reinterpret_cast<float*>(smem);
     for (int e = threadIdx.x; e < rows * HD; e += threads) {
         const int row = e / HD;
         float top = kLeast, sum = 0.f, value = 0.f;
 #pragma unroll
         for (int w = 0; w < C::kMostWarps; ++w)
-            if (w < warps) top = fmaxf(top, first[w * kRing + kM + row]);
+            if (w < warps) top = fmaxf(top, first[w * ring_floats + kM + row]);
 #pragma unroll
         for (int w = 0; w < C::kMostWarps; ++w) {
             if (w >= warps) break;
-            const float f = fast_exp2(first[w * kRing + kM + row] - top);
-            sum += f * first[w * kRing + kL + row];
-            value += f * first[w * kRing + e];
+            const float f = fast_exp2(first[w * ring_floats + kM + row] - top);
+            sum += f * first[w * ring_floats + kL + row];
+            value += f * first[w * ring_floats + e];
         }
         if (p.split == 1) {
             finish(e, value, top, sum);
@@ -449,7 +458,7 @@ template <int HD, bool kE4M3, int kRowTiles>
 cudaError_t configure_one() {
     auto kernel = s2a_paged_split_kernel<HD, kE4M3, kRowTiles>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               SplitCfg<HD, kE4M3>::smem_bytes(SplitCfg<HD, kE4M3>::kMostWarps));
+                                               SplitCfg<HD, kE4M3>::smem_bytes(1, SplitCfg<HD, kE4M3>::kMostWarps));
     return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
@@ -460,7 +469,7 @@ struct SplitLaunch {
     SplitLaunch(const PagedSplitParams& p, unsigned grid, cudaStream_t stream) {
         config.gridDim = dim3(grid);
         config.blockDim = dim3(32u * static_cast<unsigned>(p.warps));
-        config.dynamicSmemBytes = SplitCfg<HD, kE4M3>::smem_bytes(p.warps);
+        config.dynamicSmemBytes = SplitCfg<HD, kE4M3>::smem_bytes(p.blocks, p.warps);
         config.stream = stream;
         attribute[0].id = cudaLaunchAttributeClusterDimension;
         attribute[0].val.clusterDim.x = static_cast<unsigned>(p.split), attribute[0].val.clusterDim.y = attribute[0].val.clusterDim.z = 1;
@@ -480,26 +489,32 @@ cudaError_t launch_one(const PagedSplitParams& p, cudaStream_t stream) {
 
 }  // namespace
 
+int split_stages(bool e4m3, int d, int blocks) {
+    return d == 64 ? (e4m3 ? SplitCfg<64, true>::stages(blocks) : SplitCfg<64, false>::stages(blocks))
+                   : (e4m3 ? SplitCfg<128, true>::stages(blocks) : SplitCfg<128, false>::stages(blocks));
+}
+
 int split_keys(bool e4m3, int d) {
     return d == 64 ? (e4m3 ? SplitCfg<64, true>::kKeys : SplitCfg<64, false>::kKeys) : (e4m3 ? SplitCfg<128, true>::kKeys : SplitCfg<128, false>::kKeys);
 }
 
-cudaError_t configure_paged_split(int* slots) {
+cudaError_t configure_paged_split(int (*slots)[kMostSplit + 1]) {
     for (const cudaError_t e : {configure_one<64, false, 1>(), configure_one<64, false, 2>(), configure_one<64, true, 1>(), configure_one<64, true, 2>(),
                                 configure_one<128, false, 1>(), configure_one<128, false, 2>(), configure_one<128, true, 1>(), configure_one<128, true, 2>()})
         if (e != cudaSuccess) return e;
     // (what limits the blocks on an SM is shared memory, of which all forms take the same)
-    for (int split = 1; split <= kMostSplit; ++split) {
-        PagedSplitParams p = {};
-        p.warps = 4, p.split = split;
-        SplitLaunch<128, true> launch(p, static_cast<unsigned>(split), nullptr);
-        int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, s2a_paged_split_kernel<128, true, 1>, &launch.config) != cudaSuccess) {
-            cudaGetLastError();  // clusters of this size are not to be had
-            clusters = 0;
+    for (int blocks = 1; blocks <= 3; ++blocks)
+        for (int split = 1; split <= kMostSplit; ++split) {
+            PagedSplitParams p = {};
+            p.warps = 4, p.split = split, p.blocks = blocks;
+            SplitLaunch<128, true> launch(p, static_cast<unsigned>(split), nullptr);
+            int clusters = 0;
+            if (cudaOccupancyMaxActiveClusters(&clusters, s2a_paged_split_kernel<128, true, 1>, &launch.config) != cudaSuccess) {
+                cudaGetLastError();  // clusters of this size are not to be had
+                clusters = 0;
+            }
+            slots[blocks][split] = clusters * split;
         }
-        slots[split] = clusters * split;
-    }
     return cudaSuccess;
 }
 
