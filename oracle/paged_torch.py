@@ -84,16 +84,26 @@ def visible(position, length, window, sinks):
 
 
 def paged_fwd(q, cache, table, starts, lengths, scale, window=0, sinks=0):
-    """o, lse and the sum of weight * |v| (for error bounds), rows of no sequence NaN."""
+    """o, lse and, for error bounds, the sum of weight * |v| and (0 unless the cache has exponents) the largest product, over the blocks of 128
+    keys, of the largest weight and the largest power of two of v in the block.  Rows of no sequence are NaN."""
     T, H, d = q.shape
     o = torch.full((T, H, d), math.nan, dtype=torch.float64)
     size, lse = o.clone(), torch.full((H, T), math.nan, dtype=torch.float64)
+    largest = torch.zeros((T, H), dtype=torch.float64)
     for b in range(len(lengths)):
         row0, n, length = int(starts[b]), int(starts[b + 1] - starts[b]), int(lengths[b])
         if n == 0:
             continue
         k, v = (sequence_values(cache, x, table, b, length) for x in ("k", "v"))
         rep = H // k.shape[0]
+        blocks = -(-length // 128)
+        powers = None
+        if "v_exp" in cache:
+            page = cache["v"].shape[2]
+            e = cache["v_exp"][table[b, :-(-length // page)].long()].double().transpose(0, 1).reshape(k.shape[0], -1)[:, :length]
+            powers = torch.full((k.shape[0], blocks * 128), -1e9, dtype=torch.float64)
+            powers[:, :length] = e
+            powers = torch.exp2(powers.view(k.shape[0], blocks, 128).amax(-1))
         for i in range(n):
             seen = visible(length - n + i, length, window, sinks)
             for h in range(H):
@@ -102,4 +112,8 @@ def paged_fwd(q, cache, table, starts, lengths, scale, window=0, sinks=0):
                 w = torch.exp(s - lse[h, row0 + i])
                 o[row0 + i, h] = w @ v[h // rep][seen]
                 size[row0 + i, h] = w @ v[h // rep][seen].abs()
-    return o, lse, size
+                if powers is not None:
+                    of_block = torch.zeros(blocks * 128, dtype=torch.float64)
+                    of_block[:length][seen] = w
+                    largest[row0 + i, h] = (of_block.view(blocks, 128).amax(-1) * powers[h // rep]).max()
+    return o, lse, size, largest

@@ -20,10 +20,11 @@
 // warps 8-11 write them where the products read them, each row times its power of two relative to the tile's largest (6 binary
 // places up: the tile's largest value is below 2^15 and values down to 2^-29 of it keep all their bits).  Q they turn from bf16 to fp16, each row times
 // a power of two that brings its largest value to [2^14, 2^15).  What is the tile's, or the row's, then multiplies scores and weights for
-// nothing: it goes into the constants of exp2(score * c - m).  Weights are 2^7 as large as with bf16, so that those down to 2^-21 of the
-// largest have all of fp16's 11 bits (bf16 has 8) and those below 2^-32 of it vanish; O is in units of the largest tile exponent of V so far,
-// rescaled like a running maximum.  As bf16, values take five instructions instead of one and a half and the four warps cannot
-// keep up: 32k tokens, 2048 new ones, 64 heads over 8 3.03 ms.
+// nothing: it goes into the constants of exp2(score * c - m).  With x a score in units of log2 and 2^e the tile's power of V the weight of
+// the second product is 2^(x + e - r + 7), r a running maximum of x + e of the row: the largest term's weight is 2^7 or more, those
+// down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), those below 2^-32 of it vanish.  O is in units of 2^(r - m), m being
+// the running maximum of x that the sum of weights goes by.  As bf16, values take five instructions instead of one and a half and the
+// four warps cannot keep up: 32k tokens, 2048 new ones, 64 heads over 8 3.03 ms.
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -315,7 +316,9 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 }
                 __syncwarp();
                 if (!mbar_wait_uniform(&bars->clc, n_clc & 1, ctx, kWaitPagedFwd + 1)) {
-                    if (lane == 0) mbar_wait_drain(&bars->clc, n_clc & 1);  // the answer must not land after the block has gone
+                    if (lane == 0) {
+                        mbar_wait_drain(&bars->clc, n_clc & 1);  // the answer must not land after the block has gone
+                    }
                     ok = false;
                     return -1;
                 }
@@ -427,12 +430,14 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 if (ok) id = next_id();
             }
             // nothing may land after the block has gone
-            if (__any_sync(0xffffffffu, bars->abort_flag != 0) && lane == 0) {
-                for (int t = 0; t < 2; ++t)
-                    if (n_q[t] > 0) mbar_wait_drain(&bars->q_full[t], (n_q[t] - 1) & 1);
-                constexpr uint32_t kIn = kE4M3 ? C::kRawRing : C::kRing;
-                for (uint32_t x = (kv > kIn ? kv - kIn : 0); x < kv; ++x)
-                    mbar_wait_drain(kE4M3 ? &bars->raw_full[x % kIn] : &bars->kv_full[x % kIn], (x / kIn) & 1);
+            if (lane == 0) {
+                if (bars->abort_flag != 0) {
+                    for (int t = 0; t < 2; ++t)
+                        if (n_q[t] > 0) mbar_wait_drain(&bars->q_full[t], (n_q[t] - 1) & 1);
+                    constexpr uint32_t kIn = kE4M3 ? C::kRawRing : C::kRing;
+                    for (uint32_t x = (kv > kIn ? kv - kIn : 0); x < kv; ++x)
+                        mbar_wait_drain(kE4M3 ? &bars->raw_full[x % kIn] : &bars->kv_full[x % kIn], (x / kIn) & 1);
+                }
             }
             __syncwarp();
         } else if (warp <= 14) {
@@ -730,7 +735,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             float m_used = 0.f;   // running maximum in use, scaled to log2 units
             float l[2] = {0.f, 0.f};
             float c2 = a.scale_log2;
-            int up = 0, v_most = 0;  // 8 bits: the exponent of the row of Q, the largest tile exponent of V so far
+            int up = 0;              // 8 bits: the exponent of the row of Q
+            float ref = 0.f;         // 8 bits: r, the running maximum that O goes by
             for (int j = 0; j < n; ++j, ++n_s) {
                 const int key0 = w.key_tile(j) * kTile;
                 if (!mbar_wait_uniform(&bars->s_full[group], n_s & 1, ctx, kWaitPagedFwd + 15)) { ok = false; break; }
@@ -771,29 +777,22 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 // the P.V product of this tile's step before is done: P and O may be written
                 if (n_s > 0 && !mbar_wait_uniform(&bars->p_empty[group], (n_s - 1) & 1, ctx, kWaitPagedFwd + 17)) { ok = false; break; }
                 tc_fence_after();
-                float down_v = 1.f, tile_up = 1.f, shift = 0.f;  // of O; of the sums of the tile's weights; of their exponents
+                float v_exp = 0.f;  // 8 bits: the tile's of V
                 if constexpr (kE4M3) {
                     // (V of this step has been written by now, or is about to be)
                     const uint32_t x = w.kv0 + 2 * j + 1;
                     if (!mbar_wait_uniform(&bars->kv_full[x % C::kRing], (x / C::kRing) & 1, ctx, kWaitPagedFwd + 21)) { ok = false; break; }
-                    const int v_exp = bars->tile_exp[x % 16];
-                    if (j == 0) {
-                        v_most = v_exp;
-                    } else if (v_exp > v_most) {
-                        down_v = power_of_two(max(v_most - v_exp, -127));
-                        v_most = v_exp;
-                    }
-                    const int below = max(v_exp - v_most, -60);  // (weights of 2^-45 are none in fp16: V that small counts for nothing beside the largest)
-                    shift = static_cast<float>(7 + below), tile_up = power_of_two(-below);
+                    v_exp = static_cast<float>(bars->tile_exp[x % 16]);
                 }
                 if (j == 0) {
                     m_used = fmaxf(m_new, kLeast);  // (a row can have no key in the first tile of a window)
+                    ref = m_used + v_exp;
                 } else {
-                    const bool need = (m_new - m_used) > kLazyRescale;
-                    if (__any_sync(0xffffffffu, need || (kE4M3 && down_v != 1.f))) {
-                        float alpha = need ? fast_exp2(m_used - m_new) : 1.0f;
-                        l[0] *= alpha, l[1] *= alpha;
-                        if (kE4M3) alpha *= down_v;
+                    const bool need = (m_new - m_used) > kLazyRescale, need_o = kE4M3 ? (m_new + v_exp - ref) > kLazyRescale : need;
+                    if (__any_sync(0xffffffffu, need || need_o)) {
+                        const float alpha_l = need ? fast_exp2(m_used - m_new) : 1.0f;
+                        const float alpha = kE4M3 ? (need_o ? fast_exp2(ref - (m_new + v_exp)) : 1.0f) : alpha_l;
+                        l[0] *= alpha_l, l[1] *= alpha_l;
 #pragma unroll 1
                         for (int c = 0; c < HD / 16; ++c) {
                             uint32_t o[16];
@@ -805,8 +804,12 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                             tmem_st_32x16(t_o, o);
                         }
                         if (need) m_used = m_new;
+                        if (need_o) ref = m_new + v_exp;
                     }
                 }
+                // Exponents of the weights are x - m + shift.  (Below 2^-45 a weight is none in fp16; the sum still wants the weights.)
+                const float shift = kE4M3 ? 7.f + fmaxf(v_exp + m_used - ref, -60.f) : 0.f;
+                const float tile_up = kE4M3 ? fast_exp2(-shift) : 1.f;  // of the sums of the tile's weights
                 const uint64_t nm = f2_pack(shift - m_used, shift - m_used);
                 uint64_t sum[2];  // of a half of the tile: chains 0 and 1, chains 2 and 3 (see key_of_column in fwd_kernel.cu)
                 auto add_chunk = [&](int c) {
@@ -849,9 +852,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             }
             if (!ok || !mbar_wait_uniform(&bars->stat_empty[group], (n_it & 1) ^ 1, ctx, kWaitPagedFwd + 16)) break;
             ++n_it;
-            // O is in units of 2^(v_most - 6) (8 bits), weights and their sums in units of 2^-7
             const float sum_l = l[0] + l[1];
-            const float unit = kE4M3 ? power_of_two(v_most) * 0.015625f : 1.0f;
+            const float unit = kE4M3 ? fast_exp2(ref - m_used - 13.f) : 1.0f;  // (V is 2^6 and the weights are 2^7 as large)
             sStat[group * kTile + row] = w.piece >= 0 ? unit : unit / sum_l;
             mbar_arrive_warp(&bars->stat_full[group]);
             if (w.piece >= 0) {
@@ -861,7 +863,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             }
             const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
             if (token < w.tokens_of(tile))  // natural-log sum-exp of the scaled scores
-                a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = (m_used - (kE4M3 ? 7.f : 0.f) + log2f(sum_l)) * 0.6931471805599453f;
+                a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = (m_used + log2f(sum_l)) * 0.6931471805599453f;
         }
     }
 
@@ -908,7 +910,7 @@ __global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_consta
         pk.x = pack_bf16(o[0] * inv_l, o[1] * inv_l), pk.y = pack_bf16(o[2] * inv_l, o[3] * inv_l);
         pk.z = pack_bf16(o[4] * inv_l, o[5] * inv_l), pk.w = pack_bf16(o[6] * inv_l, o[7] * inv_l);
         reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD)[c] = pk;
-        if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m - (kE4M3 ? 7.f : 0.f) + log2f(l)) * 0.6931471805599453f;
+        if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
     }
 }
 

@@ -13,8 +13,9 @@
 //
 // Cached 8-bit floats become fp16, which has them all (one conversion for two values; as bf16 they take five instructions).  Q, in bf16, goes
 // to fp16 with a power of two that brings the unit's largest value near fp16's: nothing is lost of values within 2^-29 of it.  K's
-// power of two multiplies the scores.  V's multiplies the weights, relative to the largest V's of the warp so far, so that they stay in
-// fp16's range: with weights up to 2^15 for the largest, those down to 2^-29 of it have all 11 bits (bf16 has 8).
+// power of two multiplies the scores.  V's goes into the exponents of the weights: with x a score in units of log2 and 2^e V's power
+// the weight of the second product is 2^(x + e - r + 7), r a running maximum of x + e.  So the largest term has a weight of 2^7 or more, those
+// down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), and O is in units of 2^(r - 7); the sum of weights takes an exponential of its own.
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -78,7 +79,6 @@ template <int HD, bool kE4M3, int kRowTiles>
 __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_paged_split_kernel(const __grid_constant__ PagedSplitParams p) {
     using C = SplitCfg<HD, kE4M3>;
     constexpr int kRows = 8 * kRowTiles;     // of a unit
-    constexpr float kUp = kE4M3 ? 7.f : 0.f;  // weights are 2^kUp as large, see above
     extern __shared__ __align__(1024) uint8_t smem[];
     const PagedFwdParams& a = p.a;
     const int warps = p.warps, threads = 32 * warps;
@@ -204,7 +204,9 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     float m[kRowTiles][2], l[kRowTiles][2];  // running maximum in use and this thread's part of the sum, rows 2 t and 2 t + 1
 #pragma unroll
     for (int r = 0; r < kRowTiles; ++r) m[r][0] = m[r][1] = kLeast, l[r][0] = l[r][1] = 0.f;
-    int v_most = kExpLeast;  // the largest exponent of V so far (8 bits): O is in units of 2^v_most
+    float ref[kRowTiles][2];  // 8 bits: r, see above
+#pragma unroll
+    for (int r = 0; r < kRowTiles; ++r) ref[r][0] = ref[r][1] = kLeast;
     bool ok = true;
     int c = 0, st = 0, phase = 0;  // step, its stage, and which use of the stage it is (odd or even)
     for (; c < steps; ++c) {
@@ -247,23 +249,24 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             }
         }
         // Exponents of the step's keys (8 bits): lane i has those of key i, as what a score is multiplied with and as it is.
-        float k_scale = score_scale;
-        int v_exp = kExpLeast;
+        float k_scale = score_scale, v_exp = 0.f;
         bool grows = false;
         if constexpr (kE4M3) {
             k_scale *= exponent_factor(lds_s8(sE + lane));
-            v_exp = lds_s8(sE + C::kKeys + lane);
-            // (what lies there for keys past the end of the sequence can be anything: it must not set the scale)
-            if (masked && !any_attends(first_pos, last_pos, key0 + lane, a.window, a.sinks)) v_exp = kExpLeast;
-            grows = v_exp > v_most;
+            const int e = lds_s8(sE + C::kKeys + lane);
+            v_exp = e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : static_cast<float>(e);
         }
+        float v_exps[kTiles][2];
         // scores in units of log2: keys 16 u + g + 8 (x >> 1), rows 8 r + 2 t + (x & 1)
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
             float scale[2] = {k_scale, k_scale};
             if constexpr (kE4M3) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) scale[x] = __shfl_sync(0xffffffffu, k_scale, 16 * u + 8 * x + g);
+                for (int x = 0; x < 2; ++x) {
+                    scale[x] = __shfl_sync(0xffffffffu, k_scale, 16 * u + 8 * x + g);
+                    v_exps[u][x] = __shfl_sync(0xffffffffu, v_exp, 16 * u + 8 * x + g);
+                }
             }
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r)
@@ -272,15 +275,10 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                     sc[u][r][x] *= scale[x >> 1];
                     if (masked && !attends(pos[r][x & 1], key0 + 16 * u + 8 * (x >> 1) + g, a.window, a.sinks)) sc[u][r][x] = -INFINITY;
                     grows |= sc[u][r][x] > m[r][x & 1] + kLazy;
+                    if constexpr (kE4M3) grows |= sc[u][r][x] + v_exps[u][x >> 1] > ref[r][x & 1] + kLazy;
                 }
         }
         if (__any_sync(0xffffffffu, grows)) {
-            float v_down = 1.f;
-            if constexpr (kE4M3) {
-                const int most = max(v_most, __reduce_max_sync(0xffffffffu, v_exp));
-                v_down = power_of_two(max(v_most - most, -127));
-                v_most = most;
-            }
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r) {
                 float down[2];
@@ -294,30 +292,32 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                     down[h] = fast_exp2(m[r][h] - top);
                     m[r][h] = top;
                     l[r][h] *= down[h];
-                    down[h] *= v_down;
+                    if constexpr (kE4M3) {
+                        top = ref[r][h];
+#pragma unroll
+                        for (int u = 0; u < kTiles; ++u) top = fmax3(top, sc[u][r][h] + v_exps[u][0], sc[u][r][h + 2] + v_exps[u][1]);
+#pragma unroll
+                        for (int off = 4; off < 32; off *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                        down[h] = fast_exp2(ref[r][h] - top);
+                        ref[r][h] = top;
+                    }
                 }
 #pragma unroll
                 for (int x = 0; x < HD / 16; ++x) o[r][x][0] *= down[0], o[r][x][1] *= down[1], o[r][x][2] *= down[0], o[r][x][3] *= down[1];
             }
         }
-        float v_scale = 1.f;  // lane i's of key i
-        if constexpr (kE4M3) v_scale = v_exp == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(v_exp - v_most, -127));
         uint32_t w[kTiles][kRowTiles][2];  // weights of rows 8 r + g, keys 16 u + 2 t.. and 16 u + 8 + 2 t.. as pairs
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
-            float v_factor[2] = {1.f, 1.f};
-            if constexpr (kE4M3) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) v_factor[x] = __shfl_sync(0xffffffffu, v_scale, 16 * u + 8 * x + g);
-            }
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r) {
                 float e[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    e[x] = fast_exp2(sc[u][r][x] - (m[r][x & 1] - kUp));
+                    e[x] = fast_exp2(sc[u][r][x] - m[r][x & 1]);
                     l[r][x & 1] += e[x];
-                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : e[x] * v_factor[x >> 1];
+                    // (a key that is not attended can have any exponent, also that of a row that is not finite)
+                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : fast_exp2(sc[u][r][x] + v_exps[u][x >> 1] - (ref[r][x & 1] - 7.f));
                 }
                 w[u][r][0] = transpose_8x8(kE4M3 ? pack_f16(e[0], e[1]) : pack_bf16(e[0], e[1]));
                 w[u][r][1] = transpose_8x8(kE4M3 ? pack_f16(e[2], e[3]) : pack_bf16(e[2], e[3]));
@@ -369,30 +369,32 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         if (c + stages < steps) request(c + stages, st);
         if (++st == stages) st = 0, phase ^= 1;
     }
-    if (!ok && lane == 0)  // loads in flight land before the memory is used for something else
-        for (int x = c; x < steps && x < c + stages; ++x) {
+    if (lane == 0) {
+        // of a warp that gave up, loads in flight land before the memory is used for something else
+        for (int x = c; !ok && x < steps && x < c + stages; ++x) {
             mbar_wait_drain(&full[st], phase);
             if (++st == stages) st = 0, phase ^= 1;
         }
+    }
     __syncwarp();
 
     // ---- this warp's result into its ring: O of the rows, then m and l
     float* mine = reinterpret_cast<float*>(ring);
     constexpr int kM = kRows * HD, kL = kM + kRows, kJoined = kL + kRows;
     constexpr int kCols = kE4M3 ? HD / 8 : 8;  // columns of a thread that lie together
-    const float v_up = kE4M3 ? power_of_two(v_most) : 1.f;
 #pragma unroll
     for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row = 8 * r + 2 * t + h;
+            const float unit = kE4M3 ? fast_exp2(ref[r][h] - 7.f - m[r][h]) : 1.f;  // of O, beside the sum of weights
 #pragma unroll
             for (int off = 4; off < 32; off *= 2) l[r][h] += __shfl_xor_sync(0xffffffffu, l[r][h], off);
             if (g == 0) mine[kM + row] = m[r][h], mine[kL + row] = l[r][h];
 #pragma unroll
             for (int x = 0; x < HD / 16; ++x) {
                 float2* to = reinterpret_cast<float2*>(mine + row * HD + 2 * x / kCols * (8 * kCols) + kCols * g + 2 * x % kCols);
-                *to = make_float2(o[r][x][h] * v_up, o[r][x][h + 2] * v_up);
+                *to = make_float2(o[r][x][h] * unit, o[r][x][h + 2] * unit);
             }
         }
     __syncthreads();
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         const long long to = static_cast<long long>(s.row0 + i);
         if (abort_flag != 0) return;
         a.o[(to * a.H + h) * HD + col] = __float2bfloat16(value / sum);
-        if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top - kUp + log2f(sum)) * 0.6931471805599453f;
+        if (col == 0) a.lse[static_cast<long long>(h) * a.batch.T + to] = (top + log2f(sum)) * 0.6931471805599453f;
     };
     // ---- the warps' results joined, into the first ring
     const int ring_floats = ring_bytes / 4;

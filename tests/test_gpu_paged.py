@@ -77,20 +77,25 @@ class Job:
         o, lse = self.attend(scale=scale, window=window, sinks=sinks, o=mark, lse=torch.full((self.H, self.T), 7.0, device="cuda"), **kw)
         torch.cuda.synchronize()
         assert s2a.device_status() == (0, 0)
-        want, want_lse, size = ref.paged_fwd(self.q.cpu(), self.host_cache(), self.table.cpu(), self.starts.cpu(), self.lengths.cpu(), scale, window, sinks)
-        compare(o.cpu(), lse.cpu(), want, want_lse, size, self.rows(), max(length for _, length in self.sizes), self.d, scale,
+        want, want_lse, size, largest = ref.paged_fwd(self.q.cpu(), self.host_cache(), self.table.cpu(), self.starts.cpu(), self.lengths.cpu(), scale, window, sinks)
+        compare(o.cpu(), lse.cpu(), want, want_lse, size, largest, self.rows(), max(length for _, length in self.sizes), self.d, scale,
                 float(self.q.cpu()[self.rows()].double().norm(dim=-1).max()) if self.rows().any() else 0.0, self.all_k)
 
 
-def compare(o, lse, want, want_lse, size, inside, longest, d, scale, q_norm, k):
+def compare(o, lse, want, want_lse, size, largest, inside, longest, d, scale, q_norm, k):
     """Rows of no sequence untouched; the others as near as the roundings allow: weights and results to bf16 (half a step, 2^-8, each),
-    scores as sums of d products in 32 bits (each addition 2^-24 of a partial sum, that at most |q| |k|), sums over the keys likewise."""
+    scores as sums of d products in 32 bits (each addition 2^-24 of a partial sum, that at most |q| |k|), sums over the keys likewise.
+
+    Over a cache in 8 bits the weights are fp16 numbers, 2^7 as large relative to 2^r, where r is at most the largest log2(weight) + e of a block of
+    128 keys and 2^e the largest power of two of v there (`largest` = 2^r with normalised weights).  Below 2^-14 the step of fp16 is 2^-24, so each
+    weight, times 2^-e of its block, is off by up to 2^-25 * 2^-7 * 2^r; v times 2^-e is at most 448, and there are at most `longest` of them."""
     assert (o[~inside] == 7).all() and (lse[:, ~inside] == 7).all()
     o, want, size = o[inside].double(), want[inside], size[inside]
     score = d * 2.0**-24 * scale * q_norm * float(k.double().norm(dim=-1).max()) + 2.0**-20
     slack = longest * 2.0**-24
     off = (o - want).abs()
     allowed = (2.0**-8 + 2 * score + slack) * size + 2.0**-8 * (want.abs() + 2.0**-8 * size) + 1e-30
+    allowed += 2.0**-32 * 448 * longest * largest[inside][..., None]
     assert (off <= allowed).all(), float((off / allowed).max())
     off = (lse[:, inside].double() - want_lse[:, inside]).abs()
     assert (off <= score + slack + want_lse[:, inside].abs() * 2.0**-22).all(), float(off.max())
@@ -216,6 +221,117 @@ def test_a_long_sequence(new, dtype):
     Job([(new, 5000)], H=2, Hkv=1, d=64, page=64, dtype=dtype).check(window=3001, sinks=5)
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("form", [(71, 1, 64, 16), (96, 1, 128, 32), (22, 2, 64, 64)])
+def test_many_query_heads_of_a_kv_head(form, dtype):
+    H, Hkv, d, page = form
+    Job([(1, 200), (2, 5), (0, 3), (3, 131)], H=H, Hkv=Hkv, d=d, page=page, dtype=dtype, after=2).check()
+    Job([(1, 150)], H=H, Hkv=Hkv, d=d, page=page, dtype=dtype).check(max_new=1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_more_sequences_than_are_put_in_order(dtype):
+    sizes = [(n, n + 3 * b) for b, n in enumerate([40, 1, 0, 33, 70, 2, 65] * 10)]
+    Job(sizes, H=2, Hkv=1, d=64, dtype=dtype, before=3, after=1).check()
+    Job(sizes, H=2, Hkv=1, d=64, dtype=dtype).check(window=50, sinks=2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("sizes", [SINGLE, PIECES], ids=["single", "pieces"])
+def test_tokens_of_very_different_size(sizes, dtype):
+    """Keys and values whose rows differ by factors of up to 2^20: in 8 bits they have different powers of two."""
+    job = Job(sizes, H=4, Hkv=2, d=64, dtype=dtype)
+    g = torch.Generator().manual_seed(7)
+    for x in (job.all_k, job.all_v):
+        x.mul_(torch.exp2(torch.randint(-10, 11, (x.shape[0], x.shape[1], 1), generator=g).float()).cuda().to(BF16))
+    s2a.s2a_cache_write(job.cache, job.all_k, job.all_v, job.table, job.all_starts, job.lengths)
+    job.q *= 2.0**-6
+    job.check()
+    job.check(window=100, sinks=20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("new", [40, 130])
+def test_split_pieces_join_to_the_same_result(new, dtype):
+    """One sequence whose items are split over their keys if there is a workspace, whatever that holds."""
+    job = Job([(new, 3333)], H=4, Hkv=2, d=128, page=32, dtype=dtype, after=1)
+    rows = job.rows().cuda()
+    cache, batch = _structs(job)
+    need = s2a.load().s2a_paged_workspace_bytes(cache, batch, 4, new, 0, 0)
+    assert need > 0
+    job.check()
+    want = [t.clone() for t in job.attend()]
+    for bytes_, bits in ((need, True), (need + 1000, True), (need - 1, False), (0, False)):
+        ws = torch.full((bytes_,), 255, dtype=torch.uint8, device="cuda")
+        job.check(workspace=ws)
+        got = job.attend(workspace=ws)
+        assert not bits or (torch.equal(got[0][rows], want[0][rows]) and torch.equal(got[1][:, rows], want[1][:, rows]))
+
+
+def _structs(job):
+    """The two structs of include/s2a.h, as a program that calls the library through ctypes fills them in."""
+    import ctypes
+
+    class Cache(ctypes.Structure):
+        _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + [(n, ctypes.c_int) for n in ("type", "pages", "Hkv", "page_size", "d")]
+
+    class Batch(ctypes.Structure):
+        _fields_ = [(n, ctypes.c_void_p) for n in ("table", "starts", "lengths")] + [(n, ctypes.c_int) for n in ("width", "B", "T")]
+
+    c, e4m3 = job.cache, job.dtype == E4M3
+    cache = Cache(c.k.data_ptr(), c.v.data_ptr(), c.k_exp.data_ptr() if e4m3 else None, c.v_exp.data_ptr() if e4m3 else None, int(e4m3), *c.k.shape)
+    batch = Batch(*(t.data_ptr() for t in job.where), job.table.shape[1], len(job.sizes), job.T)
+    return ctypes.byref(cache), ctypes.byref(batch)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_the_library_is_called_directly(dtype):
+    for sizes in (SINGLE, PIECES):
+        job = Job(sizes, H=4, Hkv=2, d=64, dtype=dtype)
+        want = job.attend()
+        cache, batch = _structs(job)
+        got = torch.full_like(want[0], 7), torch.full_like(want[1], 7)
+        rc = s2a.load().s2a_paged_fwd(job.q.data_ptr(), cache, batch, got[0].data_ptr(), got[1].data_ptr(), 4, max(n for n, _ in sizes), 0.125, 0, 0, None, 0,
+                                      torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_pages_beyond_two_to_the_31_values(dtype):
+    """A pool of more than 2^32 values whose last pages are used: offsets pass 32 bits, row numbers do not."""
+    H, Hkv, d, page = 4, 2, 128, 128
+    small = Job([(1, 300), (150, 290), (2, 140)], H=H, Hkv=Hkv, d=d, page=page, dtype=dtype)
+    pages = (1 << 32) // (Hkv * page * d) + 40
+    big = s2a.PagedCache.empty(pages, Hkv, page, d, dtype)
+    assert big.k.numel() > 1 << 32
+    table = torch.arange(pages - 1, pages - 1 - small.table.numel(), -1, dtype=torch.int32, device="cuda").view(small.table.shape)
+    s2a.s2a_cache_write(big, small.all_k, small.all_v, table, small.all_starts, small.lengths)
+    for x in ("k", "v"):  # what the last pages hold past the ends
+        getattr(big, x)[pages - 1 - table.numel()].view(torch.uint8).fill_(255)
+    k, v = s2a.s2a_cache_read(big, table, small.all_starts, small.lengths, tokens=small.all_k.shape[0])
+    wk, wv = s2a.s2a_cache_read(small.cache, small.table, small.all_starts, small.lengths, tokens=small.all_k.shape[0])
+    assert torch.equal(k, wk) and torch.equal(v, wv)
+    want = small.attend()
+    got = s2a.s2a_paged_fwd(small.q, big, table, small.starts, small.lengths, max_new=150)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and s2a.device_status() == (0, 0)
+
+
+def test_a_nan_stays_in_its_sequence():
+    for sizes, dtype in ((SINGLE, BF16), (PIECES, BF16), (SINGLE, E4M3), (PIECES, E4M3)):
+        job = Job(sizes, H=4, Hkv=2, d=64, dtype=dtype)
+        want = [t.clone() for t in job.attend()]
+        b = len(sizes) - 2 if sizes[-1][0] == 0 else 1
+        n, length = sizes[b]
+        page, slot = int(job.table[b, (length - n) // job.page]), (length - n) % job.page
+        for x in (job.cache.k, job.cache.v):
+            x[page, :, slot].view(torch.uint8).fill_(255)
+        got = job.attend()
+        rows = torch.ones(job.T, dtype=torch.bool, device="cuda")
+        rows[int(job.starts[b]):int(job.starts[b + 1])] = False
+        assert torch.equal(got[0][rows], want[0][rows]) and torch.equal(got[1][:, rows], want[1][:, rows])
+        assert torch.isnan(got[0][~rows].float()).any()
+
+
 def test_a_loose_bound_on_the_new_tokens_changes_no_more_than_roundings():
     for sizes in (SINGLE, DRAFTS):
         job = Job(sizes, H=4, Hkv=2, d=128)
@@ -301,6 +417,77 @@ def test_a_captured_step_follows_the_lengths():
     assert s2a.device_status() == (0, 0)
 
 
+def test_a_captured_step_of_pieces_and_single_tokens():
+    """A server's step captured once, with room for 40 new tokens of each sequence; starts and lengths change between the replays."""
+    for B in (1, 3):
+        job = Job([(40, 2000)] * B, H=4, Hkv=2, d=64, dtype=E4M3)
+        T = job.T
+        k, v = (torch.randn(T, 2, 64, device="cuda").to(BF16) for _ in range(2))
+        o = torch.zeros_like(job.q)
+
+        def step():
+            s2a.s2a_cache_write(job.cache, k, v, *job.where)
+            return s2a.s2a_paged_fwd(job.q, job.cache, *job.where, max_new=40, o=o)
+
+        step()
+        torch.cuda.synchronize()
+        graphs = []
+        for _ in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1]):
+                got = step()
+        for new in ([40] * B, [1] * B, [0] * (B - 1) + [39]):
+            job.starts.copy_(torch.tensor([0] + [sum(new[:b + 1]) for b in range(B)], dtype=torch.int32))
+            job.lengths.copy_(torch.tensor([1500 + n for n in new], dtype=torch.int32))
+            job.q.normal_(), k.normal_(), v.normal_()
+            graphs[0].replay()
+            graphs[1].replay()
+            replayed, rows = got[0].clone(), sum(new)
+            want = step()
+            assert torch.equal(replayed[:rows], want[0][:rows])
+    assert s2a.device_status() == (0, 0)
+
+
+def test_calls_from_several_threads():
+    import threading
+
+    jobs = [(Job(sizes, H=4, Hkv=2, d=64, dtype=dtype, seed=seed), torch.cuda.Stream()) for seed, (sizes, dtype) in
+            enumerate([(SINGLE, BF16), (PIECES, E4M3), ([(130, 3000)], BF16), (DRAFTS, E4M3)])]
+    want = [[t.clone() for t in job.attend()] for job, _ in jobs]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(job, stream, want):
+        try:
+            rows = job.rows().cuda()
+            for _ in range(20):
+                o, lse = job.attend(stream=stream)
+                stream.synchronize()
+                failed.extend([1] if not (torch.equal(o[rows], want[0][rows]) and torch.equal(lse[:, rows], want[1][:, rows])) else [])
+        except Exception as e:  # noqa: BLE001 - reported below
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(job, stream, w)) for (job, stream), w in zip(jobs, want)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    assert not failed and s2a.device_status() == (0, 0)
+
+
+def test_an_expired_wait_stops_the_paged_calls_too():
+    job = Job(SINGLE, H=4, Hkv=2, d=64)
+    o = torch.full((job.T, 4, 64), 7.0, dtype=BF16, device="cuda")
+    s2a.selftest_wait_expiry(20_000_000)
+    job.attend(o=o)
+    torch.cuda.synchronize()
+    assert (o == 7).all()
+    with pytest.raises(s2a.S2AError) as e:
+        job.attend()
+    assert e.value.status == s2a.S2A_ERR_TIMEOUT and s2a.device_status()[0] == s2a.S2A_ERR_TIMEOUT
+    job.check()
+
+
 def test_another_stream():
     for sizes in (SINGLE, PIECES):
         job = Job(sizes, H=4, Hkv=2, d=64)
@@ -338,6 +525,11 @@ def test_refusals_reach_the_caller():
         s2a.s2a_paged_fwd(job.q.cpu(), job.cache, *job.where)
     with pytest.raises(ValueError, match="lse must have dtype"):
         job.attend(lse=torch.empty((4, 2), dtype=torch.float64, device="cuda"))
+    with pytest.raises(ValueError, match="workspace must have dtype"):
+        job.attend(workspace=torch.empty(100, device="cuda"))
+    with pytest.raises(s2a.S2AError) as e:
+        job.attend(workspace=torch.empty(1024, dtype=torch.uint8, device="cuda")[16:])
+    assert e.value.status == s2a.S2A_ERR_INVALID_ARG
     with pytest.raises(ValueError, match="tokens must be"):
         s2a.s2a_cache_read(job.cache, *job.where, tokens=-1)
     cache = s2a.PagedCache.empty(2, 2, 24, 64)

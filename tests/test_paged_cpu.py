@@ -59,7 +59,7 @@ def test_oracle_attends_like_one_softmax_over_the_whole_sequence():
         cache["v"][table[0, t // page], :, t % page] = v[t]
     starts, lengths = [1, 1 + n], [L]
     for window, sinks in ((0, 0), (7, 0), (7, 3), (100, 5), (1, 0)):
-        o, lse, size = ref.paged_fwd(torch.cat((q[:1], q[-n:], q[:1])), cache, table, starts, lengths, 0.3, window, sinks)
+        o, lse, size, _ = ref.paged_fwd(torch.cat((q[:1], q[-n:], q[:1])), cache, table, starts, lengths, 0.3, window, sinks)
         assert torch.isnan(o[0]).all() and torch.isnan(o[-1]).all() and torch.isnan(lse[:, 0]).all()
         i, j = torch.arange(L)[:, None], torch.arange(L)[None]
         mask = (j <= i) & ((i - j < window) | (j < sinks) if window else True)
