@@ -24,9 +24,9 @@
  *   - `stream` is a cudaStream_t passed as void* (NULL = legacy default stream).  Calls only enqueue
  *     work and return without synchronising.
  *   - Return value: S2A_OK (0) or a negative s2a_status.  Arguments are checked before anything is
- *     enqueued, so S2A_ERR_INVALID_ARG, S2A_ERR_UNSUPPORTED, S2A_ERR_TOO_LARGE and S2A_ERR_TIMEOUT mean
+ *     enqueued, so S2A_ERR_INVALID_ARG, S2A_ERR_UNSUPPORTED, S2A_ERR_TOO_LARGE, S2A_ERR_TIMEOUT and S2A_ERR_BAD_INDEX mean
  *     that nothing was enqueued.  S2A_ERR_CUDA means a CUDA call failed while enqueuing: an entry
- *     point that makes several launches or copies (s2a_bwd and its variants, s2a_fwd_bwd_host) may by
+ *     point that makes several launches or copies (s2a_bwd and its variants, s2a_paged_fwd, s2a_fwd_bwd_host) may by
  *     then have enqueued the earlier ones, so the outputs are unspecified; `stream` still covers
  *     everything that was enqueued (s2a_fwd_bwd_host joins its copy streams into it on every path).
  *   - Supported shapes: d in {64, 128}; N a multiple of G, N >= 128; G a multiple of 8 (so that every
@@ -52,6 +52,7 @@
  *     S2A_ERR_TIMEOUT instead (a host-side check of the copy; no synchronisation).  So a caller that
  *     sees S2A_ERR_TIMEOUT calls s2a_device_status(), discards the results since the last clean
  *     check, and goes on.
+ *     Values out of range that the kernels of the paged cache meet (below) are reported in the same way, as S2A_ERR_BAD_INDEX.
  *   - The first call on a device sets the library up for it (kernel attributes, the address of the
  *     status word, page-locking of a 4 KiB static status area); it allocates nothing, and should be
  *     made outside any stream capture.
@@ -253,8 +254,8 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
  * pages * Hkv * page_size must not exceed 2^31 - 1.
  *
  * A batch holds new tokens of B sequences.  Row starts[b] + i of its tensors is new token i of sequence b, which has
- * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows, and rows that belong to no sequence are neither read
- * nor written.  lengths[b] counts the tokens that sequence b has in the cache INCLUDING its new ones, so new token i is at
+ * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows.  Rows that belong to no sequence are left as they
+ * are in outputs, and what they hold in inputs does not matter.  lengths[b] counts the tokens that sequence b has in the cache INCLUDING its new ones, so new token i is at
  * position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
  * (j + 1) * page_size - 1; entries past a sequence's last page are not used.  Sequences may share pages, but not those that one call
  * writes to.
@@ -297,10 +298,11 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
  * cached tokens j <= p of its sequence, all of them (window = 0) or those with j > p - window or j < sinks.  Query head h reads KV head
  * floor(h / (H / Hkv)); H a multiple of Hkv.
  *   in : q [T, H, d] bf16        out: o [T, H, d] bf16, rounded once from fp32; lse [H, T] fp32, natural-log sum-exp of the scaled scores
+ * o must not overlap q.
  * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels, so a tight value is
  * fastest (1 where every sequence has one new token).
- * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 (to fp16 over an S2A_CACHE_E4M3 cache) before the second
- * product.  Cached values at positions that a token does not see are not assumed finite if they lie past the end of the sequence; a NaN
+ * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product (over an S2A_CACHE_E4M3 cache to
+ * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  Cached values at positions that a token does not see are not assumed finite if they lie past the end of the sequence; a NaN
  * or infinity at a position of the sequence itself can reach the outputs of the other new tokens of the same call and sequence.
  * Deterministic: no atomics.
  *   workspace: caller-owned device scratch, 256-byte aligned, or NULL.  Pieces of a prompt that do not fill the GPU evenly are split over

@@ -120,7 +120,7 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
 
 // The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.
 // A single tile's step of 128 keys takes as long as a pair's, so items are pairs unless the GPU can work on all single tiles at a time (1024
-// new tokens of 8192 on 32 heads, 128 pairs: 105 us, as 256 single tiles 201).  One sequence that has fewer items than the GPU works
+// new tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201).  One sequence that has fewer items than the GPU works
 // on at a time is split: each item into pieces of its keys, a step of which counts as one and the start and end of a piece as two.  (With
 // more items than that, splitting those of the last, partial wave brings nothing: with fewer multiprocessors busy those
 // run at a higher clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
@@ -220,42 +220,41 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
     const long long most_rows = static_cast<long long>(max_new) * (H / cache->Hkv);
     PagedFwdParams p = fwd_params(cache, batch, H, max_new, window, sinks);
-    window = p.window, sinks = p.sinks;
     p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     p.scale_log2 = scale * 1.4426950408889634f;
-    cudaError_t e;
-    if (p.few_rows > 0) {
-        PagedSplitParams ps;
-        memset(&ps, 0, sizeof ps);
+    // everything that can be refused comes before the first launch
+    const bool few = p.few_rows > 0, many = most_rows > kFewRows;
+    PagedSplitParams ps;
+    memset(&ps, 0, sizeof ps);
+    if (few) {
         ps.a = p;
         if ((rc = cache_tmap(&ps.tm_k, cache, cache->k, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         ps.unit_rows = most_rows <= 8 ? 8 : 16;
         ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + ps.unit_rows - 1) / ps.unit_rows;
         long long reach = longest;
-        if (window > 0 && reach > static_cast<long long>(window) + sinks + max_new) reach = static_cast<long long>(window) + sinks + max_new;
+        if (p.window > 0 && reach > static_cast<long long>(p.window) + p.sinks + max_new) reach = static_cast<long long>(p.window) + p.sinks + max_new;
         choose_pieces(&ps, ds, reach, 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
         if (static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
         ps.by_split = FastDiv(ps.split), ps.by_row_blocks = FastDiv(ps.row_blocks), ps.by_heads = FastDiv(cache->Hkv), ps.by_rep = FastDiv(p.rep);
-        e = launch_paged_split(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));
-        if (e != cudaSuccess) return cuda_fail(e);
     }
-    if (most_rows > kFewRows) {
-        PagedTileParams pt;
-        memset(&pt, 0, sizeof pt);
+    PagedTileParams pt;
+    memset(&pt, 0, sizeof pt);
+    if (many) {
         pt.a = p;
         if (!plan_tiles(&pt, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
-        pt.beside = p.few_rows > 0;
-        const size_t piece_bytes = paged_piece_bytes(cache->d), items = static_cast<size_t>(pt.slots) * (H >> pt.pack_log2);
-        if (!workspace || (items - pt.first_split) * pt.split * piece_bytes > workspace_bytes) pt.first_split = static_cast<int>(items), pt.split = 1;
+        pt.beside = few;
+        const size_t items = static_cast<size_t>(pt.slots) * (H >> pt.pack_log2);
+        if (!workspace || (items - pt.first_split) * pt.split * paged_piece_bytes(cache->d) > workspace_bytes) pt.first_split = static_cast<int>(items), pt.split = 1;
         pt.pieces = static_cast<float*>(workspace);
         pt.by_split = FastDiv(pt.split);
         if ((rc = tile_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
-        e = launch_paged_fwd(pt, e4m3, cache->d, static_cast<cudaStream_t>(stream));
-        if (e != cudaSuccess) return cuda_fail(e);
     }
-    return S2A_OK;
+    cudaError_t e = cudaSuccess;
+    if (few) e = launch_paged_split(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+    if (many && e == cudaSuccess) e = launch_paged_fwd(pt, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? S2A_OK : cuda_fail(e);
 }
 
 size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {

@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kCopyThreads) s2a_cache_copy_kernel(const __gr
 #pragma unroll
             for (int y = 0; y < C::kValues / 8; ++y) {
                 x[i][y] = make_uint4(0, 0, 0, 0);
-                if (kWrite && r < rows && t0 + token[i] < p.batch.T) x[i][y] = __ldcs(dense[i] + y);  // before it is known where they go
+                if (kWrite && r < rows && t0 + token[i] < p.batch.T) x[i][y] = __ldcg(dense[i] + y);  // before it is known where they go
             }
         }
         if (turn == 0) __syncthreads();  // s_row is there
@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(kCopyThreads) s2a_cache_copy_kernel(const __gr
             cached[i] = base < 0 ? nullptr : reinterpret_cast<Cached*>(static_cast<uint8_t*>(is_v ? p.pool.v : p.pool.k) + row * (HD * (kE4M3 ? 1 : 2))) + part;
             exponent[i] = kE4M3 ? (is_v ? p.pool.v_exp : p.pool.k_exp) + row : nullptr;
             if (!kWrite && cached[i]) {
-                code[i] = *cached[i];
-                if constexpr (kE4M3) e[i] = *exponent[i];
+                code[i] = __ldcg(cached[i]);
+                if constexpr (kE4M3) e[i] = __ldcg(reinterpret_cast<const signed char*>(exponent[i]));
             }
         }
 #pragma unroll

@@ -49,8 +49,9 @@ struct Sequence {
     int row0, n, length;  // first row, new tokens, tokens in the cache
 };
 
+// Kernels of this library can be resident before their predecessors are done (see launch_kernel), so what those may write is read from the L2.
 #if defined(__CUDA_ARCH__)
-#define S2A_LOAD(p) __ldg(p)
+#define S2A_LOAD(p) __ldcg(p)
 #else
 #define S2A_LOAD(p) (*(p))
 #endif

@@ -143,7 +143,7 @@ __device__ __forceinline__ bool whole_item(const PagedTileParams& p, int item, P
     const int group = p.by_slots(item, &slot);
     slot = p.slots - 1 - slot;
     const int b = find_slot(p.a.batch.starts, p.a.batch.B, p.span_log2, slot);
-    return item_at(p, group, b, static_cast<long long>(slot - first_slot(__ldg(p.a.batch.starts + b), b, p.span_log2)) << p.span_log2, w);
+    return item_at(p, group, b, static_cast<long long>(slot - first_slot(S2A_LOAD(p.a.batch.starts + b), b, p.span_log2)) << p.span_log2, w);
 }
 
 // Batches of 2 .. kRanked sequences: a warp knows how many items each has (of a head group) and puts them in order, those with most keys
@@ -878,7 +878,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
 }
 
 // Joins the pieces of the split items, one block for each tile.  A thread has eight columns of a row at a time.
-template <int HD, bool kE4M3>
+template <int HD>
 __global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_constant__ PagedTileParams p) {
     const PagedFwdParams& a = p.a;
     release_successor();
@@ -894,13 +894,13 @@ __global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_consta
         const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
         if (token >= w.tokens_of(t)) continue;
         float m = kLeast;
-        for (int y = 0; y < pieces; ++y) m = fmaxf(m, piece_result<HD>(p, x * p.split + y, t)[kTile * HD + row]);
+        for (int y = 0; y < pieces; ++y) m = fmaxf(m, __ldcg(piece_result<HD>(p, x * p.split + y, t) + kTile * HD + row));
         float l = 0.f, o[8] = {};
         for (int y = 0; y < pieces; ++y) {
             const float* from = piece_result<HD>(p, x * p.split + y, t);
-            const float f = fast_exp2(from[kTile * HD + row] - m);
-            l = fmaf(from[kTile * HD + kTile + row], f, l);
-            const float4 u = reinterpret_cast<const float4*>(from)[2 * c * kTile + row], v = reinterpret_cast<const float4*>(from)[(2 * c + 1) * kTile + row];
+            const float f = fast_exp2(__ldcg(from + kTile * HD + row) - m);
+            l = fmaf(__ldcg(from + kTile * HD + kTile + row), f, l);
+            const float4 u = __ldcg(reinterpret_cast<const float4*>(from) + 2 * c * kTile + row), v = __ldcg(reinterpret_cast<const float4*>(from) + (2 * c + 1) * kTile + row);
             o[0] = fmaf(u.x, f, o[0]), o[1] = fmaf(u.y, f, o[1]), o[2] = fmaf(u.z, f, o[2]), o[3] = fmaf(u.w, f, o[3]);
             o[4] = fmaf(v.x, f, o[4]), o[5] = fmaf(v.y, f, o[5]), o[6] = fmaf(v.z, f, o[6]), o[7] = fmaf(v.w, f, o[7]);
         }
@@ -939,7 +939,7 @@ static cudaError_t launch_one(const PagedTileParams& p, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>(p.first_split) + static_cast<unsigned>(split_items) * static_cast<unsigned>(p.split);
     const cudaError_t e = launch_kernel(s2a_paged_fwd_kernel<HD, kE4M3>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
     if (e != cudaSuccess || split_items == 0) return e;
-    return launch_kernel(s2a_paged_join_kernel<HD, kE4M3>, 2u * static_cast<unsigned>(split_items), 256, 0, stream, p, true);
+    return launch_kernel(s2a_paged_join_kernel<HD>, 2u * static_cast<unsigned>(split_items), 256, 0, stream, p, true);
 }
 
 cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream) {

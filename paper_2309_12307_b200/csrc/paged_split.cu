@@ -2,7 +2,7 @@
 //
 // A row is a new token and a query head; the rows of a sequence and KV head (new tokens times query heads of a KV head) read the
 // same keys.  With at most 64 of them the work is reading the cache: 4 d multiply-adds for each row and key against 4 d
-// bytes of bf16.  So the keys are split: a unit, 16 rows of one sequence and KV head, is worked on by a cluster of blocks, each
+// bytes of bf16.  So the keys are split: a unit, 8 or 16 rows of one sequence and KV head, is worked on by a cluster of blocks, each
 // with a share of the keys, its warps taking 16 or 32 keys in turn.  A warp has a ring of its own that TMA fills, a
 // running maximum and sum for its rows and the weighted sum of v in registers.  What the warps and then the blocks have is
 // joined through shared memory and the cluster's: no second launch, no workspace, no atomics.
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         const __nv_bfloat16* src = a.q + (static_cast<long long>(s.row0 + i) * a.H + hk * a.rep + hh) * HD + kPer * t;
 #pragma unroll
         for (int c = 0; c < HD / 32; ++c) {
-            const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * c + (c * 8 / kPer) * (64 - kPer) * (kE4M3 ? 0 : 1));
+            const uint4 w = __ldcg(reinterpret_cast<const uint4*>(src + 8 * c + (c * 8 / kPer) * (64 - kPer) * (kE4M3 ? 0 : 1)));
             q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
         }
     }
