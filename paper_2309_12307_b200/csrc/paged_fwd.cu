@@ -53,7 +53,9 @@ struct PagedCfg {
     static constexpr int kScoreBufs = (HD == 128) ? 1 : 2;
     static_assert(kColS + kScoreBufs * kTile <= kTmemCols, "tensor memory");
     // registers per thread after the split; the launch gives kRegsLaunch to each of the 512
-    static constexpr int kRegsLaunch = 128, kRegsSoftmax = 192, kRegsReadOut = 80, kRegsIssue = 48;
+    // (the softmax, whose rows are in registers, can spare some for the warps that turn codes into operands: 32k tokens in 8 bits with 192, 80 and
+    // 48 2170 us, with 184, 88 and 56 2068, with these 2046)
+    static constexpr int kRegsLaunch = 128, kRegsSoftmax = kE4M3 && HD == 128 ? 176 : 184, kRegsReadOut = kE4M3 && HD == 128 ? 104 : 88, kRegsIssue = 56;
     static_assert(2 * kRegsSoftmax + kRegsReadOut + kRegsIssue <= 4 * kRegsLaunch, "register split");
 };
 
@@ -343,12 +345,17 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 }
                 __syncwarp();
             };
-            // pool row (in head hk) of the piece of key tile `tile` that is this lane's, -1: none
-            auto look_up = [&](const PagedItem& w, int hk, int length, int tile) {
+            // The table's entry for the piece of key tile `tile` that is this lane's.  (Every lane has one, and it is looked at when it is used, one
+            // tile later: its latency is then nobody's.)
+            auto look_up = [&](const int* table, int length, int tile) {
+                const int key = tile * kTile + (lane << piece_log2);
+                return S2A_LOAD(table + ((key < length ? key : length - 1) >> a.pool.page_log2));
+            };
+            // Pool row (in head hk) of that piece, -1: none.
+            auto piece_row = [&](int page, int hk, int length, int tile) {
                 const int key = tile * kTile + (lane << piece_log2);
                 if (lane >= kTile >> piece_log2 || key >= length) return -1;
-                const int page = page_of(a.batch, a.pool.pages, w.b, key >> a.pool.page_log2);
-                if (page < 0) {
+                if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.pool.pages)) {
                     report_bad_index(a.status, a.host_status, kBadPage);
                     return -1;
                 }
@@ -404,29 +411,19 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 __syncwarp();
                 if (id < 0) break;
                 const int hk = p.by_groups_of_kv(w.group), length = w.pos + w.tokens[1];  // (keys behind the last token are nobody's)
-                int row = look_up(w, hk, length, w.key_tile(0));
-                if constexpr (kE4M3) {  // in the order of TileOfItem
-                    int next = w.n[1] > 1 ? look_up(w, hk, length, w.key_tile(1)) : -1;
-                    load_kv(row, true);
-                    if (ok) load_q(w, 1, g1);
-                    if (ok && w.n[0] > 0) load_q(w, 0, g0);
-                    for (int j = 1; ok && j < w.n[1]; ++j) {
-                        const int before = row;
-                        row = next;
-                        next = j + 1 < w.n[1] ? look_up(w, hk, length, w.key_tile(j + 1)) : -1;
-                        load_kv(row, true);
-                        if (ok) load_kv(before, false);
-                    }
-                    if (ok) load_kv(row, false);
-                }
-                for (int j = 0; !kE4M3 && ok && j < w.n[1]; ++j) {
-                    const int next = j + 1 < w.n[1] ? look_up(w, hk, length, w.key_tile(j + 1)) : -1;
+                const int* table = a.batch.table + static_cast<long long>(w.b) * a.batch.width;
+                int row = -1, page = look_up(table, length, w.key_tile(0));
+                for (int j = 0; ok && j < w.n[1]; ++j) {
+                    const int before = row;
+                    row = piece_row(page, hk, length, w.key_tile(j));
+                    page = look_up(table, length, w.key_tile(j + 1 < w.n[1] ? j + 1 : j));
                     load_kv(row, true);
                     if (j == 0 && ok) load_q(w, 1, g1);
                     if (j == 0 && ok && w.n[0] > 0) load_q(w, 0, g0);
-                    if (ok) load_kv(row, false);
-                    row = next;
+                    // (8 bits: in the order of TileOfItem)
+                    if (ok && (!kE4M3 || j > 0)) load_kv(kE4M3 ? before : row, false);
                 }
+                if (kE4M3 && ok) load_kv(row, false);
                 if (ok) id = next_id();
             }
             // nothing may land after the block has gone
