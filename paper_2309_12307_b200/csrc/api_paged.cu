@@ -78,6 +78,12 @@ int tile_tmaps(PagedTileParams* p, const s2a_cache* c, const void* q, int H, int
     return rc != S2A_OK ? rc : encode_tmap(&p->tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->v, 2, dims, &row_bytes, box);
 }
 
+// Keys that `tokens` tokens of a sequence together attend at most, of `longest`.
+long long reach_of(const PagedFwdParams& a, long long longest, int tokens) {
+    const long long most = static_cast<long long>(a.window) + a.sinks + tokens;
+    return a.window > 0 && most < longest ? most : longest;
+}
+
 // How the keys of the units (8 or 16 rows of a sequence and KV head) are dealt out: blocks of `warps` warps, `split` of them in a cluster
 // for each unit, whatever should be done first by this estimate, in microseconds.
 //   - All units' bytes at the memory's rate.  A batch's sequences differ in length: the average is taken as 0.7 of the longest.
@@ -120,8 +126,8 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
 
 // The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.
 // A single tile's step of 128 keys takes as long as a pair's, so items are pairs unless the GPU can work on all single tiles at a time (1024
-// new tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201).  One sequence that has fewer items than the GPU works
-// on at a time is split: each item into pieces of its keys, a step of which counts as one and the start and end of a piece as two.  (With
+// new tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201).  Batches that have fewer items than the GPU works on
+// at a time are split: each item into pieces of its keys, a step of which counts as one and the start and end of a piece as two.  (With
 // more items than that, splitting those of the last, partial wave brings nothing: with fewer multiprocessors busy those
 // run at a higher clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
 bool plan_tiles(PagedTileParams* p, int n_sm, long long longest) {
@@ -137,10 +143,8 @@ bool plan_tiles(PagedTileParams* p, int n_sm, long long longest) {
     if (items * kMostSplit > 0x7fffffffLL) return false;
     p->ranked = a.batch.B > 1 && a.batch.B <= kMostRanked;
     p->first_split = static_cast<int>(items), p->split = 1;
-    if (a.batch.B == 1 && items < n_sm) {
-        long long keys = longest;
-        if (a.window > 0 && keys > static_cast<long long>(a.window) + a.sinks + (1 << p->span_log2)) keys = static_cast<long long>(a.window) + a.sinks + (1 << p->span_log2);
-        const double tiles = static_cast<double>(keys + kTile - 1) / kTile;
+    if (a.batch.B <= kMostRanked && items < n_sm) {
+        const double tiles = static_cast<double>(reach_of(a, longest, 1 << p->span_log2) + kTile - 1) / kTile;
         double best = 0.9 * tiles - 6;  // (the second launch)
         for (int split = 2; split <= kMostSplit && 4 * split <= tiles; ++split) {
             const double t = static_cast<double>((items * split + n_sm - 1) / n_sm) * (tiles / split + 2);
@@ -156,6 +160,26 @@ int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_n
     return static_cast<long long>(batch->T) * H > kIntMax ? S2A_ERR_UNSUPPORTED : S2A_OK;
 }
 
+// Up to how many rows (new tokens times query heads of a KV head) a sequence is the splitting kernel's.  Each 16 rows of a sequence
+// read its keys again there, and make legacy tensor products of them; the tiling kernel does all 128 rows of a tile at once, but starts and
+// joins more slowly and has fewer loads in flight.  Up to 16 rows are always the former's and more than 64 never.  Between them the tiling kernel
+// takes batches with many keys to read: `visits`, of a key by 16 rows.  Measured, in us, splitting and tiling kernel, heads of 128:
+//   - one sequence, 8 KV heads, 32 rows: 32k 77 and 108, 100,000 159 and 130 (8 bits 157 and 156); 64 rows: 1000 17 and 22, 4000 26 and 46, 32k 107
+//     and 98; 32 KV heads, 20 rows: 8192 55 and 56, 32k 175 and 151 (8 bits 139 and 175)
+//   - 4 sequences: 8 KV heads, 64 rows, 1000 28 and 25; 32 KV heads, 40 rows, 8192 218 and 107 (8 bits 217 and 140); 16 sequences, 8 KV heads, 32 rows:
+//     2000 77 and 44, 8000 148 and 104; 64 rows: 2000 104 and 45; 32 of 4096, 64 rows, 271 and 117; 8 of 32k, 32 rows, 311 and 217 (8 bits 289 and 273)
+//   - heads of 64: 4 sequences of 1000, 8 KV heads, 24 rows 14 and 26; 32 of 4096 103 and 107; 64 of 2000, 20 rows, 105 and 119.
+// Several sequences are different: of the splitting kernel's clusters more than the GPU runs at a time wait for one another.
+int few_rows(long long most_rows, long long reach, int B, int Hkv, int d, bool e4m3) {
+    if (most_rows <= 16) return 16;
+    const long long blocks = most_rows < kFewRows ? (most_rows + 15) / 16 : kFewRows / 16;
+    const double visits = static_cast<double>(B) * Hkv * blocks * reach * (d / 128.0);
+    const bool many_keys = visits >= (B > 1 ? 1.0 : e4m3 ? 16.0 : 4.0) * (1 << 18);
+    if (B > 1) return many_keys ? 16 : kFewRows;
+    // one sequence: without a second launch, however few rows it turns out to have
+    return many_keys || most_rows > kFewRows ? 0 : kFewRows;
+}
+
 // What a call's sizes say; its pointers and the scale are still missing.
 PagedFwdParams fwd_params(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
     PagedFwdParams p;
@@ -164,9 +188,7 @@ PagedFwdParams fwd_params(const s2a_cache* cache, const s2a_batch* batch, int H,
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
     p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new;
     p.window = window >= longest ? 0 : window, p.sinks = sinks > longest ? longest : sinks;
-    // Sequences with few rows are the splitting kernel's, the others the other one's.  A batch of one sequence that may have many is
-    // the latter's without a second launch, however many it turns out to have.
-    p.few_rows = static_cast<long long>(max_new) * p.rep > kFewRows && batch->B == 1 ? 0 : kFewRows;
+    p.few_rows = few_rows(static_cast<long long>(max_new) * p.rep, reach_of(p, longest, max_new), batch->B, cache->Hkv, cache->d, cache->type == S2A_CACHE_E4M3);
     return p;
 }
 
@@ -224,7 +246,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     p.scale_log2 = scale * 1.4426950408889634f;
     // everything that can be refused comes before the first launch
-    const bool few = p.few_rows > 0, many = most_rows > kFewRows;
+    const bool few = p.few_rows > 0, many = most_rows > p.few_rows;
     PagedSplitParams ps;
     memset(&ps, 0, sizeof ps);
     if (few) {
@@ -232,10 +254,8 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         if ((rc = cache_tmap(&ps.tm_k, cache, cache->k, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         ps.unit_rows = most_rows <= 8 ? 8 : 16;
-        ps.row_blocks = static_cast<int>((most_rows < kFewRows ? most_rows : kFewRows) + ps.unit_rows - 1) / ps.unit_rows;
-        long long reach = longest;
-        if (p.window > 0 && reach > static_cast<long long>(p.window) + p.sinks + max_new) reach = static_cast<long long>(p.window) + p.sinks + max_new;
-        choose_pieces(&ps, ds, reach, 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
+        ps.row_blocks = static_cast<int>((most_rows < p.few_rows ? most_rows : p.few_rows) + ps.unit_rows - 1) / ps.unit_rows;
+        choose_pieces(&ps, ds, reach_of(p, longest, max_new), 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
         if (static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
         ps.by_split = FastDiv(ps.split), ps.by_row_blocks = FastDiv(ps.row_blocks), ps.by_heads = FastDiv(cache->Hkv), ps.by_rep = FastDiv(p.rep);
     }
@@ -260,10 +280,10 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
 size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
     DeviceState* ds = nullptr;
     if (check_cache(cache) != S2A_OK || check_batch(batch, cache) != S2A_OK || check_heads(cache, batch, H, max_new, window, sinks) != S2A_OK) return 0;
-    if (static_cast<long long>(max_new) * (H / cache->Hkv) <= kFewRows || prepare_device(&ds) != S2A_OK) return 0;
     PagedTileParams p;
     memset(&p, 0, sizeof p);
     p.a = fwd_params(cache, batch, H, max_new, window, sinks);
+    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_device(&ds) != S2A_OK) return 0;
     if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size)) return 0;
     return (static_cast<size_t>(p.slots) * (H >> p.pack_log2) - p.first_split) * p.split * paged_piece_bytes(cache->d);
 }

@@ -139,7 +139,7 @@ __host__ __device__ inline bool all_attend(int first, int last, int j, int n, in
     return j + n - 1 <= first && (window == 0 || j > last - window || j + n <= sinks);
 }
 
-// Rows (new tokens times query heads of a KV head) up to which a sequence is worked on by the kernel that splits its keys.
+// Rows (new tokens times query heads of a KV head) up to which a sequence may be worked on by the kernel that splits its keys.
 constexpr int kFewRows = 64;
 
 // What both attention kernels take.
@@ -196,7 +196,7 @@ struct alignas(64) PagedTileParams {
     bool ranked;             // the items' order follows the sequences' lengths, see Ranking
     bool beside;             // launched behind the splitting kernel of the same call
     int slots;               // of a head group: slot_count()
-    // Items from first_split on are split (batches of one sequence only): `split` pieces of their keys each, which leave their results in `pieces`.
+    // Items from first_split on are split: `split` pieces of their keys each, which leave their results in `pieces`.
     int first_split, split;
     float* pieces;
     FastDiv by_split, by_slots, by_groups, by_groups_of_kv;  // head groups, and those of a KV head: rep / pack

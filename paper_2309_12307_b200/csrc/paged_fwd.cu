@@ -196,13 +196,17 @@ struct Ranking {
 // Key tiles of a piece of a split item (the last piece has fewer, or there are fewer pieces).
 __device__ __forceinline__ int piece_tiles(const PagedTileParams& p, const PagedItem& whole) { return (whole.n[1] + p.split - 1) / p.split; }
 
+// Item `item` as a whole, by a whole warp.
+__device__ __forceinline__ bool any_item(const PagedTileParams& p, const Ranking& ranking, int item, PagedItem* w) {
+    return p.ranked ? ranking.item(p, item, w) : whole_item(p, item, w);
+}
+
 // Work item `id`, by a whole warp: the items before first_split, then the pieces of the others.
 __device__ __forceinline__ bool paged_item(const PagedTileParams& p, const Ranking& ranking, int id, PagedItem* w) {
-    if (p.ranked) return ranking.item(p, id, w);
-    if (id < p.first_split) return whole_item(p, id, w);
+    if (id < p.first_split) return any_item(p, ranking, id, w);
     const int piece = id - p.first_split;
     int part;
-    if (!whole_item(p, p.first_split + p.by_split(piece, &part), w)) return false;
+    if (!any_item(p, ranking, p.first_split + p.by_split(piece, &part), w)) return false;
     const int tiles = piece_tiles(p, *w), j0 = part * tiles;
     if (j0 >= w->n[1]) return false;
     w->j0 = j0, w->piece = piece;
@@ -883,7 +887,9 @@ __global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_consta
     if (*reinterpret_cast<volatile int*>(a.status) != 0) return;
     PagedItem w;
     const int x = static_cast<int>(blockIdx.x) >> 1, t = static_cast<int>(blockIdx.x) & 1;
-    if (!whole_item(p, p.first_split + x, &w)) return;
+    Ranking ranking;
+    if (p.ranked) ranking.set(p);  // (every warp for itself)
+    if (!any_item(p, ranking, p.first_split + x, &w)) return;
     const int tiles = piece_tiles(p, w), n = t ? w.n[1] : w.n[0], pieces = (n + tiles - 1) / tiles;
     if (pieces == 0) return;
     for (int i = threadIdx.x; i < kTile * (HD / 8); i += 256) {

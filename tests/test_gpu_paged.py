@@ -222,6 +222,23 @@ def test_a_long_sequence(new, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("wider", [0, 4000], ids=["narrow", "wide"])  # which kernel has 17 to 64 rows goes by what the table can hold
+@pytest.mark.parametrize("sizes", [
+    [(4, 700), (1, 900), (0, 300), (2, 2), (16, 1500), (9, 40), (0, 0)],
+    [(16, 2100)],
+    [(1, 2100)],
+    [(5, 600), (40, 1700), (3, 1), (1, 1), (5, 5), (129, 400)],
+], ids=["drafts", "one", "one token", "mixed"])
+@pytest.mark.parametrize("d,window,sinks", [(128, 0, 0), (64, 0, 0), (128, 300, 4)])
+def test_between_few_and_many_rows(sizes, wider, d, window, sinks, dtype):
+    sizes = [(min(n, length), length) for n, length in sizes]
+    job = Job(sizes, H=32, Hkv=8, d=d, page=64, dtype=dtype, before=1, after=2, wider=wider)
+    job.check(window=window, sinks=sinks)
+    # a bound that more sequences might reach: other kernels, the same results
+    job.check(window=window, sinks=sinks, max_new=min(job.T, max(n for n, _ in sizes) + 3))
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("form", [(71, 1, 64, 16), (96, 1, 128, 32), (22, 2, 64, 64)])
 def test_many_query_heads_of_a_kv_head(form, dtype):
     H, Hkv, d, page = form
