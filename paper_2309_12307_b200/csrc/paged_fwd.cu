@@ -878,43 +878,50 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
     }
 }
 
-// Joins the pieces of the split items, one block for each tile.  A thread has eight columns of a row at a time.
+// Joins the pieces of the split items.  A thread has eight columns of a row, a block 16 columns of a tile: with a block for each tile the few
+// items that are split left most of the GPU idle here (4000 keys, 64 rows of 8 KV heads: JOINA and JOINB us for both kernels).
 template <int HD>
-__global__ void __launch_bounds__(256) s2a_paged_join_kernel(const __grid_constant__ PagedTileParams p) {
+struct JoinCfg {
+    static constexpr int kThreads = 256;
+    static constexpr int kBlocks = kTile * (HD / 8) / kThreads;  // for each tile
+};
+template <int HD>
+__global__ void __launch_bounds__(JoinCfg<HD>::kThreads) s2a_paged_join_kernel(const __grid_constant__ PagedTileParams p) {
     const PagedFwdParams& a = p.a;
     release_successor();
     wait_for_predecessor();
     if (*reinterpret_cast<volatile int*>(a.status) != 0) return;
     PagedItem w;
-    const int x = static_cast<int>(blockIdx.x) >> 1, t = static_cast<int>(blockIdx.x) & 1;
+    const int tile = static_cast<int>(blockIdx.x) / JoinCfg<HD>::kBlocks, x = tile >> 1, t = tile & 1;
     Ranking ranking;
     if (p.ranked) ranking.set(p);  // (every warp for itself)
     if (!any_item(p, ranking, p.first_split + x, &w)) return;
     const int tiles = piece_tiles(p, w), n = t ? w.n[1] : w.n[0], pieces = (n + tiles - 1) / tiles;
     if (pieces == 0) return;
-    for (int i = threadIdx.x; i < kTile * (HD / 8); i += 256) {
-        const int row = i % kTile, c = i / kTile;
-        const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
-        if (token >= w.tokens_of(t)) continue;
-        float m = kLeast;
-        for (int y = 0; y < pieces; ++y) m = fmaxf(m, __ldcg(piece_result<HD>(p, x * p.split + y, t) + kTile * HD + row));
-        float l = 0.f, o[8] = {};
-        for (int y = 0; y < pieces; ++y) {
-            const float* from = piece_result<HD>(p, x * p.split + y, t);
-            const float f = fast_exp2(__ldcg(from + kTile * HD + row) - m);
-            l = fmaf(__ldcg(from + kTile * HD + kTile + row), f, l);
-            const float4 u = __ldcg(reinterpret_cast<const float4*>(from) + 2 * c * kTile + row), v = __ldcg(reinterpret_cast<const float4*>(from) + (2 * c + 1) * kTile + row);
-            o[0] = fmaf(u.x, f, o[0]), o[1] = fmaf(u.y, f, o[1]), o[2] = fmaf(u.z, f, o[2]), o[3] = fmaf(u.w, f, o[3]);
-            o[4] = fmaf(v.x, f, o[4]), o[5] = fmaf(v.y, f, o[5]), o[6] = fmaf(v.z, f, o[6]), o[7] = fmaf(v.w, f, o[7]);
-        }
-        const float inv_l = 1.0f / l;
-        const long long at = w.row_of(t) + token;
-        uint4 pk;
-        pk.x = pack_bf16(o[0] * inv_l, o[1] * inv_l), pk.y = pack_bf16(o[2] * inv_l, o[3] * inv_l);
-        pk.z = pack_bf16(o[4] * inv_l, o[5] * inv_l), pk.w = pack_bf16(o[6] * inv_l, o[7] * inv_l);
-        reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD)[c] = pk;
-        if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
+    const int i = static_cast<int>(blockIdx.x) % JoinCfg<HD>::kBlocks * JoinCfg<HD>::kThreads + static_cast<int>(threadIdx.x);
+    const int row = i % kTile, c = i / kTile;
+    const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
+    if (token >= w.tokens_of(t)) return;
+    float m = kLeast;
+#pragma unroll 4
+    for (int y = 0; y < pieces; ++y) m = fmaxf(m, __ldcg(piece_result<HD>(p, x * p.split + y, t) + kTile * HD + row));
+    float l = 0.f, o[8] = {};
+#pragma unroll 4
+    for (int y = 0; y < pieces; ++y) {
+        const float* from = piece_result<HD>(p, x * p.split + y, t);
+        const float f = fast_exp2(__ldcg(from + kTile * HD + row) - m);
+        l = fmaf(__ldcg(from + kTile * HD + kTile + row), f, l);
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(from) + 2 * c * kTile + row), v = __ldcg(reinterpret_cast<const float4*>(from) + (2 * c + 1) * kTile + row);
+        o[0] = fmaf(u.x, f, o[0]), o[1] = fmaf(u.y, f, o[1]), o[2] = fmaf(u.z, f, o[2]), o[3] = fmaf(u.w, f, o[3]);
+        o[4] = fmaf(v.x, f, o[4]), o[5] = fmaf(v.y, f, o[5]), o[6] = fmaf(v.z, f, o[6]), o[7] = fmaf(v.w, f, o[7]);
     }
+    const float inv_l = 1.0f / l;
+    const long long at = w.row_of(t) + token;
+    uint4 pk;
+    pk.x = pack_bf16(o[0] * inv_l, o[1] * inv_l), pk.y = pack_bf16(o[2] * inv_l, o[3] * inv_l);
+    pk.z = pack_bf16(o[4] * inv_l, o[5] * inv_l), pk.w = pack_bf16(o[6] * inv_l, o[7] * inv_l);
+    reinterpret_cast<uint4*>(a.o + (at * a.H + head) * HD)[c] = pk;
+    if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <int HD, bool kE4M3>
@@ -942,7 +949,7 @@ static cudaError_t launch_one(const PagedTileParams& p, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>(p.first_split) + static_cast<unsigned>(split_items) * static_cast<unsigned>(p.split);
     const cudaError_t e = launch_kernel(s2a_paged_fwd_kernel<HD, kE4M3>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
     if (e != cudaSuccess || split_items == 0) return e;
-    return launch_kernel(s2a_paged_join_kernel<HD>, 2u * static_cast<unsigned>(split_items), 256, 0, stream, p, true);
+    return launch_kernel(s2a_paged_join_kernel<HD>, 2u * JoinCfg<HD>::kBlocks * static_cast<unsigned>(split_items), JoinCfg<HD>::kThreads, 0, stream, p, true);
 }
 
 cudaError_t launch_paged_fwd(const PagedTileParams& p, bool e4m3, int d, cudaStream_t stream) {
