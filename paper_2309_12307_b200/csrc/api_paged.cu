@@ -127,10 +127,11 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
 // The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.
 // A single tile's step of 128 keys takes as long as a pair's, so items are pairs unless the GPU can work on all single tiles at a time (1024
 // new tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201).  Batches that have fewer items than the GPU works on
-// at a time are split: each item into pieces of its keys, a step of which counts as one and the start and end of a piece as two.  (With
+// at a time are split: each item into pieces of its keys, a step of which counts as one, the start and end of a piece as two, joining
+// it as a quarter and the second launch as three (8 KV heads of 128 and one sequence, splits of 1 to 16 by this and by nearby rules within 10 %).  With
 // more items than that, splitting those of the last, partial wave brings nothing: with fewer multiprocessors busy those
-// run at a higher clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
-bool plan_tiles(PagedTileParams* p, int n_sm, long long longest) {
+// run at a higher clock.  (2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
+bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d) {
     const PagedFwdParams& a = p->a;
     p->pack_log2 = 0;
     while (p->pack_log2 < 6 && a.rep % (2 << p->pack_log2) == 0) ++p->pack_log2;
@@ -144,10 +145,10 @@ bool plan_tiles(PagedTileParams* p, int n_sm, long long longest) {
     p->ranked = a.batch.B > 1 && a.batch.B <= kMostRanked;
     p->first_split = static_cast<int>(items), p->split = 1;
     if (a.batch.B <= kMostRanked && items < n_sm) {
-        const double tiles = static_cast<double>(reach_of(a, longest, 1 << p->span_log2) + kTile - 1) / kTile;
-        double best = 0.9 * tiles - 6;  // (the second launch)
-        for (int split = 2; split <= kMostSplit && 4 * split <= tiles; ++split) {
-            const double t = static_cast<double>((items * split + n_sm - 1) / n_sm) * (tiles / split + 2);
+        const int tiles = static_cast<int>((reach_of(a, longest, 1 << p->span_log2) + kTile - 1) / kTile);
+        double best = tiles - 3;
+        for (int split = 2; split <= kMostSplit && split <= tiles; ++split) {
+            const double t = static_cast<double>((items * split + n_sm - 1) / n_sm) * ((tiles + split - 1) / split + 2) + 0.25 * split * d / 128;
             if (t < best) best = t, p->split = split, p->first_split = 0;
         }
     }
@@ -162,22 +163,22 @@ int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_n
 
 // Up to how many rows (new tokens times query heads of a KV head) a sequence is the splitting kernel's.  Each 16 rows of a sequence
 // read its keys again there, and make legacy tensor products of them; the tiling kernel does all 128 rows of a tile at once, but starts and
-// joins more slowly and has fewer loads in flight.  Up to 16 rows are always the former's and more than 64 never.  Between them the tiling kernel
-// takes batches with many keys to read: `visits`, of a key by 16 rows.  Measured, in us, splitting and tiling kernel, heads of 128:
-//   - one sequence, 8 KV heads, 32 rows: 32k 77 and 108, 100,000 159 and 130 (8 bits 157 and 156); 64 rows: 1000 17 and 22, 4000 26 and 46, 32k 107
-//     and 98; 32 KV heads, 20 rows: 8192 55 and 56, 32k 175 and 151 (8 bits 139 and 175)
-//   - 4 sequences: 8 KV heads, 64 rows, 1000 28 and 25; 32 KV heads, 40 rows, 8192 218 and 107 (8 bits 217 and 140); 16 sequences, 8 KV heads, 32 rows:
-//     2000 77 and 44, 8000 148 and 104; 64 rows: 2000 104 and 45; 32 of 4096, 64 rows, 271 and 117; 8 of 32k, 32 rows, 311 and 217 (8 bits 289 and 273)
-//   - heads of 64: 4 sequences of 1000, 8 KV heads, 24 rows 14 and 26; 32 of 4096 103 and 107; 64 of 2000, 20 rows, 105 and 119.
-// Several sequences are different: of the splitting kernel's clusters more than the GPU runs at a time wait for one another.
-int few_rows(long long most_rows, long long reach, int B, int Hkv, int d, bool e4m3) {
+// joins more slowly.  Up to 16 rows are the former's and more than 64 never.  Between them the tiling kernel takes batches with many keys to
+// read: `visits`, of a key by 16 rows of an average sequence.  Measured, in us, splitting and tiling kernel, heads of 128:
+//   - one sequence, 8 KV heads: 32 rows, 1000 15 and 21, 8000 26 and 24 (8 bits 26 and 28), 16,000 40 and 31, 32k 63 and 48, 100,000 160 and 87 (8 bits 157 and
+//     111); 64 rows, 1000 16 and 21, 4000 25 and 21; 32 KV heads, 8192, in 8 bits: 20 rows 49 and 52, 40 rows 64 and 52
+//   - several, 8 KV heads: 32 rows, 2 x 2000 20 and 23, 4 x 4000 31 and 33 (8 bits 34 and 38), 2 x 8000 in 8 bits 55 and 37, 16 x 2000 77 and 37; 64 rows, 4 x 1000
+//     26 and 22, 4 x 4000 70 and 36
+//   - heads of 64: 4 x 1000, 24 rows 13 and 22, 32 x 4000 104 and 97, 2 x 32,000, 20 rows 70 and 57
+//   - 6 x 16,700, 1 to 20 rows, 10 on average, in 8 bits 146 and 187.
+// With both kernels a call takes 5 to 8 us longer, so where no sequence has more than 64 rows the tiling kernel takes them all.
+int few_rows(long long most_rows, long long all_rows, long long reach, int B, int Hkv, int d) {
     if (most_rows <= 16) return 16;
-    const long long blocks = most_rows < kFewRows ? (most_rows + 15) / 16 : kFewRows / 16;
-    const double visits = static_cast<double>(B) * Hkv * blocks * reach * (d / 128.0);
-    const bool many_keys = visits >= (B > 1 ? 1.0 : e4m3 ? 16.0 : 4.0) * (1 << 18);
-    if (B > 1) return many_keys ? 16 : kFewRows;
-    // one sequence: without a second launch, however few rows it turns out to have
-    return many_keys || most_rows > kFewRows ? 0 : kFewRows;
+    if (B == 1 && most_rows > kFewRows) return 0;
+    const double rows = static_cast<double>(all_rows) / B < kFewRows ? static_cast<double>(all_rows) / B : kFewRows;
+    const double visits = static_cast<double>(B) * Hkv * ceil(rows / 16) * reach * d / 128;
+    if (rows <= 16 || visits < 1 << 18) return kFewRows;
+    return most_rows <= kFewRows ? 0 : 16;
 }
 
 // What a call's sizes say; its pointers and the scale are still missing.
@@ -188,7 +189,7 @@ PagedFwdParams fwd_params(const s2a_cache* cache, const s2a_batch* batch, int H,
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
     p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new;
     p.window = window >= longest ? 0 : window, p.sinks = sinks > longest ? longest : sinks;
-    p.few_rows = few_rows(static_cast<long long>(max_new) * p.rep, reach_of(p, longest, max_new), batch->B, cache->Hkv, cache->d, cache->type == S2A_CACHE_E4M3);
+    p.few_rows = few_rows(static_cast<long long>(max_new) * p.rep, static_cast<long long>(batch->T) * p.rep, reach_of(p, longest, max_new), batch->B, cache->Hkv, cache->d);
     return p;
 }
 
@@ -263,7 +264,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     memset(&pt, 0, sizeof pt);
     if (many) {
         pt.a = p;
-        if (!plan_tiles(&pt, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
+        if (!plan_tiles(&pt, ds->n_sm, longest, cache->d)) return S2A_ERR_UNSUPPORTED;
         pt.beside = few;
         const size_t items = static_cast<size_t>(pt.slots) * (H >> pt.pack_log2);
         if (!workspace || (items - pt.first_split) * pt.split * paged_piece_bytes(cache->d) > workspace_bytes) pt.first_split = static_cast<int>(items), pt.split = 1;
@@ -284,7 +285,7 @@ size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch,
     memset(&p, 0, sizeof p);
     p.a = fwd_params(cache, batch, H, max_new, window, sinks);
     if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_device(&ds) != S2A_OK) return 0;
-    if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size)) return 0;
+    if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size, cache->d)) return 0;
     return (static_cast<size_t>(p.slots) * (H >> p.pack_log2) - p.first_split) * p.split * paged_piece_bytes(cache->d);
 }
 

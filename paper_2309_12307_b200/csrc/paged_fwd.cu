@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
 }
 
 // Joins the pieces of the split items.  A thread has eight columns of a row, a block 16 columns of a tile: with a block for each tile the few
-// items that are split left most of the GPU idle here (4000 keys, 64 rows of 8 KV heads: JOINA and JOINB us for both kernels).
+// items that are split left most of the GPU idle here (32k keys, 32 rows of 8 KV heads, both kernels: 108 us and 48).
 template <int HD>
 struct JoinCfg {
     static constexpr int kThreads = 256;
