@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "../../include/s2a.h"
 #include "host_state.h"
 #include "paged.h"
@@ -124,34 +126,41 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
     p->stages = split_stages(e4m3, d, p->blocks);  // where fewer blocks run at a time, each has more in flight
 }
 
-// The items of the tiling kernel: how many rows and tokens one has, in which order they come and which are split.
-// A single tile's step of 128 keys takes as long as a pair's, so items are pairs unless the GPU can work on all single tiles at a time (1024
-// new tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201).  Batches that have fewer items than the GPU works on
-// at a time are split: each item into pieces of its keys, a step of which counts as one, the start and end of a piece as two, joining
-// it as a quarter and the second launch as three (8 KV heads of 128 and one sequence, splits of 1 to 16 by this and by nearby rules within 10 %).  With
-// more items than that, splitting those of the last, partial wave brings nothing: with fewer multiprocessors busy those
-// run at a higher clock.  (2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
+// The items of the tiling kernel: how many rows and tokens one has, in which order they come and into how many pieces of its keys each is split,
+// whatever should be done first.  Counted in steps of 128 keys of a pair, 1.8 us and more: a single tile's takes four fifths of it (1024 new
+// tokens of 8192 on 32 heads: as 128 pairs 128 us, as 256 single tiles 201), so single tiles are for what the GPU works on at a time.  The
+// start and end of an item or piece take two steps, a second launch five and a tenth for every piece, and what pieces leave goes to the L2 and
+// back at 6.5 MB a microsecond.  A batch's sequences are taken to have the same number of new tokens.  Measured, one sequence, without
+// this splitting and with it: 1024 new tokens of 16,384 on 40 heads (160 pairs, in three) 422 us and 324; 257 of 23,219 on 16 heads over 8 in
+// 8 bits as 40 single tiles in three 131, as 24 pairs in six 90.
+// (Splitting the items of the last, partial wave alone brings nothing: with fewer multiprocessors busy those run at a higher
+// clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
 bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d) {
     const PagedFwdParams& a = p->a;
     p->pack_log2 = 0;
     while (p->pack_log2 < 6 && a.rep % (2 << p->pack_log2) == 0) ++p->pack_log2;
     const long long groups = a.H >> p->pack_log2;
-    p->span_log2 = 7 - p->pack_log2;
-    p->single = slot_count(a.batch.T, a.batch.B, p->span_log2) * groups <= n_sm;
-    if (!p->single) ++p->span_log2;
-    p->slots = slot_count(a.batch.T, a.batch.B, p->span_log2);
-    const long long items = p->slots * groups;
-    if (items * kMostSplit > 0x7fffffffLL) return false;
     p->ranked = a.batch.B > 1 && a.batch.B <= kMostRanked;
-    p->first_split = static_cast<int>(items), p->split = 1;
-    if (a.batch.B <= kMostRanked && items < n_sm) {
-        const int tiles = static_cast<int>((reach_of(a, longest, 1 << p->span_log2) + kTile - 1) / kTile);
-        double best = tiles - 3;
-        for (int split = 2; split <= kMostSplit && split <= tiles; ++split) {
-            const double t = static_cast<double>((items * split + n_sm - 1) / n_sm) * ((tiles + split - 1) / split + 2) + 0.25 * split * d / 128;
-            if (t < best) best = t, p->split = split, p->first_split = 0;
+    double best = 0;
+    int best_split = 1;
+    for (const bool single : {false, true}) {
+        const int span_log2 = 7 - p->pack_log2 + (single ? 0 : 1), slots = slot_count(a.batch.T, a.batch.B, span_log2);
+        const int likely = std::min(slots, a.batch.B * (((a.batch.T + a.batch.B - 1) / a.batch.B + (1 << span_log2) - 1) >> span_log2));
+        const long long items = slots * groups, busy = likely * groups;
+        const int tiles = static_cast<int>((reach_of(a, longest, 1 << span_log2) + kTile - 1) / kTile);
+        if (single && items > n_sm) break;
+        for (int split = 1; split <= kMostSplit && split <= tiles; ++split) {
+            if (split > 1 && (a.batch.B > kMostRanked || items * split > 4 * n_sm)) break;
+            double t = static_cast<double>((busy * split + n_sm - 1) / n_sm) * ((tiles + split - 1) / split + 2) * (single ? 0.8 : 1.0);
+            if (split > 1) t += 5 + 0.1 * split + 2.0 * busy * split * paged_piece_bytes(d) / 6.5e6 / 1.8;
+            if (best != 0 && t > (split > 1 ? 0.95 : 1.0) * best) continue;
+            best = t, best_split = split;
+            p->single = single, p->span_log2 = span_log2, p->slots = slots;
         }
     }
+    const long long items = p->slots * groups;
+    if (items * kMostSplit > 0x7fffffffLL) return false;
+    p->split = best_split, p->first_split = best_split > 1 ? 0 : static_cast<int>(items);
     p->by_slots = FastDiv(p->slots), p->by_groups = FastDiv(static_cast<int>(groups)), p->by_groups_of_kv = FastDiv(a.rep >> p->pack_log2);
     return true;
 }
@@ -169,15 +178,15 @@ int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_n
 //     111); 64 rows, 1000 16 and 21, 4000 25 and 21; 32 KV heads, 8192, in 8 bits: 20 rows 49 and 52, 40 rows 64 and 52
 //   - several, 8 KV heads: 32 rows, 2 x 2000 20 and 23, 4 x 4000 31 and 33 (8 bits 34 and 38), 2 x 8000 in 8 bits 55 and 37, 16 x 2000 77 and 37; 64 rows, 4 x 1000
 //     26 and 22, 4 x 4000 70 and 36
-//   - heads of 64: 4 x 1000, 24 rows 13 and 22, 32 x 4000 104 and 97, 2 x 32,000, 20 rows 70 and 57
+//   - heads of 64: 4 x 1000, 24 rows 13 and 22, 32 x 4000 104 and 97, 2 x 32,000, 20 rows 70 and 57; in 8 bits, one of 24,700, 40 KV heads, 22 rows 88 and 121
 //   - 6 x 16,700, 1 to 20 rows, 10 on average, in 8 bits 146 and 187.
 // With both kernels a call takes 5 to 8 us longer, so where no sequence has more than 64 rows the tiling kernel takes them all.
-int few_rows(long long most_rows, long long all_rows, long long reach, int B, int Hkv, int d) {
+int few_rows(long long most_rows, long long all_rows, long long reach, int B, int Hkv, int d, bool e4m3) {
     if (most_rows <= 16) return 16;
     if (B == 1 && most_rows > kFewRows) return 0;
     const double rows = static_cast<double>(all_rows) / B < kFewRows ? static_cast<double>(all_rows) / B : kFewRows;
     const double visits = static_cast<double>(B) * Hkv * ceil(rows / 16) * reach * d / 128;
-    if (rows <= 16 || visits < 1 << 18) return kFewRows;
+    if (rows <= (e4m3 && d == 64 ? 32 : 16) || visits < 1 << 18) return kFewRows;
     return most_rows <= kFewRows ? 0 : 16;
 }
 
@@ -189,7 +198,7 @@ PagedFwdParams fwd_params(const s2a_cache* cache, const s2a_batch* batch, int H,
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
     p.H = H, p.rep = H / cache->Hkv, p.most_new = max_new;
     p.window = window >= longest ? 0 : window, p.sinks = sinks > longest ? longest : sinks;
-    p.few_rows = few_rows(static_cast<long long>(max_new) * p.rep, static_cast<long long>(batch->T) * p.rep, reach_of(p, longest, max_new), batch->B, cache->Hkv, cache->d);
+    p.few_rows = few_rows(static_cast<long long>(max_new) * p.rep, static_cast<long long>(batch->T) * p.rep, reach_of(p, longest, max_new), batch->B, cache->Hkv, cache->d, cache->type == S2A_CACHE_E4M3);
     return p;
 }
 

@@ -239,6 +239,18 @@ def test_between_few_and_many_rows(sizes, wider, d, window, sinks, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("sizes,form,window", [
+    ([(300, 5000), (1, 700), (260, 2900)], (4, 4, 128), 0),
+    ([(300, 5000), (0, 0), (129, 130), (1, 1), (257, 2500)], (6, 2, 64), 0),
+    ([(515, 4000), (200, 4100)], (8, 2, 128), 1900),
+    ([(1030, 3000)], (40, 10, 64), 0),
+])
+def test_batches_in_pieces(sizes, form, window, dtype):
+    H, Hkv, d = form
+    Job(sizes, H=H, Hkv=Hkv, d=d, page=32, dtype=dtype, after=1).check(window=window, sinks=3 if window else 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("form", [(71, 1, 64, 16), (96, 1, 128, 32), (22, 2, 64, 64)])
 def test_many_query_heads_of_a_kv_head(form, dtype):
     H, Hkv, d, page = form
