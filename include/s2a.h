@@ -299,11 +299,12 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
  * floor(h / (H / Hkv)); H a multiple of Hkv.
  *   in : q [T, H, d] bf16        out: o [T, H, d] bf16, rounded once from fp32; lse [H, T] fp32, natural-log sum-exp of the scaled scores
  * o must not overlap q.
- * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels, so a tight value is
- * fastest (1 where every sequence has one new token).
+ * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels with T and the tokens
+ * that a row of the table has room for, so tight values are fastest (max_new 1 where every sequence has one new token).  Any are right.
  * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product (over an S2A_CACHE_E4M3 cache to
- * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  Cached values at positions that a token does not see are not assumed finite if they lie past the end of the sequence; a NaN
- * or infinity at a position of the sequence itself can reach the outputs of the other new tokens of the same call and sequence.
+ * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  Cached
+ * values past the end of a sequence are not assumed finite; a NaN or infinity at a position of the sequence itself can reach the
+ * outputs of the other new tokens of the same call and sequence.
  * Deterministic: no atomics.
  *   workspace: caller-owned device scratch, 256-byte aligned, or NULL.  Pieces of a prompt that do not fill the GPU evenly are split over
  *              their keys where it has s2a_paged_workspace_bytes(...) bytes; without it, or with less, they are not.  Its contents before
