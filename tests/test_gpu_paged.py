@@ -568,7 +568,7 @@ def test_refusals_reach_the_caller():
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
-@pytest.mark.parametrize("sizes", [[(1, 40), (1, 100)], [(1, 40), (150, 190)]], ids=["single", "pieces"])
+@pytest.mark.parametrize("sizes", [[(1, 40), (1, 100)], [(1, 40), (150, 190)], [(40, 3000), (36, 2500)]], ids=["single", "pieces", "split pieces"])
 @pytest.mark.parametrize("what", ["page", "negative page", "length", "short length", "starts", "new"])
 def test_values_out_of_range_are_reported_and_not_followed(what, sizes, dtype):
     job = Job(sizes, H=4, Hkv=2, d=64, dtype=dtype)
