@@ -130,6 +130,13 @@ __host__ __device__ inline KeyBlocks key_blocks(int first, int last, int window,
 }
 // Whether a token at position `p` attends key j.
 __host__ __device__ inline bool attends(int p, int j, int window, int sinks) { return j <= p && (window == 0 || j > p - window || j < sinks); }
+// Bit i: whether it attends key j + i.  (No sum of two sizes that are near 2^31.)
+__host__ __device__ inline uint32_t attended(int p, int j, int window, int sinks) {
+    auto below = [](int n) { return n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u; };
+    const int ahead = p - j;
+    const uint32_t low = window > 0 && ahead >= window ? below(ahead - window + 1) & ~below(sinks - j) : 0u;
+    return below(ahead + 1) & ~low;
+}
 // Whether any of the tokens at positions first .. last does.
 __host__ __device__ inline bool any_attends(int first, int last, int j, int window, int sinks) {
     return j <= last && (window == 0 || j > first - window || j < sinks);

@@ -755,17 +755,17 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 tmem_wait_ld();
                 tc_fence_before();
                 mbar_arrive_warp(&bars->s_empty[C::kScoreBufs == 1 ? 0 : group]);
+                // (as bits of the columns: comparing positions for every score costs the steps that need no mask, whose code lies around it,
+                // as well: 2048 new of 8192 tokens on 32 heads 219 us instead of 204, 4096 with a window of 8192 on 40 697 instead of 568)
                 if (!all_attend(first_pos, last_pos, key0, kTile, a.window, a.sinks)) {
-                    const int last = pos - key0;                                // keys up to here,
-                    const int low = a.window > 0 ? last - a.window + 1 : -1;    // from here on
-                    const int sinks = a.window > 0 ? a.sinks - key0 : 0;        // or below this
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t keys = attended(pos, key0 + 32 * c, a.window, a.sinks);
+                        const uint32_t columns = (keys & 0x99999999u) | (keys & 0x22222222u) << 1 | (keys & 0x44444444u) >> 1;  // see key_of_column()
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int x = c * 32 + key_of_column(e);
-                            if (x > last || (x < low && x >= sinks)) s[c][e] = 0xff800000u;  // -inf
-                        }
+                        for (int e = 0; e < 32; ++e)
+                            if ((columns >> e & 1) == 0) s[c][e] = 0xff800000u;  // -inf
+                    }
                 }
                 float mx4[4];
 #pragma unroll

@@ -160,7 +160,23 @@ static int blocks() {
     return 0;
 }
 
+// The bits of 32 keys at a time, positions, windows and sinks near 2^31 too.
+static int bits() {
+    std::srand(9);
+    const int most = 0x7fffffff;
+    for (int round = 0; round < 200000; ++round) {
+        const int far = round % 4 == 0 ? most - 1100 : 0, j = far + std::rand() % 40 * 16, p = j - std::rand() % 200 + std::rand() % 400;
+        if (p < 0) continue;
+        const int pick = std::rand() % 4, window = pick == 0 ? 0 : pick == 1 ? most - std::rand() % 40 : 1 + std::rand() % 300;
+        const int sinks = std::rand() % 3 == 0 ? 0 : std::rand() % 5 == 0 ? most : std::rand() % 700;
+        const uint32_t got = attended(p, j, window, sinks);
+        for (int i = 0; i < 32; ++i)
+            if ((got >> i & 1) != static_cast<uint32_t>(attends(p, j + i, window, sinks))) return fail("bit of a key", p, j + i);
+    }
+    return 0;
+}
+
 int main() {
-    if (batches() || exponents() || slots() || blocks()) return 1;
+    if (batches() || exponents() || slots() || blocks() || bits()) return 1;
     std::printf("ok\n");
 }
