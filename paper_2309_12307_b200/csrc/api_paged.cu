@@ -80,6 +80,9 @@ int tile_tmaps(PagedTileParams* p, const s2a_cache* c, const void* q, int H, int
     return rc != S2A_OK ? rc : encode_tmap(&p->tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->v, 2, dims, &row_bytes, box);
 }
 
+// Bytes of a token's k and v of a head.
+int key_bytes(const s2a_cache* c) { return c->type == S2A_CACHE_E4M3 ? 2 * c->d + 2 : 4 * c->d; }
+
 // Keys that `tokens` tokens of a sequence together attend at most, of `longest`.
 long long reach_of(const PagedFwdParams& a, long long longest, int tokens) {
     const long long most = static_cast<long long>(a.window) + a.sinks + tokens;
@@ -135,7 +138,7 @@ void choose_pieces(PagedSplitParams* p, const DeviceState* ds, long long reach, 
 // 8 bits as 40 single tiles in three 131, as 24 pairs in six 90.
 // (Splitting the items of the last, partial wave alone brings nothing: with fewer multiprocessors busy those run at a higher
 // clock.  2048 new tokens of 8192 on 32 heads 246 us without and 263 with it, of 32k on 64 over 8 2.09 and 2.06 ms.)
-bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d) {
+bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d, int key_bytes) {
     const PagedFwdParams& a = p->a;
     p->pack_log2 = 0;
     while (p->pack_log2 < 6 && a.rep % (2 << p->pack_log2) == 0) ++p->pack_log2;
@@ -161,7 +164,17 @@ bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d) {
     const long long items = p->slots * groups;
     if (items * kMostSplit > 0x7fffffffLL) return false;
     p->split = best_split, p->first_split = best_split > 1 ? 0 : static_cast<int>(items);
-    p->by_slots = FastDiv(p->slots), p->by_groups = FastDiv(static_cast<int>(groups)), p->by_groups_of_kv = FastDiv(a.rep >> p->pack_log2);
+    // The last items to begin should be short ones, so the head groups are taken in chunks that together have an item for every multiprocessor, all
+    // chunks alike, as far as the keys of a chunk leave half of the L2.  (One sequence, a group at a time and so: 8192 tokens on 32 heads of 64
+    // 415 us and 373, of 128 454 and 422; 2048 of 8192 204 and 200.  Without a look at the L2, 2048 of 65,536 1755 and 1890.)
+    const double group_bytes = static_cast<double>(reach_of(a, longest, a.batch.T)) * key_bytes / (a.rep >> p->pack_log2);
+    const int room = static_cast<int>(std::min<double>(static_cast<double>(groups), std::max(1.0, 64e6 / group_bytes)));
+    int chunk = std::min(room, (n_sm + p->slots - 1) / p->slots);
+    for (const int least = chunk; groups % chunk != 0;) {
+        if (chunk < least || ++chunk > room) chunk = std::min(chunk, least) - 1;
+    }
+    p->order = BlockOrder(static_cast<int>(groups), p->slots, chunk);
+    p->by_groups = FastDiv(static_cast<int>(groups)), p->by_groups_of_kv = FastDiv(a.rep >> p->pack_log2);
     return true;
 }
 
@@ -265,7 +278,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
         if ((rc = cache_tmap(&ps.tm_v, cache, cache->v, split_keys(e4m3, cache->d))) != S2A_OK) return rc;
         ps.unit_rows = most_rows <= 8 ? 8 : 16;
         ps.row_blocks = static_cast<int>((most_rows < p.few_rows ? most_rows : p.few_rows) + ps.unit_rows - 1) / ps.unit_rows;
-        choose_pieces(&ps, ds, reach_of(p, longest, max_new), 2 * cache->d * (e4m3 ? 1 : 2) + (e4m3 ? 2 : 0), e4m3, cache->d);
+        choose_pieces(&ps, ds, reach_of(p, longest, max_new), key_bytes(cache), e4m3, cache->d);
         if (static_cast<long long>(batch->B) * cache->Hkv * ps.row_blocks * ps.split > kIntMax) return S2A_ERR_UNSUPPORTED;
         ps.by_split = FastDiv(ps.split), ps.by_row_blocks = FastDiv(ps.row_blocks), ps.by_heads = FastDiv(cache->Hkv), ps.by_rep = FastDiv(p.rep);
     }
@@ -273,7 +286,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     memset(&pt, 0, sizeof pt);
     if (many) {
         pt.a = p;
-        if (!plan_tiles(&pt, ds->n_sm, longest, cache->d)) return S2A_ERR_UNSUPPORTED;
+        if (!plan_tiles(&pt, ds->n_sm, longest, cache->d, key_bytes(cache))) return S2A_ERR_UNSUPPORTED;
         pt.beside = few;
         const size_t items = static_cast<size_t>(pt.slots) * (H >> pt.pack_log2);
         if (!workspace || (items - pt.first_split) * pt.split * paged_piece_bytes(cache->d) > workspace_bytes) pt.first_split = static_cast<int>(items), pt.split = 1;
@@ -294,7 +307,7 @@ size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch,
     memset(&p, 0, sizeof p);
     p.a = fwd_params(cache, batch, H, max_new, window, sinks);
     if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_device(&ds) != S2A_OK) return 0;
-    if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size, cache->d)) return 0;
+    if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size, cache->d, key_bytes(cache))) return 0;
     return (static_cast<size_t>(p.slots) * (H >> p.pack_log2) - p.first_split) * p.split * paged_piece_bytes(cache->d);
 }
 

@@ -203,10 +203,11 @@ struct alignas(64) PagedTileParams {
     bool ranked;             // the items' order follows the sequences' lengths, see Ranking
     bool beside;             // launched behind the splitting kernel of the same call
     int slots;               // of a head group: slot_count()
+    BlockOrder order;        // of items that are not ranked: head groups in chunks, see plan_tiles()
     // Items from first_split on are split: `split` pieces of their keys each, which leave their results in `pieces`.
     int first_split, split;
     float* pieces;
-    FastDiv by_split, by_slots, by_groups, by_groups_of_kv;  // head groups, and those of a KV head: rep / pack
+    FastDiv by_split, by_groups, by_groups_of_kv;  // head groups, and those of a KV head: rep / pack
 };
 
 // Enqueue on `stream`; return the launch error, if any.

@@ -138,12 +138,12 @@ __device__ __forceinline__ bool item_at(const PagedTileParams& p, int group, int
     return true;
 }
 
-// Item `item` as a whole, of a batch of one sequence or of more than kRanked.  The places of one head group lie together (they read the
+// Item `item` as a whole, of a batch of one sequence or of more than kRanked: the places of some head groups side by side (their items read the
 // same keys), the last ones first: they have most.
 __device__ __forceinline__ bool whole_item(const PagedTileParams& p, int item, PagedItem* w) {
-    int slot;
-    const int group = p.by_slots(item, &slot);
-    slot = p.slots - 1 - slot;
+    int group, rank;
+    p.order.decode(item, &group, &rank);
+    const int slot = p.slots - 1 - rank;
     const int b = find_slot(p.a.batch.starts, p.a.batch.B, p.span_log2, slot);
     return item_at(p, group, b, static_cast<long long>(slot - first_slot(S2A_LOAD(p.a.batch.starts + b), b, p.span_log2)) << p.span_log2, w);
 }
