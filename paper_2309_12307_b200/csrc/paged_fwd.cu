@@ -113,6 +113,14 @@ __device__ __forceinline__ int tile_of_group(int item, int group) { return (item
 // times 2^e, -127 (which stands for less than that) <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
 
+// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, masked ones (-inf) and zeros too, so it must
+// neither vanish nor become infinite.  Sums of products of fp16 operands are below 2^37: where it is held from below they are scores below 2^-89.
+// (In two steps towards the result: a step of the other sign could lose bits that the result has.)
+__device__ __forceinline__ float score_factor(float x, int e) {
+    const int half = e >> 1;
+    return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
+}
+
 constexpr float kLazyRescale = 8.0f;
 constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
 __device__ __forceinline__ constexpr int key_of_column(int x) { return (x & ~3) | ((x & 1) << 1) | ((x >> 1) & 1); }
@@ -613,7 +621,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                     for (int y = 0; y < 4; ++y) most = max(most, max(x[y] & 0x7fffu, x[y] >> 16 & 0x7fffu));
                 }
                 int up = most >= 0x7f80u || most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);  // (a row that is not finite stays so)
-                up = up > 126 ? 126 : up;
+                up = up > 112 ? 112 : up;  // (2^-133, the least bf16 number, is still one of fp16 then)
                 const float f = power_of_two(up);
 #pragma unroll 4
                 for (int c = 0; c < HD / 8; ++c) {
@@ -744,7 +752,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 tc_fence_after();
                 if constexpr (kE4M3) {
                     if (j == 0) up = sQExp[(2 * group + (n_it & 1)) * kTile + row];
-                    c2 = a.scale_log2 * 0.015625f * power_of_two(bars->tile_exp[(w.kv0 + 2 * j) % 16]) * power_of_two(-up);  // (K is 2^6 as large)
+                    c2 = score_factor(a.scale_log2, bars->tile_exp[(w.kv0 + 2 * j) % 16] - 6 - up);  // (K is 2^6 as large)
                 }
                 const uint64_t c2x2 = f2_pack(c2, c2);
                 uint32_t s[4][32];

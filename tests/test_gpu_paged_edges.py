@@ -1,0 +1,83 @@
+"""The paged cache on the GPU at the edges of its number ranges and masks, against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+from test_gpu_paged import BF16, E4M3, PIECES, Job, compare
+
+from oracle import paged_torch as ref
+from paper_2309_12307_b200 import binding as s2a
+
+pytestmark = pytest.mark.gpu
+
+
+def refill(job):
+    """all_k and all_v, as they are now, into the cache."""
+    s2a.s2a_cache_write(job.cache, job.all_k, job.all_v, job.table, job.all_starts, job.lengths)
+
+
+def zero_keys(job, which):
+    """Keys of zeros: those of the whole sequences, of the last (ragged, masked) block of 128, or of the blocks with an odd number."""
+    at = 0
+    for _, length in job.sizes:
+        j = torch.arange(length, device="cuda")
+        last = j // 128 == max(0, length - 1) // 128
+        job.all_k[at:at + length][{"all": j >= 0, "last": last, "odd": j // 128 % 2 == 1}[which]] = 0
+        at += length
+    refill(job)
+
+
+# ---------------------------------------------------------------------------------------------- keys that are zero or tiny
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 4), (129, 130)])
+@pytest.mark.parametrize("which", ["all", "last", "odd"])
+@pytest.mark.parametrize("d,scale", [(64, 64**-0.5), (128, 128**-0.5), (64, 1 / 64), (128, 2.0**-130)])
+def test_blocks_of_keys_that_are_zero(d, scale, which, window, sinks, dtype):
+    """Scores of zero beside masked ones, with small queries: what scores are multiplied with must not vanish."""
+    for sizes, down in ((PIECES, 2.0**-10), ([(200, 3000)], 2.0**-2), ([(1, 1), (1, 129), (1, 300)], 2.0**-10)):
+        job = Job(sizes, H=4, Hkv=2, d=d, page=16, dtype=dtype)
+        zero_keys(job, which)
+        job.q *= down
+        job.check(scale=scale, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("new", [1, 30, 200])
+@pytest.mark.parametrize("q_power,k_power", [(-100, 100), (100, -117), (120, -126), (-118, 118), (0, -120), (-120, 0)])
+def test_queries_and_keys_at_the_ends_of_the_range(q_power, k_power, new):
+    """8-bit keys whose powers of two and those of the queries cancel, or leave next to nothing."""
+    for window, sinks in ((0, 0), (70, 3)):
+        job = Job([(new, 300)], H=4, Hkv=2, d=64, page=32, dtype=E4M3)
+        job.all_k *= 2.0**k_power
+        refill(job)
+        job.q *= 2.0**q_power
+        job.check(window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [200])
+def test_scores_that_are_zero_between_the_largest_numbers(d, new):
+    """Queries and keys near 2^127 with nothing in common: the scores are zero, whatever power of two they would be multiplied with."""
+    job = Job([(new, 300)], H=4, Hkv=2, d=d, page=32, dtype=E4M3)
+    job.all_k[..., :d // 2] = 0
+    job.all_k[..., d // 2:] = 2.0**127
+    job.q[..., d // 2:] = 0
+    job.q[..., :d // 2] = 2.0**127
+    refill(job)
+    o, lse = job.attend(o=torch.full((job.T, 4, d), 7.0, dtype=BF16, device="cuda"), lse=torch.full((4, job.T), 7.0, device="cuda"))
+    want = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5)
+    # (no score is off: they are sums of zeros)
+    compare(o.cpu(), lse.cpu(), *want, job.rows(), 300, d, d**-0.5, 0.0, torch.zeros(1))
+
+
+def test_keys_marked_as_not_finite_reach_no_token_before_them():
+    """The last block's keys are NaN throughout; tokens that attend none of them have what they have without it."""
+    for d in (64, 128):
+        job = Job([(150, 170)], H=4, Hkv=2, d=d, page=16, dtype=E4M3)
+        job.q *= 2.0**-6
+        want = [t.clone() for t in job.attend()]
+        job.all_k[128:] = math.inf
+        refill(job)
+        o, lse = job.attend()
+        # (new token i is at position 20 + i)
+        assert torch.equal(o[:108], want[0][:108]) and torch.equal(lse[:, :108], want[1][:, :108])
+        assert torch.isnan(lse[:, 108:]).all() and s2a.device_status() == (0, 0)
