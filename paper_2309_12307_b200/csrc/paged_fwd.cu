@@ -110,19 +110,7 @@ struct TileOfItem {
 __device__ __forceinline__ int group_of_tile(int item, int t) { return (item & 1) ^ t ^ 1; }
 __device__ __forceinline__ int tile_of_group(int item, int group) { return (item & 1) ^ group ^ 1; }
 
-// times 2^e, -127 (which stands for less than that) <= e <= 127
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
-
-// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, masked ones (-inf) and zeros too, so it must
-// neither vanish nor become infinite.  Sums of products of fp16 operands are below 2^37: where it is held from below they are scores below 2^-89.
-// (In two steps towards the result: a step of the other sign could lose bits that the result has.)
-__device__ __forceinline__ float score_factor(float x, int e) {
-    const int half = e >> 1;
-    return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
-}
-
 constexpr float kLazyRescale = 8.0f;
-constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
 __device__ __forceinline__ constexpr int key_of_column(int x) { return (x & ~3) | ((x & 1) << 1) | ((x >> 1) & 1); }
 
 // The item of head group `group` whose tokens begin with token `first` of sequence b; false: the sequence has none.

@@ -12,10 +12,10 @@
 // long as K and Q agree, so a thread takes what lies together in shared memory.
 //
 // Cached 8-bit floats become fp16, which has them all (one conversion for two values; as bf16 they take five instructions).  Q, in bf16, goes
-// to fp16 with a power of two that brings the unit's largest value near fp16's: nothing is lost of values within 2^-29 of it.  K's
-// power of two multiplies the scores.  V's goes into the exponents of the weights: with x a score in units of log2 and 2^e V's power
-// the weight of the second product is 2^(x + e - r + 7), r a running maximum of x + e.  So the largest term has a weight of 2^7 or more, those
-// down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), and O is in units of 2^(r - 7); the sum of weights takes an exponential of its own.
+// to fp16, each row with a power of two that brings its largest value near fp16's: nothing is lost of values within 2^-29 of it, and no row
+// reaches another (with one power for the unit 8 x 32k tokens of 8 heads take the same 87.5 us).  The row's power of two and K's multiply the scores.
+// V's goes into the exponents of the weights: with x a score in units of log2 and 2^e V's power the weight of the second product is
+// 2^(x + e - r + 7), r a running maximum of x + e.  So the largest term has a weight of 2^7 or more, those down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), and O is in units of 2^(r - 7); the sum of weights takes an exponential of its own.
 #include "paged_device.cuh"
 
 namespace s2a {
@@ -66,13 +66,6 @@ __device__ __forceinline__ int lds_s8(uint32_t a) {
     asm volatile("ld.shared.s8 %0, [%1];" : "=r"(r) : "r"(a));
     return r;
 }
-__device__ __forceinline__ float exponent_factor(int e) {
-    return e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-}
-
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }  // -127 <= e <= 127, -127: zero
-
-constexpr float kLeast = -3.0e38f;   // stands for "no key yet": finite, so that differences are numbers
 constexpr float kLazy = 8.0f;        // a running maximum (of log2) that is exceeded by less stays
 
 template <int HD, bool kE4M3, int kRowTiles>
@@ -180,26 +173,30 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
         }
     }
-    float score_scale = a.scale_log2;
+    // 8 bits: what the scores of rows 2 t and 2 t + 1 of every eight are multiplied with beside a key's power of two, and what is taken off that
+    // one's exponent: the unit's least row exponent, so that no product of the two is out of range unless the score is.
+    float row_scale[kRowTiles][2];
+    int least_up = 0;
     if constexpr (kE4M3) {
-        uint32_t most = 0;
+        int up[kRowTiles];  // exponent of row 8 r + g
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
-            uint32_t row_most = 0;
+            uint32_t most = 0;
 #pragma unroll
-            for (int c = 0; c < HD / 8; ++c) row_most = max(row_most, max(q[r][c] & 0x7fffu, q[r][c] >> 16 & 0x7fffu));
-            most = max(most, row_most < 0x7f80u ? row_most : 0u);  // (a row that is not finite stays so, and sets no scale)
+            for (int c = 0; c < HD / 8; ++c) most = max(most, max(q[r][c] & 0x7fffu, q[r][c] >> 16 & 0x7fffu));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1)), most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            // the largest goes to [2^14, 2^15), or as near as 2^112 brings it, with which 2^-133, the least bf16 number, is one of fp16
+            up[r] = most == 0 ? 112 : most >= 0x7f80u ? 0 : min(127 + 14 - static_cast<int>(most >> 7), 112);  // (a row that is not finite stays so)
+            const float f = power_of_two(up[r]);
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) q[r][c] = pack_f16(bf16_low(q[r][c]) * f, bf16_high(q[r][c]) * f);
+            least_up = r == 0 ? up[0] : min(least_up, up[r]);
         }
-        most = __reduce_max_sync(0xffffffffu, most);
-        // the largest goes to [2^14, 2^15)
-        int up = most == 0 ? 0 : 127 + 14 - static_cast<int>(most >> 7);
-        up = up > 126 ? 126 : up;
-        const float f = power_of_two(up);
-        score_scale *= power_of_two(-up);
+        least_up = __reduce_min_sync(0xffffffffu, least_up);
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-            for (int c = 0; c < HD / 8; ++c) q[r][c] = pack_f16(bf16_low(q[r][c]) * f, bf16_high(q[r][c]) * f);
+            for (int h = 0; h < 2; ++h) row_scale[r][h] = score_factor(a.scale_log2, least_up - __shfl_sync(0xffffffffu, up[r], 4 * (2 * t + h)));
     }
 
     float o[kRowTiles][HD / 16][4] = {};
@@ -251,10 +248,11 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             }
         }
         // Exponents of the step's keys (8 bits): lane i has those of key i, as what a score is multiplied with and as it is.
-        float k_scale = score_scale, v_exp = 0.f;
+        float k_scale = a.scale_log2, v_exp = 0.f;
         bool grows = false;
         if constexpr (kE4M3) {
-            k_scale *= exponent_factor(lds_s8(sE + lane));
+            const int k_exp = lds_s8(sE + lane);
+            k_scale = k_exp == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(min(max(k_exp - least_up, -126), 127));
             const int e = lds_s8(sE + C::kKeys + lane);
             v_exp = e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : static_cast<float>(e);
         }
@@ -275,6 +273,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     sc[u][r][x] *= scale[x >> 1];
+                    if constexpr (kE4M3) sc[u][r][x] *= row_scale[r][x & 1];
                     if (masked && !attends(pos[r][x & 1], key0 + 16 * u + 8 * (x >> 1) + g, a.window, a.sinks)) sc[u][r][x] = -INFINITY;
                     grows |= sc[u][r][x] > m[r][x & 1] + kLazy;
                     if constexpr (kE4M3) grows |= sc[u][r][x] + v_exps[u][x >> 1] > ref[r][x & 1] + kLazy;

@@ -54,7 +54,7 @@ def test_queries_and_keys_at_the_ends_of_the_range(q_power, k_power, new):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("new", [200])
+@pytest.mark.parametrize("new", [1, 30, 200])
 def test_scores_that_are_zero_between_the_largest_numbers(d, new):
     """Queries and keys near 2^127 with nothing in common: the scores are zero, whatever power of two they would be multiplied with."""
     job = Job([(new, 300)], H=4, Hkv=2, d=d, page=32, dtype=E4M3)
@@ -81,3 +81,27 @@ def test_keys_marked_as_not_finite_reach_no_token_before_them():
         # (new token i is at position 20 + i)
         assert torch.equal(o[:108], want[0][:108]) and torch.equal(lse[:, :108], want[1][:, :108])
         assert torch.isnan(lse[:, 108:]).all() and s2a.device_status() == (0, 0)
+
+
+# ---------------------------------------------------------------------------------------------- rows stay by themselves
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("sizes,power", [([(1, 300)], 20), ([(1, 300)], 40), ([(1, 300)], 100), ([(1, 40), (4, 500), (1, 1)], 20), ([(1, 40), (4, 500), (1, 1)], 40),
+                                         ([(1, 40), (4, 500), (1, 1)], 100), ([(200, 500)], 20)])
+def test_a_large_query_reaches_no_other_row(sizes, power, dtype):
+    """One head's queries, and one token's, are 2^power times as large as the others of their KV head and sequence."""
+    H, Hkv, d = 8, 2, 64
+    job = Job(sizes, H=H, Hkv=Hkv, d=d, page=16, dtype=dtype)
+    large = torch.zeros(job.T, H, dtype=torch.bool)
+    large[:, 1] = True
+    if job.T > 1:
+        large[job.T // 2] = True
+    job.q[large.cuda()] *= 2.0**power
+    o, lse = job.attend()
+    assert s2a.device_status() == (0, 0) and torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+    want, want_lse, size, largest = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5)
+    q_norm = float(job.q.cpu()[~large].double().norm(dim=-1).max())
+    # the other rows, one after the other, as rows of one head
+    flat = [x[~large][:, None] for x in (o.cpu(), want, size, largest)]
+    rows = flat[0].shape[0]
+    compare(flat[0], lse.cpu().T[~large][None], flat[1], want_lse.T[~large][None], flat[2], flat[3], torch.ones(rows, dtype=torch.bool), max(n for _, n in sizes), d, d**-0.5,
+            q_norm, job.all_k)
