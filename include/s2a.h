@@ -257,7 +257,8 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
  * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows.  Rows that belong to no sequence are left as they
  * are in outputs, and what they hold in inputs does not matter.  lengths[b] counts the tokens that sequence b has in the cache INCLUDING its new ones, so new token i is at
  * position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
- * (j + 1) * page_size - 1; entries past a sequence's last page are not used.  Sequences may share pages, but not those that one call
+ * (j + 1) * page_size - 1; entries past a sequence's last page are not used, and s2a_paged_fwd uses none of a page that no new token of the
+ * sequence attends (in front of the windows: such pages may be given back).  Sequences may share pages, but not those that one call
  * writes to.
  * table, starts and lengths are DEVICE pointers and read on the device when the kernels run: a captured graph follows what they
  * hold when it is replayed.  Their contents are checked there.  What is out of range (starts that fall or leave [0, T], a length
@@ -302,9 +303,9 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
  * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels with T and the tokens
  * that a row of the table has room for, so tight values are fastest (max_new 1 where every sequence has one new token).  Any are right.
  * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product (over an S2A_CACHE_E4M3 cache to
- * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  Cached
- * values past the end of a sequence are not assumed finite; a NaN or infinity at a position of the sequence itself can reach the
- * outputs of the other new tokens of the same call and sequence.
+ * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  What
+ * the cache holds where no new token of the sequence attends it, past the end and in front of the windows, does not matter; a NaN or infinity
+ * that one of them attends can reach the outputs of the other new tokens of the same call and sequence.
  * Deterministic: no atomics.
  *   workspace: caller-owned device scratch, 256-byte aligned, or NULL.  Pieces of a prompt that do not fill the GPU evenly are split over
  *              their keys where it has s2a_paged_workspace_bytes(...) bytes; without it, or with less, they are not.  Its contents before

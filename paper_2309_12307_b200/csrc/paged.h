@@ -145,6 +145,19 @@ __host__ __device__ inline bool any_attends(int first, int last, int j, int wind
 __host__ __device__ inline bool all_attend(int first, int last, int j, int n, int window, int sinks) {
     return j + n - 1 <= first && (window == 0 || j > last - window || j + n <= sinks);
 }
+// Of the keys from `key0` on those that none of the tokens at positions first .. last attends, counted from key0: from .. to - 1, in front of their
+// windows, and from `end` on.  They may hold anything, and pages that hold no other keys need not be there.
+struct HiddenKeys {
+    int from, to, end;
+    __host__ __device__ bool has(int i) const { return i >= end || (i >= from && i < to); }
+    __host__ __device__ bool any(int n) const { return end < n || (from < to && from < n && to > 0); }      // of the first n
+    __host__ __device__ bool all(int i, int n) const { return i >= end || (i >= from && i + n <= to); }  // from the i-th on n of them
+};
+__host__ __device__ inline HiddenKeys hidden_keys(int first, int last, int key0, int window, int sinks) {
+    HiddenKeys h;
+    h.from = sinks - key0, h.to = window > 0 ? first - window + 1 - key0 : h.from, h.end = last + 1 - key0;
+    return h;
+}
 
 // Rows (new tokens times query heads of a KV head) up to which a sequence may be worked on by the kernel that splits its keys.
 constexpr int kFewRows = 64;

@@ -73,6 +73,8 @@ struct PagedItem {
     __device__ __forceinline__ int row_of(int t) const { return t ? row[1] : row[0]; }
     __device__ __forceinline__ int tokens_of(int t) const { return t ? tokens[1] : tokens[0]; }
     __device__ __forceinline__ int first_pos(int t) const { return t ? pos : pos - (row[1] - row[0]); }
+    // of the keys from key0 on, what none of its tokens attends
+    __device__ __forceinline__ HiddenKeys hidden(int key0, int window, int sinks) const { return hidden_keys(pos - tokens[0], pos + tokens[1] - 1, key0, window, sinks); }
 };
 
 template <int HD, bool kE4M3>
@@ -217,7 +219,9 @@ __device__ __forceinline__ float* piece_result(const PagedTileParams& p, int pie
     return p.pieces + (2ll * piece + t) * (kTile * (HD + 2));
 }
 
-template <int HD, bool kE4M3>
+// kWindow: whether the call has one.  (Pages and values in front of a window are left alone, see hidden_keys(); looked for in every call, they cost
+// 2048 new tokens of 32k on 64 heads over 8 in 8 bits 2170 us instead of 2134.)
+template <int HD, bool kE4M3, bool kWindow>
 __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fwd_kernel(const __grid_constant__ PagedTileParams p) {
     using C = PagedCfg<HD, kE4M3>;
     using Bars = PagedBars<HD, kE4M3>;
@@ -230,6 +234,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
     float* sStat = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + C::kBarBytes);  // [group][128 rows]
     int8_t* sQExp = reinterpret_cast<int8_t*>(sStat + 2 * kTile);  // [group][item of the group, odd or even][128 rows]
     const PagedFwdParams& a = p.a;
+    const int window = kWindow ? a.window : 0;
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
@@ -351,10 +356,10 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 const int key = tile * kTile + (lane << piece_log2);
                 return S2A_LOAD(table + ((key < length ? key : length - 1) >> a.pool.page_log2));
             };
-            // Pool row (in head hk) of that piece, -1: none.
-            auto piece_row = [&](int page, int hk, int length, int tile) {
+            // Pool row (in head hk) of that piece, -1: none of its keys is attended.
+            auto piece_row = [&](int page, int hk, const HiddenKeys& hidden, int tile) {
                 const int key = tile * kTile + (lane << piece_log2);
-                if (lane >= kTile >> piece_log2 || key >= length) return -1;
+                if (lane >= kTile >> piece_log2 || hidden.all(key, 1 << piece_log2)) return -1;
                 if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.pool.pages)) {
                     report_bad_index(a.status, a.host_status, kBadPage);
                     return -1;
@@ -412,10 +417,11 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 if (id < 0) break;
                 const int hk = p.by_groups_of_kv(w.group), length = w.pos + w.tokens[1];  // (keys behind the last token are nobody's)
                 const int* table = a.batch.table + static_cast<long long>(w.b) * a.batch.width;
+                const HiddenKeys hidden = w.hidden(0, window, a.sinks);
                 int row = -1, page = look_up(table, length, w.key_tile(0));
                 for (int j = 0; ok && j < w.n[1]; ++j) {
                     const int before = row;
-                    row = piece_row(page, hk, length, w.key_tile(j));
+                    row = piece_row(page, hk, hidden, w.key_tile(j));
                     page = look_up(table, length, w.key_tile(j + 1 < w.n[1] ? j + 1 : j));
                     load_kv(row, true);
                     if (j == 0 && ok) load_q(w, 1, g1);
@@ -451,7 +457,6 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 PagedItem w;
                 if (!next_item(k, kWaitPagedFwd + 10, &w)) break;
                 const int n1 = w.n[1], n0 = w.n[0];
-                const int end = w.pos + w.tokens[1];  // keys from here on are no key of the item
 #pragma unroll 1
                 for (int h = 0; ok && h < 2 * n1; ++h) {
                     const int t = (h & 1) ^ 1, j = h >> 1, n = t ? n1 : n0, g = group_of_tile(k, t);
@@ -482,13 +487,13 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         ++n_s;
                     } else {
                         if (!kE4M3 && t == 1) {
-                            // The rows of V past the last key hold whatever the page held before, or what the ring did: a weight of
-                            // zero does not make a NaN go away.  (8-bit tiles are written without them.)
-                            const int valid = end - w.key_tile(j) * kTile;
-                            if (valid < kTile) {
-                                for (int c = valid * 8 + lane; c < kTile * 8; c += 32)
-                                    for (int bx = 0; bx < C::kBoxes; ++bx)
-                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(aKV + (x % C::kRing) * C::kTileBytes + bx * C::kBoxBytes + c * 16),
+                            // The rows of V that no row of the item attends hold whatever the page held before, or what the ring did: a weight
+                            // of zero does not make a NaN go away.  (8-bit tiles are written without them.)
+                            const HiddenKeys hidden = w.hidden(w.key_tile(j) * kTile, window, a.sinks);
+                            if (hidden.any(kTile)) {
+                                for (int key = lane >> 3; key < kTile; key += 4)
+                                    for (int bx = 0; hidden.has(key) && bx < C::kBoxes; ++bx)
+                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(aKV + (x % C::kRing) * C::kTileBytes + bx * C::kBoxBytes + key * 128 + (lane & 7) * 16),
                                                      "r"(0)
                                                      : "memory");
                                 fence_proxy_async();
@@ -640,7 +645,6 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 PagedItem w;
                 const bool more = next_item(k, kWaitPagedFwd + 11, &w);
                 const int tiles = more ? 2 * w.n[1] : 0, pause = tiles < C::kRing - 1 ? tiles : C::kRing - 1;
-                const int end = more ? w.pos + w.tokens[1] : 0;
                 for (int x = 0; ok && x <= tiles; ++x) {
                     if (x == pause) {
                         if (more) ok = convert_q(group_of_tile(k, 1)) && (w.n[0] == 0 || convert_q(group_of_tile(k, 0)));
@@ -656,14 +660,14 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         break;
                     }
                     const bool is_v = tile.is_v;
-                    const int valid = end - w.key_tile(tile.j) * kTile;  // rows of the tile that hold keys
+                    const HiddenKeys hidden = w.hidden(w.key_tile(tile.j) * kTile, window, a.sinks);
                     const uint32_t src = smem_u32(sRaw + raw * C::kRawBytes), dst = smem_u32(sKV + st * C::kTileBytes);
-                    // the largest exponent of the rows that hold keys: four rows a lane
+                    // the largest exponent of the rows that are attended: four rows a lane
                     const uint32_t four = *reinterpret_cast<const volatile uint32_t*>(&bars->exps[raw][4 * lane]);
                     int most = kExpNotFinite;
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
-                        if (4 * lane + y < valid) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
+                        if (!hidden.has(4 * lane + y)) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
                     most = max(__reduce_max_sync(0xffffffffu, most), kExpLeast);
                     // A warp takes 32 rows, kRows at a time, 16 codes a lane.  Lane i has the factor of the warp's row i.
                     const int e = bars->exps[raw][32 * quad + lane];
@@ -695,11 +699,12 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         }
                         from += 2 * kRows * HD, to += 2 * kRows * 128;
                     }
-                    if (is_v && valid < kTile) {
-                        // rows past the last key: whatever lies there (a weight of zero does not make a NaN go away)
+                    if (is_v && hidden.any(kTile)) {
+                        // rows that are not attended: whatever lies there (a weight of zero does not make a NaN go away)
                         __syncwarp();
-                        for (int c = max(valid - 32 * quad, 0) * 8 + lane; c < 32 * 8; c += 32)
-                            for (int bx = 0; bx < C::kBoxes; ++bx) sts(dst + bx * C::kBoxBytes + quad * 32 * 128 + c * 16, 0, 0, 0, 0);
+#pragma unroll 1
+                        for (int key = 32 * quad + (lane >> 3); key < 32 * quad + 32; key += 4)
+                            for (int bx = 0; hidden.has(key) && bx < C::kBoxes; ++bx) sts(dst + bx * C::kBoxBytes + key * 128 + (lane & 7) * 16, 0, 0, 0, 0);
                     }
                     if (threadIdx.x == 256) bars->tile_exp[at % 16] = static_cast<int8_t>(most);
                     fence_proxy_async();
@@ -753,10 +758,10 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 mbar_arrive_warp(&bars->s_empty[C::kScoreBufs == 1 ? 0 : group]);
                 // (as bits of the columns: comparing positions for every score costs the steps that need no mask, whose code lies around it,
                 // as well: 2048 new of 8192 tokens on 32 heads 219 us instead of 204, 4096 with a window of 8192 on 40 697 instead of 568)
-                if (!all_attend(first_pos, last_pos, key0, kTile, a.window, a.sinks)) {
+                if (!all_attend(first_pos, last_pos, key0, kTile, window, a.sinks)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t keys = attended(pos, key0 + 32 * c, a.window, a.sinks);
+                        const uint32_t keys = attended(pos, key0 + 32 * c, window, a.sinks);
                         const uint32_t columns = (keys & 0x99999999u) | (keys & 0x22222222u) << 1 | (keys & 0x44444444u) >> 1;  // see key_of_column()
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
@@ -920,15 +925,20 @@ __global__ void __launch_bounds__(JoinCfg<HD>::kThreads) s2a_paged_join_kernel(c
     if (c == 0) a.lse[static_cast<long long>(head) * a.batch.T + at] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int HD, bool kE4M3>
-cudaError_t configure_one() {
+template <int HD, bool kE4M3, bool kWindow>
+cudaError_t configure_form() {
     using C = PagedCfg<HD, kE4M3>;
     // the register split of the kernel draws on what a block is launched with
     cudaFuncAttributes attributes;
-    cudaError_t e = cudaFuncGetAttributes(&attributes, s2a_paged_fwd_kernel<HD, kE4M3>);
+    cudaError_t e = cudaFuncGetAttributes(&attributes, s2a_paged_fwd_kernel<HD, kE4M3, kWindow>);
     if (e != cudaSuccess) return e;
     if (attributes.numRegs < C::kRegsLaunch || attributes.sharedSizeBytes != 0) return cudaErrorInvalidConfiguration;
-    return cudaFuncSetAttribute(s2a_paged_fwd_kernel<HD, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    return cudaFuncSetAttribute(s2a_paged_fwd_kernel<HD, kE4M3, kWindow>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+}
+template <int HD, bool kE4M3>
+cudaError_t configure_one() {
+    const cudaError_t e = configure_form<HD, kE4M3, false>();
+    return e != cudaSuccess ? e : configure_form<HD, kE4M3, true>();
 }
 
 }  // namespace
@@ -943,7 +953,7 @@ template <int HD, bool kE4M3>
 static cudaError_t launch_one(const PagedTileParams& p, cudaStream_t stream) {
     const int items = p.slots * (p.a.H >> p.pack_log2), split_items = items - p.first_split;
     const unsigned grid = static_cast<unsigned>(p.first_split) + static_cast<unsigned>(split_items) * static_cast<unsigned>(p.split);
-    const cudaError_t e = launch_kernel(s2a_paged_fwd_kernel<HD, kE4M3>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
+    const cudaError_t e = launch_kernel(p.a.window > 0 ? s2a_paged_fwd_kernel<HD, kE4M3, true> : s2a_paged_fwd_kernel<HD, kE4M3, false>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
     if (e != cudaSuccess || split_items == 0) return e;
     return launch_kernel(s2a_paged_join_kernel<HD>, 2u * JoinCfg<HD>::kBlocks * static_cast<unsigned>(split_items), JoinCfg<HD>::kThreads, 0, stream, p, true);
 }

@@ -105,3 +105,41 @@ def test_a_large_query_reaches_no_other_row(sizes, power, dtype):
     rows = flat[0].shape[0]
     compare(flat[0], lse.cpu().T[~large][None], flat[1], want_lse.T[~large][None], flat[2], flat[3], torch.ones(rows, dtype=torch.bool), max(n for _, n in sizes), d, d**-0.5,
             q_norm, job.all_k)
+
+
+# ---------------------------------------------------------------------------------------------- behind the window
+def leave_behind(job, window, sinks, fill):
+    """What no new token of a sequence attends, in front of its window, goes: table entries of whole pages, and the values of the other keys become
+    NaN or the largest numbers there are (a page that was given back holds another sequence's tokens)."""
+    table = job.table.cpu()
+    for b, (n, length) in enumerate(job.sizes):
+        low = max(0, length - n - window + 1)
+        for i in range(-(-length // job.page)):
+            gone = torch.tensor([sinks <= j < low for j in range(i * job.page, (i + 1) * job.page)]).cuda()
+            page = int(table[b, i])
+            if gone.all() and n > 0:
+                table[b, i] = -1
+            if n > 0:
+                for x in ("k", "v"):
+                    pool = getattr(job.cache, x)
+                    pool[page][:, gone] = torch.tensor(math.nan if fill == "nan" else 3e38, device="cuda").to(pool.dtype) if job.dtype == BF16 else \
+                        torch.full((), 127 if fill == "nan" else 126, dtype=torch.uint8, device="cuda").view(E4M3)
+                    if job.dtype == E4M3:
+                        getattr(job.cache, x + "_exp")[page][:, gone] = ref.NOT_FINITE if fill == "nan" else 119
+    job.table.copy_(table)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("fill", ["nan", "large"])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 4), (33, 40), (100, 1), (129, 130)])
+@pytest.mark.parametrize("form", [(4, 2, 64, 16), (4, 4, 128, 32), (8, 1, 64, 256)])
+def test_what_lies_behind_a_window_does_not_matter(form, window, sinks, fill, dtype):
+    H, Hkv, d, page = form
+    for sizes in ([(1, 600), (1, 40), (4, 333)], [(150, 700), (1, 300), (0, 20), (70, 400)], [(40, 1500)]):
+        job = Job(sizes, H=H, Hkv=Hkv, d=d, page=page, dtype=dtype, after=1)
+        want, want_lse, size, largest = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5, window, sinks)
+        leave_behind(job, window, sinks, fill)
+        o, lse = job.attend(window=window, sinks=sinks, o=torch.full((job.T, H, d), 7.0, dtype=BF16, device="cuda"), lse=torch.full((H, job.T), 7.0, device="cuda"))
+        assert s2a.device_status() == (0, 0)
+        compare(o.cpu(), lse.cpu(), want, want_lse, size, largest, job.rows(), max(n for _, n in sizes), d, d**-0.5, float(job.q.cpu()[job.rows()].double().norm(dim=-1).max()),
+                job.all_k)
