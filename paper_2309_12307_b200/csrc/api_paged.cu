@@ -1,4 +1,5 @@
 // Host side of the paged cache's part of include/s2a.h: argument validation and kernel launches.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -267,7 +268,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     PagedFwdParams p = fwd_params(cache, batch, H, max_new, window, sinks);
     p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
-    p.scale_log2 = scale * 1.4426950408889634f;
+    p.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);  // (a score of zero times infinity would be NaN)
     // everything that can be refused comes before the first launch
     const bool few = p.few_rows > 0, many = most_rows > p.few_rows;
     PagedSplitParams ps;

@@ -734,11 +734,15 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             const int tile = tile_of_group(slot, group), n = tile ? w.n[1] : w.n[0];
             const int first_pos = w.first_pos(tile), last_pos = first_pos + w.tokens_of(tile) - 1;
             const int pos = first_pos + (row >> p.pack_log2);
-            float m_used = 0.f;   // running maximum in use, scaled to log2 units
+            float m_used = 0.f;   // running maximum in use; times c2_part it is in log2 units
             float l[2] = {0.f, 0.f};
+            // A product is multiplied with c2 = c2_power * c2_part, a power of two and 1 <= c2_part < 2.  The maximum goes with the power alone, which
+            // rounds nothing.
             float c2 = a.scale_log2;
+            const float c2_part = __uint_as_float((__float_as_uint(c2 < 1.17549435e-38f ? c2 * 0x1p64f : c2) & 0x007fffffu) | 0x3f800000u);
+            float c2_power = c2 / c2_part;
             int up = 0;              // 8 bits: the exponent of the row of Q
-            float ref = 0.f;         // 8 bits: r, the running maximum that O goes by
+            float delta = 0.f;       // 8 bits: r less the maximum.  (r itself, near 2^24, would lose V's power.)
             for (int j = 0; j < n; ++j, ++n_s) {
                 const int key0 = w.key_tile(j) * kTile;
                 if (!mbar_wait_uniform(&bars->s_full[group], n_s & 1, ctx, kWaitPagedFwd + 15)) { ok = false; break; }
@@ -746,8 +750,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 if constexpr (kE4M3) {
                     if (j == 0) up = sQExp[(2 * group + (n_it & 1)) * kTile + row];
                     c2 = score_factor(a.scale_log2, bars->tile_exp[(w.kv0 + 2 * j) % 16] - 6 - up);  // (K is 2^6 as large)
+                    c2_power = __uint_as_float(__float_as_uint(c2) & 0x7f800000u);
                 }
-                const uint64_t c2x2 = f2_pack(c2, c2);
                 uint32_t s[4][32];
                 tmem_ld_32x32(tS, s[0]);
                 tmem_ld_32x32(tS + 32, s[1]);
@@ -775,7 +779,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
 #pragma unroll
                     for (int e = 2; e < 32; e += 2) mx4[c] = fmax3(mx4[c], __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
                 }
-                const float m_new = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c2;
+                const float m_new = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c2_power;
                 // the P.V product of this tile's step before is done: P and O may be written
                 if (n_s > 0 && !mbar_wait_uniform(&bars->p_empty[group], (n_s - 1) & 1, ctx, kWaitPagedFwd + 17)) { ok = false; break; }
                 tc_fence_after();
@@ -788,12 +792,13 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 }
                 if (j == 0) {
                     m_used = fmaxf(m_new, kLeast);  // (a row can have no key in the first tile of a window)
-                    ref = m_used + v_exp;
+                    delta = v_exp;
                 } else {
-                    const bool need = (m_new - m_used) > kLazyRescale, need_o = kE4M3 ? (m_new + v_exp - ref) > kLazyRescale : need;
+                    const float up_m = (m_new - m_used) * c2_part;
+                    const bool need = up_m > kLazyRescale, need_o = kE4M3 ? up_m + v_exp - delta > kLazyRescale : need;
                     if (__any_sync(0xffffffffu, need || need_o)) {
-                        const float alpha_l = need ? fast_exp2(m_used - m_new) : 1.0f;
-                        const float alpha = kE4M3 ? (need_o ? fast_exp2(ref - (m_new + v_exp)) : 1.0f) : alpha_l;
+                        const float alpha_l = need ? fast_exp2(-up_m) : 1.0f;
+                        const float alpha = kE4M3 ? (need_o ? fast_exp2(delta - (up_m + v_exp)) : 1.0f) : alpha_l;
                         l[0] *= alpha_l, l[1] *= alpha_l;
 #pragma unroll 1
                         for (int c = 0; c < HD / 16; ++c) {
@@ -806,13 +811,19 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                             tmem_st_32x16(t_o, o);
                         }
                         if (need) m_used = m_new;
-                        if (need_o) ref = m_new + v_exp;
+                        if (need_o) delta = need ? v_exp : up_m + v_exp;
+                        else if (need) delta -= up_m;
                     }
                 }
                 // Exponents of the weights are x - m + shift.  (Below 2^-45 a weight is none in fp16; the sum still wants the weights.)
-                const float shift = kE4M3 ? 7.f + fmaxf(v_exp + m_used - ref, -60.f) : 0.f;
+                const float shift = kE4M3 ? 7.f + fmaxf(v_exp - delta, -60.f) : 0.f;
                 const float tile_up = kE4M3 ? fast_exp2(-shift) : 1.f;  // of the sums of the tile's weights
-                const uint64_t nm = f2_pack(shift - m_used, shift - m_used);
+                // Far from zero the product, which the fused multiply-add has in full, is off the rounded maximum by more than the weights' type takes
+                // (fp16 2^16, bf16 2^128).  There fp32 holds scores that are as far apart, or equal: the power alone, with which the maximum is exact,
+                // gives them weights of nothing, or 1.
+                const bool far = fabsf(m_used) >= (kE4M3 ? 0x1p22f : 0x1p29f);
+                const float by = far ? c2_power : c2, neg_m = fmaf(-m_used, far ? 1.f : c2_part, shift);
+                const uint64_t c2x2 = f2_pack(by, by), nm = f2_pack(neg_m, neg_m);
                 uint64_t sum[2];  // of a half of the tile: chains 0 and 1, chains 2 and 3 (see key_of_column in fwd_kernel.cu)
                 auto add_chunk = [&](int c) {
 #pragma unroll
@@ -855,17 +866,17 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             if (!ok || !mbar_wait_uniform(&bars->stat_empty[group], (n_it & 1) ^ 1, ctx, kWaitPagedFwd + 16)) break;
             ++n_it;
             const float sum_l = l[0] + l[1];
-            const float unit = kE4M3 ? fast_exp2(ref - m_used - 13.f) : 1.0f;  // (V is 2^6 and the weights are 2^7 as large)
+            const float unit = kE4M3 ? fast_exp2(delta - 13.f) : 1.0f;  // (V is 2^6 and the weights are 2^7 as large)
             sStat[group * kTile + row] = w.piece >= 0 ? unit : unit / sum_l;
             mbar_arrive_warp(&bars->stat_full[group]);
             if (w.piece >= 0) {
                 float* stats = piece_result<HD>(p, w.piece, tile) + kTile * HD;
-                stats[row] = m_used, stats[kTile + row] = sum_l;
+                stats[row] = fmaxf(m_used * c2_part, kLeast), stats[kTile + row] = sum_l;
                 continue;
             }
             const int token = row >> p.pack_log2, head = (w.group << p.pack_log2) + (row & ((1 << p.pack_log2) - 1));
             if (token < w.tokens_of(tile))  // natural-log sum-exp of the scaled scores
-                a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = (m_used + log2f(sum_l)) * 0.6931471805599453f;
+                a.lse[static_cast<long long>(head) * a.batch.T + w.row_of(tile) + token] = fmaf(m_used, c2_part, log2f(sum_l)) * 0.6931471805599453f;
         }
     }
 

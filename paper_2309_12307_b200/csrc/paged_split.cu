@@ -207,9 +207,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     float m[kRowTiles][2], l[kRowTiles][2];  // running maximum in use and this thread's part of the sum, rows 2 t and 2 t + 1
 #pragma unroll
     for (int r = 0; r < kRowTiles; ++r) m[r][0] = m[r][1] = kLeast, l[r][0] = l[r][1] = 0.f;
-    float ref[kRowTiles][2];  // 8 bits: r, see above
-#pragma unroll
-    for (int r = 0; r < kRowTiles; ++r) ref[r][0] = ref[r][1] = kLeast;
+    float delta[kRowTiles][2] = {};  // 8 bits: r - m, see above.  (Not r: near 2^24 the power of V would be lost in it.)
     bool ok = true;
     int c = 0, st = 0, phase = 0;  // step, its stage, and which use of the stage it is (odd or even)
     for (; c < steps; ++c) {
@@ -279,8 +277,9 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                     sc[u][r][x] *= scale[x >> 1];
                     if constexpr (kE4M3) sc[u][r][x] *= row_scale[r][x & 1];
                     if (masked && !attends(pos[r][x & 1], key0 + 16 * u + 8 * (x >> 1) + g, window, a.sinks)) sc[u][r][x] = -INFINITY;
-                    grows |= sc[u][r][x] > m[r][x & 1] + kLazy;
-                    if constexpr (kE4M3) grows |= sc[u][r][x] + v_exps[u][x >> 1] > ref[r][x & 1] + kLazy;
+                    const float over = sc[u][r][x] - m[r][x & 1];
+                    grows |= over > kLazy;
+                    if constexpr (kE4M3) grows |= over + v_exps[u][x >> 1] > delta[r][x & 1] + kLazy;
                 }
         }
         if (__any_sync(0xffffffffu, grows)) {
@@ -294,17 +293,19 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                     for (int u = 0; u < kTiles; ++u) top = fmax3(top, sc[u][r][h], sc[u][r][h + 2]);
 #pragma unroll
                     for (int off = 4; off < 32; off *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                    down[h] = fast_exp2(m[r][h] - top);
+                    const float up = top - m[r][h];
+                    down[h] = fast_exp2(-up);
                     m[r][h] = top;
                     l[r][h] *= down[h];
                     if constexpr (kE4M3) {
-                        top = ref[r][h];
+                        const float before = delta[r][h] - up;  // (of a row without a key so far -3e38, and all there is of it is zeros)
+                        top = before;
 #pragma unroll
-                        for (int u = 0; u < kTiles; ++u) top = fmax3(top, sc[u][r][h] + v_exps[u][0], sc[u][r][h + 2] + v_exps[u][1]);
+                        for (int u = 0; u < kTiles; ++u) top = fmax3(top, (sc[u][r][h] - m[r][h]) + v_exps[u][0], (sc[u][r][h + 2] - m[r][h]) + v_exps[u][1]);
 #pragma unroll
                         for (int off = 4; off < 32; off *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                        down[h] = fast_exp2(ref[r][h] - top);
-                        ref[r][h] = top;
+                        down[h] = fast_exp2(before - top);
+                        delta[r][h] = top;
                     }
                 }
 #pragma unroll
@@ -319,10 +320,11 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
                 float e[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    e[x] = fast_exp2(sc[u][r][x] - m[r][x & 1]);
+                    const float over = sc[u][r][x] - m[r][x & 1];
+                    e[x] = fast_exp2(over);
                     l[r][x & 1] += e[x];
                     // (a key that is not attended can have any exponent, also that of a row that is not finite)
-                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : fast_exp2(sc[u][r][x] + v_exps[u][x >> 1] - (ref[r][x & 1] - 7.f));
+                    if constexpr (kE4M3) e[x] = masked && sc[u][r][x] == -INFINITY ? 0.f : fast_exp2(over + v_exps[u][x >> 1] - (delta[r][x & 1] - 7.f));
                 }
                 w[u][r][0] = transpose_8x8(kE4M3 ? pack_f16(e[0], e[1]) : pack_bf16(e[0], e[1]));
                 w[u][r][1] = transpose_8x8(kE4M3 ? pack_f16(e[2], e[3]) : pack_bf16(e[2], e[3]));
@@ -392,7 +394,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row = 8 * r + 2 * t + h;
-            const float unit = kE4M3 ? fast_exp2(ref[r][h] - 7.f - m[r][h]) : 1.f;  // of O, beside the sum of weights
+            const float unit = kE4M3 ? fast_exp2(delta[r][h] - 7.f) : 1.f;  // of O, beside the sum of weights
 #pragma unroll
             for (int off = 4; off < 32; off *= 2) l[r][h] += __shfl_xor_sync(0xffffffffu, l[r][h], off);
             if (g == 0) mine[kM + row] = m[r][h], mine[kL + row] = l[r][h];

@@ -83,10 +83,20 @@ def test_keys_marked_as_not_finite_reach_no_token_before_them():
         assert torch.isnan(lse[:, 108:]).all() and s2a.device_status() == (0, 0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("scale", [2.0**-149, 2.0**-130, 2.0**-126, 2.0**127, 3e38])
+def test_the_least_and_the_largest_scales(scale, dtype):
+    for sizes, window in (([(1, 300), (30, 130)], 0), ([(200, 300)], 0), ([(200, 300), (1, 200)], 150)):
+        job = Job(sizes, H=4, Hkv=2, d=64, page=16, dtype=dtype)
+        if scale > 1:
+            zero_keys(job, "all")
+        job.check(scale=scale, window=window)
+
+
 # ---------------------------------------------------------------------------------------------- rows stay by themselves
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("sizes,power", [([(1, 300)], 20), ([(1, 300)], 40), ([(1, 300)], 100), ([(1, 40), (4, 500), (1, 1)], 20), ([(1, 40), (4, 500), (1, 1)], 40),
-                                         ([(1, 40), (4, 500), (1, 1)], 100), ([(200, 500)], 20)])
+                                         ([(1, 40), (4, 500), (1, 1)], 100), ([(200, 500)], 20), ([(200, 500)], 40), ([(200, 500)], 100)])
 def test_a_large_query_reaches_no_other_row(sizes, power, dtype):
     """One head's queries, and one token's, are 2^power times as large as the others of their KV head and sequence."""
     H, Hkv, d = 8, 2, 64
@@ -105,6 +115,26 @@ def test_a_large_query_reaches_no_other_row(sizes, power, dtype):
     rows = flat[0].shape[0]
     compare(flat[0], lse.cpu().T[~large][None], flat[1], want_lse.T[~large][None], flat[2], flat[3], torch.ones(rows, dtype=torch.bool), max(n for _, n in sizes), d, d**-0.5,
             q_norm, job.all_k)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("power", [0, 10, 14, 18, 22, 26, 30, 40, 90])
+@pytest.mark.parametrize("sizes", [[(1, 300), (1, 1)], [(4, 300)], [(200, 500), (1, 40)]], ids=["one", "drafts", "pieces"])
+def test_a_token_that_attends_itself_alone_has_its_own_value(sizes, power, dtype):
+    """The weight of the only key is 1, however large its score: sums of weights and of weighted values must go by the same maximum."""
+    H, Hkv, d = 4, 2, 64
+    job = Job(sizes, H=H, Hkv=Hkv, d=d, page=16, dtype=dtype)
+    job.q *= 2.0**power
+    o, lse = job.attend(window=1)
+    assert s2a.device_status() == (0, 0)
+    _, held = s2a.s2a_cache_read(job.cache, *job.where, tokens=job.T)
+    want = held.repeat_interleave(H // Hkv, 1).double()
+    # the weight and the result are rounded, to 8 bits at least, half a step each; the exponential is off by 2^-20 and less
+    assert ((o.double() - want).abs() <= (2 * 2.0**-8 + 2.0**-15) * want.abs()).all(), float(((o.double() - want).abs() / want.abs()).max())
+    k, _ = s2a.s2a_cache_read(job.cache, *job.where, tokens=job.T)
+    score = (job.q.double() * k.repeat_interleave(H // Hkv, 1).double()).sum(-1).T * d**-0.5
+    most = (job.q.double().norm(dim=-1) * k.repeat_interleave(H // Hkv, 1).double().norm(dim=-1)).T * d**-0.5
+    assert ((lse.double() - score).abs() <= most * d * 2.0**-24 + score.abs() * 2.0**-21 + 2.0**-20).all()
 
 
 # ---------------------------------------------------------------------------------------------- behind the window
