@@ -668,7 +668,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
                         if (!hidden.has(4 * lane + y)) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
-                    most = max(__reduce_max_sync(0xffffffffu, most), kExpLeast);
+                    // (of V no less than 2^-100: O's unit, 2^13 below it and divided by the sum of weights, is a number of fp32 then)
+                    most = max(__reduce_max_sync(0xffffffffu, most), is_v ? -100 : kExpLeast);
                     // A warp takes 32 rows, kRows at a time, 16 codes a lane.  Lane i has the factor of the warp's row i.
                     const int e = bars->exps[raw][32 * quad + lane];
                     const float f = e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(max(e - most + 6, -127));

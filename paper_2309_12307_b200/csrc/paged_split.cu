@@ -394,14 +394,15 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row = 8 * r + 2 * t + h;
-            const float unit = kE4M3 ? fast_exp2(delta[r][h] - 7.f) : 1.f;  // of O, beside the sum of weights
+            // unit^2 is O's, beside the sum of weights (which fp32's numbers reach, where exp2 does not)
+            const float unit = kE4M3 ? fast_exp2(0.5f * (delta[r][h] - 7.f)) : 1.f;
 #pragma unroll
             for (int off = 4; off < 32; off *= 2) l[r][h] += __shfl_xor_sync(0xffffffffu, l[r][h], off);
             if (g == 0) mine[kM + row] = m[r][h], mine[kL + row] = l[r][h];
 #pragma unroll
             for (int x = 0; x < HD / 16; ++x) {
                 float2* to = reinterpret_cast<float2*>(mine + row * HD + 2 * x / kCols * (8 * kCols) + kCols * g + 2 * x % kCols);
-                *to = make_float2(o[r][x][h] * unit, o[r][x][h + 2] * unit);
+                *to = make_float2(o[r][x][h] * unit * unit, o[r][x][h + 2] * unit * unit);
             }
         }
     __syncthreads();

@@ -93,6 +93,27 @@ def test_the_least_and_the_largest_scales(scale, dtype):
         job.check(scale=scale, window=window)
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("power", [-100, -108, -115, -120, -126])
+@pytest.mark.parametrize("sizes", [[(1, 300), (3, 40)], [(200, 300)], [(40, 3000)]], ids=["few", "pieces", "split pieces"])
+def test_values_near_the_least_number(sizes, power, dtype):
+    H, Hkv, d = 4, 2, 64
+    job = Job(sizes, H=H, Hkv=Hkv, d=d, page=16, dtype=dtype)
+    job.all_v *= 2.0**power
+    refill(job)
+    o, _ = job.attend()
+    assert s2a.device_status() == (0, 0)
+    want, _, size, largest = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5)
+    score = d * 2.0**-24 * d**-0.5 * float(job.q.double().norm(dim=-1).max()) * float(job.all_k.double().norm(dim=-1).max()) + 2.0**-20
+    longest = max(n for _, n in sizes)
+    # as in compare(), without its absolute slack.  The result's step is 2^-133 and more; values of a tile are fp16 numbers, times 2^6 and 2^-e with e no
+    # less than -100: steps of 2^-24 * 2^-106, half of one each (and as much again for sums in 32 bits that are as small).
+    allowed = (2.0**-8 + 2 * score + longest * 2.0**-24) * size + 2.0**-8 * (want.abs() + 2.0**-8 * size) + 2.0**-134 + 2.0**-32 * 448 * longest * largest[..., None]
+    allowed += 2.0**-130 if dtype == E4M3 else 2.0**-140
+    off = (o.cpu().double() - want).abs()
+    assert (off <= allowed).all(), float((off / allowed).max())
+
+
 # ---------------------------------------------------------------------------------------------- rows stay by themselves
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("sizes,power", [([(1, 300)], 20), ([(1, 300)], 40), ([(1, 300)], 100), ([(1, 40), (4, 500), (1, 1)], 20), ([(1, 40), (4, 500), (1, 1)], 40),
