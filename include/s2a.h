@@ -303,7 +303,12 @@ int s2a_cache_read(const s2a_cache* cache, const s2a_batch* batch, void* k, void
  * max_new (1 .. T) is the largest number of new tokens any sequence of the batch has; it chooses the kernels with T and the tokens
  * that a row of the table has room for, so tight values are fastest (max_new 1 where every sequence has one new token).  Any are right.
  * Scores and the weighted sum accumulate in fp32, weights are rounded to bf16 before the second product (over an S2A_CACHE_E4M3 cache to
- * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  What
+ * fp16, relative to the largest product of a weight and v's power of two: 11 bits down to 2^-21 of it, none below 2^-32).  Over such a cache
+ * the values of a query row count in full down to 2^-29 of its largest.  Where a sequence has more rows than a few (above 16 to 64 query heads of a
+ * KV head times new tokens) the same holds by blocks of 128 keys: that product is then the block's largest weight times its largest power, and a
+ * key's k (or v) counts in full where its power of two is 2^-21 of the block's largest or more, with values off by up to 2^-31 of that largest power
+ * below, and as zeros below 2^-30.  A block's largest is that of the keys that any of up to 256 neighbouring rows attends, so a later token of the
+ * call whose k or v is more than a million times as large can move the tokens before it by that much.  What
  * the cache holds where no new token of the sequence attends it, past the end and in front of the windows, does not matter; a NaN or infinity
  * that one of them attends can reach the outputs of the other new tokens of the same call and sequence.
  * Deterministic: no atomics.

@@ -11,18 +11,19 @@
 // One persistent block per SM, 512 threads, with the roles and the tensor-memory layout of s2a_fwd_kernel (fwd_kernel.cu), whose
 // comments say what they are for:
 //   warps 0-3, 4-7   softmax, two groups that take the tiles of an item in turn: one thread per score row
-//   warps 8-11       O / l -> bf16 -> global memory; with a cache in 8 bits also K and V to bf16
+//   warps 8-11       O / l -> bf16 -> global memory; with a cache in 8 bits also Q, K and V to fp16
 //   warp 12          work items (cluster launch control), pages and TMA loads, running ahead across items
 //   warps 13, 14     tcgen05 MMAs: S = Q K_j^T of both tiles in turn / O += P V_j
 // Tensor memory: O of either tile, P of either tile, then one score buffer (HD = 128) or two.
 //
 // 8-bit caches are multiplied in fp16, which has their values with room for a power of two.  TMA brings the codes to a ring of two raw tiles;
-// warps 8-11 write them where the products read them, each row times its power of two relative to the tile's largest (6 binary
-// places up: the tile's largest value is below 2^15 and values down to 2^-29 of it keep all their bits).  Q they turn from bf16 to fp16, each row times
+// warps 8-11 write them where the products read them, each row times its power of two relative to the tile's largest (6 binary places
+// up: the tile's largest value is below 2^15, rows whose power is 2^-21 of the largest keep all their bits, those below 2^-30 become zeros).  Q they turn from bf16 to fp16, each row times
 // a power of two that brings its largest value to [2^14, 2^15).  What is the tile's, or the row's, then multiplies scores and weights for
 // nothing: it goes into the constants of exp2(score * c - m).  With x a score in units of log2 and 2^e the tile's power of V the weight of
 // the second product is 2^(x + e - r + 7), r a running maximum of x + e of the row: the largest term's weight is 2^7 or more, those
-// down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), those below 2^-32 of it vanish.  O is in units of 2^(r - m), m being
+// down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), those below 2^-32 of it vanish.  (Largest of a tile means its largest weight
+// times its largest power: rows of V that a row does not attend count for it.)  O is in units of 2^(r - m), m being
 // the running maximum of x that the sum of weights goes by.  As bf16, values take five instructions instead of one and a half and the
 // four warps cannot keep up: 32k tokens, 2048 new ones, 64 heads over 8 3.03 ms.
 #include "paged_device.cuh"
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             __syncwarp();
         }
     } else if (warp >= 8) {
-        // =========================== read-out, codes to bf16 ==========================================
+        // =========================== read-out, codes to fp16 ==========================================
         setmaxnreg_dec<C::kRegsReadOut>();
         const int quad = warp & 3;
         const int row = quad * 32 + lane;

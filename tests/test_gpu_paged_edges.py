@@ -158,6 +158,43 @@ def test_a_token_that_attends_itself_alone_has_its_own_value(sizes, power, dtype
     assert ((lse.double() - score).abs() <= most * d * 2.0**-24 + score.abs() * 2.0**-21 + 2.0**-20).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("power", [12, 20, 26, 30])
+@pytest.mark.parametrize("sizes", [[(4, 100)], [(150, 170)], [(200, 3000)]], ids=["drafts", "pieces", "split pieces"])
+def test_how_far_a_later_token_moves_earlier_ones(sizes, power, dtype):
+    """The last token's k and v are 2^power times as large as the others'.  Only it attends itself; in 8 bits the tokens before it share its fp16 tile."""
+    H, Hkv, d, page = 4, 2, 64, 16
+    job = Job(sizes, H=H, Hkv=Hkv, d=d, page=page, dtype=dtype)
+    length = sizes[0][1]
+    others = job.all_k[:-1].clone()
+    job.all_k[-1] *= 2.0**power
+    job.all_v[-1] *= 2.0**power
+    refill(job)
+    o, lse = (t.cpu() for t in job.attend())
+    assert s2a.device_status() == (0, 0)
+    want, want_lse, size, largest = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5)
+    inside = torch.ones(job.T, dtype=torch.bool)
+    inside[-1] = False
+    o[-1], lse[:, -1] = 7, 7
+
+    def lost(exponents):
+        """What a value of the last 128 rows is off by at most: a row goes to fp16 times 2^(e - most + 6), most the largest e.  An 8-bit float is a multiple of
+        2^-9, so nothing is lost of multiples of 2^-24 (e >= most - 21).  Below that the product is rounded, by 2^-25 at most; and the factor, an
+        fp16 number itself, is no less than 2^-24 or zero (e < most - 30: values up to 448 * 2^e go)."""
+        j = torch.arange((length - 1) // 128 * 128, length)
+        e = exponents.cpu()[job.table.cpu()[0, j // page].long(), :, j % page].double()
+        off = torch.where(e >= e.max() - 21, 0.0, torch.where(e >= e.max() - 30, 2.0 ** (e.max() - 31), 448 * torch.exp2(e)))
+        return float(off.max())
+
+    off_k, off_v = (lost(job.cache.k_exp), lost(job.cache.v_exp)) if dtype == E4M3 and job.T > 16 else (0.0, 0.0)
+    q_norm = float(job.q.double().norm(dim=-1).max())
+    score = d**-0.5 * float(job.q.double().abs().sum(-1).max()) * off_k
+    # compare() allows 2^-8 of `size`, and of scores what their sums in 32 bits are off by, d * 2^-24 * scale * |q| |k|
+    size = size * (1 + 2.0**8 * 2 * score) + 2.0**8 * off_v
+    k_norm = float(others.double().norm(dim=-1).max()) + score / (d * 2.0**-24 * d**-0.5 * q_norm)
+    compare(o, lse, want, want_lse, size, largest, inside, length, d, d**-0.5, q_norm, torch.full((1, d), k_norm / math.sqrt(d), dtype=torch.float64))
+
+
 # ---------------------------------------------------------------------------------------------- behind the window
 def leave_behind(job, window, sinks, fill):
     """What no new token of a sequence attends, in front of its window, goes: table entries of whole pages, and the values of the other keys become
