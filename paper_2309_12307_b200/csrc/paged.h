@@ -78,9 +78,12 @@ __host__ __device__ inline int find_sequence(const int* starts, int B, int row) 
     return lo;
 }
 
+// Where the entries of sequence b begin in the table: past 32 bits in a large one.
+__host__ __device__ inline long long table_row(const PagedBatch& batch, int b) { return static_cast<long long>(b) * batch.width; }
+
 // Page of the tokens i * page_size on of sequence b, or -1 where the table holds none of the pool's.
 __host__ __device__ inline int page_of(const PagedBatch& batch, int pages, int b, int i) {
-    const int page = S2A_LOAD(batch.table + static_cast<long long>(b) * batch.width + i);
+    const int page = S2A_LOAD(batch.table + table_row(batch, b) + i);
     return static_cast<unsigned>(page) < static_cast<unsigned>(pages) ? page : -1;
 }
 

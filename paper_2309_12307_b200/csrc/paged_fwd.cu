@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 __syncwarp();
                 if (id < 0) break;
                 const int hk = p.by_groups_of_kv(w.group), length = w.pos + w.tokens[1];  // (keys behind the last token are nobody's)
-                const int* table = a.batch.table + static_cast<long long>(w.b) * a.batch.width;
+                const int* table = a.batch.table + table_row(a.batch, w.b);
                 const HiddenKeys hidden = w.hidden(0, window, a.sinks);
                 int row = -1, page = look_up(table, length, w.key_tile(0));
                 for (int j = 0; ok && j < w.n[1]; ++j) {

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
     auto look_up = [&](int c) {
         next_key = blocks.at(i0 + c * warps) * C::kKeys + (lane << piece_log2);
         const int at = (next_key < last_pos ? next_key : last_pos) >> a.pool.page_log2;
-        next_page = S2A_LOAD(a.batch.table + static_cast<long long>(b) * a.batch.width + at);
+        next_page = S2A_LOAD(a.batch.table + table_row(a.batch, b) + at);
     };
     auto request = [&](int c, int st) {
         int row = -1;  // of the pool: what this lane requests

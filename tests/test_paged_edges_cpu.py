@@ -16,6 +16,12 @@ def run_host(name, tmp_path):
 
 
 @pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(CUDA_INC), reason="needs g++ and the CUDA headers")
-@pytest.mark.parametrize("name", ["paged_hidden"])
+@pytest.mark.parametrize("name", ["paged_hidden", "paged_table"])
 def test_on_the_host(name, tmp_path):
     run_host(name, tmp_path)
+
+
+@pytest.mark.parametrize("name", ["paged.h", "paged_fwd.cu", "paged_split.cu", "cache_kernels.cu"])
+def test_entries_of_the_table_are_found_by_its_one_function(name):
+    text = open(os.path.join(CSRC, name)).read()
+    assert text.count("batch.table +") == text.count("batch.table + table_row(")
