@@ -74,10 +74,9 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_bwd();
         if (e != cudaSuccess) return cuda_fail(e);
-        e = configure_paged_split(ds.cluster_slots);
-        if (e != cudaSuccess) return cuda_fail(e);
-        e = configure_paged_fwd();
-        if (e != cudaSuccess) return cuda_fail(e);
+        ds.paged_error = configure_paged_split(ds.cluster_slots);
+        if (ds.paged_error == cudaSuccess) ds.paged_error = configure_paged_fwd();
+        if (ds.paged_error != cudaSuccess) cudaGetLastError();  // s2a_paged_fwd's to report, and no other call's
         e = cudaGetSymbolAddress(reinterpret_cast<void**>(&ds.status_ptr), g_status_word);
         if (e != cudaSuccess) return cuda_fail(e);
         if (!g_host_status_registered) {
@@ -92,6 +91,11 @@ int prepare_device(DeviceState** out) {
     }
     *out = &ds;
     return S2A_OK;
+}
+
+int prepare_paged(DeviceState** out) {
+    const int rc = prepare_device(out);
+    return rc != S2A_OK || (*out)->paged_error == cudaSuccess ? rc : cuda_fail((*out)->paged_error);
 }
 
 int standing_status(const DeviceState* ds) {

@@ -260,7 +260,7 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     if (!(scale > 0.f) || !isfinite(scale)) return S2A_ERR_INVALID_ARG;
     if ((rc = check_heads(cache, batch, H, max_new, window, sinks)) != S2A_OK) return rc;
     DeviceState* ds = nullptr;
-    if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
+    if ((rc = prepare_paged(&ds)) != S2A_OK) return rc;
     if ((rc = standing_status(ds)) != S2A_OK) return rc;
     const bool e4m3 = cache->type == S2A_CACHE_E4M3;
     const int longest = batch->width * cache->page_size;  // no sequence has more tokens
@@ -307,7 +307,7 @@ size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch,
     PagedTileParams p;
     memset(&p, 0, sizeof p);
     p.a = fwd_params(cache, batch, H, max_new, window, sinks);
-    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_device(&ds) != S2A_OK) return 0;
+    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_paged(&ds) != S2A_OK) return 0;
     if (!plan_tiles(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size, cache->d, key_bytes(cache))) return 0;
     return (static_cast<size_t>(p.slots) * (H >> p.pack_log2) - p.first_split) * p.split * paged_piece_bytes(cache->d);
 }

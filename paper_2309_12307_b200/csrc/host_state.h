@@ -15,6 +15,7 @@ struct DeviceState {
     volatile int* host_word = nullptr;  // this device's mirror, host address
     int* host_word_dev = nullptr;     // the same word as the device sees it
     int n_sm = 0;                     // multiprocessors
+    cudaError_t paged_error = cudaSuccess;  // what kept the paged cache's attention kernels from being set up
     int cluster_slots[4][17] = {};    // of the paged cache's splitting kernel, see configure_paged_split()
     // s2a_fwd_bwd_host only: copy streams and the events that order them against the caller's stream
     bool host_path_ready = false;
@@ -28,6 +29,8 @@ struct DeviceState {
 int cuda_fail(cudaError_t e);
 // Per-device set-up (once): architecture check, kernel attributes, address of the status word.
 int prepare_device(DeviceState** out);
+// The same for attention over the paged cache: an error too where its kernels could not be set up.
+int prepare_paged(DeviceState** out);
 // S2A_OK, or what an earlier launch on the device has reported and s2a_device_status() has not read yet.
 int standing_status(const DeviceState* ds);
 // Tensor map of `rank` dimensions over a tensor of `type`; strides (bytes) of all dimensions but the first.

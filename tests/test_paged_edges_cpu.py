@@ -25,3 +25,25 @@ def test_on_the_host(name, tmp_path):
 def test_entries_of_the_table_are_found_by_its_one_function(name):
     text = open(os.path.join(CSRC, name)).read()
     assert text.count("batch.table +") == text.count("batch.table + table_row(")
+
+
+def _body(text, head):
+    """The braces after `head`."""
+    i = text.index("{", text.index(head))
+    depth = 0
+    for x in range(i, len(text)):
+        depth += (text[x] == "{") - (text[x] == "}")
+        if depth == 0:
+            return text[i:x + 1]
+
+
+def test_what_keeps_the_paged_kernels_from_running_keeps_no_other():
+    """An error of the paged kernels' set-up is kept for s2a_paged_fwd; the device is ready all the same."""
+    api, paged = (open(os.path.join(CSRC, name)).read() for name in ("api.cu", "api_paged.cu"))
+    setup = _body(api, "int prepare_device(DeviceState** out)")
+    for line in setup.splitlines():
+        if "configure_paged" in line:
+            assert "ds.paged_error = configure_paged" in line and "return" not in line
+    assert setup.count("configure_paged") == 2 and "return cuda_fail(ds.paged_error)" not in setup and "cudaGetLastError();" in setup
+    assert "prepare_paged(" in _body(paged, "int s2a_paged_fwd(") and "prepare_device(" not in _body(paged, "int s2a_paged_fwd(")
+    assert "prepare_device(" in _body(paged, "int copy_impl(")
