@@ -442,8 +442,8 @@ def _check_cache_write(cache, k, v, table, starts, lengths):
 
 def _check_cache_read(cache, table, starts, lengths, tokens, k, v):
     device = _check_cache(cache, table, starts, lengths)
-    if tokens < 0 or tokens > 0x7FFFFFFF:
-        raise ValueError(f"tokens must be in [0, 2^31), not {tokens}")
+    if tokens < 1 or tokens > 0x7FFFFFFF:
+        raise ValueError(f"tokens must be in [1, 2^31), not {tokens}")
     for t, name in ((k, "k"), (v, "v")):
         if t is not None:
             _require(t, torch.bfloat16, name, shape=(tokens, cache.k.shape[1], cache.k.shape[3]), device=device)

@@ -378,7 +378,7 @@ py::object cache_read(py::handle kp, py::handle vp, py::handle ke, py::handle ve
                       py::handle k_, py::handle v_, std::optional<int64_t> stream) {
     PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
     Arg k(k_), v(v_);
-    if (k.bad || v.bad || !a.check() || !fits_int(tokens)) return py::none();
+    if (k.bad || v.bad || !a.check() || !fits_int(tokens) || tokens == 0) return py::none();
     a.batch.T = static_cast<int>(tokens);
     CallStream on(stream, a.k.t);
     const at::DimVector shape{tokens, a.cache.Hkv, a.cache.d};

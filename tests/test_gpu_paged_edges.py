@@ -231,3 +231,14 @@ def test_what_lies_behind_a_window_does_not_matter(form, window, sinks, fill, dt
         assert s2a.device_status() == (0, 0)
         compare(o.cpu(), lse.cpu(), want, want_lse, size, largest, job.rows(), max(n for _, n in sizes), d, d**-0.5, float(job.q.cpu()[job.rows()].double().norm(dim=-1).max()),
                 job.all_k)
+
+
+def test_no_rows_are_refused():
+    job = Job([(1, 20)])
+    with pytest.raises(ValueError, match="tokens must be in"):
+        s2a.s2a_cache_read(job.cache, *job.where, tokens=0)
+    empty = job.q[:0]
+    for call in (lambda: s2a.s2a_paged_fwd(empty, job.cache, *job.where), lambda: s2a.s2a_cache_write(job.cache, empty[:, :2].contiguous(), empty[:, :2].contiguous(), *job.where)):
+        with pytest.raises(s2a.S2AError) as e:
+            call()
+        assert e.value.status == s2a.S2A_ERR_INVALID_ARG

@@ -4,7 +4,9 @@ import shutil
 import subprocess
 
 import pytest
-from test_paged_cpu import CSRC, CUDA_INC, ROOT
+from test_paged_cpu import CSRC, CUDA_INC, ROOT, _cpu
+
+from paper_2309_12307_b200 import binding as s2a
 
 
 def run_host(name, tmp_path):
@@ -47,3 +49,13 @@ def test_what_keeps_the_paged_kernels_from_running_keeps_no_other():
     assert setup.count("configure_paged") == 2 and "return cuda_fail(ds.paged_error)" not in setup and "cudaGetLastError();" in setup
     assert "prepare_paged(" in _body(paged, "int s2a_paged_fwd(") and "prepare_device(" not in _body(paged, "int s2a_paged_fwd(")
     assert "prepare_device(" in _body(paged, "int copy_impl(")
+
+
+def test_no_rows_are_refused_with_the_range_that_the_library_takes(monkeypatch):
+    real = s2a._require
+    monkeypatch.setattr(s2a, "_require", lambda t, dtype, name, shape=None, device=None, cuda=True: real(t, dtype, name, shape, device, cuda=False))
+    cache, _, where = _cpu()
+    for tokens in (0, 1 << 31):
+        with pytest.raises(ValueError, match=r"tokens must be in \[1, 2\^31\)"):
+            s2a._check_cache_read(cache, *where, tokens, None, None)
+    s2a._check_cache_read(cache, *where, 1, None, None)
