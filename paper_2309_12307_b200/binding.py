@@ -461,7 +461,7 @@ def _check_paged_fwd(q, cache, table, starts, lengths, o, lse, workspace=None):
 
 
 def _pools(cache):
-    return (cache.k, cache.v, cache.k_exp, cache.v_exp) if cache.__class__ is PagedCache else (None,) * 4
+    return (cache.k, cache.v, cache.k_exp, cache.v_exp) if isinstance(cache, PagedCache) else (None,) * 4
 
 
 def s2a_cache_write(cache, k, v, table, starts, lengths, stream=None) -> None:

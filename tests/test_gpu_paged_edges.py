@@ -242,3 +242,13 @@ def test_no_rows_are_refused():
         with pytest.raises(s2a.S2AError) as e:
             call()
         assert e.value.status == s2a.S2A_ERR_INVALID_ARG
+
+
+def test_a_cache_of_a_derived_class_is_a_cache():
+    class Marked(s2a.PagedCache):
+        pass
+
+    job = Job([(1, 20), (3, 40)])
+    want = [t.clone() for t in job.attend()]
+    job.cache = Marked(job.cache.k, job.cache.v, job.cache.k_exp, job.cache.v_exp)
+    assert all(torch.equal(a, b) for a, b in zip(want, job.attend()))

@@ -59,3 +59,13 @@ def test_no_rows_are_refused_with_the_range_that_the_library_takes(monkeypatch):
         with pytest.raises(ValueError, match=r"tokens must be in \[1, 2\^31\)"):
             s2a._check_cache_read(cache, *where, tokens, None, None)
     s2a._check_cache_read(cache, *where, 1, None, None)
+
+
+def test_a_cache_of_a_derived_class_is_a_cache():
+    class Marked(s2a.PagedCache):
+        pass
+
+    cache, k, where = _cpu(codes=True)
+    marked = Marked(cache.k, cache.v, cache.k_exp, cache.v_exp)
+    assert all(a is b for a, b in zip(s2a._pools(marked), (cache.k, cache.v, cache.k_exp, cache.v_exp)))
+    assert s2a._pools((k, k)) == (None,) * 4
