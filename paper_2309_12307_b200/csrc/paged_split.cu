@@ -1,8 +1,8 @@
 // Attention of few rows over the paged cache: sequences with one new token, or a handful.
 //
 // A row is a new token and a query head; the rows of a sequence and KV head (new tokens times query heads of a KV head) read the
-// same keys.  With few of them, at most 64, the work is reading the cache: 4 d multiply-adds for each row and key against 4 d
-// bytes of bf16.  So the keys are split: a unit, 8 or 16 rows of one sequence and KV head, is worked on by a cluster of blocks, each
+// same keys.  With few of them, at most 64, the work is reading the cache: 2 d multiply-adds for each row and key against 4 d
+// bytes of bf16 for the key.  So the keys are split: a unit, 8 or 16 rows of one sequence and KV head, is worked on by a cluster of blocks, each
 // with a share of the keys, its warps taking 16 or 32 keys in turn.  A warp has a ring of its own that TMA fills, a
 // running maximum and sum for its rows and the weighted sum of v in registers.  What the warps and then the blocks have is
 // joined through shared memory and the cluster's: no second launch, no workspace, no atomics.

@@ -222,11 +222,6 @@ __device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) 
 // ---------------------------------------------------------------------------------------------
 // Thread-block clusters
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
