@@ -269,6 +269,8 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
     p.q = static_cast<const __nv_bfloat16*>(q), p.o = static_cast<__nv_bfloat16*>(o), p.lse = lse;
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     p.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);  // (a score of zero times infinity would be NaN)
+    const float half_part = frexpf(p.scale_log2, &p.scale_field);  // 0.5 <= half_part < 1
+    p.scale_part = 2 * half_part, p.scale_field += 126, p.scale_power = ldexpf(1.f, p.scale_field - 127);
     // everything that can be refused comes before the first launch
     const bool few = p.few_rows > 0, many = most_rows > p.few_rows;
     PagedSplitParams ps;

@@ -177,7 +177,9 @@ struct PagedFwdParams {
     int H, rep, most_new;
     int window, sinks;       // window 0: none
     int few_rows;            // sequences with at most so many rows are the splitting kernel's, the others the other one's
-    float scale_log2;
+    float scale_log2;                  // scale / ln 2 = scale_power * scale_part, a power of two (2^(scale_field - 127)) and 1 <= scale_part < 2
+    float scale_power, scale_part;
+    int scale_field;
 };
 
 constexpr int kMostSplit = 16;

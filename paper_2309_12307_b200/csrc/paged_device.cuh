@@ -28,14 +28,6 @@ __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(
 // 2^e, -127 (which stands for less than that) <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }
 
-// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, masked ones (-inf) and zeros too, so it must
-// neither vanish nor become infinite.  Sums of products of fp16 operands are below 2^38: where it is held from below they are scores below 2^-88.
-// (In two steps towards the result: a step of the other sign could lose bits that the result has.)
-__device__ __forceinline__ float score_factor(float x, int e) {
-    const int half = e >> 1;
-    return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
-}
-
 constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
 
 }  // namespace s2a

@@ -645,6 +645,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             for (int k = 0; ok; ++k) {
                 PagedItem w;
                 const bool more = next_item(k, kWaitPagedFwd + 11, &w);
+                const int front = kWindow ? w.hidden(0, window, a.sinks).to : 0;
                 const int tiles = more ? 2 * w.n[1] : 0, pause = tiles < C::kRing - 1 ? tiles : C::kRing - 1;
                 for (int x = 0; ok && x <= tiles; ++x) {
                     if (x == pause) {
@@ -661,14 +662,20 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         break;
                     }
                     const bool is_v = tile.is_v;
-                    const HiddenKeys hidden = w.hidden(w.key_tile(tile.j) * kTile, window, a.sinks);
+                    // only the last tile and those that begin in front of the window can have rows that are not attended
+                    const bool edge = tile.j == w.n[1] - 1 || (kWindow && w.key_tile(tile.j) * kTile < front);
                     const uint32_t src = smem_u32(sRaw + raw * C::kRawBytes), dst = smem_u32(sKV + st * C::kTileBytes);
                     // the largest exponent of the rows that are attended: four rows a lane
-                    const uint32_t four = *reinterpret_cast<const volatile uint32_t*>(&bars->exps[raw][4 * lane]);
+                    uint32_t four = *reinterpret_cast<const volatile uint32_t*>(&bars->exps[raw][4 * lane]);
+                    if (edge) {
+                        const HiddenKeys hidden = w.hidden(w.key_tile(tile.j) * kTile, window, a.sinks);
+#pragma unroll 1  // (rarely run, and beside the softmax code costs: 2048 new of 8192 tokens on 32 heads of 64 234 us when written out, 228 so)
+                        for (int y = 0; y < 4; ++y)
+                            if (hidden.has(4 * lane + y)) four = (four & ~(0xffu << (8 * y))) | 0x80u << (8 * y);  // kExpNotFinite
+                    }
                     int most = kExpNotFinite;
 #pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if (!hidden.has(4 * lane + y)) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
+                    for (int y = 0; y < 4; ++y) most = max(most, static_cast<int>(static_cast<int8_t>(four >> (8 * y))));
                     // (of V no less than 2^-100: O's unit, 2^13 below it and divided by the sum of weights, is a number of fp32 then)
                     most = max(__reduce_max_sync(0xffffffffu, most), is_v ? -100 : kExpLeast);
                     // A warp takes 32 rows, kRows at a time, 16 codes a lane.  Lane i has the factor of the warp's row i.
@@ -701,7 +708,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                         }
                         from += 2 * kRows * HD, to += 2 * kRows * 128;
                     }
-                    if (is_v && hidden.any(kTile)) {
+                    if (is_v && edge) {
+                        const HiddenKeys hidden = w.hidden(w.key_tile(tile.j) * kTile, window, a.sinks);
                         // rows that are not attended: whatever lies there (a weight of zero does not make a NaN go away)
                         __syncwarp();
 #pragma unroll 1
@@ -740,19 +748,22 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
             float l[2] = {0.f, 0.f};
             // A product is multiplied with c2 = c2_power * c2_part, a power of two and 1 <= c2_part < 2.  The maximum goes with the power alone, which
             // rounds nothing.
-            float c2 = a.scale_log2;
-            const float c2_part = __uint_as_float((__float_as_uint(c2 < 1.17549435e-38f ? c2 * 0x1p64f : c2) & 0x007fffffu) | 0x3f800000u);
-            float c2_power = c2 / c2_part;
-            int up = 0;              // 8 bits: the exponent of the row of Q
+            float c2 = a.scale_log2, c2_power = a.scale_power;
+            const float c2_part = a.scale_part;
+            int c2_exp = 0;          // 8 bits: the exponent field of c2 for a tile of K whose power is 2^0
             float delta = 0.f;       // 8 bits: r less the maximum.  (r itself, near 2^24, would lose V's power.)
             for (int j = 0; j < n; ++j, ++n_s) {
                 const int key0 = w.key_tile(j) * kTile;
                 if (!mbar_wait_uniform(&bars->s_full[group], n_s & 1, ctx, kWaitPagedFwd + 15)) { ok = false; break; }
                 tc_fence_after();
                 if constexpr (kE4M3) {
-                    if (j == 0) up = sQExp[(2 * group + (n_it & 1)) * kTile + row];
-                    c2 = score_factor(a.scale_log2, bars->tile_exp[(w.kv0 + 2 * j) % 16] - 6 - up);  // (K is 2^6 as large)
-                    c2_power = __uint_as_float(__float_as_uint(c2) & 0x7f800000u);
+                    // c2 = scale * 2^(K's exponent - 6 - that of the row of Q), K being 2^6 as large, held to the normal numbers: scores are multiplied with it,
+                    // masked ones (-inf) and zeros too, so it must neither vanish nor become infinite.  Products are below 2^38: held from below, scores
+                    // are below 2^-88.
+                    if (j == 0) c2_exp = a.scale_field - 6 - sQExp[(2 * group + (n_it & 1)) * kTile + row];
+                    const int e = min(max(c2_exp + bars->tile_exp[(w.kv0 + 2 * j) % 16], 1), 254);
+                    c2_power = __uint_as_float(static_cast<uint32_t>(e) << 23);
+                    c2 = c2_power * c2_part;
                 }
                 uint32_t s[4][32];
                 tmem_ld_32x32(tS, s[0]);

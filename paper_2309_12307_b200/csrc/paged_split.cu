@@ -67,6 +67,14 @@ __device__ __forceinline__ int lds_s8(uint32_t a) {
     asm volatile("ld.shared.s8 %0, [%1];" : "=r"(r) : "r"(a));
     return r;
 }
+// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, masked ones (-inf) and zeros too, so it must
+// neither vanish nor become infinite.  Sums of products of fp16 operands are below 2^38: where it is held from below they are scores below 2^-88.
+// (In two steps towards the result: a step of the other sign could lose bits that the result has.)
+__device__ __forceinline__ float score_factor(float x, int e) {
+    const int half = e >> 1;
+    return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
+}
+
 constexpr float kLazy = 8.0f;        // a running maximum (of log2) that is exceeded by less stays
 
 // kWindow: whether the call has one.  (Pages in front of a window are not asked for; where every call looks, one token over 100,000 of 32 heads in
