@@ -54,8 +54,8 @@ struct PagedCfg {
     static constexpr int kScoreBufs = (HD == 128) ? 1 : 2;
     static_assert(kColS + kScoreBufs * kTile <= kTmemCols, "tensor memory");
     // registers per thread after the split; the launch gives kRegsLaunch to each of the 512
-    // (the softmax, whose rows are in registers, can spare some for the warps that turn codes into operands: 32k tokens in 8 bits with 192, 80 and
-    // 48 2170 us, with 184, 88 and 56 2068, with these 2046)
+    // (the softmax, whose rows are in registers, can spare some for the warps that turn codes into operands: 32k tokens in 8 bits with 184, 88
+    // and 56 2150 us, with these 2095)
     static constexpr int kRegsLaunch = 128, kRegsSoftmax = kE4M3 && HD == 128 ? 176 : 184, kRegsReadOut = kE4M3 && HD == 128 ? 104 : 88, kRegsIssue = 56;
     static_assert(2 * kRegsSoftmax + kRegsReadOut + kRegsIssue <= 4 * kRegsLaunch, "register split");
 };
@@ -685,8 +685,8 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                     constexpr int kRows = 512 / HD;
                     const int src_row = is_v ? to_row : key_of_column(to_row);
                     uint32_t from = src + (32 * quad + src_row) * HD + part * 16, to = dst + (part >> 2) * C::kBoxBytes + (32 * quad + to_row) * 128;
-                    // (one short loop: written out, the code that the softmax warps run beside costs more than its branches, 604 against 467 us
-                    // for 1024 new tokens of 12,000 on 64 heads over 8)
+                    // (one short loop: written out, the code that the softmax warps run beside costs more than its branches, 2140 against 2095 us
+                    // for 2048 new tokens of 32k on 64 heads over 8)
 #pragma unroll 1
                     for (int i0 = 0; i0 < 32 / kRows; i0 += 2) {
                         uint32_t codes[2][4];
@@ -774,7 +774,7 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                 tc_fence_before();
                 mbar_arrive_warp(&bars->s_empty[C::kScoreBufs == 1 ? 0 : group]);
                 // (as bits of the columns: comparing positions for every score costs the steps that need no mask, whose code lies around it,
-                // as well: 2048 new of 8192 tokens on 32 heads 219 us instead of 204, 4096 with a window of 8192 on 40 697 instead of 568)
+                // as well: 4096 new tokens with a window of 8192 on 40 heads 752 us instead of 669, 2048 of 8192 on 32 237 instead of 235)
                 if (!all_attend(first_pos, last_pos, key0, kTile, window, a.sinks)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
