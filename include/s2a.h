@@ -254,9 +254,9 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
  * pages * Hkv * page_size must not exceed 2^31 - 1.
  *
  * A batch holds new tokens of B sequences.  Row starts[b] + i of its tensors is new token i of sequence b, which has
- * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows.  B, T and width are at least 1: a batch without a row is refused.  Rows that belong to no sequence are left as they
- * are in outputs, and what they hold in inputs does not matter.  lengths[b] counts the tokens that sequence b has in the cache INCLUDING its new ones, so new token i is at
- * position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
+ * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows.  (B, T and width are at least 1.)  Rows that belong to
+ * no sequence are left as they are in outputs, and what they hold in inputs does not matter.  lengths[b] counts the tokens that
+ * sequence b has in the cache INCLUDING its new ones, so new token i is at position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
  * (j + 1) * page_size - 1; entries past a sequence's last page are not used, and s2a_paged_fwd uses none of a page that no new token of the
  * sequence attends (in front of the windows: such pages may be given back).  Sequences may share pages, but not those that one call
  * writes to.

@@ -18,9 +18,9 @@
 //
 // 8-bit caches are multiplied in fp16, which has their values with room for a power of two.  TMA brings the codes to a ring of two raw tiles;
 // warps 8-11 write them where the products read them, each row times its power of two relative to the tile's largest (6 binary places
-// up: the tile's largest value is below 2^15, rows whose power is 2^-21 of the largest keep all their bits, those below 2^-30 become zeros).  Q they turn from bf16 to fp16, each row times
-// a power of two that brings its largest value to [2^14, 2^15).  What is the tile's, or the row's, then multiplies scores and weights for
-// nothing: it goes into the constants of exp2(score * c - m).  With x a score in units of log2 and 2^e the tile's power of V the weight of
+// up: the tile's largest value is below 2^15, rows whose power is 2^-21 of the largest keep all their bits, those below 2^-30 become zeros).
+// Q they turn from bf16 to fp16, each row times a power of two that brings its largest value to [2^14, 2^15).  What is the tile's, or the
+// row's, then multiplies scores and weights for nothing: it goes into the constants of exp2(score * c - m).  With x a score in units of log2 and 2^e the tile's power of V the weight of
 // the second product is 2^(x + e - r + 7), r a running maximum of x + e of the row: the largest term's weight is 2^7 or more, those
 // down to 2^-21 of it have all of fp16's 11 bits (bf16 has 8), those below 2^-32 of it vanish.  (Largest of a tile means its largest weight
 // times its largest power: rows of V that a row does not attend count for it.)  O is in units of 2^(r - m), m being
@@ -492,11 +492,10 @@ __global__ void __launch_bounds__(PagedCfg<HD, kE4M3>::kThreads, 1) s2a_paged_fw
                             // of zero does not make a NaN go away.  (8-bit tiles are written without them.)
                             const HiddenKeys hidden = w.hidden(w.key_tile(j) * kTile, window, a.sinks);
                             if (hidden.any(kTile)) {
+                                const uint32_t chunk = aKV + (x % C::kRing) * C::kTileBytes + (lane & 7) * 16;
                                 for (int key = lane >> 3; key < kTile; key += 4)
                                     for (int bx = 0; hidden.has(key) && bx < C::kBoxes; ++bx)
-                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(aKV + (x % C::kRing) * C::kTileBytes + bx * C::kBoxBytes + key * 128 + (lane & 7) * 16),
-                                                     "r"(0)
-                                                     : "memory");
+                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(chunk + bx * C::kBoxBytes + key * 128), "r"(0) : "memory");
                                 fence_proxy_async();
                                 __syncwarp();
                             }
@@ -977,7 +976,8 @@ template <int HD, bool kE4M3>
 static cudaError_t launch_one(const PagedTileParams& p, cudaStream_t stream) {
     const int items = p.slots * (p.a.H >> p.pack_log2), split_items = items - p.first_split;
     const unsigned grid = static_cast<unsigned>(p.first_split) + static_cast<unsigned>(split_items) * static_cast<unsigned>(p.split);
-    const cudaError_t e = launch_kernel(p.a.window > 0 ? s2a_paged_fwd_kernel<HD, kE4M3, true> : s2a_paged_fwd_kernel<HD, kE4M3, false>, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
+    const auto kernel = p.a.window > 0 ? s2a_paged_fwd_kernel<HD, kE4M3, true> : s2a_paged_fwd_kernel<HD, kE4M3, false>;
+    const cudaError_t e = launch_kernel(kernel, grid, PagedCfg<HD, kE4M3>::kThreads, PagedCfg<HD, kE4M3>::kSmemBytes, stream, p, true);
     if (e != cudaSuccess || split_items == 0) return e;
     return launch_kernel(s2a_paged_join_kernel<HD>, 2u * JoinCfg<HD>::kBlocks * static_cast<unsigned>(split_items), JoinCfg<HD>::kThreads, 0, stream, p, true);
 }

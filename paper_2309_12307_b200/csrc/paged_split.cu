@@ -67,9 +67,8 @@ __device__ __forceinline__ int lds_s8(uint32_t a) {
     asm volatile("ld.shared.s8 %0, [%1];" : "=r"(r) : "r"(a));
     return r;
 }
-// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, masked ones (-inf) and zeros too, so it must
-// neither vanish nor become infinite.  Sums of products of fp16 operands are below 2^38: where it is held from below they are scores below 2^-88.
-// (In two steps towards the result: a step of the other sign could lose bits that the result has.)
+// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, zeros and infinite ones too, so it must neither
+// become infinite nor vanish.  (In two steps towards the result: a step of the other sign could lose bits that the result has.)
 __device__ __forceinline__ float score_factor(float x, int e) {
     const int half = e >> 1;
     return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
