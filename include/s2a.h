@@ -326,6 +326,68 @@ int s2a_paged_fwd(const void* q, const s2a_cache* cache, const s2a_batch* batch,
 size_t s2a_paged_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks);
 
 /*
+ * Norms of queries and keys for each head, and the rotation of positions, in one pass: what stands between a model's projections and s2a_fwd, or
+ * the paged cache.  (The paper's models rotate queries and keys by their positions, which it interpolates: Section 3.1 and the experimental
+ * settings.  It gives no code for that.)
+ *
+ * For a row x, the d values of one head of token t, which stands at position p:
+ *   y = w * x / sqrt(mean of x^2 + eps)          with `norm`, w the weight of q or of k (all ones where it is NULL); else y = x
+ *   the first r values of y are r / 2 pairs (u, v), of which pair i turns by a = 2 pi p turns[i] / 2^64:
+ *   (u, v) -> (u cos a - v sin a, u sin a + v cos a)
+ * and the other values stay.  Arithmetic is fp32, results are rounded to bf16 once.  An angle is off by no more than 10^-7 at any position.  A row with
+ * a NaN comes out as NaN with a norm; one with an infinity, but for zeros, too.  (A row of zeros with eps = 0 is 0 / 0.)
+ */
+enum { S2A_WEIGHT_BF16 = 0, S2A_WEIGHT_F32 = 1 };
+typedef struct s2a_rotation {
+    const long long* turns; /* device [r / 2], 8-byte aligned: round(2^64 * radians of a position / (2 pi)), modulo 2^64.  The usual frequencies, with
+                               positions interpolated by `s`, are s * base^(-2 i / r) radians for pair i.  May be NULL where r = 0 */
+    const int* positions;   /* device [n_positions], any 32-bit numbers: row t stands at positions[t % n_positions].  NULL: at t % n_positions, for
+                               s2a_rotate_write at the token's place in the cache */
+    int n_positions;        /* >= 1 (s2a_rotate_write without positions: ignored) */
+    int r;                  /* values of a row that are rotated: a multiple of 16, 0 .. d */
+    int interleaved;        /* 0: pair i is values i and i + r / 2; 1: values 2 i and 2 i + 1 */
+    int norm;               /* 0 or 1; what follows is read with 1 only, and weights must be NULL with 0 */
+    int weight_type;        /* S2A_WEIGHT_... */
+    const void* q_weight;   /* device [d], 16-byte aligned, or NULL */
+    const void* k_weight;
+    float eps;              /* >= 0 */
+} s2a_rotation;
+
+/*
+ * q [T, H, d] and k [T, Hkv, d] (bf16) -> q_out, k_out of the same shapes.  d in {64, 128}; H need not be a multiple of Hkv.  *_stride: values from a token to the next,
+ * a multiple of 8 and at least heads * d (T = 1: ignored), so that the slices of a projection's output [T, H + 2 Hkv, d], or of qkv [B, N, 3, H, d], are taken and
+ * written as they lie.  An output may be its input (same pointer and stride); otherwise the four must not overlap.  T * (H + 2 Hkv) must not exceed 2^31 - 1.
+ * One kernel launch.
+ */
+int s2a_rotate(const void* q, long long q_stride, const void* k, long long k_stride, void* q_out, long long q_out_stride, void* k_out,
+               long long k_out_stride, const s2a_rotation* rotation, int T, int H, int Hkv, int d, void* stream);
+
+/*
+ * Gradients of sum(q_out * dq_out) + sum(k_out * dk_out) of s2a_rotate.
+ *   in : q, k (what s2a_rotate was given; without a norm they are not read and may be NULL), dq_out, dk_out (strides as above)
+ *   out: dq [T, H, d], dk [T, Hkv, d] (bf16, dense, overwritten; each may be its dense dq_out or dk_out), dq_weight, dk_weight [d] (fp32, overwritten; NULL where not wanted, and
+ *        without a norm)
+ *   workspace: with a norm at least s2a_rotate_bwd_workspace_bytes(d), 256-byte aligned; its contents before the call do not matter, and calls that can
+ *        overlap on the GPU need one each.  Without a norm it is not looked at.
+ * The weights' gradients are sums in fp32 over all tokens and heads, in an order that the sizes and the device fix: deterministic, no atomics.  One launch without a norm, two
+ * with one.
+ */
+int s2a_rotate_bwd(const void* q, long long q_stride, const void* k, long long k_stride, const void* dq_out, long long dq_out_stride, const void* dk_out,
+                   long long dk_out_stride, void* dq, void* dk, float* dq_weight, float* dk_weight, const s2a_rotation* rotation, int T, int H, int Hkv,
+                   int d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of scratch that s2a_rotate_bwd needs with a norm on the current device (0: d is not supported, or the device). */
+size_t s2a_rotate_bwd_workspace_bytes(int d);
+
+/*
+ * The same for new tokens that are served: q [T, H, d] -> q_out (dense), k [T, Hkv, d], rotated, and v as it is into their places in the cache, in one
+ * launch.  Bit for bit s2a_rotate and then s2a_cache_write.  Strides are those of s2a_rotate.  The cache's rules apply: what the batch holds is checked on the device, rows of no
+ * sequence are left as they are.  A cache that tokens have been evicted from holds fewer tokens than the sequence has had: then positions are given.  q_out may be q where it is dense.
+ */
+int s2a_rotate_write(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride, void* q_out,
+                     const s2a_rotation* rotation, const s2a_cache* cache, const s2a_batch* batch, int H, void* stream);
+
+/*
  * Diagnostic (the paper has no counterpart): enqueues one tiny kernel on `stream` in which a single
  * warp waits, with the library's own bounded wait and a limit of `limit_cycles` SM clock cycles
  * (1 .. 2,000,000,000; a million is well under a millisecond), on a barrier that nothing ever arrives

@@ -1,4 +1,4 @@
-"""torch.autograd front end of S2-Attn (Algorithm 1 of the LongLoRA paper).
+"""torch.autograd front end of S2-Attn (Algorithm 1 of the LongLoRA paper) and of the rotation in front of it.
 
 `s2_attn(q, k, v, G)` behaves like a differentiable function of q [B,N,H,d] and k, v [B,N,Hkv,d]
 (bf16, CUDA, contiguous): the forward runs `s2a_fwd_ex`, the backward `s2a_bwd_ex`.  Everything is
@@ -29,6 +29,27 @@ def s2_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, G: int, *, scale:
     if o is None:
         binding._result(o, "s2_attn", _check, q, k, v)
     return o if q.__class__ in binding._PLAIN else binding._typed((o,), (q,))[0]
+
+
+def s2_rotate(q: torch.Tensor, k: torch.Tensor, turns: torch.Tensor, positions: torch.Tensor | None = None, *, q_weight: torch.Tensor | None = None,
+              k_weight: torch.Tensor | None = None, eps: float | None = None, interleaved: bool = False):
+    """(q, k) normalised for each head (with `eps`) and rotated by their positions, as s2_attn takes them: a differentiable function of q [.., H, d],
+    k [.., Hkv, d] and the norms' weights.  Arguments as in `binding.s2a_rotate`; the weights' gradients are summed in fp32 and
+    have the weights' type.  A step that is captured into a CUDA graph needs, as with every function of torch's autograd, that no graph of the same
+    leaves from another stream is alive."""
+    args = q, k, turns, positions, q_weight, k_weight, eps
+    hot = binding._hot or binding._hot_for(_check_rotate, *args)
+    r = hot.s2_rotate(*args, bool(interleaved))
+    if r.__class__ is not tuple:
+        binding._result(r, "s2_rotate", _check_rotate, *args)
+    return r if q.__class__ in binding._PLAIN and k.__class__ in binding._PLAIN else binding._typed(r, (q, k))
+
+
+def _check_rotate(q, k, *args) -> None:
+    for t, name in ((q, "q"), (k, "k")):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} must be a torch.Tensor")
+    binding._check_rotate(q.contiguous(), k.contiguous(), *args)
 
 
 def _check(q, k, v) -> None:

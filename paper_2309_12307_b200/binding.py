@@ -10,7 +10,9 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import os
+from fractions import Fraction
 
 import torch
 
@@ -28,7 +30,7 @@ S2A_ERR_BAD_INDEX = -6
 EXPORTS = [
     "s2a_fwd", "s2a_bwd", "s2a_bwd_workspace_bytes", "s2a_bwd_workspace_bytes_fast", "s2a_fwd_ex", "s2a_bwd_ex", "s2a_bwd_stage", "s2a_fwd_bwd_host",
     "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed", "s2a_cache_write", "s2a_cache_read", "s2a_paged_fwd",
-    "s2a_paged_workspace_bytes",
+    "s2a_paged_workspace_bytes", "s2a_rotate", "s2a_rotate_bwd", "s2a_rotate_bwd_workspace_bytes", "s2a_rotate_write",
     "s2a_selftest_wait_expiry", "s2a_device_status", "s2a_status_string", "s2a_last_cuda_error", "s2a_version",
 ]
 
@@ -86,6 +88,15 @@ def load() -> ctypes.CDLL:
     lib.s2a_paged_workspace_bytes.argtypes = [P, P, I, I, I, I]
     lib.s2a_paged_workspace_bytes.restype = Z
     lib.s2a_paged_fwd.restype = I
+    L = ctypes.c_longlong  # (the rotation is passed by reference too)
+    lib.s2a_rotate.argtypes = [P, L, P, L, P, L, P, L, P, I, I, I, I, P]
+    lib.s2a_rotate.restype = I
+    lib.s2a_rotate_bwd.argtypes = [P, L, P, L, P, L, P, L, P, P, P, P, P, I, I, I, I, P, Z, P]
+    lib.s2a_rotate_bwd.restype = I
+    lib.s2a_rotate_bwd_workspace_bytes.argtypes = [I]
+    lib.s2a_rotate_bwd_workspace_bytes.restype = Z
+    lib.s2a_rotate_write.argtypes = [P, L, P, L, P, L, P, P, P, P, I, P]
+    lib.s2a_rotate_write.restype = I
     lib.s2a_selftest_wait_expiry.argtypes = [ctypes.c_longlong, P]
     lib.s2a_selftest_wait_expiry.restype = I
     lib.s2a_device_status.argtypes = [ctypes.POINTER(I)]
@@ -500,6 +511,124 @@ def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, wi
     if r.__class__ is not tuple:
         _result(r, "s2a_paged_fwd", _check_paged_fwd, q, cache, table, starts, lengths, o, lse, workspace)
     return r if q.__class__ in _PLAIN else _typed(r, (None if o is not None else q, None))
+
+
+def rotary_turns(r: int, base: float = 10000.0, scale: float = 1.0, device="cuda"):
+    """The frequencies of the usual rotation of r values of a head, int64 [r / 2]: pair i turns by scale * base^(-2 i / r) radians from one position to
+    the next, in units of 2^-64 of a full turn.  `scale` interpolates positions (the length a model was trained on / the length it is extended to)."""
+    if r < 0 or r % 2 != 0:
+        raise ValueError(f"r must be an even number of values, not {r}")
+    if not base > 0 or not math.isfinite(base) or not math.isfinite(scale):
+        raise ValueError(f"base must be above zero and scale a number, not {base} and {scale}")
+    return turns_of([scale * base ** (-2 * i / r) for i in range(r // 2)], device)
+
+
+def turns_of(radians, device="cuda"):
+    """The same of any frequencies, numbers of radians from one position to the next (frequency-dependent scalings, for instance)."""
+    turns = [round(Fraction(f / (2 * math.pi)) * 2**64) % 2**64 for f in radians]
+    return torch.tensor([t - 2**64 if t >= 2**63 else t for t in turns], dtype=torch.int64).to(device)
+
+
+def _require_rows(x, name: str, shape=None, device=None):
+    """x [.., heads, d] whose tokens are at one distance from one another, like a slice of a projection's output."""
+    if not isinstance(x, torch.Tensor):
+        raise ValueError(f"{name} must be a torch.Tensor")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if x.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must have dtype {torch.bfloat16}, not {x.dtype}")
+    if x.dim() < 3 or x.numel() == 0:
+        raise ValueError(f"{name} must be [.., heads, d] with at least one token, not {tuple(x.shape)}")
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+    if device is not None and x.device != device:
+        raise ValueError(f"{name} must be on {device}, not {x.device}")
+    dims = [(n, s) for n, s in zip(x.shape[:-2], x.stride()[:-2]) if n > 1]
+    if (x.stride(-1) != 1 and x.shape[-1] > 1) or (x.stride(-2) != x.shape[-1] and x.shape[-2] > 1) or any(a[1] != b[0] * b[1] for a, b in zip(dims, dims[1:])):
+        raise ValueError(f"{name} must have dense heads and tokens at one distance, not strides {x.stride()}")
+
+
+def _check_rotation(q, turns, positions, q_weight, k_weight, eps, in_cache=False):
+    d, device, tokens = q.shape[-1], q.device, tuple(q.shape[:-2])
+    _require(turns, torch.int64, "turns", device=device)
+    if turns.dim() != 1 or 2 * turns.shape[0] > d:
+        raise ValueError(f"turns must be [r / 2] with r <= {d}, not {tuple(turns.shape)}")
+    if positions is not None:
+        _require(positions, torch.int32, "positions", device=device)
+        all_tokens = math.prod(tokens)
+        if positions.numel() != all_tokens and (in_cache or positions.numel() != tokens[-1]):
+            raise ValueError(f"positions must be one for each of the tokens {tokens}, or of their last dimension, not {tuple(positions.shape)}")
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("q_weight and k_weight belong to a norm, which is made where eps is given")
+    some = q_weight if q_weight is not None else k_weight
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            if isinstance(some, torch.Tensor) and some.dtype not in (torch.bfloat16, torch.float32):
+                raise ValueError(f"{name} must have dtype {torch.bfloat16} or {torch.float32}, not {some.dtype}")
+            _require(w, getattr(some, "dtype", None), name, shape=(d,), device=device)
+
+
+def _check_rotate(q, k, turns, positions, q_weight, k_weight, eps, q_out=None, k_out=None, names=("q", "k")):
+    _require_rows(q, names[0])
+    _require_rows(k, names[1], device=q.device)
+    if k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or k.shape[-1] != q.shape[-1]:
+        raise ValueError(f"{names[1]} must be {(*q.shape[:-2], 'Hkv', q.shape[-1])}, not {tuple(k.shape)}")
+    _check_rotation(q, turns, positions, q_weight, k_weight, eps)
+    for t, name, like in ((q_out, "q_out", q), (k_out, "k_out", k)):
+        if t is not None:
+            _require_rows(t, name, shape=like.shape, device=q.device)
+
+
+def _check_rotate_bwd(q, k, dq_out, dk_out, turns, positions, q_weight, k_weight, eps):
+    _check_rotate(dq_out, dk_out, turns, positions, q_weight, k_weight, eps, names=("dq_out", "dk_out"))
+    if eps is not None:
+        _require_rows(q, "q", shape=dq_out.shape, device=dq_out.device)
+        _require_rows(k, "k", shape=dk_out.shape, device=dq_out.device)
+
+
+def _check_rotate_write(cache, q, k, v, turns, table, starts, lengths, positions, q_weight, k_weight, eps, q_out):
+    device = _check_cache(cache, table, starts, lengths)
+    d = cache.k.shape[3]
+    for x, name, heads in ((q, "q", None), (k, "k", cache.k.shape[1]), (v, "v", cache.k.shape[1])):
+        _require_rows(x, name, device=device)
+        if x.dim() != 3 or x.shape[2] != d or (heads is not None and x.shape[1] != heads) or x.shape[0] != q.shape[0]:
+            raise ValueError(f"{name} must be [{'T' if x is q else q.shape[0]}, {'H' if heads is None else heads}, {d}], not {tuple(x.shape)}")
+    _check_rotation(q, turns, positions, q_weight, k_weight, eps, in_cache=True)
+    if q_out is not None:
+        _require(q_out, torch.bfloat16, "q_out", shape=q.shape, device=device)
+
+
+def s2a_rotate(q, k, turns, positions=None, q_weight=None, k_weight=None, eps=None, interleaved=False, q_out=None, k_out=None, stream=None):
+    """q [.., H, d] and k [.., Hkv, d] with the first 2 * len(turns) values of every head rotated by its token's position; with `eps` every head's row is
+    normalised first (times q_weight, k_weight [d] in bf16 or fp32 where they are given).  `turns` as rotary_turns() makes it.  `positions` (int32): one for each
+    token, or for each of the last dimension of tokens; default 0, 1, .. along that.  Pairs are values i and i + r / 2, or neighbours (`interleaved`).
+    Tokens may be at any one distance (slices of a projection's output); q_out may be q, and k_out k."""
+    args = q, k, turns, positions, q_weight, k_weight, eps
+    hot = _hot or _hot_for(_check_rotate, *args, q_out, k_out)
+    r = hot.rotate(*args, bool(interleaved), q_out, k_out, _given_stream(stream))
+    if r.__class__ is not tuple:
+        _result(r, "s2a_rotate", _check_rotate, *args, q_out, k_out)
+    return r if q.__class__ in _PLAIN and k.__class__ in _PLAIN else _typed(r, (None if q_out is not None else q, None if k_out is not None else k))
+
+
+def s2a_rotate_bwd(q, k, dq_out, dk_out, turns, positions=None, q_weight=None, k_weight=None, eps=None, interleaved=False, stream=None):
+    """dq, dk (bf16) and the gradients of q_weight and k_weight (fp32; None for one that is not given) of sum(q_out * dq_out) + sum(k_out * dk_out) of
+    s2a_rotate with the same arguments.  Without `eps` q and k are not looked at."""
+    args = q, k, dq_out, dk_out, turns, positions, q_weight, k_weight, eps
+    hot = _hot or _hot_for(_check_rotate_bwd, *args)
+    return _result(hot.rotate_bwd(*args, bool(interleaved), _given_stream(stream)), "s2a_rotate_bwd", _check_rotate_bwd, *args)
+
+
+def s2a_rotate_write(cache, q, k, v, turns, table, starts, lengths, positions=None, q_weight=None, k_weight=None, eps=None, interleaved=False, q_out=None,
+                     stream=None):
+    """q_out [T, H, d]: the new tokens' q rotated (s2a_rotate); their k, rotated, and v go into the pages of `cache` as s2a_cache_write puts them there.  `positions`
+    (int32 [T]): default the tokens' places in the cache, which is where they stand unless tokens have been evicted."""
+    args = cache, q, k, v, turns, table, starts, lengths, positions, q_weight, k_weight, eps
+    hot = _hot or _hot_for(_check_rotate_write, *args, q_out)
+    r = hot.rotate_write(*_pools(cache), *args[1:], bool(interleaved), q_out, _given_stream(stream))
+    if r is None or r.__class__ is int:
+        _result(r, "s2a_rotate_write", _check_rotate_write, *args, q_out)
+    return r if q.__class__ in _PLAIN else _typed((r,), (None if q_out is not None else q,))[0]
 
 
 def selftest_wait_expiry(limit_cycles: int = 1_000_000, stream=None) -> None:

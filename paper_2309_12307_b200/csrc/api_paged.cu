@@ -6,14 +6,16 @@
 #include <algorithm>
 
 #include "../../include/s2a.h"
+#include "host_paged.h"
 #include "host_state.h"
 #include "paged.h"
 #include "s2a_params.h"
 
 namespace s2a {
-namespace {
 
+namespace {
 constexpr long long kIntMax = 0x7fffffffLL;
+}  // namespace
 
 int check_cache(const s2a_cache* c) {
     if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return S2A_ERR_INVALID_ARG;
@@ -46,6 +48,8 @@ PagedPool pool_of(const s2a_cache* c) {
     while ((1 << r.page_log2) < c->page_size) ++r.page_log2;
     return r;
 }
+
+namespace {
 
 // The rows of a pool, as lines of 128 bytes (or of a row, where that is less); a box is `keys` rows, or a page where that is less, one line after
 // the other.  See swizzled() for how a line's box lies in shared memory.

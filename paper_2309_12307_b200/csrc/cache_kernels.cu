@@ -99,30 +99,9 @@ __global__ void __launch_bounds__(kCopyThreads) s2a_cache_copy_kernel(const __gr
                 }
             } else if constexpr (kWrite) {
                 const uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
-                uint32_t pair = 0;  // the largest magnitudes of either half (a NaN stays one)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(pair) : "r"(w[c] & 0x7fff7fffu));
-                uint32_t most = max(pair & 0xffffu, pair >> 16);
                 // (all lanes of a warp are here: a block's rows are gone through in whole turns)
-#pragma unroll
-                for (int off = C::kLanes / 2; off > 0; off >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
-                const int exp = row_exponent(most);
-                uint32_t codes[4] = {};
-                if (exp != kExpNotFinite) {
-                    const float down = __uint_as_float(static_cast<uint32_t>(127 - exp) << 23);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint16_t two[2];
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            float a = bf16_low(w[2 * c + y]) * down, b = bf16_high(w[2 * c + y]) * down;
-                            // 256 * 2^120 would be no bf16 number: the next smaller code
-                            if (exp == 120) a = fminf(fmaxf(a, -240.f), 240.f), b = fminf(fmaxf(b, -240.f), 240.f);
-                            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[y]) : "f"(b), "f"(a));
-                        }
-                        asm("mov.b32 %0, {%1, %2};" : "=r"(codes[c]) : "h"(two[0]), "h"(two[1]));
-                    }
-                }
+                uint32_t codes[4];
+                const int exp = row_to_e4m3<C::kLanes>(w, codes);
                 if (cached[i]) {
                     *cached[i] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
                     if (part == 0) *exponent[i] = static_cast<int8_t>(exp);

@@ -429,6 +429,178 @@ py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke,
 }
 
 // ---------------------------------------------------------------------------------------------
+// norms and rotation of queries and keys
+// ---------------------------------------------------------------------------------------------
+// x [.., heads, d] of bf16, tokens at one distance from one another: that distance in values, or nothing
+std::optional<int64_t> token_stride(const Tensor& x) {
+    if (!x.defined() || !x.is_cuda() || x.scalar_type() != at::kBFloat16 || x.dim() < 3 || x.numel() == 0) return {};
+    const int64_t n = x.dim(), d = x.size(n - 1);
+    if ((d > 1 && x.stride(n - 1) != 1) || (x.size(n - 2) > 1 && x.stride(n - 2) != d)) return {};
+    int64_t stride = x.size(n - 2) * d, next = -1;  // (a single token's does not matter)
+    for (int64_t i = n - 3; i >= 0; --i) {
+        if (x.size(i) == 1) continue;
+        if (next < 0) stride = x.stride(i), next = stride;
+        else if (x.stride(i) != next) return {};
+        next *= x.size(i);
+    }
+    return stride;
+}
+
+bool rows_like(const Tensor& x, const Tensor& like) { return token_stride(x) && x.sizes() == like.sizes() && x.device() == like.device(); }
+
+struct HeadSizes {
+    int64_t T, N, H, Hkv, d;  // tokens, those of the last dimension of tokens
+};
+// q [.., H, d] and k [.., Hkv, d]
+std::optional<HeadSizes> head_sizes(const Tensor& q, const Tensor& k) {
+    if (!token_stride(q) || !token_stride(k) || k.device() != q.device() || k.dim() != q.dim()) return {};
+    const int64_t n = q.dim();
+    if (q.sizes().slice(0, n - 2) != k.sizes().slice(0, n - 2) || q.size(n - 1) != k.size(n - 1)) return {};
+    const HeadSizes s{c10::multiply_integers(q.sizes().slice(0, n - 2)), q.size(n - 3), q.size(n - 2), k.size(n - 2), q.size(n - 1)};
+    for (int64_t x : {s.T, s.H, s.Hkv, s.d})
+        if (!fits_int(x)) return {};
+    return s;
+}
+
+// What a rotation is made of; tensors that are not there are undefined.
+struct RotationArgs {
+    Tensor turns, positions, q_weight, k_weight;
+    std::optional<double> eps;
+    bool interleaved = false;
+    // false: binding.py names what is wrong.  `N` 0: without positions the cache says where tokens stand.
+    bool fill(s2a_rotation* r, const Tensor& like, int64_t T, int64_t N, int64_t d) const {
+        auto beside = [&](const Tensor& t, at::ScalarType type) { return is_dense(t, type) && t.device() == like.device(); };
+        if (!beside(turns, at::kLong) || turns.dim() != 1 || 2 * turns.size(0) > d) return false;
+        *r = {};
+        r->turns = static_cast<const long long*>(turns.data_ptr()), r->r = static_cast<int>(2 * turns.size(0));
+        r->n_positions = static_cast<int>(N), r->interleaved = interleaved;
+        if (positions.defined()) {
+            if (!beside(positions, at::kInt) || (positions.numel() != T && positions.numel() != N) || positions.numel() == 0) return false;
+            r->positions = static_cast<const int*>(positions.data_ptr()), r->n_positions = static_cast<int>(positions.numel());
+        }
+        if (!eps) return !q_weight.defined() && !k_weight.defined();
+        r->norm = 1, r->eps = static_cast<float>(*eps);
+        const Tensor& some = q_weight.defined() ? q_weight : k_weight;
+        const auto type = some.defined() ? some.scalar_type() : at::kBFloat16;
+        if (type != at::kBFloat16 && type != at::kFloat) return false;
+        for (const Tensor* w : {&q_weight, &k_weight})
+            if (w->defined() && !(beside(*w, type) && w->dim() == 1 && w->size(0) == d)) return false;
+        r->weight_type = type == at::kFloat ? S2A_WEIGHT_F32 : S2A_WEIGHT_BF16;
+        r->q_weight = q_weight.defined() ? q_weight.data_ptr() : nullptr, r->k_weight = k_weight.defined() ? k_weight.data_ptr() : nullptr;
+        return true;
+    }
+};
+// The same from Python.
+struct RotationGiven : RotationArgs {
+    bool bad = false;
+    RotationGiven(py::handle turns_, py::handle positions_, py::handle q_weight_, py::handle k_weight_, std::optional<double> eps_, bool interleaved_) {
+        Arg t(turns_), p(positions_), qw(q_weight_), kw(k_weight_);
+        bad = t.bad || p.bad || qw.bad || kw.bad;
+        turns = t.t, positions = p.t, q_weight = qw.t, k_weight = kw.t, eps = eps_, interleaved = interleaved_;
+    }
+};
+
+int call_rotate(const Tensor& q, const Tensor& k, const Tensor& q_out, const Tensor& k_out, const s2a_rotation& r, const HeadSizes& s, void* stream) {
+    return s2a_rotate(q.data_ptr(), *token_stride(q), k.data_ptr(), *token_stride(k), q_out.data_ptr(), *token_stride(q_out), k_out.data_ptr(),
+                      *token_stride(k_out), &r, s.T, s.H, s.Hkv, s.d, stream);
+}
+
+py::object rotate(py::handle q_, py::handle k_, py::handle turns, py::handle positions, py::handle q_weight, py::handle k_weight, std::optional<double> eps,
+                  bool interleaved, py::handle q_out_, py::handle k_out_, std::optional<int64_t> stream) {
+    Arg q(q_), k(k_), q_out(q_out_), k_out(k_out_);
+    const RotationGiven given(turns, positions, q_weight, k_weight, eps, interleaved);
+    if (q.bad || k.bad || q_out.bad || k_out.bad || given.bad) return py::none();
+    const auto s = head_sizes(q.t, k.t);
+    s2a_rotation r;
+    if (!s || !given.fill(&r, q.t, s->T, s->N, s->d)) return py::none();
+    const c10::cuda::CUDAGuard device(q.t.device());
+    CallStream on(stream, q.t);
+    for (auto [out, like] : {std::pair{&q_out, &q}, std::pair{&k_out, &k}}) {
+        if (!out->given) out->t = on.output(new_like(like->t));
+        else if (!rows_like(out->t, like->t)) return py::none();
+    }
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = call_rotate(q.t, k.t, q_out.t, k_out.t, r, *s, st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    return py::make_tuple(q_out.t, k_out.t);
+}
+
+// The gradients of a rotation; `x`, `gx`: q and k, and what came back for their outputs.  What is made belongs to the stream that is current.
+struct RotationGrads {
+    Tensor dq, dk, dq_weight, dk_weight, workspace;
+    RotationGrads(const Tensor& dq_out, const Tensor& dk_out, const s2a_rotation& r, const HeadSizes& s) {
+        dq = new_like(dq_out), dk = new_like(dk_out);
+        if (!r.norm) return;
+        const auto options = dq_out.options().dtype(at::kFloat);
+        if (r.q_weight) dq_weight = at::empty({s.d}, options);
+        if (r.k_weight) dk_weight = at::empty({s.d}, options);
+        workspace = at::empty({static_cast<int64_t>(s2a_rotate_bwd_workspace_bytes(static_cast<int>(s.d)))}, options.dtype(at::kByte));
+    }
+    int call(const Tensor& q, const Tensor& k, const Tensor& dq_out, const Tensor& dk_out, const s2a_rotation& r, const HeadSizes& s, void* stream) const {
+        auto f32 = [](const Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; };
+        return s2a_rotate_bwd(r.norm ? q.data_ptr() : nullptr, r.norm ? *token_stride(q) : 0, r.norm ? k.data_ptr() : nullptr, r.norm ? *token_stride(k) : 0,
+                              dq_out.data_ptr(), *token_stride(dq_out), dk_out.data_ptr(), *token_stride(dk_out), dq.data_ptr(), dk.data_ptr(), f32(dq_weight),
+                              f32(dk_weight), &r, s.T, s.H, s.Hkv, s.d, workspace.defined() ? workspace.data_ptr() : nullptr,
+                              workspace.defined() ? static_cast<size_t>(workspace.numel()) : 0, stream);
+    }
+};
+
+py::object rotate_bwd(py::handle q_, py::handle k_, py::handle dq_out_, py::handle dk_out_, py::handle turns, py::handle positions, py::handle q_weight,
+                      py::handle k_weight, std::optional<double> eps, bool interleaved, std::optional<int64_t> stream) {
+    Arg q(q_), k(k_), dq_out(dq_out_), dk_out(dk_out_);
+    const RotationGiven given(turns, positions, q_weight, k_weight, eps, interleaved);
+    if (q.bad || k.bad || dq_out.bad || dk_out.bad || given.bad) return py::none();
+    const auto s = head_sizes(dq_out.t, dk_out.t);
+    s2a_rotation r;
+    if (!s || !given.fill(&r, dq_out.t, s->T, s->N, s->d)) return py::none();
+    if (r.norm && (!rows_like(q.t, dq_out.t) || !rows_like(k.t, dk_out.t))) return py::none();
+    const c10::cuda::CUDAGuard device(dq_out.t.device());
+    CallStream on(stream, dq_out.t);
+    RotationGrads g(dq_out.t, dk_out.t, r, *s);
+    for (Tensor* t : {&g.dq, &g.dk, &g.dq_weight, &g.dk_weight})
+        if (t->defined()) *t = on.output(*t);
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = g.call(q.t, k.t, dq_out.t, dk_out.t, r, *s, st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    auto or_none = [](const Tensor& t) -> py::object { return t.defined() ? py::cast(t) : py::none(); };
+    return py::make_tuple(g.dq, g.dk, or_none(g.dq_weight), or_none(g.dk_weight));
+}
+
+py::object rotate_write(py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle q_, py::handle k_, py::handle v_, py::handle turns,
+                        py::handle table, py::handle starts, py::handle lengths, py::handle positions, py::handle q_weight, py::handle k_weight,
+                        std::optional<double> eps, bool interleaved, py::handle q_out_, std::optional<int64_t> stream) {
+    PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
+    Arg q(q_), k(k_), v(v_), q_out(q_out_);
+    const RotationGiven given(turns, positions, q_weight, k_weight, eps, interleaved);
+    if (q.bad || k.bad || v.bad || q_out.bad || given.bad || !a.check()) return py::none();
+    const auto s = head_sizes(q.t, k.t);
+    s2a_rotation r;
+    if (!s || q.t.dim() != 3 || q.t.device() != a.k.t.device() || s->Hkv != a.cache.Hkv || s->d != a.cache.d || !rows_like(v.t, k.t)) return py::none();
+    if (!given.fill(&r, q.t, s->T, 0, s->d)) return py::none();
+    a.batch.T = static_cast<int>(s->T);
+    CallStream on(stream, q.t);
+    if (!q_out.given) q_out.t = on.output(at::empty(q.t.sizes(), q.t.options()));
+    else if (!same_shape(q_out.t, q.t.sizes(), q.t, at::kBFloat16)) return py::none();
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_rotate_write(q.t.data_ptr(), *token_stride(q.t), k.t.data_ptr(), *token_stride(k.t), v.t.data_ptr(), *token_stride(v.t), q_out.t.data_ptr(), &r,
+                              &a.cache, &a.batch, static_cast<int>(s->H), st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    return py::cast(q_out.t);
+}
+
+// ---------------------------------------------------------------------------------------------
 // differentiable front end
 // ---------------------------------------------------------------------------------------------
 // Raises binding.S2AError; callable from the threads of the autograd engine.
@@ -495,6 +667,68 @@ py::object s2_attn(py::handle q_, py::handle k_, py::handle v_, int G, std::opti
     return o.defined() ? py::cast(o) : py::none();
 }
 
+// Norms and rotation as a differentiable function of q, k and the norms' weights.
+struct S2Rotate : public torch::autograd::Function<S2Rotate> {
+    using MaybeTensor = std::optional<Tensor>;  // (autograd does not take undefined ones)
+    static MaybeTensor maybe(const Tensor& t) { return t.defined() ? MaybeTensor(t) : std::nullopt; }
+    static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const MaybeTensor& q_weight_, const MaybeTensor& k_weight_,
+                                 const Tensor& turns, const MaybeTensor& positions_, std::optional<double> eps, bool interleaved) {
+        const Tensor q_weight = q_weight_.value_or(Tensor()), k_weight = k_weight_.value_or(Tensor()), positions = positions_.value_or(Tensor());
+        const RotationArgs args{turns, positions, q_weight, k_weight, eps, interleaved};
+        const auto s = head_sizes(q, k);
+        s2a_rotation r;
+        TORCH_CHECK_VALUE(s && args.fill(&r, q, s->T, s->N, s->d), "q, k");  // checked by s2_rotate
+        const c10::cuda::CUDAGuard device(q.device());
+        Tensor q_out = new_like(q), k_out = new_like(k);
+        const int rc = call_rotate(q, k, q_out, k_out, r, *s, current_stream());
+        if (rc != S2A_OK) raise_status(rc, "s2a_rotate");
+        // without a norm the gradients do not depend on what went in
+        ctx->save_for_backward({eps ? q : Tensor(), eps ? k : Tensor(), q_weight, k_weight, turns, positions});
+        ctx->saved_data["eps"] = eps;
+        ctx->saved_data["interleaved"] = interleaved;
+        return {q_out, k_out};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        const variable_list saved = ctx->get_saved_variables();
+        const Tensor &q = saved[0], &k = saved[1], &q_weight = saved[2], &k_weight = saved[3];
+        const RotationArgs args{saved[4], saved[5], q_weight, k_weight, ctx->saved_data["eps"].toOptional<double>(), ctx->saved_data["interleaved"].toBool()};
+        auto in_rows = [](const Tensor& t) { return token_stride(t) ? t : t.contiguous(); };
+        const Tensor dq_out = in_rows(grads[0]), dk_out = in_rows(grads[1]);
+        const auto s = head_sizes(dq_out, dk_out);
+        s2a_rotation r;
+        // saved-tensor hooks decide what comes back
+        TORCH_CHECK_VALUE(s && args.fill(&r, dq_out, s->T, s->N, s->d) && (!r.norm || (rows_like(q, dq_out) && rows_like(k, dk_out))),
+                          "the gradients must be bf16 CUDA tensors of the shapes of q and k, and what was saved must have come back as it was");
+        at::NoGradGuard no_grad;
+        const c10::cuda::CUDAGuard device(dq_out.device());
+        const RotationGrads g(dq_out, dk_out, r, *s);
+        const int rc = g.call(q, k, dq_out, dk_out, r, *s, current_stream());
+        if (rc != S2A_OK) raise_status(rc, "s2a_rotate_bwd");
+        auto like = [](const Tensor& grad, const Tensor& weight) { return grad.defined() ? grad.to(weight.scalar_type()) : Tensor(); };
+        return {g.dq, g.dk, like(g.dq_weight, q_weight), like(g.dk_weight, k_weight), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+// (q_out, k_out), or None where the arguments are not what the kernels take
+py::object s2_rotate(py::handle q_, py::handle k_, py::handle turns, py::handle positions, py::handle q_weight, py::handle k_weight,
+                     std::optional<double> eps, bool interleaved) {
+    Arg q(q_), k(k_);
+    const RotationGiven given(turns, positions, q_weight, k_weight, eps, interleaved);
+    if (!q.given || !k.given || q.bad || k.bad || given.bad) return py::none();
+    variable_list out;
+    {
+        py::gil_scoped_release nogil;
+        if (!token_stride(q.t)) q.t = q.t.contiguous();
+        if (!token_stride(k.t)) k.t = k.t.contiguous();
+        const auto s = head_sizes(q.t, k.t);
+        s2a_rotation r;
+        if (s && given.fill(&r, q.t, s->T, s->N, s->d))
+            out = S2Rotate::apply(q.t, k.t, S2Rotate::maybe(given.q_weight), S2Rotate::maybe(given.k_weight), given.turns,
+                                  S2Rotate::maybe(given.positions), eps, interleaved);
+    }
+    return out.empty() ? py::none() : py::object(py::make_tuple(out[0], out[1]));
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_s2a_torch, m) {
@@ -510,5 +744,9 @@ PYBIND11_MODULE(_s2a_torch, m) {
     m.def("cache_write", &cache_write);
     m.def("cache_read", &cache_read);
     m.def("paged_fwd", &paged_fwd);
+    m.def("rotate", &rotate);
+    m.def("rotate_bwd", &rotate_bwd);
+    m.def("rotate_write", &rotate_write);
+    m.def("s2_rotate", torch::wrap_pybind_function(&s2_rotate));
     m.def("s2_attn", torch::wrap_pybind_function(&s2_attn));
 }
