@@ -388,6 +388,35 @@ int s2a_rotate_write(const void* q, long long q_stride, const void* k, long long
                      const s2a_rotation* rotation, const s2a_cache* cache, const s2a_batch* batch, int H, void* stream);
 
 /*
+ * What attention weight the cached tokens get from the new tokens of a call, for eviction.  (The paper has no counterpart: the models it extends are served at
+ * lengths whose caches outgrow the memory.)  With p the position of a new token, s = scale * q . k_j over the keys j it attends (s2a_paged_fwd's rule) and lse what
+ * s2a_paged_fwd left for it:
+ *   received[j] = before[j] + sum of exp(s - lse) over the new tokens of the sequence that attend j and the H / Hkv query heads of the KV head
+ * with before[j] = 0 for the sequence's new tokens, and for all where `before` is NULL: a page's tokens need no clearing when they are written.  Only tokens that a new token of the
+ * call attends are written.  Both are fp32 [pages, Hkv, page_size], beside the cache's pools; received may be before.
+ *   in : q [T, H, d] bf16, lse [H, T] fp32, before        out: received
+ * Other arguments and rules are those of s2a_paged_fwd.  Sequences of a batch must not share pages of which they attend tokens (this call writes beside them).
+ * Scores and sums are fp32.  Over an S2A_CACHE_E4M3 cache the values of a query row count in full down to 2^-29 of its largest.  What the cache holds of tokens that
+ * none of the new ones attends does not matter.  Deterministic: no atomics.
+ */
+int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, const s2a_batch* batch, const float* before, float* received, int H,
+                      int max_new, float scale, int window, int sinks, void* stream);
+
+/*
+ * Eviction: of each of B sequences, and for each KV head by itself, m = min(lengths[b], budget) tokens stay: the first `sinks`, the last `recent`, and of those between the ones with
+ * the largest `received` (of equal ones the earlier; -0 is 0, NaN counts as larger than all numbers).  In their order they become tokens 0 .. m - 1 of the pages in
+ * to_table [B, to_width]: keys, values, their exponents and `received` are copied there; the old pages stay as they are, and so do the new ones behind token m - 1.
+ *   out: new_lengths [B] = m; kept [B, Hkv, budget], the places the tokens had, ascending, -1 from m on
+ * A sequence that attends with new_lengths and to_table from then on goes on at its old position (keys are cached rotated, see s2a_rotate_write); its heads hold
+ * different tokens at one place, so sinks and windows count places in the cache.
+ * budget >= 1, sinks + recent <= budget, to_width * page_size >= min(budget, width * page_size).  lengths[b] may be 0.  new_lengths must not be lengths.  The new pages must differ
+ * from one another and from all pages of the old sequences, which may share theirs.
+ * table, lengths and to_table are read and checked on the device like a batch (a length above width * page_size, a page outside the pool).  Two kernel launches.  Deterministic.
+ */
+int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, int width, const int* lengths, const int* to_table, int to_width, int B,
+                    int budget, int sinks, int recent, int* new_lengths, int* kept, void* stream);
+
+/*
  * Diagnostic (the paper has no counterpart): enqueues one tiny kernel on `stream` in which a single
  * warp waits, with the library's own bounded wait and a limit of `limit_cycles` SM clock cycles
  * (1 .. 2,000,000,000; a million is well under a millisecond), on a barrier that nothing ever arrives

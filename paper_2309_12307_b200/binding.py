@@ -30,7 +30,7 @@ S2A_ERR_BAD_INDEX = -6
 EXPORTS = [
     "s2a_fwd", "s2a_bwd", "s2a_bwd_workspace_bytes", "s2a_bwd_workspace_bytes_fast", "s2a_fwd_ex", "s2a_bwd_ex", "s2a_bwd_stage", "s2a_fwd_bwd_host",
     "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed", "s2a_cache_write", "s2a_cache_read", "s2a_paged_fwd",
-    "s2a_paged_workspace_bytes", "s2a_rotate", "s2a_rotate_bwd", "s2a_rotate_bwd_workspace_bytes", "s2a_rotate_write",
+    "s2a_paged_workspace_bytes", "s2a_paged_weights", "s2a_cache_evict", "s2a_rotate", "s2a_rotate_bwd", "s2a_rotate_bwd_workspace_bytes", "s2a_rotate_write",
     "s2a_selftest_wait_expiry", "s2a_device_status", "s2a_status_string", "s2a_last_cuda_error", "s2a_version",
 ]
 
@@ -88,6 +88,10 @@ def load() -> ctypes.CDLL:
     lib.s2a_paged_workspace_bytes.argtypes = [P, P, I, I, I, I]
     lib.s2a_paged_workspace_bytes.restype = Z
     lib.s2a_paged_fwd.restype = I
+    lib.s2a_paged_weights.argtypes = [P, P, P, P, P, P, I, I, F, I, I, P]
+    lib.s2a_paged_weights.restype = I
+    lib.s2a_cache_evict.argtypes = [P, P, P, I, P, P, I, I, I, I, I, P, P, P]
+    lib.s2a_cache_evict.restype = I
     L = ctypes.c_longlong  # (the rotation is passed by reference too)
     lib.s2a_rotate.argtypes = [P, L, P, L, P, L, P, L, P, I, I, I, I, P]
     lib.s2a_rotate.restype = I
@@ -414,7 +418,7 @@ class PagedCache:
         return cls(*pools)
 
 
-def _check_cache(cache, table, starts, lengths):
+def _check_pools(cache):
     if not isinstance(cache, PagedCache):
         raise ValueError("cache must be a PagedCache")
     codes = isinstance(cache.k, torch.Tensor) and cache.k.dtype == torch.float8_e4m3fn
@@ -429,6 +433,11 @@ def _check_cache(cache, table, starts, lengths):
             _require(t, torch.int8, name, shape=cache.k.shape[:3], device=device)
         elif t is not None:
             raise ValueError(f"{name} belongs to a cache in float8_e4m3fn")
+    return device
+
+
+def _check_cache(cache, table, starts, lengths):
+    device = _check_pools(cache)
     _require(table, torch.int32, "table", device=device)
     if table.dim() != 2:
         raise ValueError(f"table must be [B, pages of a sequence], not {tuple(table.shape)}")
@@ -471,6 +480,29 @@ def _check_paged_fwd(q, cache, table, starts, lengths, o, lse, workspace=None):
         _check_workspace(workspace, device)
 
 
+def _check_paged_weights(q, lse, cache, table, starts, lengths, received, before):
+    device = _check_cache(cache, table, starts, lengths)
+    _check_rows(q, "q", cache, device)
+    _require(lse, torch.float32, "lse", shape=(q.shape[1], q.shape[0]), device=device)
+    for t, name in ((received, "received"), (before, "before")):
+        if t is not None or t is received:
+            _require(t, torch.float32, name, shape=cache.k.shape[:3], device=device)
+
+
+def _check_cache_evict(cache, received, table, lengths, to_table, budget, new_lengths, kept):
+    device = _check_pools(cache)
+    _require(received, torch.float32, "received", shape=cache.k.shape[:3], device=device)
+    for t, name in ((table, "table"), (to_table, "to_table")):
+        _require(t, torch.int32, name, device=device)
+        if t.dim() != 2 or t.shape[0] != table.shape[0]:
+            raise ValueError(f"{name} must be [B, pages of a sequence], not {tuple(t.shape)}")
+    _require(lengths, torch.int32, "lengths", shape=(table.shape[0],), device=device)
+    if new_lengths is not None:
+        _require(new_lengths, torch.int32, "new_lengths", shape=(table.shape[0],), device=device)
+    if kept is not None:
+        _require(kept, torch.int32, "kept", shape=(table.shape[0], cache.k.shape[1], budget), device=device)
+
+
 def _pools(cache):
     return (cache.k, cache.v, cache.k_exp, cache.v_exp) if isinstance(cache, PagedCache) else (None,) * 4
 
@@ -511,6 +543,27 @@ def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, wi
     if r.__class__ is not tuple:
         _result(r, "s2a_paged_fwd", _check_paged_fwd, q, cache, table, starts, lengths, o, lse, workspace)
     return r if q.__class__ in _PLAIN else _typed(r, (None if o is not None else q, None))
+
+
+def s2a_paged_weights(q, lse, cache, table, starts, lengths, received, before=None, max_new=None, scale=None, window=0, sinks=0, stream=None) -> None:
+    """received [pages, Hkv, page_size] (fp32) of every cached token that a new token attends: before (0 for the new tokens themselves, and for all where it is None)
+    plus the attention weight that it gets from the new tokens, all query heads of its KV head together.  `q` and `lse` are those of s2a_paged_fwd, as are the other
+    arguments; `before` may be `received`.  Sequences must not share pages here."""
+    args = q, lse, cache, table, starts, lengths, received, before
+    hot = _hot or _hot_for(_check_paged_weights, *args)
+    rc = hot.paged_weights(q, lse, *_pools(cache), *args[3:], max_new, scale, window, sinks, _given_stream(stream))
+    if rc != S2A_OK:
+        _result(rc, "s2a_paged_weights", _check_paged_weights, *args)
+
+
+def s2a_cache_evict(cache, received, table, lengths, to_table, budget, sinks=0, recent=0, new_lengths=None, kept=None, stream=None):
+    """(new_lengths [B], kept [B, Hkv, budget]), int32: of every sequence and KV head at most `budget` tokens stay, the first `sinks`, the last `recent` and the
+    others with the largest `received`, and are copied, in their order, to the pages of `to_table` (with their `received`).  kept: the places they had, -1 behind
+    the last one.  The new pages must not be pages of the old sequences."""
+    args = cache, received, table, lengths, to_table, budget
+    hot = _hot or _hot_for(_check_cache_evict, *args, new_lengths, kept)
+    r = hot.cache_evict(*_pools(cache), received, table, lengths, to_table, budget, sinks, recent, new_lengths, kept, _given_stream(stream))
+    return r if r.__class__ is tuple else _result(r, "s2a_cache_evict", _check_cache_evict, *args, new_lengths, kept)
 
 
 def rotary_turns(r: int, base: float = 10000.0, scale: float = 1.0, device="cuda"):

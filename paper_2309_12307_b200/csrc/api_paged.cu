@@ -35,6 +35,11 @@ int check_batch(const s2a_batch* b, const s2a_cache* c) {
     return S2A_OK;
 }
 
+int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    if (H <= 0 || H % cache->Hkv != 0 || max_new <= 0 || max_new > batch->T || window < 0 || sinks < 0) return S2A_ERR_INVALID_ARG;
+    return static_cast<long long>(batch->T) * H > kIntMax ? S2A_ERR_UNSUPPORTED : S2A_OK;
+}
+
 PagedBatch batch_of(const s2a_batch* b) {
     PagedBatch r;
     r.table = b->table, r.starts = b->starts, r.lengths = b->lengths, r.width = b->width, r.B = b->B, r.T = b->T;
@@ -181,11 +186,6 @@ bool plan_tiles(PagedTileParams* p, int n_sm, long long longest, int d, int key_
     p->order = BlockOrder(static_cast<int>(groups), p->slots, chunk);
     p->by_groups = FastDiv(static_cast<int>(groups)), p->by_groups_of_kv = FastDiv(a.rep >> p->pack_log2);
     return true;
-}
-
-int check_heads(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
-    if (H <= 0 || H % cache->Hkv != 0 || max_new <= 0 || max_new > batch->T || window < 0 || sinks < 0) return S2A_ERR_INVALID_ARG;
-    return static_cast<long long>(batch->T) * H > kIntMax ? S2A_ERR_UNSUPPORTED : S2A_OK;
 }
 
 // Up to how many rows (new tokens times query heads of a KV head) a sequence is the splitting kernel's.  Each 16 rows of a sequence

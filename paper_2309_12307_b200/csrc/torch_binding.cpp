@@ -321,17 +321,15 @@ py::object bwd_packed(py::handle qkv_, py::handle o_, py::handle lse_, py::handl
 // ---------------------------------------------------------------------------------------------
 // Pools [pages, Hkv, page_size, d] of bf16 or 8-bit floats, for the latter exponents [pages, Hkv, page_size]; `device`: where the
 // first pool is, current while the object lives.
-struct PagedArgs {
-    Arg k, v, k_exp, v_exp, table, starts, lengths;
+struct PagedPools {
+    Arg k, v, k_exp, v_exp;
     s2a_cache cache = {};
-    s2a_batch batch = {};
     c10::cuda::OptionalCUDAGuard device;
-    PagedArgs(py::handle k_, py::handle v_, py::handle k_exp_, py::handle v_exp_, py::handle table_, py::handle starts_, py::handle lengths_)
-        : k(k_), v(v_), k_exp(k_exp_), v_exp(v_exp_), table(table_), starts(starts_), lengths(lengths_) {}
+    PagedPools(py::handle k_, py::handle v_, py::handle k_exp_, py::handle v_exp_) : k(k_), v(v_), k_exp(k_exp_), v_exp(v_exp_) {}
     bool dense(const Tensor& t, int64_t dim, at::ScalarType type) const { return is_dense(t, type) && t.dim() == dim && t.device() == k.t.device(); }
     // false: binding.py names what is wrong
     bool check() {
-        for (const Arg* a : {&k, &v, &k_exp, &v_exp, &table, &starts, &lengths})
+        for (const Arg* a : {&k, &v, &k_exp, &v_exp})
             if (a->bad) return false;
         if (!k.t.defined()) return false;
         const bool codes = k.t.scalar_type() == at::kFloat8_e4m3fn;
@@ -339,19 +337,35 @@ struct PagedArgs {
         if (!dense(k.t, 4, type) || !dense(v.t, 4, type) || v.t.sizes() != k.t.sizes() || k_exp.given != codes || v_exp.given != codes) return false;
         if (codes && !(dense(k_exp.t, 3, at::kChar) && dense(v_exp.t, 3, at::kChar) && k_exp.t.sizes() == k.t.sizes().slice(0, 3) && v_exp.t.sizes() == k_exp.t.sizes()))
             return false;
-        if (!dense(table.t, 2, at::kInt) || !dense(starts.t, 1, at::kInt) || !dense(lengths.t, 1, at::kInt)) return false;
-        if (starts.t.size(0) != table.t.size(0) + 1 || lengths.t.size(0) != table.t.size(0)) return false;
-        for (int64_t x : {k.t.size(0), k.t.size(1), k.t.size(2), k.t.size(3), table.t.size(0), table.t.size(1)})
+        for (int64_t x : {k.t.size(0), k.t.size(1), k.t.size(2), k.t.size(3)})
             if (!fits_int(x)) return false;
         cache.k = k.t.data_ptr(), cache.v = v.t.data_ptr();
         cache.k_exp = codes ? static_cast<signed char*>(k_exp.t.data_ptr()) : nullptr;
         cache.v_exp = codes ? static_cast<signed char*>(v_exp.t.data_ptr()) : nullptr;
         cache.type = codes ? S2A_CACHE_E4M3 : S2A_CACHE_BF16;
         cache.pages = k.t.size(0), cache.Hkv = k.t.size(1), cache.page_size = k.t.size(2), cache.d = k.t.size(3);
+        device.reset_device(k.t.device());
+        return true;
+    }
+    // fp32 [pages, Hkv, page_size]
+    bool beside(const Tensor& t) const { return dense(t, 3, at::kFloat) && t.sizes() == k.t.sizes().slice(0, 3); }
+};
+// The same with the batch of a call.
+struct PagedArgs : PagedPools {
+    Arg table, starts, lengths;
+    s2a_batch batch = {};
+    PagedArgs(py::handle k_, py::handle v_, py::handle k_exp_, py::handle v_exp_, py::handle table_, py::handle starts_, py::handle lengths_)
+        : PagedPools(k_, v_, k_exp_, v_exp_), table(table_), starts(starts_), lengths(lengths_) {}
+    bool check() {
+        for (const Arg* a : {&table, &starts, &lengths})
+            if (a->bad) return false;
+        if (!PagedPools::check() || !dense(table.t, 2, at::kInt) || !dense(starts.t, 1, at::kInt) || !dense(lengths.t, 1, at::kInt)) return false;
+        if (starts.t.size(0) != table.t.size(0) + 1 || lengths.t.size(0) != table.t.size(0)) return false;
+        for (int64_t x : {table.t.size(0), table.t.size(1)})
+            if (!fits_int(x)) return false;
         batch.table = static_cast<const int*>(table.t.data_ptr()), batch.starts = static_cast<const int*>(starts.t.data_ptr());
         batch.lengths = static_cast<const int*>(lengths.t.data_ptr());
         batch.B = table.t.size(0), batch.width = table.t.size(1);
-        device.reset_device(k.t.device());
         return true;
     }
     // x [T, heads, d] of bf16 beside the cache
@@ -426,6 +440,62 @@ py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke,
     }
     if (rc != S2A_OK) return py::int_(rc);
     return py::make_tuple(o.t, lse.t);
+}
+
+py::object paged_weights(py::handle q_, py::handle lse_, py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle table, py::handle starts,
+                         py::handle lengths, py::handle received_, py::handle before_, std::optional<int64_t> max_new, std::optional<double> scale,
+                         int64_t window, int64_t sinks, std::optional<int64_t> stream) {
+    PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
+    Arg q(q_), lse(lse_), received(received_), before(before_);
+    if (q.bad || lse.bad || received.bad || before.bad || !a.check() || !a.rows(q.t)) return py::none();
+    const int64_t T = q.t.size(0), H = q.t.size(1), most = max_new ? *max_new : T;
+    if (!same_shape(lse.t, {H, T}, q.t, at::kFloat) || !a.beside(received.t) || (before.given && !a.beside(before.t))) return py::none();
+    // what does not fit an int is refused by the library as any negative size is
+    auto as_int = [](int64_t x) { return fits_int(x) ? static_cast<int>(x) : -1; };
+    a.batch.T = static_cast<int>(T);
+    CallStream on(stream, q.t);
+    void* st = on.begin();
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_paged_weights(q.t.data_ptr(), static_cast<const float*>(lse.t.data_ptr()), &a.cache, &a.batch,
+                               before.given ? static_cast<const float*>(before.t.data_ptr()) : nullptr, static_cast<float*>(received.t.data_ptr()),
+                               static_cast<int>(H), as_int(most), static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(a.cache.d))),
+                               as_int(window), as_int(sinks), st);
+    }
+    return py::int_(rc);
+}
+
+py::object cache_evict(py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle received_, py::handle table, py::handle lengths,
+                       py::handle to_table_, int64_t budget, int64_t sinks, int64_t recent, py::handle new_lengths_, py::handle kept_,
+                       std::optional<int64_t> stream) {
+    Arg received(received_), to_table(to_table_), new_lengths(new_lengths_), kept(kept_);
+    PagedPools a(kp, vp, ke, ve);
+    Arg from(table), n(lengths);
+    if (received.bad || to_table.bad || new_lengths.bad || kept.bad || from.bad || n.bad || !a.check()) return py::none();
+    if (!a.beside(received.t) || !a.dense(from.t, 2, at::kInt) || !a.dense(to_table.t, 2, at::kInt)) return py::none();
+    const int64_t B = from.t.size(0), Hkv = a.cache.Hkv;
+    if (!a.dense(n.t, 1, at::kInt) || n.t.size(0) != B || to_table.t.size(0) != B) return py::none();
+    for (int64_t x : {B, from.t.size(1), to_table.t.size(1)})
+        if (!fits_int(x)) return py::none();
+    auto as_int = [](int64_t x) { return fits_int(x) ? static_cast<int>(x) : -1; };
+    CallStream on(stream, a.k.t);
+    const auto ints = a.k.t.options().dtype(at::kInt);
+    if (!new_lengths.given) new_lengths.t = on.output(at::empty({B}, ints));
+    else if (!same_shape(new_lengths.t, {B}, a.k.t, at::kInt)) return py::none();
+    if (!kept.given) kept.t = on.output(at::empty({B, Hkv, std::max<int64_t>(as_int(budget), 0)}, ints));
+    else if (!same_shape(kept.t, {B, Hkv, budget}, a.k.t, at::kInt)) return py::none();
+    void* st = on.begin();
+    auto ptr = [](const Tensor& t) { return static_cast<int*>(t.data_ptr()); };
+    int rc;
+    {
+        py::gil_scoped_release nogil;
+        rc = s2a_cache_evict(&a.cache, static_cast<float*>(received.t.data_ptr()), ptr(from.t), static_cast<int>(from.t.size(1)), ptr(n.t), ptr(to_table.t),
+                             static_cast<int>(to_table.t.size(1)), static_cast<int>(B), as_int(budget), as_int(sinks), as_int(recent), ptr(new_lengths.t),
+                             ptr(kept.t), st);
+    }
+    if (rc != S2A_OK) return py::int_(rc);
+    return py::make_tuple(new_lengths.t, kept.t);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -744,6 +814,8 @@ PYBIND11_MODULE(_s2a_torch, m) {
     m.def("cache_write", &cache_write);
     m.def("cache_read", &cache_read);
     m.def("paged_fwd", &paged_fwd);
+    m.def("paged_weights", &paged_weights);
+    m.def("cache_evict", &cache_evict);
     m.def("rotate", &rotate);
     m.def("rotate_bwd", &rotate_bwd);
     m.def("rotate_write", &rotate_write);
