@@ -398,9 +398,13 @@ int s2a_rotate_write(const void* q, long long q_stride, const void* k, long long
  * Other arguments and rules are those of s2a_paged_fwd.  Sequences of a batch must not share pages of which they attend tokens (this call writes beside them).
  * Scores and sums are fp32.  Over an S2A_CACHE_E4M3 cache the values of a query row count in full down to 2^-29 of its largest.  What the cache holds of tokens that
  * none of the new ones attends does not matter.  Deterministic: no atomics.
+ *   workspace: like s2a_paged_fwd's, of s2a_paged_weights_workspace_bytes(...) bytes: pieces of prompts that do not fill the GPU evenly are split over their rows where it is there.
  */
 int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, const s2a_batch* batch, const float* before, float* received, int H,
-                      int max_new, float scale, int window, int sinks, void* stream);
+                      int max_new, float scale, int window, int sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of scratch with which s2a_paged_weights is fastest for these sizes on the current device (0: it needs none, or the sizes are invalid). */
+size_t s2a_paged_weights_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks);
 
 /*
  * Eviction: of each of B sequences, and for each KV head by itself, m = min(lengths[b], budget) tokens stay: the first `sinks`, the last `recent`, and of those between the ones with

@@ -30,7 +30,7 @@ S2A_ERR_BAD_INDEX = -6
 EXPORTS = [
     "s2a_fwd", "s2a_bwd", "s2a_bwd_workspace_bytes", "s2a_bwd_workspace_bytes_fast", "s2a_fwd_ex", "s2a_bwd_ex", "s2a_bwd_stage", "s2a_fwd_bwd_host",
     "s2a_bwd_noalloc", "s2a_bwd_noalloc_max_rows", "s2a_fwd_packed", "s2a_bwd_packed", "s2a_cache_write", "s2a_cache_read", "s2a_paged_fwd",
-    "s2a_paged_workspace_bytes", "s2a_paged_weights", "s2a_cache_evict", "s2a_rotate", "s2a_rotate_bwd", "s2a_rotate_bwd_workspace_bytes", "s2a_rotate_write",
+    "s2a_paged_workspace_bytes", "s2a_paged_weights", "s2a_paged_weights_workspace_bytes", "s2a_cache_evict", "s2a_rotate", "s2a_rotate_bwd", "s2a_rotate_bwd_workspace_bytes", "s2a_rotate_write",
     "s2a_selftest_wait_expiry", "s2a_device_status", "s2a_status_string", "s2a_last_cuda_error", "s2a_version",
 ]
 
@@ -88,8 +88,10 @@ def load() -> ctypes.CDLL:
     lib.s2a_paged_workspace_bytes.argtypes = [P, P, I, I, I, I]
     lib.s2a_paged_workspace_bytes.restype = Z
     lib.s2a_paged_fwd.restype = I
-    lib.s2a_paged_weights.argtypes = [P, P, P, P, P, P, I, I, F, I, I, P]
+    lib.s2a_paged_weights.argtypes = [P, P, P, P, P, P, I, I, F, I, I, P, Z, P]
     lib.s2a_paged_weights.restype = I
+    lib.s2a_paged_weights_workspace_bytes.argtypes = [P, P, I, I, I, I]
+    lib.s2a_paged_weights_workspace_bytes.restype = Z
     lib.s2a_cache_evict.argtypes = [P, P, P, I, P, P, I, I, I, I, I, P, P, P]
     lib.s2a_cache_evict.restype = I
     L = ctypes.c_longlong  # (the rotation is passed by reference too)
@@ -480,13 +482,15 @@ def _check_paged_fwd(q, cache, table, starts, lengths, o, lse, workspace=None):
         _check_workspace(workspace, device)
 
 
-def _check_paged_weights(q, lse, cache, table, starts, lengths, received, before):
+def _check_paged_weights(q, lse, cache, table, starts, lengths, received, before, workspace=None):
     device = _check_cache(cache, table, starts, lengths)
     _check_rows(q, "q", cache, device)
     _require(lse, torch.float32, "lse", shape=(q.shape[1], q.shape[0]), device=device)
     for t, name in ((received, "received"), (before, "before")):
         if t is not None or t is received:
             _require(t, torch.float32, name, shape=cache.k.shape[:3], device=device)
+    if workspace is not None:
+        _check_workspace(workspace, device)
 
 
 def _check_cache_evict(cache, received, table, lengths, to_table, budget, new_lengths, kept):
@@ -545,15 +549,16 @@ def s2a_paged_fwd(q, cache, table, starts, lengths, max_new=None, scale=None, wi
     return r if q.__class__ in _PLAIN else _typed(r, (None if o is not None else q, None))
 
 
-def s2a_paged_weights(q, lse, cache, table, starts, lengths, received, before=None, max_new=None, scale=None, window=0, sinks=0, stream=None) -> None:
+def s2a_paged_weights(q, lse, cache, table, starts, lengths, received, before=None, max_new=None, scale=None, window=0, sinks=0, workspace=None,
+                      stream=None) -> None:
     """received [pages, Hkv, page_size] (fp32) of every cached token that a new token attends: before (0 for the new tokens themselves, and for all where it is None)
     plus the attention weight that it gets from the new tokens, all query heads of its KV head together.  `q` and `lse` are those of s2a_paged_fwd, as are the other
     arguments; `before` may be `received`.  Sequences must not share pages here."""
     args = q, lse, cache, table, starts, lengths, received, before
-    hot = _hot or _hot_for(_check_paged_weights, *args)
-    rc = hot.paged_weights(q, lse, *_pools(cache), *args[3:], max_new, scale, window, sinks, _given_stream(stream))
+    hot = _hot or _hot_for(_check_paged_weights, *args, workspace)
+    rc = hot.paged_weights(q, lse, *_pools(cache), *args[3:], max_new, scale, window, sinks, workspace, _given_stream(stream))
     if rc != S2A_OK:
-        _result(rc, "s2a_paged_weights", _check_paged_weights, *args)
+        _result(rc, "s2a_paged_weights", _check_paged_weights, *args, workspace)
 
 
 def s2a_cache_evict(cache, received, table, lengths, to_table, budget, sinks=0, recent=0, new_lengths=None, kept=None, stream=None):

@@ -10,7 +10,7 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libs2a.so")
-SOURCES = ["api.cu", "api_evict.cu", "api_paged.cu", "api_rotate.cu", "fwd_kernel.cu", "bwd_kernels.cu", "cache_kernels.cu", "evict_kernels.cu", "paged_fwd.cu", "paged_split.cu", "rotate_kernels.cu", "weights_kernels.cu"]
+SOURCES = ["api.cu", "api_evict.cu", "api_paged.cu", "api_rotate.cu", "fwd_kernel.cu", "bwd_kernels.cu", "cache_kernels.cu", "evict_kernels.cu", "paged_fwd.cu", "paged_split.cu", "rotate_kernels.cu", "weights_kernels.cu", "weights_tile.cu"]
 HEADERS = ["evict.h", "host_paged.h", "host_plan.h", "host_state.h", "paged.h", "paged_device.cuh", "rotate.h", "s2a_params.h", "sm100_ptx.cuh", os.path.join("..", "..", "include", "s2a.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

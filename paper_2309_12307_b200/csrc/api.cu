@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include "../../include/s2a.h"
+#include "evict.h"
 #include "host_plan.h"
 #include "host_state.h"
 #include "paged.h"
@@ -76,7 +77,8 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         ds.paged_error = configure_paged_split(ds.cluster_slots);
         if (ds.paged_error == cudaSuccess) ds.paged_error = configure_paged_fwd();
-        if (ds.paged_error != cudaSuccess) cudaGetLastError();  // s2a_paged_fwd's to report, and no other call's
+        if (ds.paged_error == cudaSuccess) ds.paged_error = configure_weights_tile();
+        if (ds.paged_error != cudaSuccess) cudaGetLastError();  // s2a_paged_fwd's and s2a_paged_weights' to report, and no other call's
         e = cudaGetSymbolAddress(reinterpret_cast<void**>(&ds.status_ptr), g_status_word);
         if (e != cudaSuccess) return cuda_fail(e);
         if (!g_host_status_registered) {

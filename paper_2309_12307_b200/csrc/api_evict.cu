@@ -33,6 +33,61 @@ bool plan_stream(WeightsStreamParams* p, int n_sm, long long longest) {
     return true;
 }
 
+// Rows (new tokens times query heads of a KV head) of a sequence up to which it is the streaming kernel's.
+constexpr int kStreamedRows = 64;
+
+// The items of the tiling kernel and the pieces their rows come in.  Without a window the first key blocks have all rows and the last ones few, and the
+// longest item must not be longer than the others together: a piece has about a quarter of a multiprocessor's share of all row tiles, eight at least (an item's
+// start and the second launch cost about as much as three).
+bool plan_tile(WeightsTileParams* p, int n_sm, long long longest) {
+    const WeightsParams& a = p->a;
+    p->pack_log2 = 0;
+    while (p->pack_log2 < 6 && a.rep % (2 << p->pack_log2) == 0) ++p->pack_log2;
+    const int groups = a.rep >> p->pack_log2, tokens = kTile >> p->pack_log2;
+    const long long units = static_cast<long long>(a.batch.B) * a.pool.Hkv, blocks = most_chunks(a, longest, kWeightKeys);
+    long long attending = a.most_new;  // tokens that attend a key
+    if (a.window > 0) attending = std::min(attending, static_cast<long long>(a.window) + kWeightKeys);
+    const long long most_tiles = (attending + tokens - 1) / tokens * groups;
+    const double likely = static_cast<double>(a.batch.T) / a.batch.B / a.most_new;  // of most_new, that an average sequence has
+    const double all = 0.75 * static_cast<double>(units) * static_cast<double>(blocks) * static_cast<double>(most_tiles) * std::min(1.0, likely);
+    const double each = std::max(8.0, all / (4.0 * n_sm));
+    p->pieces = static_cast<int>(std::min<double>(16.0, std::max(1.0, ceil(static_cast<double>(most_tiles) / each))));
+    if (units * blocks > kIntMax / 16) return false;
+    p->blocks = static_cast<int>(blocks), p->items = static_cast<int>(units * blocks) * p->pieces;
+    p->by_units = FastDiv(static_cast<int>(units)), p->by_pieces = FastDiv(p->pieces), p->by_heads = FastDiv(a.pool.Hkv), p->by_groups = FastDiv(groups);
+    return true;
+}
+
+void set_pieces(WeightsTileParams* p, int pieces) {
+    p->items = p->items / p->pieces * pieces, p->pieces = pieces, p->by_pieces = FastDiv(pieces);
+}
+
+size_t tile_bytes(const WeightsTileParams& p) { return p.pieces > 1 ? static_cast<size_t>(p.items) * kWeightKeys * sizeof(float) : 0; }
+
+int weight_tmaps(WeightsTileParams* p, const s2a_cache* c, const void* q, int H, int T) {
+    const cuuint64_t d = static_cast<cuuint64_t>(c->d);
+    const cuuint64_t q_dims[3] = {d, static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(T)}, q_strides[2] = {2 * d, 2 * d * H};
+    const cuuint32_t q_box[3] = {64, 1u << p->pack_log2, static_cast<cuuint32_t>(kTile) >> p->pack_log2};
+    const int rc = encode_tmap(&p->tm_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, q, 3, q_dims, q_strides, q_box);
+    if (rc != S2A_OK || c->type == S2A_CACHE_E4M3) return rc;
+    const cuuint64_t dims[2] = {d, static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size}, stride = 2 * d;
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(std::min(c->page_size, kTile))};
+    return encode_tmap(&p->tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->k, 2, dims, &stride, box);
+}
+
+// What a call's sizes say; its pointers and the scale are still missing.
+WeightsParams weights_params(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    WeightsParams a;
+    memset(&a, 0, sizeof a);
+    const int longest = batch->width * cache->page_size;  // no sequence has more tokens
+    a.batch = batch_of(batch), a.pool = pool_of(cache);
+    a.H = H, a.rep = H / cache->Hkv, a.most_new = max_new;
+    a.window = window >= longest ? 0 : window, a.sinks = sinks > longest ? longest : sinks;
+    // a single sequence has as many new tokens as it is said to have at most, but for loose values
+    a.few_rows = batch->B == 1 && static_cast<long long>(max_new) * a.rep > kStreamedRows ? 0 : kStreamedRows;
+    return a;
+}
+
 }  // namespace
 }  // namespace s2a
 
@@ -42,27 +97,49 @@ using namespace s2a;
 extern "C" {
 
 int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, const s2a_batch* batch, const float* before, float* received, int H,
-                      int max_new, float scale, int window, int sinks, void* stream) {
+                      int max_new, float scale, int window, int sinks, void* workspace, size_t workspace_bytes, void* stream) {
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return S2A_ERR_INVALID_ARG;
     if (!q || !lse || !received || !aligned16(q) || !aligned16(lse) || !aligned16(before) || !aligned16(received)) return S2A_ERR_INVALID_ARG;
     int rc = check_cache(cache);
     if (rc != S2A_OK || (rc = check_batch(batch, cache)) != S2A_OK) return rc;
     if (!(scale > 0.f) || !isfinite(scale)) return S2A_ERR_INVALID_ARG;
     if ((rc = check_heads(cache, batch, H, max_new, window, sinks)) != S2A_OK) return rc;
     DeviceState* ds = nullptr;
-    if ((rc = prepare_device(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
-    WeightsStreamParams p;
-    memset(&p, 0, sizeof p);
-    const int longest = batch->width * cache->page_size;  // no sequence has more tokens
-    p.a.batch = batch_of(batch), p.a.pool = pool_of(cache);
-    p.a.q = static_cast<const __nv_bfloat16*>(q), p.a.lse = lse, p.a.before = before, p.a.received = received;
-    p.a.status = ds->status_ptr, p.a.host_status = ds->host_word_dev;
-    p.a.H = H, p.a.rep = H / cache->Hkv, p.a.most_new = max_new;
-    p.a.window = window >= longest ? 0 : window, p.a.sinks = sinks > longest ? longest : sinks;
-    p.a.few_rows = 0x7fffffff;
-    p.a.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);
-    if (!plan_stream(&p, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
-    const cudaError_t e = launch_weights_stream(p, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
+    if ((rc = prepare_paged(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
+    WeightsParams a = weights_params(cache, batch, H, max_new, window, sinks);
+    a.q = static_cast<const __nv_bfloat16*>(q), a.lse = lse, a.before = before, a.received = received;
+    a.status = ds->status_ptr, a.host_status = ds->host_word_dev;
+    a.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);
+    const bool e4m3 = cache->type == S2A_CACHE_E4M3, few = a.few_rows > 0, many = static_cast<long long>(max_new) * a.rep > a.few_rows;
+    const long long longest = static_cast<long long>(batch->width) * cache->page_size;
+    // everything that can be refused comes before the first launch
+    WeightsStreamParams ps;
+    memset(&ps, 0, sizeof ps);
+    ps.a = a;
+    if (few && !plan_stream(&ps, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
+    WeightsTileParams pt;
+    memset(&pt, 0, sizeof pt);
+    pt.a = a;
+    if (many) {
+        if (!plan_tile(&pt, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
+        if (!workspace || tile_bytes(pt) > workspace_bytes) set_pieces(&pt, 1);
+        pt.partial = static_cast<float*>(workspace);
+        if ((rc = weight_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
+    }
+    cudaError_t e = cudaSuccess;
+    if (few) e = launch_weights_stream(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));
+    if (many && e == cudaSuccess) e = launch_weights_tile(pt, e4m3, cache->d, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? S2A_OK : cuda_fail(e);
+}
+
+size_t s2a_paged_weights_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks) {
+    DeviceState* ds = nullptr;
+    if (check_cache(cache) != S2A_OK || check_batch(batch, cache) != S2A_OK || check_heads(cache, batch, H, max_new, window, sinks) != S2A_OK) return 0;
+    WeightsTileParams p;
+    memset(&p, 0, sizeof p);
+    p.a = weights_params(cache, batch, H, max_new, window, sinks);
+    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_paged(&ds) != S2A_OK) return 0;
+    return plan_tile(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size) ? tile_bytes(p) : 0;
 }
 
 int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, int width, const int* lengths, const int* to_table, int to_width, int B,

@@ -34,6 +34,53 @@ struct WeightsStreamParams {
     int blocks;
 };
 
+constexpr int kWeightKeys = 256;  // of an item of the tiling kernel: two tiles
+struct alignas(64) WeightsTileParams {
+    CUtensorMap tm_q;        // bf16 (d, H, T), box (64, pack, 128 / pack), 128-byte swizzle
+    CUtensorMap tm_k;        // bf16 caches: (d, rows of the pool), box (64, min(page_size, 128)), the same swizzle
+    WeightsParams a;
+    int pack_log2;           // query heads of a KV head that are rows of one tile
+    int blocks;              // of kWeightKeys keys that a sequence has at most
+    int pieces;              // that the rows of an item are split into at most
+    float* partial;          // [blocks][pieces][B * Hkv][kWeightKeys] where there is more than one
+    FastDiv by_units, by_pieces, by_heads, by_groups;  // B * Hkv, pieces, Hkv, head groups of a KV head
+    int items;               // blocks * pieces * B * Hkv
+};
+
+// What an item of the tiling kernel is: keys key0 .. key0 + 255 of a sequence and KV head, against the row tiles r0 .. r1 - 1 of those that attend any of them.
+// Row tile r is head group r % groups of the tokens from (t_lo + r / groups) * (128 / pack) on.
+struct WeightsItem {
+    int id, b, hk;           // b = -1: no more items
+    int key0, first, last;   // first key; positions of the sequence's new tokens
+    int row0;                // of q, of the first new token
+    int t_lo, r0, r1;
+    int pieces;              // that this item's rows come in
+};
+__host__ __device__ inline bool weights_item(const WeightsTileParams& p, int id, WeightsItem* w) {
+    int unit, piece;
+    w->id = id;
+    const int block = p.by_pieces(p.by_units(id, &unit), &piece);
+    w->b = p.by_heads(unit, &w->hk);
+    Sequence s;
+    const WeightsParams& a = p.a;
+    if (sequence_of(a.batch, a.pool.page_log2, a.most_new, w->b, &s) != 0 || s.n == 0 || s.n <= a.few_rows / a.rep) return false;
+    w->row0 = s.row0, w->first = s.length - s.n, w->last = s.length - 1;
+    const KeyBlocks k = key_blocks(w->first, w->last, a.window, a.sinks, kWeightKeys);
+    if (block >= k.count) return false;
+    w->key0 = k.at(block) * kWeightKeys;
+    const int tokens_log2 = 7 - p.pack_log2;
+    int high = w->last;  // the last position that attends any of the keys
+    if (a.window > 0 && w->key0 >= a.sinks && w->key0 + (kWeightKeys - 1) <= w->last - (a.window - 1)) high = w->key0 + (kWeightKeys - 1) + (a.window - 1);
+    const int low = w->key0 > w->first ? w->key0 : w->first;
+    if (high < low) return false;
+    w->t_lo = (low - w->first) >> tokens_log2;
+    const int count = (((high - w->first) >> tokens_log2) - w->t_lo + 1) * (a.rep >> p.pack_log2), each = (count + p.pieces - 1) / p.pieces;
+    w->r0 = piece * each;
+    w->r1 = w->r0 + each < count ? w->r0 + each : count;
+    w->pieces = (count + each - 1) / each;
+    return w->r0 < w->r1;
+}
+
 // Tokens of a sequence that are kept, by number or by the weight of the lightest one.
 struct EvictParams {
     PagedPool pool;
@@ -58,6 +105,8 @@ __host__ __device__ inline uint32_t weight_order(uint32_t bits) {
 }
 
 cudaError_t launch_weights_stream(const WeightsStreamParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t launch_weights_tile(const WeightsTileParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t configure_weights_tile();
 cudaError_t launch_evict(const EvictParams& p, bool e4m3, int d, cudaStream_t stream);
 
 }  // namespace s2a

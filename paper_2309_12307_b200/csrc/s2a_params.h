@@ -19,6 +19,7 @@ enum WaitCode : int {
     kWaitBwdDqSpill = 400,
     kWaitPagedSplit = 500,
     kWaitPagedFwd = 600,
+    kWaitWeights = 700,
 };
 
 // Block order shared by the tensor-core kernels.  A "unit" is one (batch, head, group); it has

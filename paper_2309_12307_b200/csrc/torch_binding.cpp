@@ -444,16 +444,21 @@ py::object paged_fwd(py::handle q_, py::handle kp, py::handle vp, py::handle ke,
 
 py::object paged_weights(py::handle q_, py::handle lse_, py::handle kp, py::handle vp, py::handle ke, py::handle ve, py::handle table, py::handle starts,
                          py::handle lengths, py::handle received_, py::handle before_, std::optional<int64_t> max_new, std::optional<double> scale,
-                         int64_t window, int64_t sinks, std::optional<int64_t> stream) {
+                         int64_t window, int64_t sinks, py::handle ws_, std::optional<int64_t> stream) {
     PagedArgs a(kp, vp, ke, ve, table, starts, lengths);
-    Arg q(q_), lse(lse_), received(received_), before(before_);
-    if (q.bad || lse.bad || received.bad || before.bad || !a.check() || !a.rows(q.t)) return py::none();
+    Arg q(q_), lse(lse_), received(received_), before(before_), ws(ws_);
+    if (q.bad || lse.bad || received.bad || before.bad || ws.bad || !a.check() || !a.rows(q.t)) return py::none();
     const int64_t T = q.t.size(0), H = q.t.size(1), most = max_new ? *max_new : T;
     if (!same_shape(lse.t, {H, T}, q.t, at::kFloat) || !a.beside(received.t) || (before.given && !a.beside(before.t))) return py::none();
     // what does not fit an int is refused by the library as any negative size is
     auto as_int = [](int64_t x) { return fits_int(x) ? static_cast<int>(x) : -1; };
     a.batch.T = static_cast<int>(T);
     CallStream on(stream, q.t);
+    if (ws.given) {
+        if (!is_dense(ws.t, at::kByte) || ws.t.device() != q.t.device()) return py::none();
+    } else if (const size_t bytes = s2a_paged_weights_workspace_bytes(&a.cache, &a.batch, static_cast<int>(H), as_int(most), as_int(window), as_int(sinks))) {
+        ws.t = at::empty({static_cast<int64_t>(bytes)}, q.t.options().dtype(at::kByte));
+    }
     void* st = on.begin();
     int rc;
     {
@@ -461,7 +466,8 @@ py::object paged_weights(py::handle q_, py::handle lse_, py::handle kp, py::hand
         rc = s2a_paged_weights(q.t.data_ptr(), static_cast<const float*>(lse.t.data_ptr()), &a.cache, &a.batch,
                                before.given ? static_cast<const float*>(before.t.data_ptr()) : nullptr, static_cast<float*>(received.t.data_ptr()),
                                static_cast<int>(H), as_int(most), static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(a.cache.d))),
-                               as_int(window), as_int(sinks), st);
+                               as_int(window), as_int(sinks), ws.t.defined() ? ws.t.data_ptr() : nullptr,
+                               ws.t.defined() ? static_cast<size_t>(ws.t.numel()) : 0, st);
     }
     return py::int_(rc);
 }

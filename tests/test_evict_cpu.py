@@ -69,10 +69,10 @@ def test_the_library_refuses_without_a_device():
     a = (ctypes.addressof(buf) + 255) & ~255  # never dereferenced on these paths
 
     def call(cache=(), batch=(), q=a, lse=a, received=a, before=None, H=4, max_new=1, scale=1.0, window=0, sinks=0, table=a, lengths=a, to_table=a, width=2, to_width=1, B=3, budget=16,
-             recent=0, new_lengths=a + 256, kept=a):
+             recent=0, new_lengths=a + 256, kept=a, workspace=None):
         c = Cache(**{**dict(k=a, v=a, k_exp=a, v_exp=a, type=1, pages=4, Hkv=2, page_size=16, d=64), **dict(cache)})
         b = Batch(**{**dict(table=a, starts=a, lengths=a, width=2, B=3, T=5), **dict(batch)})
-        return (lib.s2a_paged_weights(q, lse, ctypes.byref(c), ctypes.byref(b), before, received, H, max_new, scale, window, sinks, None),
+        return (lib.s2a_paged_weights(q, lse, ctypes.byref(c), ctypes.byref(b), before, received, H, max_new, scale, window, sinks, workspace, 0, None),
                 lib.s2a_cache_evict(ctypes.byref(c), received, table, width, lengths, to_table, to_width, B, budget, sinks, recent, new_lengths, kept, None))
 
     invalid, unsupported = s2a.S2A_ERR_INVALID_ARG, s2a.S2A_ERR_UNSUPPORTED
@@ -85,11 +85,11 @@ def test_the_library_refuses_without_a_device():
     for change in (dict(received=None), dict(received=a + 4), dict(sinks=-1)):
         assert call(**change) == (invalid,) * 2, change
     for change in (dict(q=None), dict(q=a + 8), dict(lse=None), dict(lse=a + 4), dict(before=a + 4), dict(H=3), dict(max_new=0), dict(max_new=6), dict(scale=0.0), dict(scale=float("inf")),
-                   dict(window=-1)):
+                   dict(window=-1), dict(workspace=a + 16)):
         assert call(**change)[0] == invalid, change
     for change in (dict(table=None), dict(lengths=None), dict(to_table=None), dict(width=0), dict(to_width=0), dict(B=0), dict(budget=0), dict(recent=-1), dict(sinks=10, recent=7),
                    dict(sinks=2**31 - 1, recent=2**31 - 1), dict(budget=17), dict(new_lengths=None), dict(new_lengths=a), dict(new_lengths=a + 8), dict(kept=None)):
         assert call(**change)[1] == invalid, change
     for change in (dict(width=1 << 27, to_width=1 << 26), dict(to_width=1 << 27), dict(B=1 << 30, new_lengths=a + (1 << 40))):
         assert call(**change)[1] == unsupported, change
-    assert lib.s2a_paged_weights(a, a, None, None, None, a, 4, 1, 1.0, 0, 0, None) == invalid
+    assert lib.s2a_paged_weights(a, a, None, None, None, a, 4, 1, 1.0, 0, 0, None, 0, None) == invalid
