@@ -64,15 +64,17 @@ void set_pieces(WeightsTileParams* p, int pieces) {
 
 size_t tile_bytes(const WeightsTileParams& p) { return p.pieces > 1 ? static_cast<size_t>(p.items) * kWeightKeys * sizeof(float) : 0; }
 
-int weight_tmaps(WeightsTileParams* p, const s2a_cache* c, const void* q, int H, int T) {
+int weights_tmaps(WeightsTileParams* p, const s2a_cache* c, const void* q, int H, int T) {
     const cuuint64_t d = static_cast<cuuint64_t>(c->d);
     const cuuint64_t q_dims[3] = {d, static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(T)}, q_strides[2] = {2 * d, 2 * d * H};
     const cuuint32_t q_box[3] = {64, 1u << p->pack_log2, static_cast<cuuint32_t>(kTile) >> p->pack_log2};
     const int rc = encode_tmap(&p->tm_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, q, 3, q_dims, q_strides, q_box);
-    if (rc != S2A_OK || c->type == S2A_CACHE_E4M3) return rc;
-    const cuuint64_t dims[2] = {d, static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size}, stride = 2 * d;
-    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(std::min(c->page_size, kTile))};
-    return encode_tmap(&p->tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, c->k, 2, dims, &stride, box);
+    if (rc != S2A_OK) return rc;
+    const bool codes = c->type == S2A_CACHE_E4M3;
+    const cuuint64_t dims[2] = {d, static_cast<cuuint64_t>(c->pages) * c->Hkv * c->page_size}, stride = codes ? d : 2 * d;
+    const cuuint32_t box[2] = {codes ? static_cast<cuuint32_t>(d) : 64, static_cast<cuuint32_t>(std::min(c->page_size, kTile))};
+    return encode_tmap(&p->tm_k, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                       codes && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, c->k, 2, dims, &stride, box);
 }
 
 // What a call's sizes say; its pointers and the scale are still missing.
@@ -124,7 +126,7 @@ int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, c
         if (!plan_tile(&pt, ds->n_sm, longest)) return S2A_ERR_UNSUPPORTED;
         if (!workspace || tile_bytes(pt) > workspace_bytes) set_pieces(&pt, 1);
         pt.partial = static_cast<float*>(workspace);
-        if ((rc = weight_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
+        if ((rc = weights_tmaps(&pt, cache, q, H, batch->T)) != S2A_OK) return rc;
     }
     cudaError_t e = cudaSuccess;
     if (few) e = launch_weights_stream(ps, e4m3, cache->d, static_cast<cudaStream_t>(stream));

@@ -37,7 +37,7 @@ struct WeightsStreamParams {
 constexpr int kWeightKeys = 256;  // of an item of the tiling kernel: two tiles
 struct alignas(64) WeightsTileParams {
     CUtensorMap tm_q;        // bf16 (d, H, T), box (64, pack, 128 / pack), 128-byte swizzle
-    CUtensorMap tm_k;        // bf16 caches: (d, rows of the pool), box (64, min(page_size, 128)), the same swizzle
+    CUtensorMap tm_k;        // (d, rows of the pool), box (64 values of bf16 or all of a key's codes, min(page_size, 128)), swizzled by the box's width
     WeightsParams a;
     int pack_log2;           // query heads of a KV head that are rows of one tile
     int blocks;              // of kWeightKeys keys that a sequence has at most
