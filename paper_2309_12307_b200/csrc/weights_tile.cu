@@ -1,9 +1,10 @@
 // What attention weight cached tokens get from many rows (pieces of prompts): see weights_kernels.cu for the formula.
 //
-// S^T = K Q^T on tcgen05, 128 keys by 64 rows of q at a time.  A score tile has a key in each lane of tensor memory and a row of q in each column, so
+// S^T = K Q^T on tcgen05, 128 keys by 128 rows of q at a time.  A score tile has a key in each lane of tensor memory and a row of q in each column, so
 // the thread that has a key adds up its columns' exponentials in registers: nothing crosses threads, and there is no second product.
 // An item is two key tiles of a sequence and KV head, which stay while the row tiles that attend any of them (128 rows, as s2a_paged_fwd_kernel's: query heads
-// of a KV head and neighbouring tokens, one TMA box) pass by.  Two key tiles, because a row tile is 32 KB from the L2 that would otherwise be read twice as often.
+// of a KV head and neighbouring tokens, one TMA box) pass by.  Two key tiles, because a row tile is 32 KB from the L2 that would otherwise be read twice as often.  (Where it
+// attends only one of them, the other's scores are made and not looked at.)
 //
 // The keys are the products' operand in tensor memory (8-bit codes as bf16, what they stand for exactly): read from shared memory for every product beside the rows they
 // took its whole bandwidth.
@@ -14,9 +15,9 @@
 //   warp 20         work items (cluster launch control), TMA loads of keys and of q
 //   warp 21         tcgen05 MMAs
 //   warp 22         the rows' log sums
-// Tensor memory: the keys, then three score tiles for either key tile, which the products fill in turn: they can be ahead of the exponentials by more than a row tile, so
-// that what a warp does between two of its tiles, and the change of keys between items, finds others at work.  (Three for either, not six for both: a warp that waits
-// for a use of a score tile must know that the use before is over.  It has worked on the last tile but one, and the use before was the last but two.)
+// Tensor memory: the keys, then three score tiles, which the products of the two key tiles fill in turn: they are ahead of the exponentials, so that what a warp does
+// between two of its tiles, and the change of keys between items, finds others at work.  (A warp that waits for a use of a score tile must know that the use before,
+// three score tiles ago, is over: it has worked on the one two score tiles ago.  Score tiles of 64 rows, twice as many, took the products 1630 cycles a row tile, these 1130.)
 //
 // Where there are few items their rows are split into pieces, whose sums a second kernel adds up in order.
 #include <cuda_fp16.h>
@@ -44,8 +45,8 @@ struct TileCfg {
     static constexpr int kSmemBytes = kKeysBytes + kRing * (kTileBytes + kTile * 4) + kSumBytes + kExpBytes + kBarBytes;
     static_assert(kSmemBytes <= 232448 && 2 * kSmemBytes > 232448, "shared memory: one block on an SM, since it takes all tensor memory");
     static constexpr int kTmemCols = 512, kKeyCols = HD / 2;  // columns of a key tile
-    static constexpr int kHalf = 64, kScores = 3, kColS = 2 * kKeyCols;  // score tiles of a key tile
-    static_assert(kColS + 2 * kScores * kHalf <= kTmemCols, "tensor memory");
+    static constexpr int kHalf = 64, kScores = 3, kColS = 2 * kKeyCols;
+    static_assert(kColS + kScores * kTile <= kTmemCols, "tensor memory");
 };
 
 template <int HD, bool kE4M3>
@@ -55,7 +56,7 @@ struct TileBars {
     uint64_t k_full[2], k_empty;  // in tensor memory
     uint64_t q_full[C::kRing], q_empty[C::kRing];
     uint64_t l_full[C::kRing], l_empty[C::kRing];
-    uint64_t s_full[2][C::kScores], s_empty[2][C::kScores];  // by key tile
+    uint64_t s_full[C::kScores], s_empty[C::kScores];
     uint64_t sched_full[C::kSched], sched_empty[C::kSched];
     uint64_t sum_full[2], sum_empty[2];
     uint64_t clc, drain;
@@ -73,6 +74,14 @@ struct RowTiles {
     __device__ __forceinline__ void next(int groups, int tokens_log2) {
         if (++group == groups) group = 0, first_pos += 1 << tokens_log2;
     }
+};
+
+// The score tiles in turn: which it is, and the parity of its use.
+struct ScoreTiles {
+    uint32_t n = 0;  // modulo 6
+    __device__ __forceinline__ uint32_t tile(int ahead) const { return (n + ahead) % 3; }
+    __device__ __forceinline__ uint32_t use(int ahead) const { return (n + ahead) / 3 & 1; }
+    __device__ __forceinline__ void next_row_tile() { n = n == 4 ? 0 : n + 2; }
 };
 
 // Whether any of the tokens from position first_pos to end_pos attends a key of the tile that begins with key_low.
@@ -113,10 +122,7 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
             mbar_init(&bars->l_full[x], 1);
             mbar_init(&bars->l_empty[x], 16);
         }
-        for (int x = 0; x < 2 * C::kScores; ++x) {
-            mbar_init(&bars->s_full[0][0] + x, 1);
-            mbar_init(&bars->s_empty[0][0] + x, 4);
-        }
+        for (int x = 0; x < C::kScores; ++x) mbar_init(&bars->s_full[x], 1), mbar_init(&bars->s_empty[x], 8);
         for (int x = 0; x < C::kSched; ++x) mbar_init(&bars->sched_full[x], 1), mbar_init(&bars->sched_empty[x], kConsumers);
         mbar_init(&bars->clc, 1);
         mbar_init(&bars->drain, 1);
@@ -161,10 +167,10 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
         // ======================= exponentials and sums ===========================================
         const int t = (warp >> 2) & 1, half = warp >> 3, quad = warp & 3;  // key tile, half of the columns, lanes of tensor memory
         const int in_tile = quad * 32 + lane;
-        const uint32_t at = tmem_base + C::kColS + t * C::kScores * C::kHalf + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t at = tmem_base + C::kColS + C::kHalf * half + (static_cast<uint32_t>(quad * 32) << 16);
         const uint64_t scale2 = f2_pack(a.scale_log2, a.scale_log2);
         uint32_t st = 0, q_use = 0;  // place in the ring of row tiles, and its use's parity
-        uint32_t sc = 0, s_use = 0;  // the same of the score tile of the next row tile's first half
+        ScoreTiles scores;
         bool ok = true;
         for (int k = 0; ok; ++k) {
             WeightsItem w;
@@ -177,12 +183,12 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
             for (int r = w.r0; r < w.r1; ++r, x.next(groups, tokens_log2)) {
                 const int end_pos = x.first_pos + (1 << tokens_log2) - 1;
                 if (!mbar_wait_uniform(&bars->l_full[st], q_use, ctx, kWaitWeights + 31)) { ok = false; break; }
-                if (tile_attended<kWindow>(a, w.last, x.first_pos, end_pos, key_low)) {
-                    uint32_t b = sc + half, use = s_use;
-                    if (b == C::kScores) b = 0, use ^= 1;
-                    sc += 2;
-                    if (sc >= C::kScores) sc -= C::kScores, s_use ^= 1;
-                    const uint32_t at_b = at + b * C::kHalf;
+                const uint32_t b = scores.tile(t), use = scores.use(t), at_b = at + b * kTile;
+                scores.next_row_tile();
+                if (!tile_attended<kWindow>(a, w.last, x.first_pos, end_pos, key_low)) {
+                    if (!mbar_wait_uniform(&bars->s_full[b], use, ctx, kWaitWeights + 35)) { ok = false; break; }
+                    mbar_arrive_warp(&bars->s_empty[b]);
+                } else {
                     const float4* lse = reinterpret_cast<const float4*>(sLse + st * kTile + C::kHalf * half);
                     // Most tiles are whole: every row is there and attends every key.
                     const bool whole = end_pos <= w.last && key_low + (kTile - 1) <= x.first_pos &&
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
                         from = (max(min(key - x.first_pos, kTile), 0) << p.pack_log2) - C::kHalf * half;
                         to = (last + 1) * (1 << p.pack_log2) - C::kHalf * half;
                     }
-                    if (!mbar_wait_uniform(&bars->s_full[t][b], use, ctx, kWaitWeights + 32)) { ok = false; break; }
+                    if (!mbar_wait_uniform(&bars->s_full[b], use, ctx, kWaitWeights + 32)) { ok = false; break; }
                     tc_fence_after();
                     // 16 columns at a time, the next ones on their way.  (With 32 the 64 registers did not fit beside the rest, and a register that a load in
                     // flight has yet to write must not be spilled.)
@@ -211,7 +217,7 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
                                 tmem_ld_32x16(at_b + 16 * (c + 1), s[(c + 1) & 1]);
                             } else {
                                 tc_fence_before();
-                                mbar_arrive_warp(&bars->s_empty[t][b]);
+                                mbar_arrive_warp(&bars->s_empty[b]);
                             }
                             const uint32_t(&col)[16] = s[c & 1];
 #pragma unroll
@@ -390,48 +396,35 @@ __global__ void __launch_bounds__(TileCfg<HD, kE4M3>::kThreads, 1) s2a_weights_t
         __syncwarp();
     } else if (warp == 21) {
         // ======================= MMA issuer ======================================================
-        constexpr uint32_t idesc = idesc_bf16(128, C::kHalf, 0, 0);
+        constexpr uint32_t idesc = idesc_bf16(128, kTile, 0, 0);
         const uint32_t dQ = desc_lo_k_major(smem_u32(sQ));
-        uint32_t st = 0, q_use = 0, sc[2] = {0, 0}, s_use[2] = {0, 0};  // as above, by key tile
+        uint32_t st = 0, q_use = 0;  // as above
+        ScoreTiles scores;
         bool ok = true;
         for (int k = 0; ok; ++k) {
             WeightsItem w;
             if (!next_item(k, kWaitWeights + 10, &w)) break;
-            bool fresh[2] = {true, true};  // key tiles that are not known to be there
-            RowTiles x(p, w, tokens_log2);
-            for (int r = w.r0; r < w.r1; ++r, x.next(groups, tokens_log2)) {
-                const int end_pos = x.first_pos + (1 << tokens_log2) - 1;
+            for (int r = w.r0; ok && r < w.r1; ++r, scores.next_row_tile()) {
                 if (!mbar_wait_uniform(&bars->q_full[st], q_use, ctx, kWaitWeights + 12)) { ok = false; break; }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (!ok || !tile_attended<kWindow>(a, w.last, x.first_pos, end_pos, w.key0 + t * kTile)) continue;
-                    if (fresh[t] && !mbar_wait_uniform(&bars->k_full[t], k & 1, ctx, kWaitWeights + 11)) { ok = false; continue; }
-                    fresh[t] = false;
+                    if (ok && r == w.r0 && !mbar_wait_uniform(&bars->k_full[t], k & 1, ctx, kWaitWeights + 11)) ok = false;
+                    const uint32_t b = scores.tile(t);
+                    if (!ok || !mbar_wait_uniform(&bars->s_empty[b], scores.use(t) ^ 1, ctx, kWaitWeights + 13)) { ok = false; continue; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t at_q = dQ + st * (C::kTileBytes >> 4), acc = tmem_base + C::kColS + b * kTile;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        if (!ok || !mbar_wait_uniform(&bars->s_empty[t][sc[t]], s_use[t] ^ 1, ctx, kWaitWeights + 13)) { ok = false; continue; }
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint32_t at_q = dQ + ((st * C::kTileBytes + half * C::kHalf * 128) >> 4), acc = tmem_base + C::kColS + (t * C::kScores + sc[t]) * C::kHalf;
-#pragma unroll
-                            for (int kk = 0; kk < HD / 16; ++kk)
-                                mma_ts(acc, tmem_base + t * C::kKeyCols + kk * 8, at_q + desc_step_k_major(kk, C::kBoxBytes), idesc, kk > 0);
-                            mma_commit(&bars->s_full[t][sc[t]]);
-                        }
-                        __syncwarp();
-                        if (++sc[t] == C::kScores) sc[t] = 0, s_use[t] ^= 1;
+                        for (int kk = 0; kk < HD / 16; ++kk)
+                            mma_ts(acc, tmem_base + t * C::kKeyCols + kk * 8, at_q + desc_step_k_major(kk, C::kBoxBytes), idesc, kk > 0);
+                        mma_commit(&bars->s_full[b]);
+                        if (t == 1) mma_commit(&bars->q_empty[st]);
+                        if (t == 1 && r == w.r1 - 1) mma_commit(&bars->k_empty);
                     }
+                    __syncwarp();
                 }
-                if (!ok) break;
-                if (elect_one()) mma_commit(&bars->q_empty[st]);
-                __syncwarp();
                 if (++st == C::kRing) st = 0, q_use ^= 1;
             }
-            // A key tile that no row tile of the item attends is written all the same: the next item's keys must not be there before it has been waited for.
-            for (int t = 0; t < 2 && ok; ++t)
-                if (fresh[t] && !mbar_wait_uniform(&bars->k_full[t], k & 1, ctx, kWaitWeights + 14)) ok = false;
-            if (ok && elect_one()) mma_commit(&bars->k_empty);
-            __syncwarp();
         }
         // MMAs already issued must finish before tensor memory is released
         if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&bars->abort_flag) != 0)) {
