@@ -13,7 +13,6 @@ namespace s2a {
 namespace {
 
 constexpr long long kIntMax = 0x7fffffffLL;
-constexpr int kMostRun = 8;  // heads of an item, see rotate_kernels.cu
 
 // `x` [T, heads, d] with `stride` values from a token to the next
 int check_rows(const void* x, long long stride, int T, int heads, int d) {
@@ -57,15 +56,13 @@ HeadRows rows_of(const void* x, long long stride, int heads) {
     return r;
 }
 
-// Heads of an item: as many as leave `groups` items, so that few tokens have their heads spread over the GPU.
-int run_of(long long rows, long long groups) {
-    int run = kMostRun;
-    while (run > 1 && rows / run < groups) run /= 2;
-    return run;
+// The blocks of a launch: as many tokens as have a block's rows, whole; of few tokens the heads are spread over more blocks, two for each multiprocessor.
+RowBlocks blocks_of(int T, int H, int Hk, int Hv, int d, int n_sm) {
+    const int all = H + Hk + Hv, most = rotate_rows(d);
+    int rows = most;
+    while (rows > most / 4 && static_cast<long long>(T) * all < static_cast<long long>(rows) * 2 * n_sm) rows /= 2;
+    return RowBlocks(H, Hk, Hv, std::max(1, rows / all), rows);
 }
-
-// Items that fill the GPU's multiprocessors a few times: 64 of each.
-constexpr int kItemsOfSm = 64;
 
 // One kernel for the forward pass, and for gradients that go through no norm.
 int rotate_impl(const void* q, long long q_stride, const void* k, long long k_stride, void* q_out, long long q_out_stride, void* k_out, long long k_out_stride,
@@ -79,23 +76,20 @@ int rotate_impl(const void* q, long long q_stride, const void* k, long long k_st
     p.out[0] = static_cast<__nv_bfloat16*>(q_out), p.out[1] = static_cast<__nv_bfloat16*>(k_out);
     p.out_stride[0] = q_out_stride, p.out_stride[1] = k_out_stride;
     p.rotation = rotation_of(rotation), p.backwards = backwards, p.T = T;
-    p.runs = HeadRuns(run_of(static_cast<long long>(T) * (H + Hkv), static_cast<long long>(ds->n_sm) * kItemsOfSm), H, Hkv, 0);
+    p.blocks = blocks_of(T, H, Hkv, 0, d, ds->n_sm);
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     const cudaError_t e = launch_rotate(p, RotateTo::kTensors, rotation->norm != 0 && !backwards, d, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? S2A_OK : cuda_fail(e);
 }
 
-// The blocks of the backward's grid that have q's rows and k's: in proportion, at least one each, no more than there are items.
+// The blocks of the backward's grid that have q's rows and k's: in proportion, at least one each, no more than there are chunks.
 void bwd_blocks(RotateBwdParams* p, int n_sm, int d) {
-    const int heads[2] = {p->in[0].heads, p->in[1].heads}, all = rotate_bwd_blocks(n_sm), groups = 256 * 16 / d;
+    const int heads[2] = {p->in[0].heads, p->in[1].heads}, all = rotate_bwd_blocks(n_sm);
     const int of_q = std::min(all - 1, std::max(1, static_cast<int>(static_cast<long long>(all) * heads[0] / (heads[0] + heads[1]))));
     for (int x = 0; x < 2; ++x) {
-        p->blocks[x] = x == 0 ? of_q : all - of_q;
-        const long long rows = static_cast<long long>(p->T) * heads[x];
-        p->run[x] = run_of(rows, static_cast<long long>(p->blocks[x]) * groups);
-        const int runs = (heads[x] + p->run[x] - 1) / p->run[x];
-        p->by_runs[x] = FastDiv(runs);
-        p->blocks[x] = static_cast<int>(std::min<long long>(p->blocks[x], (static_cast<long long>(p->T) * runs + groups - 1) / groups));
+        p->tokens[x] = std::min(4096 / d, std::max(1, rotate_bwd_rows(d) / heads[x]));  // (two chunks' sines and cosines in 32 KB)
+        p->by_heads[x] = FastDiv(heads[x]);
+        p->blocks[x] = std::min(x == 0 ? of_q : all - of_q, (p->T + p->tokens[x] - 1) / p->tokens[x]);
     }
 }
 
@@ -172,7 +166,7 @@ int s2a_rotate_write(const void* q, long long q_stride, const void* k, long long
     p.in[0] = rows_of(q, q_stride, H), p.in[1] = rows_of(k, k_stride, Hkv), p.in[2] = rows_of(v, v_stride, Hkv);
     p.out[0] = static_cast<__nv_bfloat16*>(q_out), p.out_stride[0] = static_cast<long long>(H) * d;
     p.rotation = rotation_of(rotation), p.T = T;
-    p.runs = HeadRuns(run_of(static_cast<long long>(T) * (H + 2 * Hkv), static_cast<long long>(ds->n_sm) * kItemsOfSm), H, Hkv, Hkv);
+    p.blocks = blocks_of(T, H, Hkv, Hkv, d, ds->n_sm);
     p.batch = batch_of(batch), p.pool = pool_of(cache);
     p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
     const RotateTo to = cache->type == S2A_CACHE_E4M3 ? RotateTo::kCacheE4M3 : RotateTo::kCacheBf16;

@@ -28,19 +28,20 @@ struct Rotation {
     float eps;
 };
 
-// Items are runs of `run` heads of a token: those of q, then of k (and of v).
-struct HeadRuns {
-    int run, first_k, first_v, count;  // `count` runs of a token, those of k from first_k on, of v from first_v on
-    FastDiv by_count;
-    HeadRuns() = default;
-    HeadRuns(int run_, int H, int Hk, int Hv) : run(run_) {
-        first_k = (H + run - 1) / run, first_v = first_k + (Hk + run - 1) / run, count = first_v + (Hv + run - 1) / run;
-        by_count = FastDiv(count);
+// A block's rows: `rows` heads, one after the other, of a tile of `tokens` tokens (their heads of q, then of k, then of v).
+struct RowBlocks {
+    int heads[2], all;       // of a token: first one of k, of v; all of them
+    int tokens, rows, count; // count: blocks of a tile
+    FastDiv by_count, by_heads;
+    RowBlocks() = default;
+    RowBlocks(int H, int Hk, int Hv, int tokens_, int rows_) : heads{H, H + Hk}, all(H + Hk + Hv), tokens(tokens_), rows(rows_) {
+        count = static_cast<int>((static_cast<long long>(tokens) * all + rows - 1) / rows);
+        by_count = FastDiv(count), by_heads = FastDiv(all);
     }
-    // run `i` of a token: 0 q, 1 k, 2 v, and its first head
-    __host__ __device__ int kind(int i, int* head) const {
-        const int kind = i < first_k ? 0 : i < first_v ? 1 : 2;
-        *head = (i - (kind == 0 ? 0 : kind == 1 ? first_k : first_v)) * run;
+    // head `h` of a token: 0 q, 1 k, 2 v, and which of them
+    __host__ __device__ int kind(int h, int* head) const {
+        const int kind = h < heads[0] ? 0 : h < heads[1] ? 1 : 2;
+        *head = h - (kind == 0 ? 0 : heads[kind - 1]);
         return kind;
     }
 };
@@ -51,7 +52,7 @@ struct RotateParams {
     long long out_stride[2];
     Rotation rotation;
     bool backwards;  // by the negative angles
-    HeadRuns runs;
+    RowBlocks blocks;
     int T;
     // into the cache
     PagedBatch batch;
@@ -66,9 +67,9 @@ struct RotateBwdParams {
     float* weight_grad[2];    // [d]
     Rotation rotation;
     int T;
-    int run[2];               // heads of an item, of either kind
     int blocks[2];            // of the grid, that have q's rows and k's
-    FastDiv by_runs[2];
+    int tokens[2];            // of a chunk of rows
+    FastDiv by_heads[2];
     float* partial;           // [blocks[0] + blocks[1]][d]
     int* status;
 };
@@ -76,6 +77,8 @@ struct RotateBwdParams {
 enum class RotateTo { kTensors, kCacheBf16, kCacheE4M3 };
 cudaError_t launch_rotate(const RotateParams& p, RotateTo to, bool norm, int d, cudaStream_t stream);
 cudaError_t launch_rotate_bwd(const RotateBwdParams& p, int d, cudaStream_t stream);
+int rotate_rows(int d);           // of a block at most
 int rotate_bwd_blocks(int n_sm);  // of the grid, of both kinds together
+int rotate_bwd_rows(int d);       // of a chunk
 
 }  // namespace s2a

@@ -6,13 +6,15 @@
 // bf16 once.
 //
 // Angles: a frequency is a whole number of 2^-64 turns, so its product with a position, modulo 2^64, is the angle's fraction of a turn
-// at any position; its upper 32 bits go to fp32 (off by 2^-25 of half a turn at most) and to sincospif.  A row is d / 16 lanes, a lane has both
-// values of eight pairs (two pieces of 16 bytes, d / 8 or r / 2 values apart), so that only the sums of a norm cross lanes.  A lane's eight sines and cosines
-// serve all heads of its item, a run of up to 8 heads of one token: of more is left for registers that hold loads in flight, and single
-// tokens need their heads spread out.
+// at any position, of which 32 bits count; 24 of them go to sincospif, the others into the first two terms of the sums of angles.  A row is d / 16 lanes, a lane has both
+// values of eight pairs (two pieces of 16 bytes, d / 8 or r / 2 values apart), so that only the sums of a norm cross lanes.  A block's tokens have their sines and cosines in shared
+// memory, each made once: a lane that made its own for the 8 heads it had of a token spent as long on them, and had no registers left for loads in flight (32768 tokens of
+// 32 + 32 heads of 128 329 us, so @).
 //
 // Bound by HBM: each value is read and written once (the backward of a norm reads two).
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "paged_device.cuh"
 #include "rotate.h"
@@ -22,12 +24,13 @@ namespace s2a {
 namespace {
 
 constexpr int kRotateThreads = 256;
-constexpr int kAtOnce = 2;  // rows whose loads a lane has in flight
+constexpr int kRowsOfLane = 4;  // whose loads a lane has in flight
 
 template <int HD>
 struct RowLanes {
     static constexpr int kLanes = HD / 16;
     static constexpr int kGroups = kRotateThreads / kLanes;  // rows of a block at a time
+    static constexpr int kTable = HD;                        // sines and cosines of a token
 };
 
 // Where a lane's two pieces of 8 values are in a row, and whether they are rotated.
@@ -68,42 +71,56 @@ __device__ __forceinline__ int position_of(const Rotation& ro, int t) {
     return ro.positions ? S2A_LOAD(ro.positions + rest) : rest;
 }
 
-// cos and sin of a lane's pairs: pair i < 8 is values i and 8 + i of its 16, or 2i and 2i + 1 where they are interleaved.
-struct Angles {
-    float cos[8], sin[8];
-    __device__ __forceinline__ void set(const Rotation& ro, const Pieces& pieces, int position, bool backwards) {
-        if (!pieces.turned) return;
+// Cosines and sines of a token's pairs in shared memory: [4][lanes of a row][4], a lane's pairs 2 j and 2 j + 1 as four numbers, so that lanes that read theirs meet in no bank.
+// Pair i < 8 of a lane is values i and 8 + i of its 16, or 2 i and 2 i + 1 where they are interleaved.
+template <int HD>
+__device__ __forceinline__ void make_angle(float* table, const Rotation& ro, int pair, int position, bool backwards) {
+    int part, i;
+    if (!ro.interleaved) part = pair / 8, i = pair % 8;
+    else part = (pair < ro.r / 4 ? pair : pair - ro.r / 4) / 4, i = pair % 4 + (pair < ro.r / 4 ? 0 : 4);
+    const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(position)) * static_cast<unsigned long long>(S2A_LOAD(ro.turns + pair));
+    const int fraction = static_cast<int>(turn >> 32);
+    float s, c;
+    sincospif(static_cast<float>(fraction & ~255) * 0x1p-31f, &s, &c);
+    const float rest = static_cast<float>(fraction & 255) * (3.14159265358979f * 0x1p-31f);
+    float2 x = make_float2(fmaf(-rest, s, c), fmaf(rest, c, s));
+    if (backwards) x.y = -x.y;
+    *reinterpret_cast<float2*>(table + (i / 2 * RowLanes<HD>::kLanes + part) * 4 + i % 2 * 2) = x;
+}
+template <int HD>
+__device__ __forceinline__ void turn_row(float (&x)[16], const float* table, const Pieces& pieces, int part, bool interleaved) {
+    if (!pieces.turned) return;
+    auto pair = [](float& u, float& v, float c, float s) {
+        const float a = u, b = v;
+        u = a * c - b * s, v = a * s + b * c;
+    };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int pair = !ro.interleaved ? pieces.at[0] + i : i < 4 ? pieces.at[0] / 2 + i : pieces.at[1] / 2 + i - 4;
-            const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(position)) * static_cast<unsigned long long>(S2A_LOAD(ro.turns + pair));
-            sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 0x1p-31f, &sin[i], &cos[i]);
-            if (backwards) sin[i] = -sin[i];
-        }
-    }
-    __device__ __forceinline__ void turn(float (&x)[16], const Pieces& pieces, bool interleaved) const {
-        if (!pieces.turned) return;
-        auto pair = [&](float& u, float& v, int i) {
-            const float a = u, b = v;
-            u = a * cos[i] - b * sin[i], v = a * sin[i] + b * cos[i];
-        };
+    for (int j = 0; j < 4; ++j) {
+        const float4 y = *reinterpret_cast<const float4*>(table + (j * RowLanes<HD>::kLanes + part) * 4);
         if (interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pair(x[2 * i], x[2 * i + 1], i);
+            pair(x[4 * j], x[4 * j + 1], y.x, y.y);
+            pair(x[4 * j + 2], x[4 * j + 3], y.z, y.w);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pair(x[i], x[8 + i], i);
+            pair(x[2 * j], x[8 + 2 * j], y.x, y.y);
+            pair(x[2 * j + 1], x[8 + 2 * j + 1], y.z, y.w);
         }
     }
-};
+}
 
-// A lane's weights of a norm.
-__device__ __forceinline__ void load_weights(const void* weight, bool f32, const Pieces& pieces, float (&w)[16]) {
+// The weights of a norm, in shared memory as a lane's values: [4][lanes of a row][4].
+template <int HD>
+__device__ __forceinline__ void stage_weights(float* to, const void* weight, bool f32, int r, int c) {
+    const int part = c / 16, i = c % 16, at = Pieces(part, r).at[i / 8] + i % 8;
+    to[(i / 4 * RowLanes<HD>::kLanes + part) * 4 + i % 4] =
+        !weight ? 1.f : f32 ? S2A_LOAD(static_cast<const float*>(weight) + at)
+                            : __uint_as_float(static_cast<uint32_t>(S2A_LOAD(static_cast<const unsigned short*>(weight) + at)) << 16);
+}
+template <int HD>
+__device__ __forceinline__ void times_weights(float (&x)[16], const float* weights, int part) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int at = pieces.at[i / 8] + i % 8;
-        w[i] = !weight ? 1.f : f32 ? S2A_LOAD(static_cast<const float*>(weight) + at)
-                                   : __uint_as_float(static_cast<uint32_t>(S2A_LOAD(static_cast<const unsigned short*>(weight) + at)) << 16);
+    for (int j = 0; j < 4; ++j) {
+        const float4 w = *reinterpret_cast<const float4*>(weights + (j * RowLanes<HD>::kLanes + part) * 4);
+        x[4 * j] *= w.x, x[4 * j + 1] *= w.y, x[4 * j + 2] *= w.z, x[4 * j + 3] *= w.w;
     }
 }
 
@@ -145,151 +162,176 @@ template <int HD, bool kNorm, RotateTo kTo>
 __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_kernel(const __grid_constant__ RotateParams p) {
     using L = RowLanes<HD>;
     constexpr bool kCache = kTo != RotateTo::kTensors, kE4M3 = kTo == RotateTo::kCacheE4M3;
+    extern __shared__ __align__(16) float s_table[];  // [tokens][kTable]
+    __shared__ __align__(16) float s_weights[kNorm ? 2 : 1][kNorm ? HD : 1];
+    __shared__ int s_place[kCache ? L::kGroups * kRowsOfLane : 1];            // of each token in the cache, -1: of no sequence
+    __shared__ long long s_cached[kCache ? L::kGroups * kRowsOfLane : 1];     // its row of the pools in head 0, -1: no page
     release_successor();
     wait_for_predecessor();
-    if (*reinterpret_cast<volatile int*>(p.status) != 0) return;
+    const int standing = *reinterpret_cast<volatile int*>(p.status);
     if (kCache && blockIdx.x == 0) check_batch(p.batch, p.pool.page_log2, 0x7fffffff, p.status, p.host_status);
-    const int part = static_cast<int>(threadIdx.x) % L::kLanes;
-    const long long item = static_cast<long long>(blockIdx.x) * L::kGroups + threadIdx.x / L::kLanes;
-    int run, head;
-    bool there = item < static_cast<long long>(p.T) * p.runs.count;
-    const int t = p.runs.by_count(there ? static_cast<int>(item) : 0, &run);
-    const int kind = p.runs.kind(run, &head);
-    const HeadRows in = p.in[kind];
-    const int heads = min(p.runs.run, in.heads - head);
-    const Pieces pieces(part, kind == 2 ? 0 : p.rotation.r);
-    const __nv_bfloat16* row = in.x + t * in.stride + head * HD;
-    uint4 next[kAtOnce][2];
-    auto load = [&](int first) {
+    const int part = static_cast<int>(threadIdx.x) % L::kLanes, group = static_cast<int>(threadIdx.x) / L::kLanes;
+    int within;
+    const int t0 = p.blocks.by_count(static_cast<int>(blockIdx.x), &within) * p.blocks.tokens, tokens = min(p.blocks.tokens, p.T - t0);
+    const int first = within * p.blocks.rows, rows = min(p.blocks.rows, tokens * p.blocks.all - first);
+    if (rows <= 0) return;
+    // this lane's rows: where they are, and what is there, before anything is known about their tokens
+    int token[kRowsOfLane], kind[kRowsOfLane], head[kRowsOfLane];
+    bool there[kRowsOfLane];
+    uint4 x[kRowsOfLane][2];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            next[i][0] = next[i][1] = make_uint4(0, 0, 0, 0);
-            if (there && first + i < heads) load_row(row + (first + i) * HD, pieces, next[i]);
-        }
-    };
-    load(0);
-    long long cached = -1;  // the token's row of the pools, in head 0
-    int place = 0;
+    for (int i = 0; i < kRowsOfLane; ++i) {
+        const int r = i * L::kGroups + group;
+        there[i] = r < rows;
+        int h;
+        token[i] = p.blocks.by_heads(first + (there[i] ? r : 0), &h);
+        kind[i] = p.blocks.kind(h, &head[i]);
+        const HeadRows& in = p.in[kind[i]];
+        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+        if (there[i]) load_row(in.x + (t0 + token[i]) * in.stride + head[i] * HD, Pieces(part, kind[i] == 2 ? 0 : p.rotation.r), x[i]);
+    }
+    // sines and cosines of the tokens that the block's rows belong to
+    const int low = p.blocks.by_heads(first), high = p.blocks.by_heads(first + rows - 1);
     if constexpr (kCache) {
-        const int b = find_sequence(p.batch.starts, p.batch.B, t);
-        Sequence s;
-        there = there && sequence_of(p.batch, p.pool.page_log2, 0x7fffffff, b, &s) == 0 && t >= s.row0 && t < s.row0 + s.n;
-        if (there) {
-            place = s.length - s.n + t - s.row0;
-            if (kind != 0) {
+        for (int i = low + static_cast<int>(threadIdx.x); i <= high; i += kRotateThreads) {
+            const int t = t0 + i, b = find_sequence(p.batch.starts, p.batch.B, t);
+            Sequence s;
+            int place = -1;
+            long long cached = -1;
+            if (sequence_of(p.batch, p.pool.page_log2, 0x7fffffff, b, &s) == 0 && t >= s.row0 && t < s.row0 + s.n) {
+                place = s.length - s.n + t - s.row0;
                 cached = pool_row(p.batch, p.pool, b, place);
-                if (cached < 0) report_bad_index(p.status, p.host_status, kBadPage), there = false;
+                if (cached < 0) report_bad_index(p.status, p.host_status, kBadPage);
             }
+            s_place[i - low] = place, s_cached[i - low] = cached;
         }
+        if (!p.rotation.positions) __syncthreads();
     }
-    Angles angles;
-    float w[16];
-    if (there && kind != 2) {
-        angles.set(p.rotation, pieces, kCache && !p.rotation.positions ? place : position_of(p.rotation, t), p.backwards);
-        if constexpr (kNorm) load_weights(p.rotation.weight[kind], p.rotation.weight_f32, pieces, w);
+    const int pairs = p.rotation.r / 2;
+    for (int i = threadIdx.x; i < (high - low + 1) * (HD / 2); i += kRotateThreads) {
+        const int at = i / (HD / 2), pair = i % (HD / 2);
+        if (pair < pairs)
+            make_angle<HD>(s_table + at * L::kTable, p.rotation, pair, kCache && !p.rotation.positions ? s_place[at] : position_of(p.rotation, t0 + low + at), p.backwards);
     }
-    // (all lanes of a warp go through all turns: sums of a row are taken by the whole warp)
-    for (int first = 0; first < p.runs.run; first += kAtOnce) {
-        uint4 now[kAtOnce][2];
+    if constexpr (kNorm) {
+        for (int i = threadIdx.x; i < 2 * HD; i += kRotateThreads) stage_weights<HD>(s_weights[i / HD], p.rotation.weight[i / HD], p.rotation.weight_f32, p.rotation.r, i % HD);
+    }
+    __syncthreads();
+    if (standing != 0) return;
+    // (all lanes of a warp go through all rows: sums of a row are taken by the whole warp)
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) now[i][0] = next[i][0], now[i][1] = next[i][1];
-        load(first + kAtOnce);
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            float x[16];
-            unpack_row(now[i], x);
-            if constexpr (kNorm) {
-                normalise_row<HD>(x, p.rotation.eps);  // (by the whole warp)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] *= w[e];
-            }
-            if (kind != 2) {
-                angles.turn(x, pieces, p.rotation.interleaved);
-                pack_row(x, now[i]);
-            }
-            const bool mine = there && first + i < heads;
-            if constexpr (kCache) {
-                const long long to = cached + (static_cast<long long>(head + first + i) << p.pool.page_log2);
-                void* pool = kind == 2 ? p.pool.v : p.pool.k;
-                if constexpr (kE4M3) {
-                    const uint32_t words[8] = {now[i][0].x, now[i][0].y, now[i][0].z, now[i][0].w, now[i][1].x, now[i][1].y, now[i][1].z, now[i][1].w};
-                    uint32_t codes[4];
-                    const int exp = row_to_e4m3<L::kLanes>(words, codes);
-                    if (mine && kind != 0) {
-                        uint8_t* cell = static_cast<uint8_t*>(pool) + to * HD;
-                        *reinterpret_cast<uint2*>(cell + pieces.at[0]) = make_uint2(codes[0], codes[1]);
-                        *reinterpret_cast<uint2*>(cell + pieces.at[1]) = make_uint2(codes[2], codes[3]);
-                        if (part == 0) (kind == 2 ? p.pool.v_exp : p.pool.k_exp)[to] = static_cast<int8_t>(exp);
-                    }
-                } else if (mine && kind != 0) {
-                    store_row(static_cast<__nv_bfloat16*>(pool) + to * HD, pieces, now[i]);
+    for (int i = 0; i < kRowsOfLane; ++i) {
+        const Pieces pieces(part, kind[i] == 2 ? 0 : p.rotation.r);
+        const int t = t0 + token[i], at = token[i] - low;
+        float y[16];
+        unpack_row(x[i], y);
+        if constexpr (kNorm) {
+            normalise_row<HD>(y, p.rotation.eps);
+            times_weights<HD>(y, s_weights[kind[i] == 0 ? 0 : 1], part);
+        }
+        if (kind[i] != 2) {
+            turn_row<HD>(y, s_table + at * L::kTable, pieces, part, p.rotation.interleaved);
+            pack_row(y, x[i]);
+        }
+        if constexpr (kCache) {
+            const bool mine = there[i] && s_place[at] >= 0;
+            const long long cached = s_cached[at], to = cached + (static_cast<long long>(head[i]) << p.pool.page_log2);
+            void* pool = kind[i] == 2 ? p.pool.v : p.pool.k;
+            if constexpr (kE4M3) {
+                const uint32_t words[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+                uint32_t codes[4];
+                const int exp = row_to_e4m3<L::kLanes>(words, codes);
+                if (mine && kind[i] != 0 && cached >= 0) {
+                    uint8_t* cell = static_cast<uint8_t*>(pool) + to * HD;
+                    *reinterpret_cast<uint2*>(cell + pieces.at[0]) = make_uint2(codes[0], codes[1]);
+                    *reinterpret_cast<uint2*>(cell + pieces.at[1]) = make_uint2(codes[2], codes[3]);
+                    if (part == 0) (kind[i] == 2 ? p.pool.v_exp : p.pool.k_exp)[to] = static_cast<int8_t>(exp);
                 }
-                if (mine && kind == 0) store_row(p.out[0] + t * p.out_stride[0] + (head + first + i) * HD, pieces, now[i]);
-            } else if (mine) {
-                store_row(p.out[kind] + t * p.out_stride[kind] + (head + first + i) * HD, pieces, now[i]);
+            } else if (mine && kind[i] != 0 && cached >= 0) {
+                store_row(static_cast<__nv_bfloat16*>(pool) + to * HD, pieces, x[i]);
             }
+            if (mine && kind[i] == 0) store_row(p.out[0] + t * p.out_stride[0] + head[i] * HD, pieces, x[i]);
+        } else if (there[i]) {
+            store_row(p.out[kind[i]] + t * p.out_stride[kind[i]] + head[i] * HD, pieces, x[i]);
         }
     }
 }
 
-// Gradients through a norm.  A block has rows of q or of k alone; its sums for the weight's gradient go to p.partial, in an order that the sizes
-// and the number of multiprocessors fix.
+// Gradients through a norm.  A block has rows of q or of k alone, in chunks of a few tokens; its sums for the weight's gradient go to p.partial, in an order that the sizes
+// and the number of multiprocessors fix.  The next chunk's sines and cosines are made, and its first rows requested, before a chunk is worked on.
+constexpr int kBwdRowsOfLane = 4;  // of a chunk
 template <int HD>
 __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_bwd_kernel(const __grid_constant__ RotateBwdParams p) {
     using L = RowLanes<HD>;
+    extern __shared__ __align__(16) float s_table[];  // [2][tokens of a chunk][kTable]
+    __shared__ __align__(16) float s_weights[HD];
     __shared__ float s_sum[kRotateThreads / 32][HD];
     release_successor();
     wait_for_predecessor();
     if (*reinterpret_cast<volatile int*>(p.status) != 0) return;
     const int kind = static_cast<int>(blockIdx.x) < p.blocks[0] ? 0 : 1;
-    const int block = static_cast<int>(blockIdx.x) - (kind ? p.blocks[0] : 0);
-    const int part = static_cast<int>(threadIdx.x) % L::kLanes;
+    const int part = static_cast<int>(threadIdx.x) % L::kLanes, group = static_cast<int>(threadIdx.x) / L::kLanes;
     const Pieces pieces(part, p.rotation.r);
     const HeadRows in = p.in[kind], grad = p.grad[kind];
-    const int run = p.run[kind], runs = static_cast<int>(p.by_runs[kind].d);
-    const long long items = static_cast<long long>(p.T) * runs, stride = static_cast<long long>(p.blocks[kind]) * L::kGroups;
-    float w[16], sum[16];
-    load_weights(p.rotation.weight[kind], p.rotation.weight_f32, pieces, w);
+    const FastDiv by_heads = p.by_heads[kind];
+    const int tokens = p.tokens[kind], blocks = p.blocks[kind], chunks = (p.T + tokens - 1) / tokens, pairs = p.rotation.r / 2;
+    for (int i = threadIdx.x; i < HD; i += kRotateThreads) stage_weights<HD>(s_weights, p.rotation.weight[kind], p.rotation.weight_f32, p.rotation.r, i);
+    auto angles = [&](int chunk, float* table) {
+        for (int i = threadIdx.x; i < tokens * (HD / 2); i += kRotateThreads) {
+            const int at = i / (HD / 2), pair = i % (HD / 2), t = chunk * tokens + at;
+            if (pair < pairs && t < p.T) make_angle<HD>(table + at * L::kTable, p.rotation, pair, position_of(p.rotation, t), true);
+        }
+    };
+    float sum[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-    const long long mine = static_cast<long long>(block) * L::kGroups + threadIdx.x / L::kLanes;
-    // (whole turns for all lanes of a warp)
-    for (long long item = mine; item - mine + static_cast<long long>(block) * L::kGroups < items; item += stride) {
-        const bool there = item < items;
-        int head;
-        const int t = p.by_runs[kind](there ? static_cast<int>(item) : 0, &head);
-        head *= run;
-        const int heads = there ? min(run, in.heads - head) : 0;
-        const __nv_bfloat16* x_row = in.x + t * in.stride + head * HD;
-        const __nv_bfloat16* g_row = grad.x + t * grad.stride + head * HD;
-        uint4 next_x[2], next_g[2];
-        auto load = [&](int i) {
-            next_x[0] = next_x[1] = next_g[0] = next_g[1] = make_uint4(0, 0, 0, 0);
-            if (i < heads) load_row(x_row + i * HD, pieces, next_x), load_row(g_row + i * HD, pieces, next_g);
-        };
-        load(0);
-        Angles angles;
-        angles.set(p.rotation, pieces, position_of(p.rotation, t), true);
-        for (int i = 0; i < run; ++i) {
-            uint4 now[2];
+    uint4 next_x[2], next_g[2];
+    int next_token = 0, next_head = 0;
+    bool next_there = false;
+    // row i of this lane's of a chunk
+    auto load = [&](int chunk, int i) {
+        const int r = i * L::kGroups + group;
+        next_there = chunk < chunks && r < min(tokens, p.T - chunk * tokens) * in.heads;
+        next_x[0] = next_x[1] = next_g[0] = next_g[1] = make_uint4(0, 0, 0, 0);
+        if (next_there) {
+            next_token = by_heads(r, &next_head);
+            const long long t = chunk * tokens + next_token;
+            load_row(in.x + t * in.stride + next_head * HD, pieces, next_x);
+            load_row(grad.x + t * grad.stride + next_head * HD, pieces, next_g);
+        }
+    };
+    int chunk = static_cast<int>(blockIdx.x) - (kind ? p.blocks[0] : 0);
+    load(chunk, 0);
+    if (chunk < chunks) angles(chunk, s_table);
+    for (int turn = 0; chunk < chunks; chunk += blocks, turn ^= 1) {
+        __syncthreads();  // this chunk's table is there, and the other one is free
+        if (chunk + blocks < chunks) angles(chunk + blocks, s_table + (turn ^ 1) * tokens * L::kTable);
+        const float* table = s_table + turn * tokens * L::kTable;
+#pragma unroll 1
+        for (int i = 0; i < kBwdRowsOfLane; ++i) {
+            const bool there = next_there;
+            const int at = next_token, head = next_head;
             float x[16], g[16];
             unpack_row(next_x, x);
             unpack_row(next_g, g);
-            load(i + 1);
-            angles.turn(g, pieces, p.rotation.interleaved);
+            if (i + 1 < kBwdRowsOfLane) load(chunk, i + 1);
+            else load(chunk + blocks, 0);
+            turn_row<HD>(g, table + at * L::kTable, pieces, part, p.rotation.interleaved);
             const float s = normalise_row<HD>(x, p.rotation.eps);
+            if (there) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[e] += g[e] * x[e];
+            }
+            times_weights<HD>(g, s_weights, part);
             float mean = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (i < heads) sum[e] += g[e] * x[e];
-                g[e] *= w[e];
-                mean += g[e] * x[e];
-            }
+            for (int e = 0; e < 16; ++e) mean += g[e] * x[e];
             mean = sum_of_row<HD>(mean) * (1.f / HD);
 #pragma unroll
             for (int e = 0; e < 16; ++e) g[e] = s * (g[e] - x[e] * mean);
-            pack_row(g, now);
-            if (i < heads) store_row(p.out[kind] + (static_cast<long long>(t) * in.heads + head + i) * HD, pieces, now);
+            uint4 out[2];
+            pack_row(g, out);
+            if (there) store_row(p.out[kind] + ((static_cast<long long>(chunk) * tokens + at) * in.heads + head) * HD, pieces, out);
         }
     }
     // the block's sums: over the rows of a warp, then over the warps
@@ -329,9 +371,9 @@ __global__ void __launch_bounds__(kJoinThreads) s2a_rotate_join_kernel(const __g
 
 template <int HD, bool kNorm, RotateTo kTo>
 cudaError_t launch_one(const RotateParams& p, cudaStream_t stream) {
-    const long long items = static_cast<long long>(p.T) * p.runs.count;
-    const unsigned grid = static_cast<unsigned>((items + RowLanes<HD>::kGroups - 1) / RowLanes<HD>::kGroups);
-    return launch_kernel(s2a_rotate_kernel<HD, kNorm, kTo>, grid, kRotateThreads, 0, stream, p, true);
+    const long long tiles = (p.T + p.blocks.tokens - 1) / p.blocks.tokens;
+    const int smem = std::min(p.blocks.tokens, p.blocks.rows) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
+    return launch_kernel(s2a_rotate_kernel<HD, kNorm, kTo>, static_cast<unsigned>(tiles * p.blocks.count), kRotateThreads, smem, stream, p, true);
 }
 template <int HD, RotateTo kTo>
 cudaError_t launch_any(const RotateParams& p, bool norm, cudaStream_t stream) {
@@ -344,7 +386,8 @@ cudaError_t launch_to(const RotateParams& p, bool norm, int d, cudaStream_t stre
 
 template <int HD>
 cudaError_t launch_gradients(const RotateBwdParams& p, cudaStream_t stream) {
-    const cudaError_t e = launch_kernel(s2a_rotate_bwd_kernel<HD>, static_cast<unsigned>(p.blocks[0] + p.blocks[1]), kRotateThreads, 0, stream, p, true);
+    const int smem = 2 * std::max(p.tokens[0], p.tokens[1]) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
+    const cudaError_t e = launch_kernel(s2a_rotate_bwd_kernel<HD>, static_cast<unsigned>(p.blocks[0] + p.blocks[1]), kRotateThreads, smem, stream, p, true);
     return e != cudaSuccess ? e : launch_kernel(s2a_rotate_join_kernel<HD>, 2u, kJoinThreads, 0, stream, p, true);
 }
 
@@ -357,6 +400,8 @@ cudaError_t launch_rotate(const RotateParams& p, RotateTo to, bool norm, int d, 
 cudaError_t launch_rotate_bwd(const RotateBwdParams& p, int d, cudaStream_t stream) {
     return d == 64 ? launch_gradients<64>(p, stream) : launch_gradients<128>(p, stream);
 }
+int rotate_rows(int d) { return (d == 64 ? RowLanes<64>::kGroups : RowLanes<128>::kGroups) * kRowsOfLane; }
 int rotate_bwd_blocks(int n_sm) { return 4 * n_sm; }
+int rotate_bwd_rows(int d) { return (d == 64 ? RowLanes<64>::kGroups : RowLanes<128>::kGroups) * kBwdRowsOfLane; }
 
 }  // namespace s2a
