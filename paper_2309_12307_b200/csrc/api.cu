@@ -11,6 +11,7 @@
 #include "host_plan.h"
 #include "host_state.h"
 #include "paged.h"
+#include "rotate.h"
 #include "s2a_params.h"
 #include "sm100_ptx.cuh"
 
@@ -74,6 +75,8 @@ int prepare_device(DeviceState** out) {
         e = configure_fwd();
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_bwd();
+        if (e != cudaSuccess) return cuda_fail(e);
+        e = configure_rotate();
         if (e != cudaSuccess) return cuda_fail(e);
         ds.paged_error = configure_paged_split(ds.cluster_slots);
         if (ds.paged_error == cudaSuccess) ds.paged_error = configure_paged_fwd();

@@ -13,12 +13,14 @@ namespace s2a {
 namespace {
 
 constexpr long long kIntMax = 0x7fffffffLL;
+constexpr long long kMostStride = 1 << 28;  // (64 tokens of it, in eights, fit an int)
 
 // `x` [T, heads, d] with `stride` values from a token to the next
 int check_rows(const void* x, long long stride, int T, int heads, int d) {
     if (!x || !aligned16(x) || heads <= 0) return S2A_ERR_INVALID_ARG;
-    if (T > 1 && (stride % 8 != 0 || stride < static_cast<long long>(heads) * d)) return S2A_ERR_INVALID_ARG;
-    return S2A_OK;
+    if (T == 1) return S2A_OK;
+    if (stride % 8 != 0 || stride < static_cast<long long>(heads) * d) return S2A_ERR_INVALID_ARG;
+    return stride > kMostStride ? S2A_ERR_UNSUPPORTED : S2A_OK;
 }
 
 int check_rotation(const s2a_rotation* ro, int d, bool counted) {
@@ -56,12 +58,17 @@ HeadRows rows_of(const void* x, long long stride, int heads) {
     return r;
 }
 
-// The blocks of a launch: as many tokens as have a block's rows, whole; of few tokens the heads are spread over more blocks, two for each multiprocessor.
+// The blocks of a launch: of few tokens the heads are spread over more blocks, two for each multiprocessor.
 RowBlocks blocks_of(int T, int H, int Hk, int Hv, int d, int n_sm) {
     const int all = H + Hk + Hv, most = rotate_rows(d);
     int rows = most;
     while (rows > most / 4 && static_cast<long long>(T) * all < static_cast<long long>(rows) * 2 * n_sm) rows /= 2;
-    return RowBlocks(H, Hk, Hv, std::max(1, rows / all), rows);
+    // a tile has as many tokens as fill its blocks, up to 16
+    int tokens = std::max(1, rows / all), best = tokens;
+    auto full = [&](int n) { return static_cast<double>(n) * all / ((static_cast<long long>(n) * all + rows - 1) / rows * rows); };
+    for (; tokens <= 16 && tokens <= T; ++tokens)
+        if (full(tokens) > full(best) + 0.02) best = tokens;
+    return RowBlocks(H, Hk, Hv, best, rows);
 }
 
 // One kernel for the forward pass, and for gradients that go through no norm.
@@ -82,15 +89,20 @@ int rotate_impl(const void* q, long long q_stride, const void* k, long long k_st
     return e == cudaSuccess ? S2A_OK : cuda_fail(e);
 }
 
-// The blocks of the backward's grid that have q's rows and k's: in proportion, at least one each, no more than there are chunks.
+// The blocks of the backward's grid that have q's rows and k's: in proportion to what their chunks cost, at least one each, no more than there are chunks.  (A chunk of k's few
+// heads has more tokens, so more sines and cosines: with 16 of them it takes 1.25 times as long as with 2.)
 void bwd_blocks(RotateBwdParams* p, int n_sm, int d) {
-    const int heads[2] = {p->in[0].heads, p->in[1].heads}, all = rotate_bwd_blocks(n_sm);
-    const int of_q = std::min(all - 1, std::max(1, static_cast<int>(static_cast<long long>(all) * heads[0] / (heads[0] + heads[1]))));
+    const int all = rotate_bwd_blocks(n_sm);
+    double cost[2];
     for (int x = 0; x < 2; ++x) {
-        p->tokens[x] = std::min(4096 / d, std::max(1, rotate_bwd_rows(d) / heads[x]));  // (two chunks' sines and cosines in 32 KB)
-        p->by_heads[x] = FastDiv(heads[x]);
-        p->blocks[x] = std::min(x == 0 ? of_q : all - of_q, (p->T + p->tokens[x] - 1) / p->tokens[x]);
+        const int heads = p->in[x].heads, rows = rotate_bwd_rows(d), parts = (heads + rows - 1) / rows;
+        p->tokens[x] = std::min(4096 / d, std::max(1, rows / heads));  // (two chunks' sines and cosines in 32 KB)
+        p->chunks[x] = (p->T + p->tokens[x] - 1) / p->tokens[x] * parts;
+        p->by_heads[x] = FastDiv(heads), p->by_parts[x] = FastDiv(parts);
+        cost[x] = p->chunks[x] * (1 + p->tokens[x] * d / (64.0 * 128));
     }
+    const int of_q = std::min(all - 1, std::max(1, static_cast<int>(all * cost[0] / (cost[0] + cost[1]))));
+    p->blocks[0] = std::min(of_q, p->chunks[0]), p->blocks[1] = std::min(all - of_q, p->chunks[1]);
 }
 
 size_t bwd_bytes(int n_sm, int d) { return static_cast<size_t>(rotate_bwd_blocks(n_sm)) * d * sizeof(float); }

@@ -68,14 +68,15 @@ struct RotateBwdParams {
     Rotation rotation;
     int T;
     int blocks[2];            // of the grid, that have q's rows and k's
-    int tokens[2];            // of a chunk of rows
-    FastDiv by_heads[2];
+    int tokens[2], chunks[2]; // tokens of a chunk of rows; where one token has more rows than a chunk, its parts are chunks
+    FastDiv by_heads[2], by_parts[2];
     float* partial;           // [blocks[0] + blocks[1]][d]
     int* status;
 };
 
 enum class RotateTo { kTensors, kCacheBf16, kCacheE4M3 };
 cudaError_t launch_rotate(const RotateParams& p, RotateTo to, bool norm, int d, cudaStream_t stream);
+cudaError_t configure_rotate();
 cudaError_t launch_rotate_bwd(const RotateBwdParams& p, int d, cudaStream_t stream);
 int rotate_rows(int d);           // of a block at most
 int rotate_bwd_blocks(int n_sm);  // of the grid, of both kinds together

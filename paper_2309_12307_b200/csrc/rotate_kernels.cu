@@ -9,7 +9,7 @@
 // at any position, of which 32 bits count; 24 of them go to sincospif, the others into the first two terms of the sums of angles.  A row is d / 16 lanes, a lane has both
 // values of eight pairs (two pieces of 16 bytes, d / 8 or r / 2 values apart), so that only the sums of a norm cross lanes.  A block's tokens have their sines and cosines in shared
 // memory, each made once: a lane that made its own for the 8 heads it had of a token spent as long on them, and had no registers left for loads in flight (32768 tokens of
-// 32 + 32 heads of 128 329 us, so @).
+// 32 + 32 heads of 128 329 us, so 160 to 173).
 //
 // Bound by HBM: each value is read and written once (the backward of a norm reads two).
 #include <cuda_fp16.h>
@@ -159,7 +159,7 @@ __device__ __forceinline__ float normalise_row(float (&x)[16], float eps) {
 }
 
 template <int HD, bool kNorm, RotateTo kTo>
-__global__ void __launch_bounds__(kRotateThreads) s2a_rotate_kernel(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kRotateThreads, 4) s2a_rotate_kernel(const __grid_constant__ RotateParams p) {
     using L = RowLanes<HD>;
     constexpr bool kCache = kTo != RotateTo::kTensors, kE4M3 = kTo == RotateTo::kCacheE4M3;
     extern __shared__ __align__(16) float s_table[];  // [tokens][kTable]
@@ -176,19 +176,26 @@ __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_kernel(const __grid
     const int first = within * p.blocks.rows, rows = min(p.blocks.rows, tokens * p.blocks.all - first);
     if (rows <= 0) return;
     // this lane's rows: where they are, and what is there, before anything is known about their tokens
-    int token[kRowsOfLane], kind[kRowsOfLane], head[kRowsOfLane];
-    bool there[kRowsOfLane];
+    struct Row {
+        int token, kind, head;
+        bool there;
+    };
+    auto row = [&](int i) -> Row {
+        Row w;
+        const int r = i * L::kGroups + group;
+        w.there = r < rows;
+        int h;
+        w.token = p.blocks.by_heads(first + (w.there ? r : 0), &h);
+        w.kind = p.blocks.kind(h, &w.head);
+        return w;
+    };
     uint4 x[kRowsOfLane][2];
 #pragma unroll
     for (int i = 0; i < kRowsOfLane; ++i) {
-        const int r = i * L::kGroups + group;
-        there[i] = r < rows;
-        int h;
-        token[i] = p.blocks.by_heads(first + (there[i] ? r : 0), &h);
-        kind[i] = p.blocks.kind(h, &head[i]);
-        const HeadRows& in = p.in[kind[i]];
+        const Row w = row(i);
+        const HeadRows& in = p.in[w.kind];
         x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-        if (there[i]) load_row(in.x + (t0 + token[i]) * in.stride + head[i] * HD, Pieces(part, kind[i] == 2 ? 0 : p.rotation.r), x[i]);
+        if (w.there) load_row(in.x + (t0 + w.token) * in.stride + w.head * HD, Pieces(part, w.kind == 2 ? 0 : p.rotation.r), x[i]);
     }
     // sines and cosines of the tokens that the block's rows belong to
     const int low = p.blocks.by_heads(first), high = p.blocks.by_heads(first + rows - 1);
@@ -221,49 +228,59 @@ __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_kernel(const __grid
     // (all lanes of a warp go through all rows: sums of a row are taken by the whole warp)
 #pragma unroll
     for (int i = 0; i < kRowsOfLane; ++i) {
-        const Pieces pieces(part, kind[i] == 2 ? 0 : p.rotation.r);
-        const int t = t0 + token[i], at = token[i] - low;
+        const Row w = row(i);
+        const Pieces pieces(part, w.kind == 2 ? 0 : p.rotation.r);
+        const int t = t0 + w.token, at = w.token - low;
         float y[16];
         unpack_row(x[i], y);
         if constexpr (kNorm) {
             normalise_row<HD>(y, p.rotation.eps);
-            times_weights<HD>(y, s_weights[kind[i] == 0 ? 0 : 1], part);
+            times_weights<HD>(y, s_weights[w.kind == 0 ? 0 : 1], part);
         }
-        if (kind[i] != 2) {
+        if (w.kind != 2) {
             turn_row<HD>(y, s_table + at * L::kTable, pieces, part, p.rotation.interleaved);
             pack_row(y, x[i]);
         }
         if constexpr (kCache) {
-            const bool mine = there[i] && s_place[at] >= 0;
-            const long long cached = s_cached[at], to = cached + (static_cast<long long>(head[i]) << p.pool.page_log2);
-            void* pool = kind[i] == 2 ? p.pool.v : p.pool.k;
+            const bool mine = w.there && s_place[at] >= 0;
+            const long long cached = s_cached[at], to = cached + (static_cast<long long>(w.head) << p.pool.page_log2);
+            void* pool = w.kind == 2 ? p.pool.v : p.pool.k;
             if constexpr (kE4M3) {
+              if (__any_sync(0xffffffffu, w.kind != 0)) {
                 const uint32_t words[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
                 uint32_t codes[4];
                 const int exp = row_to_e4m3<L::kLanes>(words, codes);
-                if (mine && kind[i] != 0 && cached >= 0) {
+                if (mine && w.kind != 0 && cached >= 0) {
                     uint8_t* cell = static_cast<uint8_t*>(pool) + to * HD;
                     *reinterpret_cast<uint2*>(cell + pieces.at[0]) = make_uint2(codes[0], codes[1]);
                     *reinterpret_cast<uint2*>(cell + pieces.at[1]) = make_uint2(codes[2], codes[3]);
-                    if (part == 0) (kind[i] == 2 ? p.pool.v_exp : p.pool.k_exp)[to] = static_cast<int8_t>(exp);
+                    if (part == 0) (w.kind == 2 ? p.pool.v_exp : p.pool.k_exp)[to] = static_cast<int8_t>(exp);
                 }
-            } else if (mine && kind[i] != 0 && cached >= 0) {
+              }
+            } else if (mine && w.kind != 0 && cached >= 0) {
                 store_row(static_cast<__nv_bfloat16*>(pool) + to * HD, pieces, x[i]);
             }
-            if (mine && kind[i] == 0) store_row(p.out[0] + t * p.out_stride[0] + head[i] * HD, pieces, x[i]);
-        } else if (there[i]) {
-            store_row(p.out[kind[i]] + t * p.out_stride[kind[i]] + head[i] * HD, pieces, x[i]);
+            if (mine && w.kind == 0) store_row(p.out[0] + t * p.out_stride[0] + w.head * HD, pieces, x[i]);
+        } else if (w.there) {
+            store_row(p.out[w.kind] + t * p.out_stride[w.kind] + w.head * HD, pieces, x[i]);
         }
     }
 }
 
 // Gradients through a norm.  A block has rows of q or of k alone, in chunks of a few tokens; its sums for the weight's gradient go to p.partial, in an order that the sizes
-// and the number of multiprocessors fix.  The next chunk's sines and cosines are made, and its first rows requested, before a chunk is worked on.
-constexpr int kBwdRowsOfLane = 4;  // of a chunk
+// and the number of multiprocessors fix.  The next chunk's sines and cosines are made before a chunk is worked on.  A lane's next rows are on their way to a place of its own
+// in shared memory: the sums, a row and its gradient take the registers (with one row ahead in them 106 us for 8192 tokens of 64 + 8 heads, so 93).
+constexpr int kBwdRowsOfLane = 4;  // of a chunk: in each of the four places one, so that three rows are on their way
+constexpr int kBwdBlocks = 2;      // of a multiprocessor
+constexpr int kAheadBytes = kBwdRowsOfLane * 4 * 16 * kRotateThreads;
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
 template <int HD>
-__global__ void __launch_bounds__(kRotateThreads) s2a_rotate_bwd_kernel(const __grid_constant__ RotateBwdParams p) {
+__global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_kernel(const __grid_constant__ RotateBwdParams p) {
     using L = RowLanes<HD>;
-    extern __shared__ __align__(16) float s_table[];  // [2][tokens of a chunk][kTable]
+    extern __shared__ __align__(16) uint4 s_rows[];  // [row ahead][two pieces of x, two of the gradient][threads], then the tables [2][tokens of a chunk][kTable]
+    float* s_table = reinterpret_cast<float*>(s_rows + kAheadBytes / 16);
     __shared__ __align__(16) float s_weights[HD];
     __shared__ float s_sum[kRotateThreads / 32][HD];
     release_successor();
@@ -274,49 +291,72 @@ __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_bwd_kernel(const __
     const Pieces pieces(part, p.rotation.r);
     const HeadRows in = p.in[kind], grad = p.grad[kind];
     const FastDiv by_heads = p.by_heads[kind];
-    const int tokens = p.tokens[kind], blocks = p.blocks[kind], chunks = (p.T + tokens - 1) / tokens, pairs = p.rotation.r / 2;
+    const int tokens = p.tokens[kind], blocks = p.blocks[kind], chunks = p.chunks[kind], pairs = p.rotation.r / 2;
+    constexpr int kRows = L::kGroups * kBwdRowsOfLane;  // of a chunk at most: some tokens', or a part of one's
     for (int i = threadIdx.x; i < HD; i += kRotateThreads) stage_weights<HD>(s_weights, p.rotation.weight[kind], p.rotation.weight_f32, p.rotation.r, i);
     auto angles = [&](int chunk, float* table) {
         for (int i = threadIdx.x; i < tokens * (HD / 2); i += kRotateThreads) {
-            const int at = i / (HD / 2), pair = i % (HD / 2), t = chunk * tokens + at;
+            const int at = i / (HD / 2), pair = i % (HD / 2), t = p.by_parts[kind](chunk) * tokens + at;
             if (pair < pairs && t < p.T) make_angle<HD>(table + at * L::kTable, p.rotation, pair, position_of(p.rotation, t), true);
         }
     };
     float sum[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-    uint4 next_x[2], next_g[2];
-    int next_token = 0, next_head = 0;
-    bool next_there = false;
-    // row i of this lane's of a chunk
-    auto load = [&](int chunk, int i) {
-        const int r = i * L::kGroups + group;
-        next_there = chunk < chunks && r < min(tokens, p.T - chunk * tokens) * in.heads;
-        next_x[0] = next_x[1] = next_g[0] = next_g[1] = make_uint4(0, 0, 0, 0);
-        if (next_there) {
-            next_token = by_heads(r, &next_head);
-            const long long t = chunk * tokens + next_token;
-            load_row(in.x + t * in.stride + next_head * HD, pieces, next_x);
-            load_row(grad.x + t * grad.stride + next_head * HD, pieces, next_g);
+    // this lane's rows of a chunk: token, and where they are from the chunk's first row on, in eights of values
+    int at[kBwdRowsOfLane], x_from[kBwdRowsOfLane], g_from[kBwdRowsOfLane];
+#pragma unroll
+    for (int i = 0; i < kBwdRowsOfLane; ++i) {
+        int head;
+        at[i] = by_heads(i * L::kGroups + group, &head);
+        if (tokens == 1) at[i] = 0, head = i * L::kGroups + group;  // (behind a part of its heads there are more)
+        if (at[i] >= tokens) at[i] = 0, head = 0;                   // (there is none)
+        x_from[i] = at[i] * static_cast<int>(in.stride / 8) + head * (HD / 8), g_from[i] = at[i] * static_cast<int>(grad.stride / 8) + head * (HD / 8);
+    }
+    // a chunk's rows, and the place of the first one: token, and head
+    auto rows_of = [&](int chunk, int* token, int* head) -> int {
+        if (chunk >= chunks) return 0;
+        int part_of;
+        *token = p.by_parts[kind](chunk, &part_of) * tokens, *head = part_of * kRows;
+        return min(kRows, min(tokens, p.T - *token) * in.heads - *head);
+    };
+    uint4* const mine = s_rows + threadIdx.x;
+    auto request = [&](int chunk, int i) {
+        int token = 0, head = 0;
+        const bool there = i * L::kGroups + group < rows_of(chunk, &token, &head);
+        const __nv_bfloat16* x = in.x + (there ? token * in.stride + (head * HD + 8ll * x_from[i]) : 0);
+        const __nv_bfloat16* g = grad.x + (there ? token * grad.stride + (head * HD + 8ll * g_from[i]) : 0);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            copy_async(mine + (4 * i + y) * kRotateThreads, x + pieces.at[y], there);
+            copy_async(mine + (4 * i + 2 + y) * kRotateThreads, g + pieces.at[y], there);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
     int chunk = static_cast<int>(blockIdx.x) - (kind ? p.blocks[0] : 0);
-    load(chunk, 0);
+#pragma unroll
+    for (int i = 0; i < kBwdRowsOfLane - 1; ++i) request(chunk, i);
     if (chunk < chunks) angles(chunk, s_table);
     for (int turn = 0; chunk < chunks; chunk += blocks, turn ^= 1) {
         __syncthreads();  // this chunk's table is there, and the other one is free
         if (chunk + blocks < chunks) angles(chunk + blocks, s_table + (turn ^ 1) * tokens * L::kTable);
         const float* table = s_table + turn * tokens * L::kTable;
-#pragma unroll 1
+        int token = 0, first_head = 0;
+        const int rows = rows_of(chunk, &token, &first_head);
+        __nv_bfloat16* const out = p.out[kind] + (static_cast<long long>(token) * in.heads + first_head + group) * HD;
+#pragma unroll
         for (int i = 0; i < kBwdRowsOfLane; ++i) {
-            const bool there = next_there;
-            const int at = next_token, head = next_head;
+            request(i == 0 ? chunk : chunk + blocks, (i + kBwdRowsOfLane - 1) % kBwdRowsOfLane);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kBwdRowsOfLane - 1) : "memory");
+            const bool there = i * L::kGroups + group < rows;
             float x[16], g[16];
-            unpack_row(next_x, x);
-            unpack_row(next_g, g);
-            if (i + 1 < kBwdRowsOfLane) load(chunk, i + 1);
-            else load(chunk + blocks, 0);
-            turn_row<HD>(g, table + at * L::kTable, pieces, part, p.rotation.interleaved);
+            {
+                const uint4* from = mine + 4 * i * kRotateThreads;
+                const uint4 now_x[2] = {from[0], from[kRotateThreads]}, now_g[2] = {from[2 * kRotateThreads], from[3 * kRotateThreads]};
+                unpack_row(now_x, x);
+                unpack_row(now_g, g);
+            }
+            turn_row<HD>(g, table + at[i] * L::kTable, pieces, part, p.rotation.interleaved);
             const float s = normalise_row<HD>(x, p.rotation.eps);
             if (there) {
 #pragma unroll
@@ -329,9 +369,9 @@ __global__ void __launch_bounds__(kRotateThreads) s2a_rotate_bwd_kernel(const __
             mean = sum_of_row<HD>(mean) * (1.f / HD);
 #pragma unroll
             for (int e = 0; e < 16; ++e) g[e] = s * (g[e] - x[e] * mean);
-            uint4 out[2];
-            pack_row(g, out);
-            if (there) store_row(p.out[kind] + ((static_cast<long long>(chunk) * tokens + at) * in.heads + head) * HD, pieces, out);
+            uint4 w[2];
+            pack_row(g, w);
+            if (there) store_row(out + i * L::kGroups * HD, pieces, w);
         }
     }
     // the block's sums: over the rows of a warp, then over the warps
@@ -372,7 +412,7 @@ __global__ void __launch_bounds__(kJoinThreads) s2a_rotate_join_kernel(const __g
 template <int HD, bool kNorm, RotateTo kTo>
 cudaError_t launch_one(const RotateParams& p, cudaStream_t stream) {
     const long long tiles = (p.T + p.blocks.tokens - 1) / p.blocks.tokens;
-    const int smem = std::min(p.blocks.tokens, p.blocks.rows) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
+    const int smem = std::min(p.blocks.tokens, (p.blocks.rows - 1) / p.blocks.all + 2) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
     return launch_kernel(s2a_rotate_kernel<HD, kNorm, kTo>, static_cast<unsigned>(tiles * p.blocks.count), kRotateThreads, smem, stream, p, true);
 }
 template <int HD, RotateTo kTo>
@@ -386,12 +426,18 @@ cudaError_t launch_to(const RotateParams& p, bool norm, int d, cudaStream_t stre
 
 template <int HD>
 cudaError_t launch_gradients(const RotateBwdParams& p, cudaStream_t stream) {
-    const int smem = 2 * std::max(p.tokens[0], p.tokens[1]) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
+    const int smem = kAheadBytes + 2 * std::max(p.tokens[0], p.tokens[1]) * RowLanes<HD>::kTable * static_cast<int>(sizeof(float));
     const cudaError_t e = launch_kernel(s2a_rotate_bwd_kernel<HD>, static_cast<unsigned>(p.blocks[0] + p.blocks[1]), kRotateThreads, smem, stream, p, true);
     return e != cudaSuccess ? e : launch_kernel(s2a_rotate_join_kernel<HD>, 2u, kJoinThreads, 0, stream, p, true);
 }
 
 }  // namespace
+
+cudaError_t configure_rotate() {
+    // (two chunks' tables are 32 KB at most)
+    const cudaError_t e = cudaFuncSetAttribute(s2a_rotate_bwd_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAheadBytes + 32768);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(s2a_rotate_bwd_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAheadBytes + 32768);
+}
 
 cudaError_t launch_rotate(const RotateParams& p, RotateTo to, bool norm, int d, cudaStream_t stream) {
     if (to == RotateTo::kTensors) return launch_to<RotateTo::kTensors>(p, norm, d, stream);
@@ -401,7 +447,7 @@ cudaError_t launch_rotate_bwd(const RotateBwdParams& p, int d, cudaStream_t stre
     return d == 64 ? launch_gradients<64>(p, stream) : launch_gradients<128>(p, stream);
 }
 int rotate_rows(int d) { return (d == 64 ? RowLanes<64>::kGroups : RowLanes<128>::kGroups) * kRowsOfLane; }
-int rotate_bwd_blocks(int n_sm) { return 4 * n_sm; }
+int rotate_bwd_blocks(int n_sm) { return kBwdBlocks * n_sm; }
 int rotate_bwd_rows(int d) { return (d == 64 ? RowLanes<64>::kGroups : RowLanes<128>::kGroups) * kBwdRowsOfLane; }
 
 }  // namespace s2a

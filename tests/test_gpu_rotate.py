@@ -96,7 +96,7 @@ class Job:
         return got
 
 
-SHAPES = [(1, 1, 1, 64), (1, 32, 8, 128), (2, 3, 5, 64), (33, 4, 2, 128), (129, 9, 1, 64), (701, 16, 4, 64), (1000, 40, 40, 128), (257, 64, 8, 128)]
+SHAPES = [(5, 300, 260, 64), (3, 129, 128, 128), (1, 1, 1, 64), (1, 32, 8, 128), (2, 3, 5, 64), (33, 4, 2, 128), (129, 9, 1, 64), (701, 16, 4, 64), (1000, 40, 40, 128), (257, 64, 8, 128)]
 
 
 @pytest.mark.parametrize("T,H,Hkv,d", SHAPES)

@@ -80,7 +80,7 @@ def test_the_library_refuses_without_a_device():
     assert call(rotation=dict(r=24)) == (unsupported,) * 3
     for change in (dict(q=None), dict(q=a + 8), dict(q_stride=252), dict(q_stride=248), dict(T=0), dict(H=0), dict(no_rotation=True)):
         assert call(**change) == (invalid,) * 3, change
-    for change in (dict(d=96, rotation=dict(r=0)), dict(T=1 << 28)):
+    for change in (dict(d=96, rotation=dict(r=0)), dict(T=1 << 28), dict(q_stride=(1 << 28) + 8)):
         assert call(**change) == (unsupported,) * 3, change
     assert call(q_out=a + 4)[::2] == (invalid,) * 2 and call(dq=None)[1] == invalid
     assert call(workspace=a + 16)[1] == invalid and call(workspace=None)[1] == invalid
