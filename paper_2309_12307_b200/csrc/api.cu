@@ -78,6 +78,8 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_rotate();
         if (e != cudaSuccess) return cuda_fail(e);
+        e = configure_evict();
+        if (e != cudaSuccess) return cuda_fail(e);
         ds.paged_error = configure_paged_split(ds.cluster_slots);
         if (ds.paged_error == cudaSuccess) ds.paged_error = configure_paged_fwd();
         if (ds.paged_error == cudaSuccess) ds.paged_error = configure_weights_tile();

@@ -156,7 +156,7 @@ int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, i
     const long long longest = static_cast<long long>(width) * cache->page_size, room = static_cast<long long>(to_width) * cache->page_size;
     if (longest > kIntMax / 2 || room > kIntMax / 2) return S2A_ERR_UNSUPPORTED;
     if (room < std::min<long long>(budget, longest)) return S2A_ERR_INVALID_ARG;
-    if (static_cast<long long>(B) * cache->Hkv > kIntMax / ((std::min<long long>(budget, longest) + 15) / 16)) return S2A_ERR_UNSUPPORTED;
+    if (static_cast<long long>(B) * cache->Hkv > kIntMax / 16 / ((std::min<long long>(budget, longest) + 15) / 16)) return S2A_ERR_UNSUPPORTED;
     DeviceState* ds = nullptr;
     if ((rc = prepare_device(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
     EvictParams p;
@@ -164,7 +164,7 @@ int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, i
     p.pool = pool_of(cache), p.received = received, p.table = table, p.lengths = lengths, p.to_table = to_table;
     p.width = width, p.to_width = to_width, p.B = B, p.budget = budget, p.sinks = sinks, p.recent = recent;
     p.new_lengths = new_lengths, p.kept = kept, p.status = ds->status_ptr, p.host_status = ds->host_word_dev;
-    const cudaError_t e = launch_evict(p, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_evict(p, ds->n_sm, cache->type == S2A_CACHE_E4M3, cache->d, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? S2A_OK : cuda_fail(e);
 }
 

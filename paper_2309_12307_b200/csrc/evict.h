@@ -81,7 +81,6 @@ __host__ __device__ inline bool weights_item(const WeightsTileParams& p, int id,
     return w->r0 < w->r1;
 }
 
-// Tokens of a sequence that are kept, by number or by the weight of the lightest one.
 struct EvictParams {
     PagedPool pool;
     float* received;
@@ -92,6 +91,7 @@ struct EvictParams {
     int budget, sinks, recent;
     int* new_lengths;     // [B]
     int* kept;            // [B, Hkv, budget]
+    int cluster, room;    // blocks of a head in the selecting kernel, weights that each keeps in shared memory
     FastDiv by_pieces;    // blocks of a head in the copying kernel
     int* status;
     int* host_status;
@@ -107,6 +107,7 @@ __host__ __device__ inline uint32_t weight_order(uint32_t bits) {
 cudaError_t launch_weights_stream(const WeightsStreamParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t launch_weights_tile(const WeightsTileParams& p, bool e4m3, int d, cudaStream_t stream);
 cudaError_t configure_weights_tile();
-cudaError_t launch_evict(const EvictParams& p, bool e4m3, int d, cudaStream_t stream);
+cudaError_t configure_evict();
+cudaError_t launch_evict(EvictParams p, int n_sm, bool e4m3, int d, cudaStream_t stream);
 
 }  // namespace s2a

@@ -261,6 +261,7 @@ def test_weights_that_are_equal_or_no_numbers(kind, budget):
 def test_long_sequences():
     evicted([100_003], 4097, 4, 1024, Hkv=1, d=64, page=128, dtype=E4M3)
     evicted([60_000, 58_000, 9, 20_000], 300, 0, 7, Hkv=2, d=64, page=16)
+    evicted([420_001], 1000, 4, 100, Hkv=1, d=64, page=256, dtype=E4M3)  # more than a cluster's shared memory holds
 
 
 def test_old_pages_may_be_shared():
