@@ -91,7 +91,7 @@ struct EvictParams {
     int budget, sinks, recent;
     int* new_lengths;     // [B]
     int* kept;            // [B, Hkv, budget]
-    int cluster, room;    // blocks of a head in the selecting kernel, weights that each keeps in shared memory
+    int cluster;          // blocks of a head in the selecting kernel
     FastDiv by_pieces;    // blocks of a head in the copying kernel
     int* status;
     int* host_status;

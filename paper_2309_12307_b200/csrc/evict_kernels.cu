@@ -4,8 +4,8 @@
 //
 // The selecting kernel finds the weight of the lightest token that stays digit by digit: 11, 11 and 10 bits of the weights as ordered whole numbers (the first digit has the exponent and two bits
 // more, over which weights spread; of 8 bits it would be the same for most of them, and its counter what all threads wait for).  A cluster of up to 8 blocks has a head: each
-// block has a part of its tokens, whose weights it reads once and keeps in shared memory, counts their digits there, and adds up the counts of all blocks.  Then each thread counts, of the
-// neighbouring tokens that are its own, those above the border and those on it; one scan over the threads, and the other blocks' totals, say where each thread's tokens go in the list
+// block has a part of its tokens, whose weights it reads once and keeps in shared memory, counts their digits there, and adds up the counts of all blocks.  Then each warp counts, of the
+// neighbouring tokens that are its own, those above the border and those on it; one scan over the warps, and the other blocks' totals, say where each warp's tokens go in the list
 // of those that stay.  What bounds it is latency: three rounds of counting, a barrier and a scan each.  (One block a head that read the weights anew for each of four 8-bit digits, 100,000
 // tokens of 8 heads: both kernels and reading back 470 us.)
 //
@@ -21,7 +21,7 @@ namespace {
 constexpr int kSelectThreads = 512;
 constexpr int kDigits = 2048;              // values of a digit
 constexpr int kMostBlocks = 8;             // of a cluster
-constexpr int kMostKept = 48 * 1024;       // weights that a block keeps in shared memory
+constexpr int kMostKept = 46 * 1024;       // weights that a block keeps in shared memory
 
 // The length of sequence b; -1: out of range.
 __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
@@ -34,6 +34,21 @@ __device__ __forceinline__ long long place_row(const PagedPool& pool, const int*
     const int page = S2A_LOAD(table + static_cast<long long>(b) * width + (j >> pool.page_log2));
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(pool.pages)) return -1;
     return ((static_cast<long long>(page) * pool.Hkv + hk) << pool.page_log2) + (j & ((1 << pool.page_log2) - 1));
+}
+
+// Four numbers of another block of the cluster, at this block's address `saddr`.
+__device__ __forceinline__ int4 load_remote_four(uint32_t saddr, uint32_t rank) {
+    int4 x;
+    asm volatile(
+        "{\n"
+        ".reg .u32 a;\n"
+        "mapa.shared::cluster.u32 a, %4, %5;\n"
+        "ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [a];\n"
+        "}\n"
+        : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+        : "r"(saddr), "r"(rank)
+        : "memory");
+    return x;
 }
 
 // By a whole block: the sums of x over the threads before this one (*before), and over all.  Two counts at a time.
@@ -59,9 +74,12 @@ __device__ __forceinline__ int2 scan_block(int2 x, int2 (&s_warp)[kSelectThreads
     return all;
 }
 
+// kKept: whether a block's weights fit its shared memory.
+template <bool kKept>
 __global__ void __launch_bounds__(kSelectThreads) s2a_evict_select_kernel(const __grid_constant__ EvictParams p) {
-    extern __shared__ __align__(16) uint32_t s_keys[];  // this block's weights, as ordered whole numbers, if there is room
-    __shared__ int s_count[3][kDigits];
+    extern __shared__ __align__(16) uint4 s_keys[];  // this block's weights, as ordered whole numbers
+    __shared__ __align__(16) int s_count[3][kDigits];
+    __shared__ __align__(16) int s_sum[3][kDigits / 2];  // of this block's part of the digits, of all blocks
     __shared__ int2 s_warp[kSelectThreads / 32];
     __shared__ int s_digit, s_left;
     __shared__ int s_totals[2];
@@ -84,104 +102,145 @@ __global__ void __launch_bounds__(kSelectThreads) s2a_evict_select_kernel(const 
         for (int i = thread; n == m && i < m; i += all_threads) kept[i] = i;
     }
     if (n == m) return;
-    // n > budget >= sinks + recent: of the tokens from .. to - 1 `left` stay.  This block has those from low to high - 1 of all.
+    // n > budget.  Tokens that stay in any case weigh more than all numbers, and places behind the last token less.
     const int from = p.sinks, to = n - p.recent;
-    int left = p.budget - p.sinks - p.recent;
-    const int part = ((n + p.cluster - 1) / p.cluster + 3) & ~3, low = min(rank * part, n), high = min(low + part, n);
-    const bool keep = part <= p.room;
-    // the weights of tokens j .. j + 3 (j a multiple of four, so they are neighbours in a page)
-    auto four = [&](int j, uint32_t (&x)[4]) {
+    int left = m;  // of those that have the digits of the border so far, how many stay
+    const int part = ((n + p.cluster - 1) / p.cluster + 3) & ~3, low = min(rank * part, n), fours = (min(low + part, n) - low + 3) / 4;
+    // the weights of four tokens of this block, neighbours in a page
+    auto read_four = [&](int i) -> uint4 {
+        const int j = low + 4 * i;
         const long long row = place_row(p.pool, p.table, p.width, b, hk, j);
         if (row < 0) report_bad_index(p.status, p.host_status, kBadPage);
         const float4 w = row < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(reinterpret_cast<const float4*>(p.received + row));
-        x[0] = weight_order(__float_as_uint(w.x)), x[1] = weight_order(__float_as_uint(w.y));
-        x[2] = weight_order(__float_as_uint(w.z)), x[3] = weight_order(__float_as_uint(w.w));
+        auto order = [&](float x, int j) -> uint32_t {
+            return j >= n ? 0u : j < from || j >= to ? 0xffffffffu : min(weight_order(__float_as_uint(x)), 0xfffffffeu);
+        };
+        return make_uint4(order(w.x, j), order(w.y, j + 1), order(w.z, j + 2), order(w.w, j + 3));
     };
-    auto key_of = [&](int j) -> uint32_t {
-        if (keep) return s_keys[j - low];
-        uint32_t x[4];
-        four(j & ~3, x);
-        return j & 2 ? (j & 1 ? x[3] : x[2]) : (j & 1 ? x[1] : x[0]);
+    auto four = [&](int i) -> uint4 {
+        if constexpr (kKept) return s_keys[i];
+        else return read_four(i);
     };
     for (int i = threadIdx.x; i < 3 * kDigits; i += kSelectThreads) s_count[0][i] = 0;
+    for (int i = threadIdx.x; i < 3 * kDigits / 2; i += kSelectThreads) s_sum[0][i] = 0;
     __syncthreads();
     // the digits: bits 21 .. 31, 10 .. 20, 0 .. 9
-    for (int j = low + 4 * static_cast<int>(threadIdx.x); j < high; j += 4 * kSelectThreads) {
-        uint32_t x[4];
-        four(j, x);
-        if (keep) *reinterpret_cast<uint4*>(s_keys + j - low) = make_uint4(x[0], x[1], x[2], x[3]);
+    constexpr int kAtOnce = 8;  // loads of a thread in flight
+    for (int base = threadIdx.x; base < fours; base += kSelectThreads * kAtOnce) {
+        uint4 x[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (j + i >= from && j + i < min(to, high)) atomicAdd(&s_count[0][x[i] >> 21], 1);
+        for (int y = 0; y < kAtOnce; ++y)
+            if (base + y * kSelectThreads < fours) x[y] = read_four(base + y * kSelectThreads);
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            if (base + y * kSelectThreads >= fours) break;
+            if constexpr (kKept) s_keys[base + y * kSelectThreads] = x[y];
+            atomicAdd(&s_count[0][x[y].x >> 21], 1);
+            atomicAdd(&s_count[0][x[y].y >> 21], 1);
+            atomicAdd(&s_count[0][x[y].z >> 21], 1);
+            atomicAdd(&s_count[0][x[y].w >> 21], 1);
+        }
     }
     uint32_t border = 0, known = 0;  // the lightest's digits so far
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
         if (round > 0) {
             const uint32_t mask = round == 1 ? 0x7ffu : 0x3ffu;
-            for (int j = low + static_cast<int>(threadIdx.x); j < high; j += kSelectThreads) {
-                if (j < from || j >= to) continue;
-                const uint32_t x = key_of(j);
-                if ((x & known) == border) atomicAdd(&s_count[round][x >> shift & mask], 1);
+#pragma unroll 4
+            for (int i = threadIdx.x; i < fours; i += kSelectThreads) {
+                const uint4 x = four(i);
+                if ((x.x & known) == border) atomicAdd(&s_count[round][x.x >> shift & mask], 1);
+                if ((x.y & known) == border) atomicAdd(&s_count[round][x.y >> shift & mask], 1);
+                if ((x.z & known) == border) atomicAdd(&s_count[round][x.z >> shift & mask], 1);
+                if ((x.w & known) == border) atomicAdd(&s_count[round][x.w >> shift & mask], 1);
             }
         }
-        cluster_sync();
-        // of all blocks: thread i has the digits kDigits - 1 - 4 i on downwards, the larger ones first
+        // the counts of all blocks: each block adds up a part of the digits, and reads the others' sums.  (Of the whole cluster's counts a block reads twice its own that way, not eight times.)
+        int4 count;  // thread i has the digits from 4 i on
         static_assert(kDigits == 4 * kSelectThreads, "a thread has four digits");
-        const int top = kDigits - 1 - 4 * static_cast<int>(threadIdx.x);
-        int count[4] = {0, 0, 0, 0};
-        for (int r = 0; r < p.cluster; ++r) {
+        if (p.cluster == 1) {
+            __syncthreads();
+            count = *reinterpret_cast<const int4*>(&s_count[round][4 * threadIdx.x]);
+        } else {
+            const int own = kDigits / p.cluster;
+            cluster_sync();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) count[i] += __float_as_int(load_remote(smem_u32(&s_count[round][top - i]), r));
+            for (int i = 0; i < 4; ++i) {
+                const int x = i * kSelectThreads + static_cast<int>(threadIdx.x), digit = x % own;
+                atomicAdd(&s_sum[round][digit], __float_as_int(load_remote(smem_u32(&s_count[round][rank * own + digit]), x / own)));
+            }
+            cluster_sync();
+            count = load_remote_four(smem_u32(&s_sum[round][4 * threadIdx.x % own]), 4 * threadIdx.x / own);
         }
-        int2 above;
-        scan_block(make_int2(count[0] + count[1] + count[2] + count[3], 0), s_warp, &above);
-        if (threadIdx.x == 0 && left == 0) s_digit = kDigits - 1, s_left = 0;
-        if (above.x < left && above.x + count[0] + count[1] + count[2] + count[3] >= left) {
-            int x = above.x, i = 0;
+        int2 before;
+        const int mine = count.x + count.y + count.z + count.w, all = scan_block(make_int2(mine, 0), s_warp, &before).x, above = all - before.x - mine;
+        if (above < left && above + mine >= left) {
+            int x = above, i = 3;
+            const int of[4] = {count.x, count.y, count.z, count.w};
 #pragma unroll
-            for (int y = 0; y < 3; ++y)
-                if (i == y && x + count[y] < left) x += count[y], ++i;
-            s_digit = top - i, s_left = left - x;
+            for (int y = 3; y > 0; --y)
+                if (i == y && x + of[y] < left) x += of[y], --i;
+            s_digit = 4 * static_cast<int>(threadIdx.x) + i, s_left = left - x;
         }
         __syncthreads();
-        // (with nothing left to find, above all numbers)
         border |= static_cast<uint32_t>(s_digit) << shift, known |= (round == 2 ? 0x3ffu : 0x7ffu) << shift;
         left = s_left;
     }
-    // Those above the border stay, and `left` of those on it, the first ones.  A thread has neighbouring tokens, an odd number of them, so that threads meet in no bank.
-    const int each = ((high - low + kSelectThreads - 1) / kSelectThreads) | 1;
-    const int first = min(low + each * static_cast<int>(threadIdx.x), high), end = min(first + each, high);
-    auto stays = [&](int j, bool* same) -> bool {
-        *same = false;
-        if (j < from || j >= to) return true;
-        const uint32_t x = key_of(j);
-        *same = x == border;
-        return x > border;
-    };
+    // Those above the border stay, and `left` of those on it, the first ones.  A warp has neighbouring tokens, four of a lane at a time: it counts them, and when it is known what is in
+    // front of them, goes through them again and writes.
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int each = (fours + kSelectThreads / 32 - 1) / (kSelectThreads / 32), first = min(each * warp, fours), end = min(first + each, fours);
+    const uint32_t in_front = (1u << lane) - 1;
+    auto lane_four = [&](int i) -> uint4 { return i + lane < end ? four(i + lane) : make_uint4(0, 0, 0, 0); };
     int2 mine = make_int2(0, 0), before;
-    for (int j = first; j < end; ++j) {
-        bool same;
-        mine.x += stays(j, &same);
-        mine.y += same;
+#pragma unroll 4
+    for (int i = first; i < end; i += 32) {
+        const uint4 x = lane_four(i);
+        mine.x += (x.x > border) + (x.y > border) + (x.z > border) + (x.w > border);
+        mine.y += (x.x == border) + (x.y == border) + (x.z == border) + (x.w == border);
     }
     const int2 all = scan_block(mine, s_warp, &before);
-    if (threadIdx.x == 0) s_totals[0] = all.x, s_totals[1] = all.y;
-    cluster_sync();
-    for (int r = 0; r < rank; ++r) {
-        before.x += __float_as_int(load_remote(smem_u32(&s_totals[0]), r));
-        before.y += __float_as_int(load_remote(smem_u32(&s_totals[1]), r));
-    }
-    cluster_sync();  // (no block is gone before the others have read its totals)
-    int at = before.x + min(before.y, left), equal = before.y;
-    for (int j = first; j < end; ++j) {
-        bool same;
-        bool stay = stays(j, &same);
-        if (same) stay = equal++ < left;
-        if (stay && at < m) {
-            if (!quiet) kept[at] = j;
-            ++at;
+    before.x = __shfl_sync(0xffffffffu, before.x, 0), before.y = __shfl_sync(0xffffffffu, before.y, 0);
+    if (p.cluster > 1) {
+        if (threadIdx.x == 0) s_totals[0] = all.x, s_totals[1] = all.y;
+        cluster_sync();
+#pragma unroll 4
+        for (int r = 0; r < rank; ++r) {
+            before.x += __float_as_int(load_remote(smem_u32(&s_totals[0]), r));
+            before.y += __float_as_int(load_remote(smem_u32(&s_totals[1]), r));
         }
+        cluster_sync();  // (no block is gone before the others have read its totals)
+    }
+    if (quiet) return;
+    int at = before.x + min(before.y, left), room = max(left - before.y, 0);  // where the next one goes, and how many on the border still stay
+    for (int i = first; i < end; i += 32) {
+        const uint4 four_of = lane_four(i);
+        const uint32_t x[4] = {four_of.x, four_of.y, four_of.z, four_of.w};
+        // on the border: in front of this lane's, and of all lanes
+        int same = 0, all_same = 0;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const uint32_t found = __ballot_sync(0xffffffffu, x[y] == border);
+            same += __popc(found & in_front), all_same += __popc(found);
+        }
+        bool stays[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            stays[y] = x[y] > border || (x[y] == border && same < room);
+            same += x[y] == border;
+        }
+        int to_place = at;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const uint32_t found = __ballot_sync(0xffffffffu, stays[y]);
+            to_place += __popc(found & in_front), at += __popc(found);
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if (stays[y] && to_place < m) kept[to_place] = low + 4 * (i + lane) + y;
+            to_place += stays[y];
+        }
+        room = max(room - all_same, 0);
     }
 }
 
@@ -237,7 +296,7 @@ cudaError_t launch_copy(EvictParams p, int most, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t configure_evict() { return cudaFuncSetAttribute(s2a_evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKept * 4); }
+cudaError_t configure_evict() { return cudaFuncSetAttribute(s2a_evict_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKept * 4); }
 
 cudaError_t launch_evict(EvictParams p, int n_sm, bool e4m3, int d, cudaStream_t stream) {
     const long long longest = static_cast<long long>(p.width) << p.pool.page_log2, units = static_cast<long long>(p.B) * p.pool.Hkv;
@@ -245,11 +304,11 @@ cudaError_t launch_evict(EvictParams p, int n_sm, bool e4m3, int d, cudaStream_t
     p.cluster = 1;
     while (p.cluster < kMostBlocks && ((units * p.cluster * 2 <= n_sm && longest > 2048ll * p.cluster) || longest > static_cast<long long>(kMostKept) * p.cluster)) p.cluster *= 2;
     const long long part = ((longest + p.cluster - 1) / p.cluster + 3) & ~3ll;
-    p.room = part <= kMostKept ? static_cast<int>(part) : 0;
+    const bool kept = part <= kMostKept;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(static_cast<unsigned>(units * p.cluster));
     config.blockDim = dim3(kSelectThreads);
-    config.dynamicSmemBytes = static_cast<size_t>(p.room) * 4;
+    config.dynamicSmemBytes = kept ? static_cast<size_t>(part) * 4 : 0;
     config.stream = stream;
     cudaLaunchAttribute attributes[2] = {};
     attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -257,7 +316,7 @@ cudaError_t launch_evict(EvictParams p, int n_sm, bool e4m3, int d, cudaStream_t
     attributes[1].id = cudaLaunchAttributeClusterDimension;
     attributes[1].val.clusterDim.x = static_cast<unsigned>(p.cluster), attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
     config.attrs = attributes, config.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&config, s2a_evict_select_kernel, p);
+    const cudaError_t e = cudaLaunchKernelEx(&config, kept ? s2a_evict_select_kernel<true> : s2a_evict_select_kernel<false>, p);
     if (e != cudaSuccess) return e;
     const int most = static_cast<int>(p.budget < longest ? p.budget : longest);  // tokens that a head keeps
     if (e4m3) return d == 64 ? launch_copy<64, true>(p, most, stream) : launch_copy<128, true>(p, most, stream);
