@@ -58,6 +58,16 @@ __device__ __forceinline__ int row_to_e4m3(const uint32_t (&w)[8], uint32_t (&co
     return exp;
 }
 
+// Copies of 16 bytes from global to shared memory, in groups; a thread waits for its own (all but the last kLeft groups).
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");  // (zeros where it is not there)
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
 constexpr float kLeast = -3.0e38f;  // a running maximum before the first key: finite, so that differences are numbers
 
 }  // namespace s2a

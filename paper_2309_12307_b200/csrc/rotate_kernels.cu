@@ -273,9 +273,6 @@ __global__ void __launch_bounds__(kRotateThreads, 4) s2a_rotate_kernel(const __g
 constexpr int kBwdRowsOfLane = 4;  // of a chunk: in each of the four places one, so that three rows are on their way
 constexpr int kBwdBlocks = 2;      // of a multiprocessor
 constexpr int kAheadBytes = kBwdRowsOfLane * 4 * 16 * kRotateThreads;
-__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
 template <int HD>
 __global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_kernel(const __grid_constant__ RotateBwdParams p) {
     using L = RowLanes<HD>;
@@ -331,7 +328,7 @@ __global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_ker
             copy_async(mine + (4 * i + y) * kRotateThreads, x + pieces.at[y], there);
             copy_async(mine + (4 * i + 2 + y) * kRotateThreads, g + pieces.at[y], there);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        copy_async_commit();
     };
     int chunk = static_cast<int>(blockIdx.x) - (kind ? p.blocks[0] : 0);
 #pragma unroll
@@ -347,7 +344,7 @@ __global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_ker
 #pragma unroll
         for (int i = 0; i < kBwdRowsOfLane; ++i) {
             request(i == 0 ? chunk : chunk + blocks, (i + kBwdRowsOfLane - 1) % kBwdRowsOfLane);
-            asm volatile("cp.async.wait_group %0;" ::"n"(kBwdRowsOfLane - 1) : "memory");
+            copy_async_wait<kBwdRowsOfLane - 1>();
             const bool there = i * L::kGroups + group < rows;
             float x[16], g[16];
             {

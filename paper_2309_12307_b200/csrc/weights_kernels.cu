@@ -8,7 +8,10 @@
 // Few rows (new tokens x query heads of a KV head): the streaming kernel.  A warp takes 16 keys at a time as the rows of S^T = K Q^T on mma.sync, eight
 // rows of q as its columns.  An instruction's 16 values of the contraction may be any, as long as K and Q agree, so a lane takes 16 bytes
 // of a key at a time (half of two instructions' worth, of 8-bit codes of four) straight from global memory to registers, the next 16
-// keys' on their way; q lies in shared memory in the order in which lanes need it.  Bound by HBM: each key is read once.
+// keys' on their way; q lies in shared memory in the order in which lanes need it.  Each key is read once; what bounds the kernel is a block's start (addresses, pages and q one after the other,
+// 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16 x up to 8192 tokens of 32 heads 116 us (5.2 TB/s) in pieces of 1024 keys,
+// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 63 us with six blocks on a multiprocessor, 71 with four.  Keys through a ring in shared memory, two or three turns
+// ahead, left room for fewer blocks: 145 and 81 us.
 //
 // 8-bit caches are multiplied in fp16, which has their codes exactly.  Each row of q goes with a power of two that brings its largest value to
 // [2^14, 2^15); that, and the key's power, multiply the score in fp32.
@@ -94,7 +97,7 @@ __device__ __forceinline__ void load_keys(const WeightsParams& a, long long row,
 }
 
 template <int HD, bool kE4M3>
-__global__ void __launch_bounds__(kStreamThreads) s2a_weights_stream_kernel(const __grid_constant__ WeightsStreamParams p) {
+__global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_stream_kernel(const __grid_constant__ WeightsStreamParams p) {
     using C = StreamCfg<HD, kE4M3>;
     const WeightsParams& a = p.a;
     __shared__ uint2 s_q[kStreamRows / 8 * C::kSteps * 32];
