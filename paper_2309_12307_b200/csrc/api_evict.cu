@@ -33,12 +33,15 @@ bool plan_stream(WeightsStreamParams* p, int n_sm, long long longest) {
     return true;
 }
 
-// Rows (new tokens times query heads of a KV head) of a sequence up to which it is the streaming kernel's.
-constexpr int kStreamedRows = 64;
+// Up to kStreamedRows rows a sequence is the streaming kernel's.  Both measured (us, streaming and tiling kernel, heads of 128 in bf16 and in 8 bits):
+//   - one sequence, 8 KV heads: 1000 keys, 16 rows 8 and 12, 64 rows 10 and 12 (8 bits 12 and 12), 128 rows 14 and 12; 8192 keys, 16 rows 14 and 16, 32 rows 16 and 16, 64 rows 21 and 16 (23 and 16);
+//     32k keys, 16 rows 31 and 33 (27 and 35), 32 rows 33 and 33 (31 and 35), 64 rows 43 and 33 (45 and 35), 256 rows 133 and 35
+//   - 8 x 4096, 8 KV heads: 16 rows 31 and 33 (25 and 35), 32 rows 33 and 33 (29 and 35), 64 rows 45 and 33 (43 and 35); heads of 64, 4 x 4096, 32 rows 23 and 21, 64 rows 29 and 21.
 
 // The items of the tiling kernel and the pieces their rows come in.  Without a window the first key blocks have all rows and the last ones few, and the
 // longest item must not be longer than the others together: a piece has about a quarter of a multiprocessor's share of all row tiles, eight at least (an item's
-// start and the second launch cost about as much as three).
+// start and the second launch cost about as much as three).  Measured, whole and in pieces, us, one prompt at once on 32 heads over 8 of 128: 512 tokens 31 and 23, 1024 51 and 25,
+// 2048 92 and 41, 4096 176 and 98; 512 new of 16,384 96 and 94.
 bool plan_tile(WeightsTileParams* p, int n_sm, long long longest) {
     const WeightsParams& a = p->a;
     p->pack_log2 = 0;
@@ -112,7 +115,7 @@ int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, c
     a.q = static_cast<const __nv_bfloat16*>(q), a.lse = lse, a.before = before, a.received = received;
     a.status = ds->status_ptr, a.host_status = ds->host_word_dev;
     a.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);
-    const bool e4m3 = cache->type == S2A_CACHE_E4M3, few = a.few_rows > 0, many = static_cast<long long>(max_new) * a.rep > a.few_rows;
+    const bool e4m3 = cache->type == S2A_CACHE_E4M3, few = a.rep <= a.few_rows, many = static_cast<long long>(max_new) * a.rep > a.few_rows;
     const long long longest = static_cast<long long>(batch->width) * cache->page_size;
     // everything that can be refused comes before the first launch
     WeightsStreamParams ps;

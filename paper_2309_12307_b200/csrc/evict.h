@@ -27,6 +27,8 @@ struct WeightsParams {
     float scale_log2;        // scale / ln 2
 };
 
+// Rows (new tokens times query heads of a KV head) of a sequence up to which it may be the streaming kernel's.
+constexpr int kStreamedRows = 32;
 struct WeightsStreamParams {
     WeightsParams a;
     int chunk_log2;          // keys of a block

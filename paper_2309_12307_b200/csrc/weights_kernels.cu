@@ -9,8 +9,8 @@
 // rows of q as its columns.  An instruction's 16 values of the contraction may be any, as long as K and Q agree, so a lane takes 16 bytes
 // of a key at a time (half of two instructions' worth, of 8-bit codes of four) straight from global memory to registers, the next 16
 // keys' on their way; q lies in shared memory in the order in which lanes need it.  Each key is read once; what bounds the kernel is a block's start (addresses, pages and q one after the other,
-// 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16 x up to 8192 tokens of 32 heads 116 us (5.2 TB/s) in pieces of 1024 keys,
-// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 63 us with six blocks on a multiprocessor, 71 with four.  Keys through a ring in shared memory, two or three turns
+// 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16 x up to 8192 tokens of 32 heads 113 us (5.4 TB/s) in pieces of 1024 keys,
+// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 61 us with six blocks on a multiprocessor, 71 with four.  Keys through a ring in shared memory, two or three turns
 // ahead, left room for fewer blocks: 145 and 81 us.
 //
 // 8-bit caches are multiplied in fp16, which has their codes exactly.  Each row of q goes with a power of two that brings its largest value to
@@ -26,7 +26,6 @@ namespace s2a {
 namespace {
 
 constexpr int kStreamThreads = 128;
-constexpr int kStreamRows = 64;       // of q in shared memory at a time
 constexpr int kMostChunkPages = 64;   // of a block's keys: 1024 keys in pages of 16
 
 template <int HD, bool kE4M3>
@@ -40,7 +39,7 @@ struct StreamCfg {
 
 // Rows of q of a sequence and KV head: row r is token r / rep, head r % rep of the KV head's.
 template <int HD, bool kE4M3>
-__device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequence& s, int hk, int row0, int rows, uint2* s_q, float* s_lse, float* s_scale, int* s_pos) {
+__device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequence& s, int hk, int rows, uint2* s_q, float* s_lse, float* s_scale, int* s_pos) {
     using C = StreamCfg<HD, kE4M3>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int padded = (rows + 7) & ~7;
@@ -48,7 +47,7 @@ __device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequenc
     for (int base = warp * 8; base < padded; base += kStreamThreads / 32 * 8) {
         const int r = base + lane / 4, t = lane % 4;
         const bool there = r < rows;
-        const int token = (row0 + (there ? r : 0)) / a.rep, head = hk * a.rep + (row0 + (there ? r : 0)) % a.rep;
+        const int token = (there ? r : 0) / a.rep, head = hk * a.rep + (there ? r : 0) % a.rep;
         const __nv_bfloat16* q = a.q + (static_cast<long long>(s.row0 + token) * a.H + head) * HD;
         uint2 w[C::kSteps];
 #pragma unroll
@@ -100,9 +99,9 @@ template <int HD, bool kE4M3>
 __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_stream_kernel(const __grid_constant__ WeightsStreamParams p) {
     using C = StreamCfg<HD, kE4M3>;
     const WeightsParams& a = p.a;
-    __shared__ uint2 s_q[kStreamRows / 8 * C::kSteps * 32];
-    __shared__ float s_lse[kStreamRows], s_scale[kStreamRows];
-    __shared__ int s_pos[kStreamRows];
+    __shared__ uint2 s_q[kStreamedRows / 8 * C::kSteps * 32];
+    __shared__ float s_lse[kStreamedRows], s_scale[kStreamedRows];
+    __shared__ int s_pos[kStreamedRows];
     __shared__ int s_page[kMostChunkPages];
     release_successor();
     wait_for_predecessor();
@@ -136,77 +135,68 @@ __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_str
         if (page < 0) return -1;
         return ((static_cast<long long>(page) * a.pool.Hkv + hk) << a.pool.page_log2) + ((key0 + at) & (page_keys - 1));
     };
-    const int all_rows = s.n * a.rep;
-    for (int row0 = 0; row0 < all_rows; row0 += kStreamRows) {
-        const int rows = min(kStreamRows, all_rows - row0);
-        if (row0 > 0) __syncthreads();
-        stage_rows<HD, kE4M3>(a, s, hk, row0, rows, s_q, s_lse, s_scale, s_pos);
-        __syncthreads();
-        const int groups = (rows + 7) / 8;
-        const int first_here = first + row0 / a.rep, last_here = first + (row0 + rows - 1) / a.rep;
-        uint4 next[2][C::kPieces];
-        int next_e[2] = {0, 0};
-        long long next_row = row_of(warp);
+    stage_rows<HD, kE4M3>(a, s, hk, s.n * a.rep, s_q, s_lse, s_scale, s_pos);
+    __syncthreads();
+    const int groups = (s.n * a.rep + 7) / 8;
+    uint4 next[2][C::kPieces];
+    int next_e[2] = {0, 0};
+    long long next_row = row_of(warp);
+    if (next_row >= 0) load_keys<HD, kE4M3>(a, next_row, next, next_e);
+    for (int i = warp; 16 * i < keys; i += kStreamThreads / 32) {
+        const long long row = next_row;
+        uint4 now[2][C::kPieces];
+        float power[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int x = 0; x < C::kPieces; ++x) now[y][x] = next[y][x];
+            power[y] = next_e[y] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(next_e[y]);
+        }
+        next_row = row_of(i + kStreamThreads / 32);
         if (next_row >= 0) load_keys<HD, kE4M3>(a, next_row, next, next_e);
-        for (int i = warp; 16 * i < keys; i += kStreamThreads / 32) {
-            const long long row = next_row;
-            uint4 now[2][C::kPieces];
-            float power[2];
+        if (row < 0) continue;
+        const int j = key0 + 16 * i + lane / 4;  // this lane's keys are j and j + 8
+        const bool whole = all_attend(first, last, key0 + 16 * i, 16, a.window, a.sinks);
+        float sum[2] = {0.f, 0.f};
+        for (int group = 0; group < groups; ++group) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                for (int x = 0; x < C::kPieces; ++x) now[y][x] = next[y][x];
-                power[y] = next_e[y] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(next_e[y]);
-            }
-            next_row = row_of(i + kStreamThreads / 32);
-            if (next_row >= 0) load_keys<HD, kE4M3>(a, next_row, next, next_e);
-            if (row < 0) continue;
-            const int j = key0 + 16 * i + lane / 4;  // this lane's keys are j and j + 8
-            const bool whole = all_attend(first_here, last_here, key0 + 16 * i, 16, a.window, a.sinks);
-            float sum[2] = {0.f, 0.f};
-            for (int group = 0; group < groups; ++group) {
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int x = 0; x < C::kSteps; ++x) {
-                    const uint2 q = s_q[(group * C::kSteps + x) * 32 + lane];
-                    const uint4 &k0 = now[0][x / C::kStepsOfPiece], &k1 = now[1][x / C::kStepsOfPiece];
-                    const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
-                    const int at = x % C::kStepsOfPiece;
-                    if constexpr (kE4M3) {
-                        uint32_t l0, h0, l1, h1;
-                        e4m3_to_f16(w0[at], l0, h0);
-                        e4m3_to_f16(w1[at], l1, h1);
-                        mma_16x8x16<true>(c, l0, l1, h0, h1, q.x, q.y);
-                    } else {
-                        mma_16x8x16<false>(c, w0[2 * at], w1[2 * at], w0[2 * at + 1], w1[2 * at + 1], q.x, q.y);
-                    }
-                }
-                const int r = 8 * group + 2 * t;
-                const float2 lse = *reinterpret_cast<const float2*>(s_lse + r), scale = *reinterpret_cast<const float2*>(s_scale + r);
-                const int2 pos = *reinterpret_cast<const int2*>(s_pos + r);
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const float s0 = kE4M3 ? c[2 * y] * power[y] : c[2 * y], s1 = kE4M3 ? c[2 * y + 1] * power[y] : c[2 * y + 1];
-                    float w0 = fast_exp2(fmaf(s0, scale.x, -lse.x)), w1 = fast_exp2(fmaf(s1, scale.y, -lse.y));
-                    if (!whole) {
-                        if (!attends(pos.x, j + 8 * y, a.window, a.sinks)) w0 = 0.f;
-                        if (!attends(pos.y, j + 8 * y, a.window, a.sinks)) w1 = 0.f;
-                    }
-                    sum[y] += w0 + w1;
+            for (int x = 0; x < C::kSteps; ++x) {
+                const uint2 q = s_q[(group * C::kSteps + x) * 32 + lane];
+                const uint4 &k0 = now[0][x / C::kStepsOfPiece], &k1 = now[1][x / C::kStepsOfPiece];
+                const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+                const int at = x % C::kStepsOfPiece;
+                if constexpr (kE4M3) {
+                    uint32_t l0, h0, l1, h1;
+                    e4m3_to_f16(w0[at], l0, h0);
+                    e4m3_to_f16(w1[at], l1, h1);
+                    mma_16x8x16<true>(c, l0, l1, h0, h1, q.x, q.y);
+                } else {
+                    mma_16x8x16<false>(c, w0[2 * at], w1[2 * at], w0[2 * at + 1], w1[2 * at + 1], q.x, q.y);
                 }
             }
+            const int r = 8 * group + 2 * t;
+            const float2 lse = *reinterpret_cast<const float2*>(s_lse + r), scale = *reinterpret_cast<const float2*>(s_scale + r);
+            const int2 pos = *reinterpret_cast<const int2*>(s_pos + r);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
-                sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
+                const float s0 = kE4M3 ? c[2 * y] * power[y] : c[2 * y], s1 = kE4M3 ? c[2 * y + 1] * power[y] : c[2 * y + 1];
+                float w0 = fast_exp2(fmaf(s0, scale.x, -lse.x)), w1 = fast_exp2(fmaf(s1, scale.y, -lse.y));
+                if (whole ? pos.x < 0 : !attends(pos.x, j + 8 * y, a.window, a.sinks)) w0 = 0.f;  // (below zero: no such row)
+                if (whole ? pos.y < 0 : !attends(pos.y, j + 8 * y, a.window, a.sinks)) w1 = 0.f;
+                sum[y] += w0 + w1;
             }
-            // lanes 0 and 1 of a key's four write keys j and j + 8
-            const int mine = j + 8 * t;
-            if (t < 2 && any_attends(first, last, mine, a.window, a.sinks)) {
-                const long long at = row + mine - (key0 + 16 * i);
-                const float old = row0 > 0 ? a.received[at] : a.before && mine < first ? __ldcg(a.before + at) : 0.f;
-                a.received[at] = old + (t == 0 ? sum[0] : sum[1]);
-            }
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
+            sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
+        }
+        // lanes 0 and 1 of a key's four write keys j and j + 8
+        const int mine = j + 8 * t;
+        if (t < 2 && any_attends(first, last, mine, a.window, a.sinks)) {
+            const long long at = row + mine - (key0 + 16 * i);
+            a.received[at] = (a.before && mine < first ? __ldcg(a.before + at) : 0.f) + (t == 0 ? sum[0] : sum[1]);
         }
     }
 }

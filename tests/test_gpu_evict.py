@@ -138,6 +138,25 @@ def test_what_is_not_attended_does_not_matter(dtype):
     assert torch.equal(want[keep], got[keep]) and not torch.isfinite(got[~keep]).any()
 
 
+@pytest.mark.parametrize("n", [1, 3, 40])
+def test_a_score_of_minus_infinity_is_a_weight_of_zero(n):
+    job = Job([(n, 60)], H=4, Hkv=2, d=64, page=16)
+    _, clean, lse, _ = weigh(job)
+    job.q[..., 5] = job.q[..., 5].abs() + 0.5
+    k = job.all_k.clone()
+    k[7, :, 5] = -math.inf
+    s2a.s2a_cache_write(job.cache, k, job.all_v, job.table, job.all_starts, job.lengths)
+    _, received, lse, _ = weigh(job, lse=lse)
+    at = int(job.table[0, 0]), slice(None), 7
+    assert (received[at] == 0).all() and torch.isfinite(received).all()
+
+
+def test_many_query_heads_of_a_kv_head():
+    """More rows a token than the streaming kernel takes."""
+    check(Job([(1, 300), (2, 90), (0, 5)], H=64, Hkv=1, d=64, page=16), before="some")
+    check(Job([(1, 1000)], H=64, Hkv=1, d=128, page=64, dtype=E4M3))
+
+
 def test_the_same_twice_on_another_stream_and_captured():
     job = Job([(1, 300), (90, 400), (3, 1000)], H=8, Hkv=2, d=128, page=32)
     _, want, lse, before = weigh(job, before="some")
