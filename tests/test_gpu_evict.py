@@ -359,6 +359,31 @@ def test_a_sequence_served_beyond_its_cache(dtype):
     assert evictions == 2 and s2a.device_status() == (0, 0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_pages_past_32_bits(dtype):
+    """The same tokens in the last pages of a large pool and in a small one."""
+    d, page, n = 128, 256, 600
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn(n, h, d, generator=g).to(BF16).cuda() for h in (2, 1, 1))
+    turns, results = s2a.rotary_turns(d), []
+    for pages in (8, 2**31 // (page * d) + 8 if dtype == BF16 else 2**32 // (page * d) + 8):
+        cache = s2a.PagedCache.empty(pages, 1, page, d, dtype)
+        received = torch.zeros((pages, 1, page), device="cuda")
+        table, to_table = (torch.tensor([[pages - 1 - i for i in x]], dtype=torch.int32).cuda() for x in ((0, 2, 4), (5, 3)))
+        where = table, torch.tensor([0, n], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+        q_out = s2a.s2a_rotate_write(cache, q, k, v, turns, *where)
+        _, lse = s2a.s2a_paged_fwd(q_out, cache, *where)
+        s2a.s2a_paged_weights(q_out, lse, cache, *where, received)
+        for few in (1, 7):  # the other kernel
+            last = table, torch.tensor([0, few], dtype=torch.int32).cuda(), where[2]
+            s2a.s2a_paged_weights(q_out[-few:], lse[:, -few:].contiguous(), cache, *last, received, before=received)
+        lengths, kept = s2a.s2a_cache_evict(cache, received, table, where[2], to_table, 400, sinks=3, recent=50)
+        back = s2a.s2a_cache_read(cache, to_table, torch.tensor([0, 400], dtype=torch.int32).cuda(), lengths, tokens=400)
+        results.append((q_out, kept, *back, received[to_table[0].long()]))
+        assert s2a.device_status() == (0, 0)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 # ---------------------------------------------------------------------------------------------- refusals
 def test_refusals():
     job = Job([(3, 50), (2, 20)], H=4, Hkv=2, d=64, page=16)
