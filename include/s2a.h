@@ -26,7 +26,7 @@
  *   - Return value: S2A_OK (0) or a negative s2a_status.  Arguments are checked before anything is
  *     enqueued, so S2A_ERR_INVALID_ARG, S2A_ERR_UNSUPPORTED, S2A_ERR_TOO_LARGE, S2A_ERR_TIMEOUT and S2A_ERR_BAD_INDEX mean
  *     that nothing was enqueued.  S2A_ERR_CUDA means a CUDA call failed while enqueuing: an entry
- *     point that makes several launches or copies (s2a_bwd and its variants, s2a_paged_fwd, s2a_fwd_bwd_host) may by
+ *     point that makes several launches or copies (s2a_bwd and its variants, s2a_paged_fwd, s2a_paged_weights, s2a_cache_evict, s2a_rotate_bwd, s2a_fwd_bwd_host) may by
  *     then have enqueued the earlier ones, so the outputs are unspecified; `stream` still covers
  *     everything that was enqueued (s2a_fwd_bwd_host joins its copy streams into it on every path).
  *   - Supported shapes: d in {64, 128}; N a multiple of G, N >= 128; G a multiple of 8 (so that every

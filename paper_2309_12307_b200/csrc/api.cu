@@ -76,14 +76,13 @@ int prepare_device(DeviceState** out) {
         if (e != cudaSuccess) return cuda_fail(e);
         e = configure_bwd();
         if (e != cudaSuccess) return cuda_fail(e);
-        e = configure_rotate();
-        if (e != cudaSuccess) return cuda_fail(e);
-        e = configure_evict();
-        if (e != cudaSuccess) return cuda_fail(e);
         ds.paged_error = configure_paged_split(ds.cluster_slots);
         if (ds.paged_error == cudaSuccess) ds.paged_error = configure_paged_fwd();
-        if (ds.paged_error == cudaSuccess) ds.paged_error = configure_weights_tile();
-        if (ds.paged_error != cudaSuccess) cudaGetLastError();  // s2a_paged_fwd's and s2a_paged_weights' to report, and no other call's
+        if (ds.paged_error != cudaSuccess) cudaGetLastError();  // s2a_paged_fwd's to report, and no other call's
+        ds.rotate_error = configure_rotate();
+        ds.evict_error = configure_weights_tile();
+        if (ds.evict_error == cudaSuccess) ds.evict_error = configure_evict();
+        if (ds.rotate_error != cudaSuccess || ds.evict_error != cudaSuccess) cudaGetLastError();
         e = cudaGetSymbolAddress(reinterpret_cast<void**>(&ds.status_ptr), g_status_word);
         if (e != cudaSuccess) return cuda_fail(e);
         if (!g_host_status_registered) {

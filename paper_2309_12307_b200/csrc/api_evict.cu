@@ -15,6 +15,12 @@ namespace {
 
 constexpr long long kIntMax = 0x7fffffffLL;
 
+// The device, set up for these kernels.
+int prepare_evict(DeviceState** ds) {
+    const int rc = prepare_device(ds);
+    return rc != S2A_OK || (*ds)->evict_error == cudaSuccess ? rc : cuda_fail((*ds)->evict_error);
+}
+
 // Blocks of `keys` keys that the new tokens of a sequence together attend at most.
 long long most_chunks(const WeightsParams& a, long long longest, int keys) {
     const long long all = (longest + keys - 1) / keys;
@@ -110,7 +116,7 @@ int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, c
     if (!(scale > 0.f) || !isfinite(scale)) return S2A_ERR_INVALID_ARG;
     if ((rc = check_heads(cache, batch, H, max_new, window, sinks)) != S2A_OK) return rc;
     DeviceState* ds = nullptr;
-    if ((rc = prepare_paged(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
+    if ((rc = prepare_evict(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
     WeightsParams a = weights_params(cache, batch, H, max_new, window, sinks);
     a.q = static_cast<const __nv_bfloat16*>(q), a.lse = lse, a.before = before, a.received = received;
     a.status = ds->status_ptr, a.host_status = ds->host_word_dev;
@@ -143,7 +149,7 @@ size_t s2a_paged_weights_workspace_bytes(const s2a_cache* cache, const s2a_batch
     WeightsTileParams p;
     memset(&p, 0, sizeof p);
     p.a = weights_params(cache, batch, H, max_new, window, sinks);
-    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_paged(&ds) != S2A_OK) return 0;
+    if (static_cast<long long>(max_new) * p.a.rep <= p.a.few_rows || prepare_evict(&ds) != S2A_OK) return 0;
     return plan_tile(&p, ds->n_sm, static_cast<long long>(batch->width) * cache->page_size) ? tile_bytes(p) : 0;
 }
 
@@ -161,7 +167,7 @@ int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, i
     if (room < std::min<long long>(budget, longest)) return S2A_ERR_INVALID_ARG;
     if (static_cast<long long>(B) * cache->Hkv > kIntMax / 16 / ((std::min<long long>(budget, longest) + 15) / 16)) return S2A_ERR_UNSUPPORTED;
     DeviceState* ds = nullptr;
-    if ((rc = prepare_device(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
+    if ((rc = prepare_evict(&ds)) != S2A_OK || (rc = standing_status(ds)) != S2A_OK) return rc;
     EvictParams p;
     memset(&p, 0, sizeof p);
     p.pool = pool_of(cache), p.received = received, p.table = table, p.lengths = lengths, p.to_table = to_table;

@@ -142,6 +142,7 @@ int s2a_rotate_bwd(const void* q, long long q_stride, const void* k, long long k
     if (!aligned16(dq_weight) || !aligned16(dk_weight) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return S2A_ERR_INVALID_ARG;
     DeviceState* ds = nullptr;
     if ((rc = prepare_device(&ds)) != S2A_OK) return rc;
+    if (ds->rotate_error != cudaSuccess) return cuda_fail(ds->rotate_error);
     if (workspace_bytes < bwd_bytes(ds->n_sm, d)) return S2A_ERR_INVALID_ARG;
     if ((rc = standing_status(ds)) != S2A_OK) return rc;
     RotateBwdParams p;

@@ -7,7 +7,7 @@
 // block has a part of its tokens, whose weights it reads once and keeps in shared memory, counts their digits there, and adds up the counts of all blocks.  Then each warp counts, of the
 // neighbouring tokens that are its own, those above the border and those on it; one scan over the warps, and the other blocks' totals, say where each warp's tokens go in the list
 // of those that stay.  What bounds it is latency: three rounds of counting, a barrier and a scan each.  (One block a head that read the weights anew for each of four 8-bit digits, 100,000
-// tokens of 8 heads: both kernels and reading back 470 us.)
+// tokens of 8 heads: both kernels and reading back 470 us; so 47.)
 //
 // The copying kernel moves the rows.  Other pages, not the same ones: tokens move independently of one another, a prefix that
 // other sequences share stays as it is, and each byte that stays is read and written once.  Bound by HBM.

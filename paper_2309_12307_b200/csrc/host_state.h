@@ -16,6 +16,7 @@ struct DeviceState {
     int* host_word_dev = nullptr;     // the same word as the device sees it
     int n_sm = 0;                     // multiprocessors
     cudaError_t paged_error = cudaSuccess;  // what kept the paged cache's attention kernels from being set up
+    cudaError_t rotate_error = cudaSuccess, evict_error = cudaSuccess;  // the same of the rotation's backward, and of weights and eviction
     int cluster_slots[4][17] = {};    // of the paged cache's splitting kernel, see configure_paged_split()
     // s2a_fwd_bwd_host only: copy streams and the events that order them against the caller's stream
     bool host_path_ready = false;
