@@ -413,7 +413,7 @@ size_t s2a_paged_weights_workspace_bytes(const s2a_cache* cache, const s2a_batch
  *   out: new_lengths [B] = m; kept [B, Hkv, budget], the places the tokens had, ascending, -1 from m on
  * A sequence that attends with new_lengths and to_table from then on goes on at its old position (keys are cached rotated, see s2a_rotate_write); its heads hold
  * different tokens at one place, so sinks and windows count places in the cache.
- * budget >= 1, sinks + recent <= budget, to_width * page_size >= min(budget, width * page_size).  lengths[b] may be 0.  new_lengths must not be lengths.  The new pages must differ
+ * budget >= 1, sinks + recent <= budget, to_width * page_size >= min(budget, width * page_size); none of the three above 2^30 - 1.  lengths[b] may be 0.  new_lengths must not be lengths.  The new pages must differ
  * from one another and from all pages of the old sequences, which may share theirs.
  * table, lengths and to_table are read and checked on the device like a batch (a length above width * page_size, a page outside the pool).  Two kernel launches.  Deterministic.
  */

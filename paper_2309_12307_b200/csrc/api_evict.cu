@@ -163,7 +163,7 @@ int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, i
     // (every head's block reads its sequence's length; one of them writes the new one)
     if (new_lengths < lengths + B && lengths < new_lengths + B) return S2A_ERR_INVALID_ARG;
     const long long longest = static_cast<long long>(width) * cache->page_size, room = static_cast<long long>(to_width) * cache->page_size;
-    if (longest > kIntMax / 2 || room > kIntMax / 2) return S2A_ERR_UNSUPPORTED;
+    if (longest > kIntMax / 2 || room > kIntMax / 2 || budget > kIntMax / 2) return S2A_ERR_UNSUPPORTED;  // (places, and steps beyond them, are ints)
     if (room < std::min<long long>(budget, longest)) return S2A_ERR_INVALID_ARG;
     if (static_cast<long long>(B) * cache->Hkv > kIntMax / 16 / ((std::min<long long>(budget, longest) + 15) / 16)) return S2A_ERR_UNSUPPORTED;
     DeviceState* ds = nullptr;

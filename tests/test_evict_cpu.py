@@ -92,4 +92,5 @@ def test_the_library_refuses_without_a_device():
         assert call(**change)[1] == invalid, change
     for change in (dict(width=1 << 27, to_width=1 << 26), dict(to_width=1 << 27), dict(B=1 << 30, new_lengths=a + (1 << 40))):
         assert call(**change)[1] == unsupported, change
+    assert call(budget=1 << 30, to_width=2)[1] == unsupported  # (places behind the last token are counted in an int)
     assert lib.s2a_paged_weights(a, a, None, None, None, a, 4, 1, 1.0, 0, 0, None, 0, None) == invalid
