@@ -121,6 +121,8 @@ int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, c
     a.q = static_cast<const __nv_bfloat16*>(q), a.lse = lse, a.before = before, a.received = received;
     a.status = ds->status_ptr, a.host_status = ds->host_word_dev;
     a.scale_log2 = std::min(scale * 1.4426950408889634f, FLT_MAX);
+    const float half_part = frexpf(a.scale_log2, &a.scale_exp);  // 0.5 <= half_part < 1
+    a.scale_part = 2 * half_part, a.scale_exp += 126;
     const bool e4m3 = cache->type == S2A_CACHE_E4M3, few = a.rep <= a.few_rows, many = static_cast<long long>(max_new) * a.rep > a.few_rows;
     const long long longest = static_cast<long long>(batch->width) * cache->page_size;
     // everything that can be refused comes before the first launch

@@ -24,7 +24,9 @@ struct WeightsParams {
     int H, rep, most_new;
     int window, sinks;       // window 0: none
     int few_rows;            // sequences with at most so many rows are the streaming kernel's, the others the tiling one's
-    float scale_log2;        // scale / ln 2
+    float scale_log2;        // scale / ln 2 = scale_part * 2^(scale_exp - 127), 1 <= scale_part < 2
+    float scale_part;
+    int scale_exp;
 };
 
 // Rows (new tokens times query heads of a KV head) of a sequence up to which it may be the streaming kernel's.

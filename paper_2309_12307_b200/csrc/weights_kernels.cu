@@ -10,13 +10,14 @@
 // of a key at a time (half of two instructions' worth, of 8-bit codes of four) straight from global memory to registers, the next 16
 // keys' on their way; q lies in shared memory in the order in which lanes need it.  Each key is read once; what bounds the kernel is a block's start (addresses, pages and q one after the other,
 // 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16 x up to 8192 tokens of 32 heads 113 us (5.4 TB/s) in pieces of 1024 keys,
-// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 61 us with six blocks on a multiprocessor, 71 with four.  Keys through a ring in shared memory, two or three turns
+// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 59 us with six blocks on a multiprocessor
+// (with four a sixth more).  Keys through a ring in shared memory, two or three turns
 // ahead, left room for fewer blocks: 145 and 81 us.
 //
 // 8-bit caches are multiplied in fp16, which has their codes exactly.  Each row of q goes with a power of two that brings its largest value to
-// [2^14, 2^15); that, and the key's power, multiply the score in fp32.
+// [2^14, 2^15).  Its exponent, the key's and that of the scale are added up before one power of two multiplies the score in fp32: the product of any
+// two of them may be out of range where the score is not.
 #include <cuda_fp16.h>
-#include <float.h>
 
 #include "evict.h"
 #include "paged_device.cuh"
@@ -37,9 +38,9 @@ struct StreamCfg {
     __device__ static constexpr int value(int s, int t) { return (kE4M3 ? 16 : 8) * (t + 4 * (s / kStepsOfPiece)) + 4 * (s % kStepsOfPiece); }
 };
 
-// Rows of q of a sequence and KV head: row r is token r / rep, head r % rep of the KV head's.
+// Rows of q of a sequence and KV head: row r is token r / rep, head r % rep of the KV head's.  s_exp (8 bits): a row's exponent, for score_power().
 template <int HD, bool kE4M3>
-__device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequence& s, int hk, int rows, uint2* s_q, float* s_lse, float* s_scale, int* s_pos) {
+__device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequence& s, int hk, int rows, uint2* s_q, float* s_lse, int* s_exp, int* s_pos) {
     using C = StreamCfg<HD, kE4M3>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int padded = (rows + 7) & ~7;
@@ -52,7 +53,7 @@ __device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequenc
         uint2 w[C::kSteps];
 #pragma unroll
         for (int x = 0; x < C::kSteps; ++x) w[x] = there ? __ldcg(reinterpret_cast<const uint2*>(q + C::value(x, t))) : make_uint2(0, 0);
-        float scale = a.scale_log2;
+        int exp = 0;
         if constexpr (kE4M3) {
             uint32_t most = 0;
 #pragma unroll
@@ -70,16 +71,22 @@ __device__ __forceinline__ void stage_rows(const WeightsParams& a, const Sequenc
                 w[x].x = pack_f16(bf16_low(w[x].x) * up, bf16_high(w[x].x) * up);
                 w[x].y = pack_f16(bf16_low(w[x].y) * up, bf16_high(w[x].y) * up);
             }
-            scale = fminf(scale * power_of_two(e), FLT_MAX);
+            exp = a.scale_exp + e;
         }
 #pragma unroll
         for (int x = 0; x < C::kSteps; ++x) s_q[((base / 8) * C::kSteps + x) * 32 + lane] = w[x];
         if (t == 0) {
             s_lse[r] = there ? __ldcg(a.lse + static_cast<long long>(head) * a.batch.T + s.row0 + token) * 1.4426950408889634f : __uint_as_float(0x7f800000u);
-            s_scale[r] = scale;
+            if constexpr (kE4M3) s_exp[r] = exp;
             s_pos[r] = there ? s.length - s.n + token : -1;
         }
     }
+}
+
+// What the product of an 8-bit key with a row of q is multiplied with: 2^(key_exp + row_exp - 127), held to what fp32 has.  Zero below 2^-126 (products
+// are below 2^31, so such a score does not count), and 2^127 above that: a product of zero is a score of zero, whatever the power.
+__device__ __forceinline__ float score_power(int key_exp, int row_exp) {
+    return __uint_as_float(static_cast<uint32_t>(__viaddmin_s32_relu(key_exp, row_exp, 254)) << 23);
 }
 
 // Keys from `row` of the pools on, 16 of them: a lane's pieces of keys lane / 4 and lane / 4 + 8.
@@ -100,8 +107,8 @@ __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_str
     using C = StreamCfg<HD, kE4M3>;
     const WeightsParams& a = p.a;
     __shared__ uint2 s_q[kStreamedRows / 8 * C::kSteps * 32];
-    __shared__ float s_lse[kStreamedRows], s_scale[kStreamedRows];
-    __shared__ int s_pos[kStreamedRows];
+    __shared__ float s_lse[kStreamedRows];
+    __shared__ int s_pos[kStreamedRows], s_exp[kStreamedRows];
     __shared__ int s_page[kMostChunkPages];
     release_successor();
     wait_for_predecessor();
@@ -135,9 +142,9 @@ __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_str
         if (page < 0) return -1;
         return ((static_cast<long long>(page) * a.pool.Hkv + hk) << a.pool.page_log2) + ((key0 + at) & (page_keys - 1));
     };
-    stage_rows<HD, kE4M3>(a, s, hk, s.n * a.rep, s_q, s_lse, s_scale, s_pos);
+    const int rows = s.n * a.rep, groups = (rows + 7) / 8;
+    stage_rows<HD, kE4M3>(a, s, hk, rows, s_q, s_lse, s_exp, s_pos);
     __syncthreads();
-    const int groups = (s.n * a.rep + 7) / 8;
     uint4 next[2][C::kPieces];
     int next_e[2] = {0, 0};
     long long next_row = row_of(warp);
@@ -145,19 +152,20 @@ __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_str
     for (int i = warp; 16 * i < keys; i += kStreamThreads / 32) {
         const long long row = next_row;
         uint4 now[2][C::kPieces];
-        float power[2];
+        const int now_e[2] = {next_e[0], next_e[1]};
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
 #pragma unroll
             for (int x = 0; x < C::kPieces; ++x) now[y][x] = next[y][x];
-            power[y] = next_e[y] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(next_e[y]);
         }
         next_row = row_of(i + kStreamThreads / 32);
         if (next_row >= 0) load_keys<HD, kE4M3>(a, next_row, next, next_e);
         if (row < 0) continue;
         const int j = key0 + 16 * i + lane / 4;  // this lane's keys are j and j + 8
         const bool whole = all_attend(first, last, key0 + 16 * i, 16, a.window, a.sinks);
-        float sum[2] = {0.f, 0.f};
+        float sum[2];  // (of an 8-bit key that is NaN throughout a NaN)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) sum[y] = kE4M3 && now_e[y] == kExpNotFinite ? __uint_as_float(0x7fffffffu) : 0.f;
         for (int group = 0; group < groups; ++group) {
             float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -176,16 +184,27 @@ __global__ void __launch_bounds__(kStreamThreads, kE4M3 ? 6 : 4) s2a_weights_str
                 }
             }
             const int r = 8 * group + 2 * t;
-            const float2 lse = *reinterpret_cast<const float2*>(s_lse + r), scale = *reinterpret_cast<const float2*>(s_scale + r);
-            const int2 pos = *reinterpret_cast<const int2*>(s_pos + r);
+            const float2 lse = *reinterpret_cast<const float2*>(s_lse + r);
+            int2 exp = {0, 0};
+            if constexpr (kE4M3) exp = *reinterpret_cast<const int2*>(s_exp + r);
+            const float scale = kE4M3 ? a.scale_part : a.scale_log2;
+            float w[2][2];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const float s0 = kE4M3 ? c[2 * y] * power[y] : c[2 * y], s1 = kE4M3 ? c[2 * y + 1] * power[y] : c[2 * y + 1];
-                float w0 = fast_exp2(fmaf(s0, scale.x, -lse.x)), w1 = fast_exp2(fmaf(s1, scale.y, -lse.y));
-                if (whole ? pos.x < 0 : !attends(pos.x, j + 8 * y, a.window, a.sinks)) w0 = 0.f;  // (below zero: no such row)
-                if (whole ? pos.y < 0 : !attends(pos.y, j + 8 * y, a.window, a.sinks)) w1 = 0.f;
-                sum[y] += w0 + w1;
+                float s0 = c[2 * y], s1 = c[2 * y + 1];
+                if constexpr (kE4M3) s0 *= score_power(now_e[y], exp.x), s1 *= score_power(now_e[y], exp.y);
+                w[y][0] = fast_exp2(fmaf(s0, scale, -lse.x)), w[y][1] = fast_exp2(fmaf(s1, scale, -lse.y));
             }
+            if (!whole || 8 * group + 8 > rows) {  // (else all eight rows are there and attend all of these keys)
+                const int2 pos = *reinterpret_cast<const int2*>(s_pos + r);  // (below zero: no such row)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if (whole ? pos.x < 0 : !attends(pos.x, j + 8 * y, a.window, a.sinks)) w[y][0] = 0.f;
+                    if (whole ? pos.y < 0 : !attends(pos.y, j + 8 * y, a.window, a.sinks)) w[y][1] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) sum[y] += w[y][0] + w[y][1];
         }
 #pragma unroll
         for (int y = 0; y < 2; ++y) {

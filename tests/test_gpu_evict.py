@@ -123,6 +123,60 @@ def test_large_and_small_keys_and_queries(by):
         check(job)
 
 
+@pytest.mark.parametrize("new", [1, 10, 30, 200])  # (of two rows each: 1 and 10 are the streaming kernel's)
+@pytest.mark.parametrize("q_power,k_power", [(-100, 100), (-112, 112), (100, -117), (120, -126), (-118, 118), (0, -120), (-120, 0)])
+def test_queries_and_keys_at_the_ends_of_the_range(q_power, k_power, new):
+    """8-bit keys whose powers of two and those of the queries cancel, or leave next to nothing."""
+    for window, sinks in ((0, 0), (70, 3)):
+        job = Job([(new, 300)], H=4, Hkv=2, d=64, page=32, dtype=E4M3)
+        job.all_k *= 2.0**k_power
+        s2a.s2a_cache_write(job.cache, job.all_k, job.all_v, job.table, job.all_starts, job.lengths)
+        job.q *= 2.0**q_power
+        check(job, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 10, 200])
+def test_scores_that_are_zero_between_the_largest_numbers(d, new):
+    """Queries and keys near 2^127 with nothing in common: the scores are zero, whatever power of two they would be multiplied with, and each weight is exp(-lse)."""
+    job = Job([(new, 300)], H=4, Hkv=2, d=d, page=32, dtype=E4M3)
+    job.all_k[..., :d // 2] = 0
+    job.all_k[..., d // 2:] = 2.0**127
+    job.q[..., d // 2:] = 0
+    job.q[..., :d // 2] = 2.0**127
+    s2a.s2a_cache_write(job.cache, job.all_k, job.all_v, job.table, job.all_starts, job.lengths)
+    start, received, lse, _ = weigh(job)
+    want, written = ref.paged_weights(job.q.cpu(), lse.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), start.cpu(), None, d**-0.5)
+    # lse (at most log 300) times 1 / ln 2, the exponential, and sums of 2 * new rows: as in check(), without scores
+    rel = 6 * 2.0**-22 + 2.0**-20 + 2 * new * 2.0**-24
+    off = (received.cpu()[written].double() - want[written]).abs()
+    assert (off <= rel * want[written]).all() and s2a.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("new", [2, 16, 40])
+def test_rows_of_one_call_far_from_one_another(new):
+    """Keys near 2^118.  Every other row of q is as large and has nothing in common with them, the others are as small: their scores are ordinary."""
+    d = 64
+    job = Job([(new, 300)], H=2, Hkv=1, d=d, page=32, dtype=E4M3)
+    job.all_k[..., :d // 2] = 0
+    job.all_k *= 2.0**118
+    s2a.s2a_cache_write(job.cache, job.all_k, job.all_v, job.table, job.all_starts, job.lengths)
+    job.q[::2, :, d // 2:] = 0
+    job.q[::2] *= 2.0**118
+    job.q[1::2] *= 2.0**-118
+    i = torch.arange(300 - new, 300)
+    host = job.host_cache()
+    from oracle.paged_torch import sequence_values
+    s = d**-0.5 * torch.einsum("thc,jc->htj", job.q.cpu().double(), sequence_values(host, "k", job.table.cpu(), 0, 300)[0])
+    lse = s.masked_fill(~ref.attends(i, 300, 0, 0), -math.inf).logsumexp(-1).float().cuda()  # (what is looked at here are the weights)
+    start, received, _, _ = weigh(job, lse=lse)
+    want, written = ref.paged_weights(job.q.cpu(), lse.cpu(), host, job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), start.cpu(), None, d**-0.5)
+    reach = d**-0.5 * float((job.q.cpu()[1::2].double() * 2.0**118).norm(dim=-1).max()) * float((job.all_k.double() * 2.0**-118).norm(dim=-1).max())
+    rel = d * 2.0**-24 * reach + (reach + float(lse.abs().max())) * 2.0**-22 + 2.0**-20 + 2 * new * 2.0**-24
+    off = (received.cpu()[written].double() - want[written]).abs()
+    assert rel < 0.02 and (off <= rel * want[written]).all() and s2a.device_status() == (0, 0)
+
+
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
 def test_what_is_not_attended_does_not_matter(dtype):
     """Keys that some rows do not attend: NaN there reaches no other key's weight."""
