@@ -355,7 +355,7 @@ typedef struct s2a_rotation {
 
 /*
  * q [T, H, d] and k [T, Hkv, d] (bf16) -> q_out, k_out of the same shapes.  d in {64, 128}; H need not be a multiple of Hkv.  *_stride: values from a token to the next,
- * a multiple of 8, at least heads * d and at most 2^28 (T = 1: ignored), so that the slices of a projection's output [T, H + 2 Hkv, d], or of qkv [B, N, 3, H, d], are taken and
+ * a multiple of 8, at least heads * d and at most 2^28 (T = 1: ignored, but heads * d is at most 2^28 too), so that the slices of a projection's output [T, H + 2 Hkv, d], or of qkv [B, N, 3, H, d], are taken and
  * written as they lie.  An output may be its input (same pointer and stride); otherwise the four must not overlap.  T * (H + 2 Hkv) must not exceed 2^31 - 1.
  * One kernel launch.
  */

@@ -13,13 +13,14 @@ namespace s2a {
 namespace {
 
 constexpr long long kIntMax = 0x7fffffffLL;
-constexpr long long kMostStride = 1 << 28;  // (64 tokens of it, in eights, fit an int)
+constexpr long long kMostStride = 1 << 28;  // (64 tokens of it, in eights, and the place of a head in a token, fit an int)
 
 // `x` [T, heads, d] with `stride` values from a token to the next
 int check_rows(const void* x, long long stride, int T, int heads, int d) {
     if (!x || !aligned16(x) || heads <= 0) return S2A_ERR_INVALID_ARG;
-    if (T == 1) return S2A_OK;
-    if (stride % 8 != 0 || stride < static_cast<long long>(heads) * d) return S2A_ERR_INVALID_ARG;
+    const long long dense = static_cast<long long>(heads) * d;
+    if (T == 1) return dense > kMostStride ? S2A_ERR_UNSUPPORTED : S2A_OK;
+    if (stride % 8 != 0 || stride < dense) return S2A_ERR_INVALID_ARG;
     return stride > kMostStride ? S2A_ERR_UNSUPPORTED : S2A_OK;
 }
 

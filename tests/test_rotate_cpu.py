@@ -84,5 +84,8 @@ def test_the_library_refuses_without_a_device():
         assert call(**change) == (unsupported,) * 3, change
     assert call(q_out=a + 4)[::2] == (invalid,) * 2 and call(dq=None)[1] == invalid
     assert call(workspace=a + 16)[1] == invalid and call(workspace=None)[1] == invalid
+    # a token's heads lie within 2^28 values, of a single token too, whose stride is not looked at
+    for change in (dict(T=1, H=(1 << 22) + 1), dict(T=1, H=1 << 25), dict(T=1, H=(1 << 21) + 1, d=128), dict(T=1, Hkv=(1 << 22) + 1)):
+        assert call(**change, q_stride=0) == (unsupported,) * 3, change
     assert call(rotation=dict(positions=None, n_positions=0))[:2] == (invalid,) * 2
     assert lib.s2a_rotate_bwd_workspace_bytes(96) == 0
