@@ -660,7 +660,8 @@ def s2a_rotate(q, k, turns, positions=None, q_weight=None, k_weight=None, eps=No
     """q [.., H, d] and k [.., Hkv, d] with the first 2 * len(turns) values of every head rotated by its token's position; with `eps` every head's row is
     normalised first (times q_weight, k_weight [d] in bf16 or fp32 where they are given).  `turns` as rotary_turns() makes it.  `positions` (int32): one for each
     token, or for each of the last dimension of tokens; default 0, 1, .. along that.  Pairs are values i and i + r / 2, or neighbours (`interleaved`).
-    Tokens may be at any one distance (slices of a projection's output); q_out may be q, and k_out k."""
+    Tokens may be at any one distance that is a multiple of 8 values and no less than a token's heads, from an address that is a multiple of 16 bytes on
+    (slices of a projection's output); q_out may be q, and k_out k."""
     args = q, k, turns, positions, q_weight, k_weight, eps
     hot = _hot or _hot_for(_check_rotate, *args, q_out, k_out)
     r = hot.rotate(*args, bool(interleaved), q_out, k_out, _given_stream(stream))

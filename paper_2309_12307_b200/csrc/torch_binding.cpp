@@ -522,6 +522,16 @@ std::optional<int64_t> token_stride(const Tensor& x) {
     return stride;
 }
 
+// Whether the library takes x as it lies: tokens apart by a row at least and by whole pieces of 16 bytes, of which one begins at x.
+bool taken_as_it_lies(const Tensor& x) {
+    const auto stride = token_stride(x);
+    if (!stride || reinterpret_cast<uintptr_t>(x.data_ptr()) % 16 != 0) return false;
+    const int64_t n = x.dim(), row = x.size(n - 2) * x.size(n - 1);
+    return x.numel() == row || (*stride >= row && *stride % 8 == 0 && *stride <= (int64_t(1) << 28));
+}
+// x, or a copy that the library takes.  (contiguous() would not move a dense tensor that begins off 16 bytes.)
+Tensor in_rows(const Tensor& x) { return taken_as_it_lies(x) ? x : x.clone(at::MemoryFormat::Contiguous); }
+
 bool rows_like(const Tensor& x, const Tensor& like) { return token_stride(x) && x.sizes() == like.sizes() && x.device() == like.device(); }
 
 struct HeadSizes {
@@ -766,16 +776,16 @@ struct S2Rotate : public torch::autograd::Function<S2Rotate> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         const variable_list saved = ctx->get_saved_variables();
-        const Tensor &q = saved[0], &k = saved[1], &q_weight = saved[2], &k_weight = saved[3];
+        const Tensor &q_weight = saved[2], &k_weight = saved[3];
         const RotationArgs args{saved[4], saved[5], q_weight, k_weight, ctx->saved_data["eps"].toOptional<double>(), ctx->saved_data["interleaved"].toBool()};
-        auto in_rows = [](const Tensor& t) { return token_stride(t) ? t : t.contiguous(); };
+        at::NoGradGuard no_grad;
         const Tensor dq_out = in_rows(grads[0]), dk_out = in_rows(grads[1]);
         const auto s = head_sizes(dq_out, dk_out);
         s2a_rotation r;
         // saved-tensor hooks decide what comes back
+        const Tensor q = saved[0].defined() ? in_rows(saved[0]) : Tensor(), k = saved[1].defined() ? in_rows(saved[1]) : Tensor();
         TORCH_CHECK_VALUE(s && args.fill(&r, dq_out, s->T, s->N, s->d) && (!r.norm || (rows_like(q, dq_out) && rows_like(k, dk_out))),
                           "the gradients must be bf16 CUDA tensors of the shapes of q and k, and what was saved must have come back as it was");
-        at::NoGradGuard no_grad;
         const c10::cuda::CUDAGuard device(dq_out.device());
         const RotationGrads g(dq_out, dk_out, r, *s);
         const int rc = g.call(q, k, dq_out, dk_out, r, *s, current_stream());
@@ -794,8 +804,7 @@ py::object s2_rotate(py::handle q_, py::handle k_, py::handle turns, py::handle 
     variable_list out;
     {
         py::gil_scoped_release nogil;
-        if (!token_stride(q.t)) q.t = q.t.contiguous();
-        if (!token_stride(k.t)) k.t = k.t.contiguous();
+        q.t = in_rows(q.t), k.t = in_rows(k.t);
         const auto s = head_sizes(q.t, k.t);
         s2a_rotation r;
         if (s && given.fill(&r, q.t, s->T, s->N, s->d))

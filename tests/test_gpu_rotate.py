@@ -293,6 +293,60 @@ def test_autograd_takes_strides_and_expanded_gradients():
     assert torch.equal(x.grad, want[0])
 
 
+def column(x, n):
+    return torch.full((x.shape[0], n), 0.5, dtype=x.dtype, device=x.device)
+
+
+# what comes back for the rotated queries is ..
+LATER = [("the same for all tokens", lambda y: y.sum(0)), ("behind three columns more", lambda y: torch.cat((y.flatten(1), column(y, 3)), 1)),
+         ("off 16 bytes", lambda y: torch.cat((column(y, 4), y.flatten(1)), 1)), ("the same for two tokens at a time", lambda y: y.view(-1, 2, *y.shape[1:]).sum(1)),
+         ("off 16 bytes and dense", lambda y: torch.cat((column(y, 1)[0], y.flatten())))]
+
+
+@pytest.mark.parametrize("later", [f for _, f in LATER], ids=[x for x, _ in LATER])
+@pytest.mark.parametrize("norm", [None, "weights"])
+def test_autograd_takes_gradients_as_they_come(later, norm):
+    g = torch.Generator().manual_seed(3)
+    job = Job(24, 4, 2, 64, norm=norm)
+    leaves = [t.clone().requires_grad_() for t in (job.on_q, job.on_k)]
+    q, k = s2_rotate(*leaves, job.turns, **job.how)
+    y = q.detach().requires_grad_()
+    out = later(y)
+    gradient = numbers(g, *out.shape).cuda()
+    dy, = torch.autograd.grad(out, y, gradient)
+    got = torch.autograd.grad((later(q), k), leaves, (gradient, job.dk_out.cuda()))
+    want = s2a.s2a_rotate_bwd(job.on_q, job.on_k, dy.clone(memory_format=torch.contiguous_format), job.dk_out.cuda(), job.turns, **job.how)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_autograd_takes_a_gradient_for_all_sequences_and_tokens():
+    job = Job(24, 4, 2, 64)
+    for B, axes in ((3, (0, 1)), (1, 1), (24, 0)):
+        x = job.on_q.view(B, 24 // B, 4, 64).detach().requires_grad_()
+        q, _ = s2_rotate(x, job.on_k.view(B, 24 // B, 2, 64), job.turns)
+        (q.sum(axes) * job.dq_out[0].cuda()).sum().backward()
+        dy = job.dq_out[:1].cuda().expand(24, 4, 64).contiguous().view_as(x)
+        want = s2a.s2a_rotate_bwd(None, None, dy, torch.zeros_like(job.on_k).view(B, 24 // B, 2, 64), job.turns)
+        assert torch.equal(x.grad, want[0])
+
+
+@pytest.mark.parametrize("norm", [None, "weights"])
+@pytest.mark.parametrize("kind", ["odd distance", "off 16 bytes", "one token for all", "rows that overlap", "far apart"])
+def test_autograd_takes_tokens_at_any_distance(norm, kind):
+    T, H, d = (2 if kind == "far apart" else 10), 4, 64
+    job = Job(T, H, 2, d, norm=norm)
+    stride, first = {"odd distance": (H * d + 3, 0), "off 16 bytes": (H * d + 8, 4), "one token for all": (0, 0), "rows that overlap": (64, 0), "far apart": (2**28 + 8, 0)}[kind]
+    memory = torch.zeros((T - 1) * stride + H * d + first, dtype=BF16, device="cuda")
+    memory[first:first + H * d * (2 if stride >= 64 else 1)].copy_(numbers(torch.Generator().manual_seed(2), 2 * H * d)[:H * d * (2 if stride >= 64 else 1)])
+    x = memory.as_strided((T, H, d), (stride, d, 1), first).requires_grad_()
+    copy = x.detach().clone(memory_format=torch.contiguous_format)
+    got = s2_rotate(x, job.on_k, job.turns, **job.how)
+    want = s2a.s2a_rotate(copy, job.on_k, job.turns, **job.how)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    dx, = torch.autograd.grad(got, x, (job.dq_out.cuda(), job.dk_out.cuda()))
+    assert torch.equal(dx, s2a.s2a_rotate_bwd(copy, job.on_k, job.dq_out.cuda(), job.dk_out.cuda(), job.turns, **job.how)[0])
+
+
 def test_gradients_into_attention():
     """Rotated queries and keys in shifted sparse attention: the whole chain's gradients against finite parts computed in 64 bits."""
     g = torch.Generator().manual_seed(4)
