@@ -35,8 +35,9 @@ def s2_rotate(q: torch.Tensor, k: torch.Tensor, turns: torch.Tensor, positions: 
               k_weight: torch.Tensor | None = None, eps: float | None = None, interleaved: bool = False):
     """(q, k) normalised for each head (with `eps`) and rotated by their positions, as s2_attn takes them: a differentiable function of q [.., H, d],
     k [.., Hkv, d] and the norms' weights.  Arguments as in `binding.s2a_rotate`, but q, k and gradients whose tokens lie as it does not take them are
-    copied.  The weights' gradients are summed in fp32 and have the weights' type.  A step that is captured into a CUDA graph needs, as with every
-    function of torch's autograd, that no graph of the same leaves from another stream is alive."""
+    copied.  The weights' gradients are summed in fp32 and have the weights' type.  Differentiating a gradient again (create_graph) is refused with a
+    NotImplementedError.  A step that is captured into a CUDA graph needs, as with every function of torch's autograd, that no graph of the same
+    leaves from another stream is alive."""
     args = q, k, turns, positions, q_weight, k_weight, eps
     hot = binding._hot or binding._hot_for(_check_rotate, *args)
     r = hot.s2_rotate(*args, bool(interleaved))

@@ -16,6 +16,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 
+#include <array>
 #include <cmath>
 #include <limits>
 #include <optional>
@@ -700,6 +701,30 @@ py::object rotate_write(py::handle kp, py::handle vp, py::handle ke, py::handle 
     throw e;
 }
 
+using MaybeTensor = std::optional<Tensor>;  // (autograd does not take undefined ones)
+MaybeTensor maybe(const Tensor& t) { return t.defined() ? MaybeTensor(t) : std::nullopt; }
+
+// A gradient as it is, which to differentiate again is an error: the backward passes have no derivative, and without one what a gradient depends
+// on would seem not to matter.
+struct FirstOnly : public torch::autograd::Function<FirstOnly> {
+    static Tensor forward(AutogradContext*, const Tensor& grad, const MaybeTensor&, const MaybeTensor&, const MaybeTensor&, const MaybeTensor&,
+                          const MaybeTensor&, const MaybeTensor&) {
+        return grad;
+    }
+    static variable_list backward(AutogradContext*, variable_list) {
+        TORCH_CHECK_NOT_IMPLEMENTED(false, "s2_rotate has no second derivatives");
+        return {};
+    }
+};
+// The gradients that a backward pass has made of `of`; create_graph: whether they may be differentiated.
+variable_list first_only(bool create_graph, variable_list grads, const std::array<Tensor, 6>& of) {
+    if (!create_graph) return grads;
+    at::AutoGradMode on(true);
+    for (Tensor& g : grads)
+        if (g.defined()) g = FirstOnly::apply(g, maybe(of[0]), maybe(of[1]), maybe(of[2]), maybe(of[3]), maybe(of[4]), maybe(of[5]));
+    return grads;
+}
+
 struct S2Attn : public torch::autograd::Function<S2Attn> {
     static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, int64_t G, std::optional<double> scale,
                           std::optional<int64_t> n_unshifted, std::optional<int64_t> shift, int64_t flags, bool fast) {
@@ -755,8 +780,6 @@ py::object s2_attn(py::handle q_, py::handle k_, py::handle v_, int G, std::opti
 
 // Norms and rotation as a differentiable function of q, k and the norms' weights.
 struct S2Rotate : public torch::autograd::Function<S2Rotate> {
-    using MaybeTensor = std::optional<Tensor>;  // (autograd does not take undefined ones)
-    static MaybeTensor maybe(const Tensor& t) { return t.defined() ? MaybeTensor(t) : std::nullopt; }
     static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const MaybeTensor& q_weight_, const MaybeTensor& k_weight_,
                                  const Tensor& turns, const MaybeTensor& positions_, std::optional<double> eps, bool interleaved) {
         const Tensor q_weight = q_weight_.value_or(Tensor()), k_weight = k_weight_.value_or(Tensor()), positions = positions_.value_or(Tensor());
@@ -778,6 +801,7 @@ struct S2Rotate : public torch::autograd::Function<S2Rotate> {
         const variable_list saved = ctx->get_saved_variables();
         const Tensor &q_weight = saved[2], &k_weight = saved[3];
         const RotationArgs args{saved[4], saved[5], q_weight, k_weight, ctx->saved_data["eps"].toOptional<double>(), ctx->saved_data["interleaved"].toBool()};
+        const bool create_graph = at::GradMode::is_enabled();
         at::NoGradGuard no_grad;
         const Tensor dq_out = in_rows(grads[0]), dk_out = in_rows(grads[1]);
         const auto s = head_sizes(dq_out, dk_out);
@@ -791,7 +815,8 @@ struct S2Rotate : public torch::autograd::Function<S2Rotate> {
         const int rc = g.call(q, k, dq_out, dk_out, r, *s, current_stream());
         if (rc != S2A_OK) raise_status(rc, "s2a_rotate_bwd");
         auto like = [](const Tensor& grad, const Tensor& weight) { return grad.defined() ? grad.to(weight.scalar_type()) : Tensor(); };
-        return {g.dq, g.dk, like(g.dq_weight, q_weight), like(g.dk_weight, k_weight), Tensor(), Tensor(), Tensor(), Tensor()};
+        const variable_list out = {g.dq, g.dk, like(g.dq_weight, q_weight), like(g.dk_weight, k_weight), Tensor(), Tensor(), Tensor(), Tensor()};
+        return first_only(create_graph, out, {grads[0], grads[1], saved[0], saved[1], q_weight, k_weight});
     }
 };
 
@@ -808,8 +833,8 @@ py::object s2_rotate(py::handle q_, py::handle k_, py::handle turns, py::handle 
         const auto s = head_sizes(q.t, k.t);
         s2a_rotation r;
         if (s && given.fill(&r, q.t, s->T, s->N, s->d))
-            out = S2Rotate::apply(q.t, k.t, S2Rotate::maybe(given.q_weight), S2Rotate::maybe(given.k_weight), given.turns,
-                                  S2Rotate::maybe(given.positions), eps, interleaved);
+            out = S2Rotate::apply(q.t, k.t, maybe(given.q_weight), maybe(given.k_weight), given.turns,
+                                  maybe(given.positions), eps, interleaved);
     }
     return out.empty() ? py::none() : py::object(py::make_tuple(out[0], out[1]));
 }

@@ -347,6 +347,29 @@ def test_autograd_takes_tokens_at_any_distance(norm, kind):
     assert torch.equal(dx, s2a.s2a_rotate_bwd(copy, job.on_k, job.dq_out.cuda(), job.dk_out.cuda(), job.turns, **job.how)[0])
 
 
+@pytest.mark.parametrize("norm", [None, "plain", "weights"])
+def test_second_derivatives_are_refused(norm):
+    job = Job(24, 4, 2, 64, norm=norm)
+    how = job.how
+    leaves = [t.clone().requires_grad_() for t in (job.on_q, job.on_k)]
+    if norm == "weights":
+        leaves += [how["q_weight"].requires_grad_(), how["k_weight"].requires_grad_()]
+
+    def first(create_graph):
+        q, k = s2_rotate(*leaves[:2], job.turns, **how)
+        return torch.autograd.grad(q.float().square().sum() + k.float().square().sum(), leaves, create_graph=create_graph)
+
+    want, got = first(False), first(True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for leaf in leaves:
+        with pytest.raises(NotImplementedError, match="second derivatives"):
+            torch.autograd.grad(sum(x.float().sum() for x in got), leaf, retain_graph=True, allow_unused=True)
+    # gradients that do not depend on anything are as ever
+    q, _ = s2_rotate(*leaves[:2], job.turns, **how)
+    dq, = torch.autograd.grad(q, leaves[0], job.dq_out.cuda(), create_graph=True)
+    assert dq.requires_grad == (norm is not None)
+
+
 def test_gradients_into_attention():
     """Rotated queries and keys in shifted sparse attention: the whole chain's gradients against finite parts computed in 64 bits."""
     g = torch.Generator().manual_seed(4)
