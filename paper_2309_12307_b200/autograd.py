@@ -23,6 +23,7 @@ def s2_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, G: int, *, scale:
     `fast_backward` chooses the backward's scratch: True allocates room for the spilled dS (2 bytes per
     attended pair of a tile, from what torch's caching allocator holds unused or within half of the free device
     memory) so that dq is a plain product, False the minimum (4 bytes per query row; dq then recomputes the scores).
+    Differentiating a gradient again (create_graph) is refused with a NotImplementedError.
     """
     hot = binding._hot or binding._hot_for(_check, q, k, v)
     o = hot.s2_attn(q, k, v, G, scale, n_unshifted, shift, binding._flags(leak_free, swap_wrapped), bool(fast_backward))

@@ -712,7 +712,7 @@ struct FirstOnly : public torch::autograd::Function<FirstOnly> {
         return grad;
     }
     static variable_list backward(AutogradContext*, variable_list) {
-        TORCH_CHECK_NOT_IMPLEMENTED(false, "s2_rotate has no second derivatives");
+        TORCH_CHECK_NOT_IMPLEMENTED(false, "s2_attn and s2_rotate have no second derivatives");
         return {};
     }
 };
@@ -755,12 +755,13 @@ struct S2Attn : public torch::autograd::Function<S2Attn> {
         TORCH_CHECK_VALUE(s && same_shape(o, q.sizes(), q, at::kBFloat16) && is_stats(lse, *s, q),
                           "the saved q, k, v, o and lse have come back with another type, shape, layout or device");
         TORCH_CHECK_VALUE(same_shape(dO, q.sizes(), q, at::kBFloat16), "dO must be a bf16 CUDA tensor of the shape of q");
+        const bool create_graph = at::GradMode::is_enabled();
         at::NoGradGuard no_grad;
         Tensor dq = new_like(q), dk = new_like(k), dv = new_like(v);
         const Tensor ws = new_workspace(*s, G, q, ctx->saved_data["fast"].toBool());
         const int rc = call_bwd(q, k, v, o, lse, dO, dq, dk, dv, ws, *s, G, &ex, current_stream());
         if (rc != S2A_OK) raise_status(rc, "s2a_bwd_ex");
-        return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        return first_only(create_graph, {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {grads[0], q, k, v});
     }
 };
 

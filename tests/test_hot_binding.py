@@ -69,6 +69,19 @@ def test_s2_attn_takes_strided_inputs_and_gradients():
 
 
 @pytest.mark.gpu
+def test_second_derivatives_of_s2_attn_are_refused():
+    q, k, v, dO = (x.cuda() for x in make_inputs(1, 512, 4, 2, 64, seed=9))
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    want = torch.autograd.grad(s2_attn(*leaves, 256), leaves, dO)
+    dO = dO.detach().requires_grad_()
+    got = torch.autograd.grad(s2_attn(*leaves, 256), leaves, dO, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for leaf in (*leaves, dO):
+        with pytest.raises(NotImplementedError, match="second derivatives"):
+            torch.autograd.grad(sum(x.float().sum() for x in got), leaf, retain_graph=True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("change", [lambda t: t.half(), lambda t: t[..., ::2], lambda t: t[..., :32].contiguous(), lambda t: t.cpu(),
                                     lambda t: t.transpose(1, 2).contiguous().transpose(1, 2)])
 @pytest.mark.parametrize("which", range(5))
