@@ -55,6 +55,11 @@ bool is_stats(const Tensor& lse, const Sizes& s, const Tensor& like) { return sa
 Tensor new_stats(const Sizes& s, const Tensor& like) { return at::empty({s.B, s.H, s.N}, like.options().dtype(at::kFloat)); }
 Tensor new_like(const Tensor& t) { return at::empty(t.sizes(), t.options()); }
 
+// t, or a dense copy where it is none or begins off 16 bytes (contiguous() would not move it then).
+Tensor dense_rows(const Tensor& t) {
+    return t.defined() && t.is_cuda() && t.is_contiguous() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0 ? t.clone(at::MemoryFormat::Contiguous) : t.contiguous();
+}
+
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 // The stream of a call of binding.py: the one it was given, or torch's current one.  What is made for a call on another
@@ -749,7 +754,7 @@ struct S2Attn : public torch::autograd::Function<S2Attn> {
         const Options ex{ctx->saved_data["scale"].toOptional<double>(), ctx->saved_data["n_unshifted"].toOptional<int64_t>(),
                          ctx->saved_data["shift"].toOptional<int64_t>(), static_cast<unsigned>(ctx->saved_data["flags"].toInt())};
         const int G = static_cast<int>(ctx->saved_data["G"].toInt());
-        const Tensor dO = grads[0].contiguous();
+        const Tensor dO = dense_rows(grads[0]);
         const auto s = sizes_of(q, k, v);
         // saved-tensor hooks decide what comes back
         TORCH_CHECK_VALUE(s && same_shape(o, q.sizes(), q, at::kBFloat16) && is_stats(lse, *s, q),
@@ -773,7 +778,7 @@ py::object s2_attn(py::handle q_, py::handle k_, py::handle v_, int G, std::opti
     Tensor o;
     {
         py::gil_scoped_release nogil;
-        q.t = q.t.contiguous(), k.t = k.t.contiguous(), v.t = v.t.contiguous();
+        q.t = dense_rows(q.t), k.t = dense_rows(k.t), v.t = dense_rows(v.t);
         if (sizes_of(q.t, k.t, v.t)) o = S2Attn::apply(q.t, k.t, v.t, G, scale, n_unshifted, shift, flags, fast);
     }
     return o.defined() ? py::cast(o) : py::none();

@@ -69,6 +69,23 @@ def test_s2_attn_takes_strided_inputs_and_gradients():
 
 
 @pytest.mark.gpu
+def test_s2_attn_takes_inputs_and_gradients_off_16_bytes():
+    inputs = [x.cuda() for x in make_inputs(1, 512, 4, 2, 64, seed=8)]
+
+    def moved(t):
+        """The same numbers, dense, two bytes behind a boundary of 16."""
+        return torch.cat((t.flatten()[:1], t.flatten()))[1:].view(t.shape)
+
+    q, k, v, dO = inputs
+    o, lse = s2a.s2a_fwd(q, k, v, 256)
+    want = (o, *s2a.s2a_bwd(q, k, v, o, lse, dO, 256))
+    leaves = [moved(t).requires_grad_() for t in (q, k, v)]
+    o = s2_attn(*leaves, 256)
+    got = (o.detach(), *torch.autograd.grad(o, leaves, moved(dO)))
+    assert all(t.data_ptr() % 16 == 2 for t in leaves) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
 def test_second_derivatives_of_s2_attn_are_refused():
     q, k, v, dO = (x.cuda() for x in make_inputs(1, 512, 4, 2, 64, seed=9))
     leaves = [t.requires_grad_() for t in (q, k, v)]
