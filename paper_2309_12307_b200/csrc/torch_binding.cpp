@@ -495,7 +495,9 @@ py::object cache_evict(py::handle kp, py::handle vp, py::handle ke, py::handle v
     const auto ints = a.k.t.options().dtype(at::kInt);
     if (!new_lengths.given) new_lengths.t = on.output(at::empty({B}, ints));
     else if (!same_shape(new_lengths.t, {B}, a.k.t, at::kInt)) return py::none();
-    if (!kept.given) kept.t = on.output(at::empty({B, Hkv, std::max<int64_t>(as_int(budget), 0)}, ints));
+    // (a budget that the library refuses needs no room: one number, so that there is an address to refuse it with)
+    const bool refused = budget <= 0 || budget > (int64_t(1) << 30) - 1;
+    if (!kept.given) kept.t = on.output(at::empty({B, Hkv, refused ? 1 : budget}, ints));
     else if (!same_shape(kept.t, {B, Hkv, budget}, a.k.t, at::kInt)) return py::none();
     void* st = on.begin();
     auto ptr = [](const Tensor& t) { return static_cast<int*>(t.data_ptr()); };

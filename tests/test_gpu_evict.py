@@ -331,6 +331,19 @@ def test_weights_that_are_equal_or_no_numbers(kind, budget):
         evicted([n], budget, 4, 16, received=w)
 
 
+def test_a_budget_that_is_too_large_takes_no_memory():
+    job = Job([(0, 20)], H=1, Hkv=1, d=64, page=16)
+    received = torch.zeros(job.cache.k.shape[:3], device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    for budget in (2**30, 2**31 - 1):
+        with pytest.raises(s2a.S2AError) as e:
+            s2a.s2a_cache_evict(job.cache, received, job.table, job.lengths, job.table, budget)
+        assert e.value.status == s2a.S2A_ERR_UNSUPPORTED
+    assert torch.cuda.max_memory_allocated() - held < 2**20 and s2a.device_status() == (0, 0)
+
+
 def test_long_sequences():
     evicted([100_003], 4097, 4, 1024, Hkv=1, d=64, page=128, dtype=E4M3)
     evicted([60_000, 58_000, 9, 20_000], 300, 0, 7, Hkv=2, d=64, page=16)
