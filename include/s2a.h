@@ -369,6 +369,7 @@ int s2a_rotate(const void* q, long long q_stride, const void* k, long long k_str
  *        without a norm)
  *   workspace: with a norm at least s2a_rotate_bwd_workspace_bytes(d), 256-byte aligned; its contents before the call do not matter, and calls that can
  *        overlap on the GPU need one each.  Without a norm it is not looked at.
+ * With a norm the gradients that come in, times the weight, are at most 2^120 in magnitude (sums of d of them are made).
  * The weights' gradients are sums in fp32 over all tokens and heads, in an order that the sizes and the device fix: deterministic, no atomics.  One launch without a norm, two
  * with one.
  */

@@ -132,10 +132,11 @@ __device__ __forceinline__ float sum_of_row(float x, uint32_t mask = 0xffffffffu
     return x;
 }
 
-// x times s = 1 / sqrt(mean x^2 + eps), which is returned; every lane of a row gets the same.  Squares that fp32 would not hold (values above
-// 2^45, or, where eps does not matter either, below 2^-50) are taken of x times a power of two.
+// x times s = 1 / sqrt(mean x^2 + eps); every lane of a row gets the same.  Squares that fp32 would not hold (values above 2^45, or, where eps does not
+// matter either, below 2^-50) are taken of x times a power of two.  Returns s, of small rows without that power (*rest, else 1): of subnormal numbers the two
+// together are infinite.
 template <int HD>
-__device__ __forceinline__ float normalise_row(float (&x)[16], float eps) {
+__device__ __forceinline__ float normalise_row(float (&x)[16], float eps, float* rest) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += x[i] * x[i];
@@ -155,7 +156,8 @@ __device__ __forceinline__ float normalise_row(float (&x)[16], float eps) {
     const float s = rsqrtf(sum * (1.f / HD) + eps);
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] *= s;
-    return s * by;
+    *rest = small ? by : 1.f;
+    return large ? s * by : s;
 }
 
 template <int HD, bool kNorm, RotateTo kTo>
@@ -234,7 +236,8 @@ __global__ void __launch_bounds__(kRotateThreads, 4) s2a_rotate_kernel(const __g
         float y[16];
         unpack_row(x[i], y);
         if constexpr (kNorm) {
-            normalise_row<HD>(y, p.rotation.eps);
+            float rest;
+            normalise_row<HD>(y, p.rotation.eps, &rest);
             times_weights<HD>(y, s_weights[w.kind == 0 ? 0 : 1], part);
         }
         if (w.kind != 2) {
@@ -354,7 +357,8 @@ __global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_ker
                 unpack_row(now_g, g);
             }
             turn_row<HD>(g, table + at[i] * L::kTable, pieces, part, p.rotation.interleaved);
-            const float s = normalise_row<HD>(x, p.rotation.eps);
+            float rest;
+            const float s = normalise_row<HD>(x, p.rotation.eps, &rest);
             if (there) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sum[e] += g[e] * x[e];
@@ -366,6 +370,10 @@ __global__ void __launch_bounds__(kRotateThreads, kBwdBlocks) s2a_rotate_bwd_ker
             mean = sum_of_row<HD>(mean) * (1.f / HD);
 #pragma unroll
             for (int e = 0; e < 16; ++e) g[e] = s * (g[e] - x[e] * mean);
+            if (rest != 1.f) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) g[e] *= rest;
+            }
             uint4 w[2];
             pack_row(g, w);
             if (there) store_row(out + i * L::kGroups * HD, pieces, w);

@@ -169,6 +169,18 @@ def test_rows_whose_squares_leave_the_range(by, eps):
     job.check_forward()
 
 
+@pytest.mark.parametrize("by,eps,power", [(2.0**125, 1e-5, 60), (2.0**125, 0.0, 110), (2.0**100, 1e-5, 0), (2.0**60, 1e30, 0), (1.0, 3e38, 40), (2.0**-60, 1e-30, 0), (2.0**-100, 1e-5, 0),
+                                          (2.0**-100, 0.0, -20), (2.0**-125, 0.0, -20), (2.0**-131, 0.0, -60), (2.0**-133, 0.0, -100)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_rows_whose_squares_leave_the_range(by, eps, power, d):
+    job = Job(9, 3, 1, d, norm="weights", by=by, eps=eps)
+    for t in (job.q, job.on_q, job.k, job.on_k):
+        t[..., 0] = by  # (no row of zeros)
+    job.dq_out *= 2.0**power
+    job.dk_out *= 2.0**power
+    job.check_backward()
+
+
 def test_what_is_not_finite_stays_in_its_row():
     job = Job(40, 4, 2, 64, norm="plain")
     clean = s2a.s2a_rotate(job.on_q, job.on_k, job.turns, **job.how)
