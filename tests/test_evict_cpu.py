@@ -51,6 +51,14 @@ def test_order_of_weights(tmp_path):
     assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout + out.stderr
 
 
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(CUDA_INC), reason="needs g++ and the CUDA headers")
+def test_items_have_each_row_and_key_once(tmp_path):
+    exe = str(tmp_path / "weight_items")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", CSRC, "-I", CUDA_INC, os.path.join(ROOT, "tests", "host", "weight_items.cpp"), "-o", exe], check=True)
+    out = subprocess.run([exe], capture_output=True, text=True)
+    assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout + out.stderr
+
+
 def test_cpu_tensors_are_refused_before_the_library_is_called():
     cache = s2a.PagedCache.empty(4, 2, 16, 64, device="cpu")
     table, starts, lengths = (torch.zeros(s, dtype=torch.int32) for s in ((3, 2), (4,), (3,)))

@@ -1,4 +1,5 @@
 """Weights of cached tokens, and eviction by them, on the GPU against their definitions in 64 bits (oracle/evict_torch.py)."""
+import ctypes
 import math
 
 import pytest
@@ -75,6 +76,36 @@ def test_weights(dtype, sizes, H, Hkv, d, page):
 def test_windows(dtype, window, sinks, sizes):
     job = Job(sizes, H=4, Hkv=2, d=64, page=16, dtype=dtype, after=1)
     check(job, window=window, sinks=sinks, before="some", in_place=True)
+
+
+def workspace_bytes(job, window, sinks):
+    """Bytes with which a call's rows are split over several blocks; 0: they are not."""
+    from test_paged_cpu import Batch, Cache
+
+    c = job.cache
+    exps = (0, 0) if c.k_exp is None else (c.k_exp.data_ptr(), c.v_exp.data_ptr())
+    cache = Cache(k=c.k.data_ptr(), v=c.v.data_ptr(), k_exp=exps[0], v_exp=exps[1], type=int(job.dtype == E4M3), pages=c.k.shape[0], Hkv=job.Hkv, page_size=job.page, d=job.d)
+    batch = Batch(table=job.table.data_ptr(), starts=job.starts.data_ptr(), lengths=job.lengths.data_ptr(), width=job.table.shape[1], B=len(job.sizes), T=job.T)
+    return s2a.load().s2a_paged_weights_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), job.H, max(n for n, _ in job.sizes), window, sinks)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 17), (100, 300), (300, 17), (300, 300), (300, 0)])
+@pytest.mark.parametrize("sizes,H,Hkv", [([(700, 1500)], 8, 1), ([(300, 301), (3, 900), (520, 700)], 14, 2)])
+def test_rows_that_are_split(dtype, window, sinks, sizes, H, Hkv):
+    """Many rows and few keys: several blocks have the same keys, with a window that leaves each key some of the rows."""
+    job = Job(sizes, H=H, Hkv=Hkv, d=64, page=16, dtype=dtype, after=1)
+    assert workspace_bytes(job, window, sinks) > 0
+    check(job, window=window, sinks=sinks, before="some", in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 17)])
+def test_a_workspace_that_is_too_small_or_as_large_as_needed(dtype, window, sinks):
+    job = Job([(700, 1500)], H=8, Hkv=1, d=64, page=16, dtype=dtype)
+    need = workspace_bytes(job, window, sinks)
+    for size in (0, 256, need - 1, need):
+        check(job, window=window, sinks=sinks, before="some", workspace=torch.full((size,), 255, dtype=torch.uint8, device="cuda"))
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
