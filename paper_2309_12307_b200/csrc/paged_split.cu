@@ -67,11 +67,15 @@ __device__ __forceinline__ int lds_s8(uint32_t a) {
     asm volatile("ld.shared.s8 %0, [%1];" : "=r"(r) : "r"(a));
     return r;
 }
-// x * 2^e, x > 0 and |e| <= 250, held to the normal numbers.  Scores are multiplied with it, zeros and infinite ones too, so it must neither
-// become infinite nor vanish.  (In two steps towards the result: a step of the other sign could lose bits that the result has.)
+// x * 2^e, x > 0 and |e| <= 250, no larger than fp32's largest number: scores of zero are multiplied with it too.  (In two steps towards the result: a
+// step of the other sign could lose bits that the result has.)
 __device__ __forceinline__ float score_factor(float x, int e) {
     const int half = e >> 1;
-    return fminf(fmaxf(x * power_of_two(half) * power_of_two(e - half), 1.17549435e-38f), 3.40282347e38f);
+    return fminf(x * power_of_two(half) * power_of_two(e - half), 3.40282347e38f);
+}
+// 2^e times `by`, likewise; NaN for kExpNotFinite.
+__device__ __forceinline__ float key_factor(int e, float by) {
+    return e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : fminf(power_of_two(e) * by, 3.40282347e38f);
 }
 
 constexpr float kLazy = 8.0f;        // a running maximum (of log2) that is exceeded by less stays
@@ -184,12 +188,13 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
         }
     }
-    // 8 bits: what the scores of rows 2 t and 2 t + 1 of every eight are multiplied with beside a key's power of two, and what is taken off that
-    // one's exponent: the unit's least row exponent, so that no product of the two is out of range unless the score is.
+    // 8 bits: a product c, at most 2^30, is a score after a multiplication with its key's power of two, 2^(exponent - off_key), and then one with its row's and the scale,
+    // 2^(off_key - up) * scale.  With off_key = 23 the first leaves at most 2^127 and loses nothing that the second would bring above 2^-23,
+    // whatever the rows beside this one are.  (It is less where a row or the scale is so large that its factor would be out of range: queries from about 2^122 on.)
     float row_scale[kRowTiles][2];
-    int least_up = 0;
+    float key_scale = 1.f;
     if constexpr (kE4M3) {
-        int up[kRowTiles];  // exponent of row 8 r + g
+        int up[kRowTiles], least_up = 112;  // exponent of row 8 r + g
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
             uint32_t most = 0;
@@ -201,13 +206,14 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             const float f = power_of_two(up[r]);
 #pragma unroll
             for (int c = 0; c < HD / 8; ++c) q[r][c] = pack_f16(bf16_low(q[r][c]) * f, bf16_high(q[r][c]) * f);
-            least_up = r == 0 ? up[0] : min(least_up, up[r]);
+            least_up = min(least_up, up[r]);
         }
-        least_up = __reduce_min_sync(0xffffffffu, least_up);
+        const int off_key = min(23, static_cast<int>(__reduce_min_sync(0xffffffffu, least_up)) + 126 + 127 - a.scale_field);
+        key_scale = power_of_two(-off_key);
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) row_scale[r][h] = score_factor(a.scale_log2, least_up - __shfl_sync(0xffffffffu, up[r], 4 * (2 * t + h)));
+            for (int h = 0; h < 2; ++h) row_scale[r][h] = score_factor(a.scale_log2, off_key - __shfl_sync(0xffffffffu, up[r], 4 * (2 * t + h)));
     }
 
     float o[kRowTiles][HD / 16][4] = {};
@@ -260,8 +266,7 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
         float k_scale = a.scale_log2, v_exp = 0.f;
         bool grows = false;
         if constexpr (kE4M3) {
-            const int k_exp = lds_s8(sE + lane);
-            k_scale = k_exp == kExpNotFinite ? __uint_as_float(0x7fffffffu) : power_of_two(min(max(k_exp - least_up, -126), 127));
+            k_scale = key_factor(lds_s8(sE + lane), key_scale);
             const int e = lds_s8(sE + C::kKeys + lane);
             v_exp = e == kExpNotFinite ? __uint_as_float(0x7fffffffu) : static_cast<float>(e);
         }

@@ -115,6 +115,25 @@ def test_values_near_the_least_number(sizes, power, dtype):
 
 
 # ---------------------------------------------------------------------------------------------- rows stay by themselves
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [60, 90, 118])
+@pytest.mark.parametrize("new", [2, 5, 16, 40])
+def test_rows_beside_much_larger_ones(new, power, d):
+    """8-bit keys near 2^power.  Every other row of q is as large and has nothing in common with them, the others are as small: their scores are ordinary."""
+    job = Job([(new, 300)], H=2, Hkv=1, d=d, page=32, dtype=E4M3)
+    job.all_k[..., :d // 2] = 0
+    job.all_k *= 2.0**power
+    refill(job)
+    job.q[::2, :, d // 2:] = 0
+    job.q[::2] *= 2.0**power
+    job.q[1::2] *= 2.0**-power
+    o, lse = job.attend(o=torch.full((job.T, 2, d), 7.0, dtype=BF16, device="cuda"), lse=torch.full((2, job.T), 7.0, device="cuda"))
+    want = ref.paged_fwd(job.q.cpu(), job.host_cache(), job.table.cpu(), job.starts.cpu(), job.lengths.cpu(), d**-0.5)
+    # (the large rows' scores are sums of zeros)
+    small = float((job.q.cpu()[1::2].double() * 2.0**power).norm(dim=-1).max())
+    compare(o.cpu(), lse.cpu(), *want, job.rows(), 300, d, d**-0.5, small, job.all_k.double() * 2.0**-power)
+
+
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
 @pytest.mark.parametrize("sizes,power", [([(1, 300)], 20), ([(1, 300)], 40), ([(1, 300)], 100), ([(1, 40), (4, 500), (1, 1)], 20), ([(1, 40), (4, 500), (1, 1)], 40),
                                          ([(1, 40), (4, 500), (1, 1)], 100), ([(200, 500)], 20), ([(200, 500)], 40), ([(200, 500)], 100)])
