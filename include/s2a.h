@@ -256,15 +256,14 @@ int s2a_fwd_bwd_host(const void* h_q, const void* h_k, const void* h_v, const vo
  * A batch holds new tokens of B sequences.  Row starts[b] + i of its tensors is new token i of sequence b, which has
  * starts[b+1] - starts[b] of them (none is allowed); the tensors have T rows.  (B, T and width are at least 1.)  Rows that belong to
  * no sequence are left as they are in outputs, and what they hold in inputs does not matter.  lengths[b] counts the tokens that
- * sequence b has in the cache INCLUDING its new ones, so new token i is at position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is the page of positions j * page_size to
- * (j + 1) * page_size - 1; entries past a sequence's last page are not used, and s2a_paged_fwd uses none of a page that no new token of the
- * sequence attends (in front of the windows: such pages may be given back).  Sequences may share pages, but not those that one call
- * writes to.
- * table, starts and lengths are DEVICE pointers and read on the device when the kernels run: a captured graph follows what they
- * hold when it is replayed.  Their contents are checked there.  What is out of range (starts that fall or leave [0, T], a length
- * below the number of new tokens or above width * page_size, a page outside the pool, more new tokens than max_new) is skipped
- * and reported like an expired wait: it is STICKY, kernels behind it return at once, entry points return S2A_ERR_BAD_INDEX until
- * s2a_device_status() has read it, and the outputs of that call are undefined.
+ * sequence b has in the cache INCLUDING its new ones, so new token i is at position lengths[b] - (starts[b+1] - starts[b]) + i.  table[b * width + j] is
+ * the page of positions j * page_size to (j + 1) * page_size - 1; entries past a sequence's last page are not used, and s2a_paged_fwd uses none of a page
+ * that no new token of the sequence attends (in front of the windows: such pages may be given back).  Sequences may share pages, but not those that one
+ * call writes to.
+ * table, starts and lengths are DEVICE pointers and read on the device when the kernels run: a captured graph follows what they hold when it is replayed.
+ *  Their contents are checked there.  What is out of range (starts that fall or leave [0, T], a length below the number of new tokens or
+ * above width * page_size, a page outside the pool, more new tokens than max_new) is skipped and reported like an expired wait: it is STICKY, kernels
+ * behind it return at once, entry points return S2A_ERR_BAD_INDEX until s2a_device_status() has read it, and the outputs of that call are undefined.
  */
 enum { S2A_CACHE_BF16 = 0, S2A_CACHE_E4M3 = 1 };
 typedef struct s2a_cache {
@@ -354,9 +353,10 @@ typedef struct s2a_rotation {
 } s2a_rotation;
 
 /*
- * q [T, H, d] and k [T, Hkv, d] (bf16) -> q_out, k_out of the same shapes.  d in {64, 128}; H need not be a multiple of Hkv.  *_stride: values from a token to the next,
- * a multiple of 8, at least heads * d and at most 2^28 (T = 1: ignored, but heads * d is at most 2^28 too), so that the slices of a projection's output [T, H + 2 Hkv, d], or of qkv [B, N, 3, H, d], are taken and
- * written as they lie.  An output may be its input (same pointer and stride); otherwise the four must not overlap.  T * (H + 2 Hkv) must not exceed 2^31 - 1.
+ * q [T, H, d] and k [T, Hkv, d] (bf16) -> q_out, k_out of the same shapes.  d in {64, 128}; H need not be a multiple of Hkv.  *_stride: values from a
+ * token to the next, a multiple of 8, at least heads * d and at most 2^28 (T = 1: ignored, but heads * d is at most 2^28 too), so that the slices of a
+ * projection's output [T, H + 2 Hkv, d], or of qkv [B, N, 3, H, d], are taken and written as they lie.  An output may be its input (same pointer and
+ * stride); otherwise the four must not overlap.  T * (H + 2 Hkv) must not exceed 2^31 - 1.
  * One kernel launch.
  */
 int s2a_rotate(const void* q, long long q_stride, const void* k, long long k_stride, void* q_out, long long q_out_stride, void* k_out,
@@ -370,8 +370,8 @@ int s2a_rotate(const void* q, long long q_stride, const void* k, long long k_str
  *   workspace: with a norm at least s2a_rotate_bwd_workspace_bytes(d), 256-byte aligned; its contents before the call do not matter, and calls that can
  *        overlap on the GPU need one each.  Without a norm it is not looked at.
  * With a norm the gradients that come in, times the weight, are at most 2^120 in magnitude (sums of d of them are made).
- * The weights' gradients are sums in fp32 over all tokens and heads, in an order that the sizes and the device fix: deterministic, no atomics.  One launch without a norm, two
- * with one.
+ * The weights' gradients are sums in fp32 over all tokens and heads, in an order that the sizes and the device fix: deterministic, no atomics.  One launch
+ * without a norm, two with one.
  */
 int s2a_rotate_bwd(const void* q, long long q_stride, const void* k, long long k_stride, const void* dq_out, long long dq_out_stride, const void* dk_out,
                    long long dk_out_stride, void* dq, void* dk, float* dq_weight, float* dk_weight, const s2a_rotation* rotation, int T, int H, int Hkv,
@@ -382,23 +382,24 @@ size_t s2a_rotate_bwd_workspace_bytes(int d);
 
 /*
  * The same for new tokens that are served: q [T, H, d] -> q_out (dense), k [T, Hkv, d], rotated, and v as it is into their places in the cache, in one
- * launch.  Bit for bit s2a_rotate and then s2a_cache_write.  Strides are those of s2a_rotate.  The cache's rules apply: what the batch holds is checked on the device, rows of no
- * sequence are left as they are.  A cache that tokens have been evicted from holds fewer tokens than the sequence has had: then positions are given.  q_out may be q where it is dense.
+ * launch.  Bit for bit s2a_rotate and then s2a_cache_write.  Strides are those of s2a_rotate.  The cache's rules apply: what the batch holds is checked on
+ * the device, rows of no sequence are left as they are.  A cache that tokens have been evicted from holds fewer tokens than the sequence has had: then
+ * positions are given.  q_out may be q where it is dense.
  */
 int s2a_rotate_write(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride, void* q_out,
                      const s2a_rotation* rotation, const s2a_cache* cache, const s2a_batch* batch, int H, void* stream);
 
 /*
  * What attention weight the cached tokens get from the new tokens of a call, for eviction.  (The paper has no counterpart: the models it extends are served at
- * lengths whose caches outgrow the memory.)  With p the position of a new token, s = scale * q . k_j over the keys j it attends (s2a_paged_fwd's rule) and lse what
- * s2a_paged_fwd left for it:
+ * lengths whose caches outgrow the memory.)  With p the position of a new token, s = scale * q . k_j over the keys j it attends (s2a_paged_fwd's rule) and
+ * lse what s2a_paged_fwd left for it:
  *   received[j] = before[j] + sum of exp(s - lse) over the new tokens of the sequence that attend j and the H / Hkv query heads of the KV head
- * with before[j] = 0 for the sequence's new tokens, and for all where `before` is NULL: a page's tokens need no clearing when they are written.  Only tokens that a new token of the
- * call attends are written.  Both are fp32 [pages, Hkv, page_size], beside the cache's pools; received may be before.
+ * with before[j] = 0 for the sequence's new tokens, and for all where `before` is NULL: a page's tokens need no clearing when they are written.  Only
+ * tokens that a new token of the call attends are written.  Both are fp32 [pages, Hkv, page_size], beside the cache's pools; received may be before.
  *   in : q [T, H, d] bf16, lse [H, T] fp32, before        out: received
  * Other arguments and rules are those of s2a_paged_fwd.  Sequences of a batch must not share pages of which they attend tokens (this call writes beside them).
- * Scores and sums are fp32.  Over an S2A_CACHE_E4M3 cache the values of a query row count in full down to 2^-29 of its largest.  What the cache holds of tokens that
- * none of the new ones attends does not matter.  Deterministic: no atomics.
+ * Scores and sums are fp32.  Over an S2A_CACHE_E4M3 cache the values of a query row count in full down to 2^-29 of its largest.  What the cache holds of
+ * tokens that none of the new ones attends does not matter.  Deterministic: no atomics.
  *   workspace: like s2a_paged_fwd's, of s2a_paged_weights_workspace_bytes(...) bytes: pieces of prompts that do not fill the GPU evenly are split over their rows where it is there.
  */
 int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, const s2a_batch* batch, const float* before, float* received, int H,
@@ -408,15 +409,17 @@ int s2a_paged_weights(const void* q, const float* lse, const s2a_cache* cache, c
 size_t s2a_paged_weights_workspace_bytes(const s2a_cache* cache, const s2a_batch* batch, int H, int max_new, int window, int sinks);
 
 /*
- * Eviction: of each of B sequences, and for each KV head by itself, m = min(lengths[b], budget) tokens stay: the first `sinks`, the last `recent`, and of those between the ones with
- * the largest `received` (of equal ones the earlier; -0 is 0, NaN counts as larger than all numbers).  In their order they become tokens 0 .. m - 1 of the pages in
- * to_table [B, to_width]: keys, values, their exponents and `received` are copied there; the old pages stay as they are, and so do the new ones behind token m - 1.
+ * Eviction: of each of B sequences, and for each KV head by itself, m = min(lengths[b], budget) tokens stay: the first `sinks`, the last `recent`, and of
+ * those between the ones with the largest `received` (of equal ones the earlier; -0 is 0, NaN counts as larger than all numbers).  In their order they
+ * become tokens 0 .. m - 1 of the pages in to_table [B, to_width]: keys, values, their exponents and `received` are copied there; the old pages stay as
+ * they are, and so do the new ones behind token m - 1.
  *   out: new_lengths [B] = m; kept [B, Hkv, budget], the places the tokens had, ascending, -1 from m on
- * A sequence that attends with new_lengths and to_table from then on goes on at its old position (keys are cached rotated, see s2a_rotate_write); its heads hold
- * different tokens at one place, so sinks and windows count places in the cache.
- * budget >= 1, sinks + recent <= budget, to_width * page_size >= min(budget, width * page_size); none of the three above 2^30 - 1.  lengths[b] may be 0.  new_lengths must not be lengths.  The new pages must differ
- * from one another and from all pages of the old sequences, which may share theirs.
- * table, lengths and to_table are read and checked on the device like a batch (a length above width * page_size, a page outside the pool).  Two kernel launches.  Deterministic.
+ * A sequence that attends with new_lengths and to_table from then on goes on at its old position (keys are cached rotated, see s2a_rotate_write); its
+ * heads hold different tokens at one place, so sinks and windows count places in the cache.
+ * budget >= 1, sinks + recent <= budget, to_width * page_size >= min(budget, width * page_size); none of the three above 2^30 - 1.  lengths[b] may be 0.
+ * new_lengths must not be lengths.  The new pages must differ from one another and from all pages of the old sequences, which may share theirs.
+ * table, lengths and to_table are read and checked on the device like a batch (a length above width * page_size, a page outside the pool).  Two kernel
+ * launches.  Deterministic.
  */
 int s2a_cache_evict(const s2a_cache* cache, float* received, const int* table, int width, const int* lengths, const int* to_table, int to_width, int B,
                     int budget, int sinks, int recent, int* new_lengths, int* kept, void* stream);

@@ -39,15 +39,10 @@ bool plan_stream(WeightsStreamParams* p, int n_sm, long long longest) {
     return true;
 }
 
-// Up to kStreamedRows rows a sequence is the streaming kernel's.  Both measured (us, streaming and tiling kernel, heads of 128 in bf16 and in 8 bits):
-//   - one sequence, 8 KV heads: 1000 keys, 16 rows 8 and 12, 64 rows 10 and 12 (8 bits 12 and 12), 128 rows 14 and 12; 8192 keys, 16 rows 14 and 16, 32 rows 16 and 16, 64 rows 21 and 16 (23 and 16);
-//     32k keys, 16 rows 31 and 33 (27 and 35), 32 rows 33 and 33 (31 and 35), 64 rows 43 and 33 (45 and 35), 256 rows 133 and 35
-//   - 8 x 4096, 8 KV heads: 16 rows 31 and 33 (25 and 35), 32 rows 33 and 33 (29 and 35), 64 rows 45 and 33 (43 and 35); heads of 64, 4 x 4096, 32 rows 23 and 21, 64 rows 29 and 21.
-
 // The items of the tiling kernel and the pieces their rows come in.  Without a window the first key blocks have all rows and the last ones few, and the
 // longest item must not be longer than the others together: a piece has about a quarter of a multiprocessor's share of all row tiles, eight at least (an item's
-// start and the second launch cost about as much as three).  Measured, whole and in pieces, us, one prompt at once on 32 heads over 8 of 128: 512 tokens 31 and 23, 1024 51 and 25,
-// 2048 92 and 41, 4096 176 and 98; 512 new of 16,384 96 and 94.
+// start and the second launch cost about as much as three).  Measured, whole and in pieces, us, one prompt at once on 32 heads over 8 of 128: 512 tokens
+// 31 and 23, 1024 51 and 25, 2048 92 and 41, 4096 176 and 98; 512 new of 16,384 96 and 94.
 bool plan_tile(WeightsTileParams* p, int n_sm, long long longest) {
     const WeightsParams& a = p->a;
     p->pack_log2 = 0;
@@ -94,7 +89,7 @@ WeightsParams weights_params(const s2a_cache* cache, const s2a_batch* batch, int
     a.batch = batch_of(batch), a.pool = pool_of(cache);
     a.H = H, a.rep = H / cache->Hkv, a.most_new = max_new;
     a.window = window >= longest ? 0 : window, a.sinks = sinks > longest ? longest : sinks;
-    // a single sequence has as many new tokens as it is said to have at most, but for loose values
+    // (kStreamedRows has the measurements.)  A single sequence has as many new tokens as it is said to have at most, but for loose values
     a.few_rows = batch->B == 1 && static_cast<long long>(max_new) * a.rep > kStreamedRows ? 0 : kStreamedRows;
     return a;
 }

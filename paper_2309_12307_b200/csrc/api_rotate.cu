@@ -90,8 +90,8 @@ int rotate_impl(const void* q, long long q_stride, const void* k, long long k_st
     return e == cudaSuccess ? S2A_OK : cuda_fail(e);
 }
 
-// The blocks of the backward's grid that have q's rows and k's: in proportion to what their chunks cost, at least one each, no more than there are chunks.  (A chunk of k's few
-// heads has more tokens, so more sines and cosines: with 16 of them it takes 1.25 times as long as with 2.)
+// The blocks of the backward's grid that have q's rows and k's: in proportion to what their chunks cost, at least one each, no more than there are chunks.
+// (A chunk of k's few heads has more tokens, so more sines and cosines: with 16 of them it takes 1.25 times as long as with 2.)
 void bwd_blocks(RotateBwdParams* p, int n_sm, int d) {
     const int all = rotate_bwd_blocks(n_sm);
     double cost[2];

@@ -29,7 +29,14 @@ struct WeightsParams {
     int scale_exp;
 };
 
-// Rows (new tokens times query heads of a KV head) of a sequence up to which it may be the streaming kernel's.
+// Rows (new tokens times query heads of a KV head) of a sequence up to which it is the streaming kernel's, unless it is the only one and may have more.
+// Both measured (us, streaming and tiling kernel, heads of 128 in bf16; 8 bits in brackets where that differs by more than one):
+//   - one sequence, 8 KV heads
+//       1000 keys   16 rows 8 and 12, 64 rows 10 and 12 (12 and 12), 128 rows 14 and 12
+//       8192 keys   16 rows 14 and 16, 32 rows 16 and 16, 64 rows 21 and 16 (23 and 16)
+//       32k keys    16 rows 31 and 33 (27 and 35), 32 rows 33 and 33 (31 and 35), 64 rows 43 and 33 (45 and 35), 256 rows 133 and 35
+//   - 8 x 4096 keys, 8 KV heads: 16 rows 31 and 33 (25 and 35), 32 rows 33 and 33 (29 and 35), 64 rows 45 and 33 (43 and 35)
+//   - 4 x 4096 keys, heads of 64: 32 rows 23 and 21, 64 rows 29 and 21
 constexpr int kStreamedRows = 32;
 struct WeightsStreamParams {
     WeightsParams a;

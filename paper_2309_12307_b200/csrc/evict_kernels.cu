@@ -2,12 +2,13 @@
 //
 // A head of n tokens keeps m = min(n, budget): the first `sinks`, the last `recent`, and of those between the heaviest, of equal ones the earlier.
 //
-// The selecting kernel finds the weight of the lightest token that stays digit by digit: 11, 11 and 10 bits of the weights as ordered whole numbers (the first digit has the exponent and two bits
-// more, over which weights spread; of 8 bits it would be the same for most of them, and its counter what all threads wait for).  A cluster of up to 8 blocks has a head: each
-// block has a part of its tokens, whose weights it reads once and keeps in shared memory, counts their digits there, and adds up the counts of all blocks.  Then each warp counts, of the
-// neighbouring tokens that are its own, those above the border and those on it; one scan over the warps, and the other blocks' totals, say where each warp's tokens go in the list
-// of those that stay.  What bounds it is latency: three rounds of counting, a barrier and a scan each.  (One block a head that read the weights anew for each of four 8-bit digits, 100,000
-// tokens of 8 heads: both kernels and reading back 470 us; so 47.)
+// The selecting kernel finds the weight of the lightest token that stays digit by digit: 11, 11 and 10 bits of the weights as ordered whole numbers (the
+// first digit has the exponent and two bits more, over which weights spread; of 8 bits it would be the same for most of them, and its counter what all
+// threads wait for).  A cluster of up to 8 blocks has a head: each block has a part of its tokens, whose weights it reads once and keeps in shared memory,
+// counts their digits there, and adds up the counts of all blocks.  Then each warp counts, of the neighbouring tokens that are its own, those above the
+// border and those on it; one scan over the warps, and the other blocks' totals, say where each warp's tokens go in the list of those that stay.  What
+// bounds it is latency: three rounds of counting, a barrier and a scan each.  (One block a head that read the weights anew for each of four 8-bit digits,
+// 100,000 tokens of 8 heads: both kernels and reading back 470 us; so 47.)
 //
 // The copying kernel moves the rows.  Other pages, not the same ones: tokens move independently of one another, a prefix that
 // other sequences share stays as it is, and each byte that stays is read and written once.  Bound by HBM.
@@ -85,7 +86,8 @@ __global__ void __launch_bounds__(kSelectThreads) s2a_evict_select_kernel(const 
     __shared__ int s_totals[2];
     release_successor();
     wait_for_predecessor();
-    // After an earlier report nothing is written.  (The block does not leave: one of its cluster may have found nothing yet, and reads this one's shared memory.)
+    // After an earlier report nothing is written.  (The block does not leave: one of its cluster may have found nothing yet, and reads this one's shared
+    // memory.)
     const bool quiet = *reinterpret_cast<volatile int*>(p.status) != 0;
     const int rank = static_cast<int>(blockIdx.x) % p.cluster, unit = static_cast<int>(blockIdx.x) / p.cluster;
     const int b = unit / p.pool.Hkv, hk = unit % p.pool.Hkv;
@@ -155,7 +157,8 @@ __global__ void __launch_bounds__(kSelectThreads) s2a_evict_select_kernel(const 
                 if ((x.w & known) == border) atomicAdd(&s_count[round][x.w >> shift & mask], 1);
             }
         }
-        // the counts of all blocks: each block adds up a part of the digits, and reads the others' sums.  (Of the whole cluster's counts a block reads twice its own that way, not eight times.)
+        // the counts of all blocks: each block adds up a part of the digits, and reads the others' sums.  (Of the whole cluster's counts a block reads
+        // twice its own that way, not eight times.)
         int4 count;  // thread i has the digits from 4 i on
         static_assert(kDigits == 4 * kSelectThreads, "a thread has four digits");
         if (p.cluster == 1) {
@@ -186,8 +189,8 @@ __global__ void __launch_bounds__(kSelectThreads) s2a_evict_select_kernel(const 
         border |= static_cast<uint32_t>(s_digit) << shift, known |= (round == 2 ? 0x3ffu : 0x7ffu) << shift;
         left = s_left;
     }
-    // Those above the border stay, and `left` of those on it, the first ones.  A warp has neighbouring tokens, four of a lane at a time: it counts them, and when it is known what is in
-    // front of them, goes through them again and writes.
+    // Those above the border stay, and `left` of those on it, the first ones.  A warp has neighbouring tokens, four of a lane at a time: it counts them,
+    // and when it is known what is in front of them, goes through them again and writes.
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int each = (fours + kSelectThreads / 32 - 1) / (kSelectThreads / 32), first = min(each * warp, fours), end = min(first + each, fours);
     const uint32_t in_front = (1u << lane) - 1;
@@ -267,7 +270,10 @@ __global__ void __launch_bounds__(kMoveThreads) s2a_evict_copy_kernel(const __gr
         s_from[threadIdx.x] = from, s_to[threadIdx.x] = to;
         if (from >= 0) {
             p.received[to] = __ldcg(p.received + from);
-            if constexpr (kE4M3) p.pool.k_exp[to] = __ldcg(reinterpret_cast<const signed char*>(p.pool.k_exp) + from), p.pool.v_exp[to] = __ldcg(reinterpret_cast<const signed char*>(p.pool.v_exp) + from);
+            if constexpr (kE4M3) {
+                p.pool.k_exp[to] = __ldcg(reinterpret_cast<const signed char*>(p.pool.k_exp) + from);
+                p.pool.v_exp[to] = __ldcg(reinterpret_cast<const signed char*>(p.pool.v_exp) + from);
+            }
         }
     }
     __syncthreads();
@@ -302,7 +308,9 @@ cudaError_t launch_evict(EvictParams p, int n_sm, bool e4m3, int d, cudaStream_t
     const long long longest = static_cast<long long>(p.width) << p.pool.page_log2, units = static_cast<long long>(p.B) * p.pool.Hkv;
     // Blocks of a cluster: as many as there are multiprocessors for, while each has 1024 tokens and more; more of them where their weights fit no other way.
     p.cluster = 1;
-    while (p.cluster < kMostBlocks && ((units * p.cluster * 2 <= n_sm && longest > 2048ll * p.cluster) || longest > static_cast<long long>(kMostKept) * p.cluster)) p.cluster *= 2;
+    while (p.cluster < kMostBlocks &&
+           ((units * p.cluster * 2 <= n_sm && longest > 2048ll * p.cluster) || longest > static_cast<long long>(kMostKept) * p.cluster))
+        p.cluster *= 2;
     const long long part = ((longest + p.cluster - 1) / p.cluster + 3) & ~3ll;
     const bool kept = part <= kMostKept;
     cudaLaunchConfig_t config = {};

@@ -188,9 +188,10 @@ __global__ void __launch_bounds__(32 * SplitCfg<HD, kE4M3>::kMostWarps, 3) s2a_p
             q[r][4 * c] = w.x, q[r][4 * c + 1] = w.y, q[r][4 * c + 2] = w.z, q[r][4 * c + 3] = w.w;
         }
     }
-    // 8 bits: a product c, at most 2^30, is a score after a multiplication with its key's power of two, 2^(exponent - off_key), and then one with its row's and the scale,
-    // 2^(off_key - up) * scale.  With off_key = 23 the first leaves at most 2^127 and loses nothing that the second would bring above 2^-23,
-    // whatever the rows beside this one are.  (It is less where a row or the scale is so large that its factor would be out of range: queries from about 2^122 on.)
+    // 8 bits: a product c, at most 2^30, is a score after a multiplication with its key's power of two, 2^(exponent - off_key), and then one with its
+    // row's and the scale, 2^(off_key - up) * scale.  With off_key = 23 the first leaves at most 2^127 and loses nothing that the second would bring above
+    // 2^-23, whatever the rows beside this one are.  (It is less where a row or the scale is so large that its factor would be out of range: queries from
+    // about 2^122 on.)
     float row_scale[kRowTiles][2];
     float key_scale = 1.f;
     if constexpr (kE4M3) {

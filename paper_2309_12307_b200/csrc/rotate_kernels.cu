@@ -6,10 +6,10 @@
 // bf16 once.
 //
 // Angles: a frequency is a whole number of 2^-64 turns, so its product with a position, modulo 2^64, is the angle's fraction of a turn
-// at any position, of which 32 bits count; 24 of them go to sincospif, the others into the first two terms of the sums of angles.  A row is d / 16 lanes, a lane has both
-// values of eight pairs (two pieces of 16 bytes, d / 8 or r / 2 values apart), so that only the sums of a norm cross lanes.  A block's tokens have their sines and cosines in shared
-// memory, each made once: a lane that made its own for the 8 heads it had of a token spent as long on them, and had no registers left for loads in flight (32768 tokens of
-// 32 + 32 heads of 128 329 us, so 160 to 173).
+// at any position, of which 32 bits count; 24 of them go to sincospif, the others into the first two terms of the sums of angles.  A row is d / 16 lanes,
+// a lane has both values of eight pairs (two pieces of 16 bytes, d / 8 or r / 2 values apart), so that only the sums of a norm cross lanes.  A block's
+// tokens have their sines and cosines in shared memory, each made once: a lane that made its own for the 8 heads it had of a token spent as long on them,
+// and had no registers left for loads in flight (32768 tokens of 32 + 32 heads of 128 329 us, so 160 to 173).
 //
 // Bound by HBM: each value is read and written once (the backward of a norm reads two).
 #include <cuda_fp16.h>
@@ -71,8 +71,8 @@ __device__ __forceinline__ int position_of(const Rotation& ro, int t) {
     return ro.positions ? S2A_LOAD(ro.positions + rest) : rest;
 }
 
-// Cosines and sines of a token's pairs in shared memory: [4][lanes of a row][4], a lane's pairs 2 j and 2 j + 1 as four numbers, so that lanes that read theirs meet in no bank.
-// Pair i < 8 of a lane is values i and 8 + i of its 16, or 2 i and 2 i + 1 where they are interleaved.
+// Cosines and sines of a token's pairs in shared memory: [4][lanes of a row][4], a lane's pairs 2 j and 2 j + 1 as four numbers, so that lanes that read
+// theirs meet in no bank.  Pair i < 8 of a lane is values i and 8 + i of its 16, or 2 i and 2 i + 1 where they are interleaved.
 template <int HD>
 __device__ __forceinline__ void make_angle(float* table, const Rotation& ro, int pair, int position, bool backwards) {
     int part, i;
@@ -270,9 +270,10 @@ __global__ void __launch_bounds__(kRotateThreads, 4) s2a_rotate_kernel(const __g
     }
 }
 
-// Gradients through a norm.  A block has rows of q or of k alone, in chunks of a few tokens; its sums for the weight's gradient go to p.partial, in an order that the sizes
-// and the number of multiprocessors fix.  The next chunk's sines and cosines are made before a chunk is worked on.  A lane's next rows are on their way to a place of its own
-// in shared memory: the sums, a row and its gradient take the registers (with one row ahead in them 106 us for 8192 tokens of 64 + 8 heads, so 93).
+// Gradients through a norm.  A block has rows of q or of k alone, in chunks of a few tokens; its sums for the weight's gradient go to p.partial, in an
+// order that the sizes and the number of multiprocessors fix.  The next chunk's sines and cosines are made before a chunk is worked on.  A lane's next
+// rows are on their way to a place of its own in shared memory: the sums, a row and its gradient take the registers (with one row ahead in them 106 us for
+// 8192 tokens of 64 + 8 heads, so 93).
 constexpr int kBwdRowsOfLane = 4;  // of a chunk: in each of the four places one, so that three rows are on their way
 constexpr int kBwdBlocks = 2;      // of a multiprocessor
 constexpr int kAheadBytes = kBwdRowsOfLane * 4 * 16 * kRotateThreads;

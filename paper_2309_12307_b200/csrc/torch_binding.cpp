@@ -57,7 +57,8 @@ Tensor new_like(const Tensor& t) { return at::empty(t.sizes(), t.options()); }
 
 // t, or a dense copy where it is none or begins off 16 bytes (contiguous() would not move it then).
 Tensor dense_rows(const Tensor& t) {
-    return t.defined() && t.is_cuda() && t.is_contiguous() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0 ? t.clone(at::MemoryFormat::Contiguous) : t.contiguous();
+    const bool moved = t.defined() && t.is_cuda() && t.is_contiguous() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0;
+    return moved ? t.clone(at::MemoryFormat::Contiguous) : t.contiguous();
 }
 
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }

@@ -8,11 +8,11 @@
 // Few rows (new tokens x query heads of a KV head): the streaming kernel.  A warp takes 16 keys at a time as the rows of S^T = K Q^T on mma.sync, eight
 // rows of q as its columns.  An instruction's 16 values of the contraction may be any, as long as K and Q agree, so a lane takes 16 bytes
 // of a key at a time (half of two instructions' worth, of 8-bit codes of four) straight from global memory to registers, the next 16
-// keys' on their way; q lies in shared memory in the order in which lanes need it.  Each key is read once; what bounds the kernel is a block's start (addresses, pages and q one after the other,
-// 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16 x up to 8192 tokens of 32 heads 113 us (5.4 TB/s) in pieces of 1024 keys,
-// 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 59 us with six blocks on a multiprocessor
-// (with four a sixth more).  Keys through a ring in shared memory, two or three turns
-// ahead, left room for fewer blocks: 145 and 81 us.
+// keys' on their way; q lies in shared memory in the order in which lanes need it.  Each key is read once; what bounds the kernel is a block's start
+// (addresses, pages and q one after the other, 2 to 3 us) and a warp's chain loads -> products -> exponentials, so it wants many warps and long pieces: 16
+// x up to 8192 tokens of 32 heads 113 us (5.4 TB/s) in pieces of 1024 keys, 124 of 512, 144 of 256; 8 x up to 32k of 64 heads over 8 in 8 bits 59 us with
+// six blocks on a multiprocessor (with four a sixth more).  Keys through a ring in shared memory, two or three turns ahead, left room for fewer blocks:
+// 145 and 81 us.
 //
 // 8-bit caches are multiplied in fp16, which has their codes exactly.  Each row of q goes with a power of two that brings its largest value to
 // [2^14, 2^15).  Its exponent, the key's and that of the scale are added up before one power of two multiplies the score in fp32: the product of any

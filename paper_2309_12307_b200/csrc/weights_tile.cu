@@ -3,11 +3,11 @@
 // S^T = K Q^T on tcgen05, 128 keys by 128 rows of q at a time.  A score tile has a key in each lane of tensor memory and a row of q in each column, so
 // the thread that has a key adds up its columns' exponentials in registers: nothing crosses threads, and there is no second product.
 // An item is two key tiles of a sequence and KV head, which stay while the row tiles that attend any of them (128 rows, as s2a_paged_fwd_kernel's: query heads
-// of a KV head and neighbouring tokens, one TMA box) pass by.  Two key tiles, because a row tile is 32 KB from the L2 that would otherwise be read twice as often.  (Where it
-// attends only one of them, the other's scores are made and not looked at.)
+// of a KV head and neighbouring tokens, one TMA box) pass by.  Two key tiles, because a row tile is 32 KB from the L2 that would otherwise be read twice
+// as often.  (Where it attends only one of them, the other's scores are made and not looked at.)
 //
-// The keys are the products' operand in tensor memory (8-bit codes as bf16, what they stand for exactly): read from shared memory for every product beside the rows they
-// took its whole bandwidth.
+// The keys are the products' operand in tensor memory (8-bit codes as bf16, what they stand for exactly): read from shared memory for every product beside
+// the rows they took its whole bandwidth.
 //
 // One persistent block per SM:
 //   warps 0-15      exponentials and sums: four warps for either key tile and either half of a row tile's columns
@@ -15,12 +15,15 @@
 //   warp 20         work items (cluster launch control), TMA loads of keys and of q
 //   warp 21         tcgen05 MMAs
 //   warp 22         the rows' log sums
-// Tensor memory: the keys, then three score tiles, which the products of the two key tiles fill in turn: they are ahead of the exponentials, so that what a warp does
-// between two of its tiles, and the change of keys between items, finds others at work.  (A warp that waits for a use of a score tile must know that the use before,
-// three score tiles ago, is over: it has worked on the one two score tiles ago.  Score tiles of 64 rows, twice as many, took the products 1630 cycles a row tile, these 1130.)
+// Tensor memory: the keys, then three score tiles, which the products of the two key tiles fill in turn: they are ahead of the exponentials, so that what
+// a warp does between two of its tiles, and the change of keys between items, finds others at work.  (A warp that waits for a use of a score tile must
+// know that the use before, three score tiles ago, is over: it has worked on the one two score tiles ago.  Score tiles of 64 rows, twice as many, took the
+// products 1630 cycles a row tile, these 1130.)
 //
-// Bound by the exp2 unit, which is busy 81 % of the time (2048 rows of 8192 keys on 32 heads of 128: 150 us, of which it alone would take 115 and the products 58): between score tiles all warps of a
-// multiprocessor's quarter wait at times.  A polynomial for some of the exponentials brought nothing, at any share, nor did warps that take whole score tiles in turn.
+// Bound by the exp2 unit.  2048 rows of 8192 keys on 32 heads of 128 take 150 us.  Counted in a cold launch of 155 us at 1.67 GHz it was busy 81 % of the
+// clocks in which a multiprocessor had a block, 77 % of all: 474 million exponentials (of score tiles that some row attends), 16 a clock, take it 120 us by
+// themselves, and the products take 58.  Between score tiles all warps of a multiprocessor's quarter wait at times.  A polynomial for some of the
+// exponentials brought nothing, at any share, nor did warps that take whole score tiles in turn.
 //
 // Where there are few items their rows are split into pieces, whose sums a second kernel adds up in order.
 #include <cuda_fp16.h>
