@@ -84,8 +84,22 @@ def test_the_library_refuses_without_a_device():
         assert call(**change) == (unsupported,) * 3, change
     assert call(q_out=a + 4)[::2] == (invalid,) * 2 and call(dq=None)[1] == invalid
     assert call(workspace=a + 16)[1] == invalid and call(workspace=None)[1] == invalid
-    # a token's heads lie within 2^28 values, of a single token too, whose stride is not looked at
-    for change in (dict(T=1, H=(1 << 22) + 1), dict(T=1, H=1 << 25), dict(T=1, H=(1 << 21) + 1, d=128), dict(T=1, Hkv=(1 << 22) + 1)):
-        assert call(**change, q_stride=0) == (unsupported,) * 3, change
     assert call(rotation=dict(positions=None, n_positions=0))[:2] == (invalid,) * 2
     assert lib.s2a_rotate_bwd_workspace_bytes(96) == 0
+
+
+@pytest.mark.parametrize("H,Hkv,d", [((1 << 22) + 1, 2, 64), (1 << 25, 2, 64), ((1 << 21) + 1, 2, 128), (4, (1 << 22) + 1, 64)])
+def test_a_tokens_heads_lie_within_a_limit(H, Hkv, d):
+    """2^28 values, of a single token too, whose stride is not looked at: the place of a head in a token is an int."""
+    from test_paged_cpu import Batch, Cache
+
+    lib = s2a.load()
+    buf = (ctypes.c_char * 4096)()
+    a = (ctypes.addressof(buf) + 255) & ~255  # never dereferenced on these paths
+    r = ctypes.byref(Rotation(turns=a, positions=a, n_positions=1, r=64, norm=1, q_weight=a, k_weight=a, eps=1e-5))
+    c = Cache(k=a, v=a, k_exp=a, v_exp=a, type=1, pages=4, Hkv=Hkv, page_size=16, d=d)
+    b = Batch(table=a, starts=a, lengths=a, width=2, B=1, T=1)
+    for status in (lib.s2a_rotate(a, 0, a, 0, a, 0, a, 0, r, 1, H, Hkv, d, None),
+                   lib.s2a_rotate_bwd(a, 0, a, 0, a, 0, a, 0, a, a, a, None, r, 1, H, Hkv, d, a, 0, None),
+                   lib.s2a_rotate_write(a, 0, a, 0, a, 0, a, r, ctypes.byref(c), ctypes.byref(b), H, None)):
+        assert status == s2a.S2A_ERR_UNSUPPORTED
